@@ -332,6 +332,140 @@ griffin_status griffin_ff_decode_static_status(void *stream);
  * (a kernel met an out-of-range expert index) or GRIFFIN_ERR_CUDA. */
 griffin_status griffin_check_device_status(const void *workspace, void *stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Around the feed-forward block: the norms with the residual stream, the paged key/value cache
+ * and attention over it.  The paper prunes the FF block only; these three calls are the rest of
+ * the decoder layer that it sits in (apart from the projections, which are plain matrix
+ * products), for the situation of Eq. 7: several continuations of one prompt.
+ * ------------------------------------------------------------------------------------- */
+
+#define GRIFFIN_MAX_NORM_D 16384    /* widest row of griffin_norm_residual                       */
+#define GRIFFIN_MAX_ATTN_SEQ 1024   /* sequences per griffin_kv_append / griffin_attn_prefix call */
+#define GRIFFIN_MAX_HEAD_GROUP 64   /* query heads per key head                                   */
+
+typedef enum {
+    GRIFFIN_NORM_NONE = 0,        /* norm(x) = x                                                */
+    GRIFFIN_NORM_RMS = 1,         /* norm(x) = x / sqrt(mean(x^2) + eps) * (w0 + w)             */
+    GRIFFIN_NORM_LAYER = 2        /* norm(x) = (x - mean) / sqrt(var + eps) * (w0 + w) + b      */
+} griffin_norm;
+
+typedef enum {
+    GRIFFIN_GATE_LINEAR = 0,      /* the gate's values as they are                              */
+    GRIFFIN_GATE_SIGMOID = 1,
+    GRIFFIN_GATE_TANH = 2
+} griffin_gate_act;
+
+/* Row width and types of griffin_norm_residual. */
+typedef struct {
+    int32_t d;                    /* row width, a multiple of 8, at most GRIFFIN_MAX_NORM_D     */
+    int32_t dtype;                /* griffin_dtype of y, h, gate and the norms' weights         */
+    int32_t res_dtype;            /* griffin_dtype of res and res_out: dtype, or F32            */
+    int32_t pre_norm;             /* griffin_norm in front of the next block                    */
+    int32_t post_norm;            /* griffin_norm behind the last block                         */
+    int32_t gate_act;             /* griffin_gate_act                                           */
+    float eps;                    /* > 0                                                        */
+    float weight_offset;          /* w0 (1 for weights that are stored less one, else 0)        */
+    float res_scale, out_scale;   /* a and c below                                              */
+} griffin_norm_desc;
+
+typedef struct {
+    const void *pre_w, *pre_b;    /* [d]; pre_b: LAYER only, may be NULL (= 0)                  */
+    const void *post_w, *post_b;  /* [d]; needed when post_norm is not NONE                     */
+} griffin_norm_weights;
+
+/* Between two blocks: what the last one put out joins the residual stream, and the next one's
+ * input is normalised.  For each of T rows
+ *   r'      = a res + c act(gate) * post_norm(y)     (y NULL: r' = a res),
+ *   res_out = r' in res_dtype, h = pre_norm(r') in dtype, both rounded once; the norm is taken
+ *             of the unrounded r'; sums and statistics are fp32.
+ * gate NULL: no gate; ld_gate = 0: one gate [d] for all rows; else [T, d].  ld_* are the rows'
+ * distances in elements, multiples of 8 and at least d.  res_out may be NULL (not wanted), and so
+ * may h when pre_norm is NONE.  res_out may be res, and h may be y, row for row; no other overlap. */
+griffin_status griffin_norm_residual(const griffin_norm_desc *desc, const griffin_norm_weights *w, int32_t T,
+                                     const void *y, int64_t ld_y, const void *gate, int64_t ld_gate,
+                                     const void *res, int64_t ld_res, void *res_out, int64_t ld_res_out,
+                                     void *h, int64_t ld_h, void *stream);
+
+/* Heads of one attention layer.  bf16 or fp32 storage; accumulation fp32. */
+typedef struct {
+    int32_t n_q_heads, n_kv_heads; /* Hq a multiple of Hkv, Hq / Hkv <= GRIFFIN_MAX_HEAD_GROUP:
+                                      query head i reads key head i / (Hq / Hkv)                */
+    int32_t head_dim;             /* D: a multiple of 8 in [64, 256]                            */
+    int32_t page_size;            /* tokens per page, a power of two in [8, 1024]               */
+    int32_t dtype;                /* griffin_dtype of q, k, v, the cache and the output         */
+    float scale;                  /* of the logits, > 0                                         */
+} griffin_attn_desc;
+
+/* A cache of pages: K and V of token o of a page, head h, at
+ *   base + page * stride_page + h * stride_head + o * stride_token   (elements; D contiguous).
+ * Strides are the same for k and v, multiples of 16 bytes, >= 0. */
+typedef struct {
+    void *k, *v;
+    int32_t n_pages;
+    int64_t stride_page, stride_head, stride_token;
+} griffin_kv_cache;
+
+/* The tokens of one call.  n_seq sequences share a prefix of prefix_len tokens, whose keys and
+ * values are in pages prefix_pages[0 ..]; behind it each has tokens of its own, in pages
+ * page_table[s * table_stride ..].  The call's new tokens are rows of q (k, v): those of sequence s
+ * are rows q_start[s] .. q_start[s+1]-1, and they are the LAST of its seq_len[s] own tokens.
+ * The arrays are on the device; the counts are host values (n_tokens: rows of q; rows from
+ * q_start[n_seq] on are left alone). */
+typedef struct {
+    int32_t n_seq, n_tokens;
+    const int32_t *q_start;       /* [n_seq + 1], ascending                                     */
+    const int32_t *seq_len;       /* [n_seq] own tokens, the new ones included                  */
+    const int32_t *page_table;    /* [n_seq, table_stride]                                      */
+    int32_t table_stride;
+    int32_t prefix_len;           /* 0: no prefix                                               */
+    const int32_t *prefix_pages;  /* ceil(prefix_len / page_size) entries                       */
+} griffin_attn_batch;
+
+/* Position rotation.  table [n_pos, rot_dim] fp32: row p holds rot_dim/2 cosines, then as many
+ * sines, of position p.  The first rot_dim entries of a head turn in pairs (x, y) ->
+ * (x cos - y sin, x sin + y cos): entries j and j + rot_dim/2 (HALF) or 2j and 2j + 1 (PAIRS). */
+#define GRIFFIN_ROPE_HALF 0
+#define GRIFFIN_ROPE_PAIRS 1
+typedef struct {
+    const float *table;
+    int32_t n_pos, rot_dim;       /* rot_dim a multiple of 16, <= head_dim                      */
+    int32_t style;
+} griffin_rope;
+
+/* Puts the new tokens' keys and values into the cache, rotated by their positions, and rotates
+ * the queries on the way.  Token t of sequence s has index i = seq_len[s] - (q_start[s+1] - t)
+ * among its own tokens, position prefix_len + i, and goes to entry i mod page_size of page
+ * page_table[s][i / page_size].  A token with i < 0 is padding: the cache is left alone and its
+ * row of q_out is zero.  q, q_out [n_tokens, Hq, D], k, v [n_tokens, Hkv, D] with ld_* elements
+ * from token to token (multiples of 16 bytes), so slices of one projection's output will do; q and
+ * q_out may both be NULL, and q_out may be q.  rope NULL: no rotation.  A page number outside
+ * [0, n_pages), an index beyond the table's row or a position from n_pos on is not followed: the
+ * token is not written (its q_out row is zero) and the workspace's status word (workspace may be
+ * NULL) is raised.  Two tokens of a call must not share a place. */
+griffin_status griffin_kv_append(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
+                                 const griffin_kv_cache *cache, const griffin_rope *rope,
+                                 const void *q, int64_t ld_q, const void *k, int64_t ld_k, const void *v, int64_t ld_v,
+                                 void *q_out, int64_t ld_q_out, void *workspace, void *stream);
+
+/* Bytes of workspace for griffin_attn_prefix calls of at most n_tokens_max new tokens and n_seq_max
+ * sequences; 0 if desc is NULL or invalid.  Clear it with griffin_workspace_init. */
+size_t griffin_attn_workspace_bytes(const griffin_attn_desc *desc, int32_t n_tokens_max, int32_t n_seq_max);
+
+/* Attention of the new tokens over the shared prefix and their own sequence, causal:
+ *   out[t, h] = sum_j softmax_j(scale q[t, h] . k_j) v_j over the prefix and own tokens 0 .. i
+ * (i as for griffin_kv_append; the new tokens' keys and values are in the cache already).  A token
+ * that sees nothing gets zeros.  The prefix is read once for all sequences of the call when their
+ * queries are few; a batch of long pieces, whose rows fill the tensor cores' tiles anyway, reads it
+ * sequence by sequence.  What lies in the cache behind a sequence's end may be anything, NaN
+ * included; among the tokens of the call, a value that is not finite may also reach
+ * tokens in front of it.  Probabilities are rounded to bf16 for the second product when the
+ * storage is bf16.  q, out [n_tokens, Hq, D], ld_* as above; out may be q only if they are the same
+ * rows.  Page numbers outside [0, n_pages) read as zeros, lengths beyond the table's row are cut, and
+ * both raise the workspace's status word. */
+griffin_status griffin_attn_prefix(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
+                                   const griffin_kv_cache *cache, const void *q, int64_t ld_q, void *out, int64_t ld_out,
+                                   void *workspace, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,6 +20,12 @@ ACT_RELU, ACT_GELU_TANH, ACT_GELU_ERF, ACT_SILU = 4, 5, 6, 7   # blocks without 
 DT_F32, DT_BF16 = 0, 1
 DECODE_DEFAULT, DECODE_OVERLAP_WEIGHT_PREFETCH, DECODE_TCGEN05, DECODE_RING, DECODE_STREAM = 0, 1, 2, 4, 8
 MAX_BATCH = 32
+NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
+GATE_LINEAR, GATE_SIGMOID, GATE_TANH = range(3)
+ROPE_HALF, ROPE_PAIRS = range(2)
+NORM_BY_NAME = {"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
+GATE_BY_NAME = {"linear": GATE_LINEAR, "sigmoid": GATE_SIGMOID, "tanh": GATE_TANH}
+ROPE_BY_NAME = {"half": ROPE_HALF, "pairs": ROPE_PAIRS}
 
 ACT_BY_NAME = {"swiglu": ACT_SWIGLU, "geglu_tanh": ACT_GEGLU_TANH, "reglu": ACT_REGLU, "geglu_erf": ACT_GEGLU_ERF,
                "relu": ACT_RELU, "gelu_tanh": ACT_GELU_TANH, "gelu_erf": ACT_GELU_ERF, "silu": ACT_SILU}
@@ -36,6 +42,7 @@ EXPORTS = (
     "griffin_combine_scores", "griffin_compact_experts", "griffin_ff_decode", "griffin_check_device_status",
     "griffin_ff_decode_static", "griffin_ff_decode_indexed", "griffin_ff_prefill_score_chunk",
     "griffin_kernel_launches", "griffin_ff_decode_static_status", "griffin_compact_experts_nm",
+    "griffin_norm_residual", "griffin_kv_append", "griffin_attn_workspace_bytes", "griffin_attn_prefix",
 )
 
 
@@ -60,6 +67,34 @@ class FFWeightsNM(C.Structure):
 class FFCompact(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("w_gate_c", "w_up_c", "w_down_c", "b_gate_c", "b_up_c")] + \
                [("k", C.c_int32), ("ldk", C.c_int32)]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("d", "dtype", "res_dtype", "pre_norm", "post_norm", "gate_act")] + \
+               [(n, C.c_float) for n in ("eps", "weight_offset", "res_scale", "out_scale")]
+
+
+class NormWeights(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("pre_w", "pre_b", "post_w", "post_b")]
+
+
+class AttnDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "page_size", "dtype")] + [("scale", C.c_float)]
+
+
+class KVCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32)] + \
+               [(n, C.c_int64) for n in ("stride_page", "stride_head", "stride_token")]
+
+
+class AttnBatch(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("n_tokens", C.c_int32)] + \
+               [(n, C.c_void_p) for n in ("q_start", "seq_len", "page_table")] + \
+               [("table_stride", C.c_int32), ("prefix_len", C.c_int32), ("prefix_pages", C.c_void_p)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("n_pos", C.c_int32), ("rot_dim", C.c_int32), ("style", C.c_int32)]
 
 
 _lib = None
@@ -111,6 +146,18 @@ def load(path=None):
     lib.griffin_ff_decode_static.argtypes = [C.POINTER(FFDesc), i32, C.POINTER(FFCompact), vp, vp, vp, u32, vp]
     lib.griffin_ff_decode_static_status.restype = C.c_int
     lib.griffin_ff_decode_static_status.argtypes = [vp]
+    i64 = C.c_int64
+    lib.griffin_norm_residual.restype = C.c_int
+    lib.griffin_norm_residual.argtypes = [C.POINTER(NormDesc), C.POINTER(NormWeights), i32, vp, i64, vp, i64, vp, i64, vp, i64,
+                                          vp, i64, vp]
+    lib.griffin_kv_append.restype = C.c_int
+    lib.griffin_kv_append.argtypes = [C.POINTER(AttnDesc), C.POINTER(AttnBatch), C.POINTER(KVCache), C.POINTER(Rope), vp, i64,
+                                      vp, i64, vp, i64, vp, i64, vp, vp]
+    lib.griffin_attn_workspace_bytes.restype = sz
+    lib.griffin_attn_workspace_bytes.argtypes = [C.POINTER(AttnDesc), i32, i32]
+    lib.griffin_attn_prefix.restype = C.c_int
+    lib.griffin_attn_prefix.argtypes = [C.POINTER(AttnDesc), C.POINTER(AttnBatch), C.POINTER(KVCache), vp, i64, vp, i64, vp, sz,
+                                        vp]
     lib.griffin_check_device_status.restype = C.c_int
     lib.griffin_check_device_status.argtypes = [vp, vp]
     _lib = lib
@@ -287,3 +334,143 @@ def griffin_ff_decode_static_status(stream=None):
 
 def griffin_check_device_status(ws, stream=None):
     return load().griffin_check_device_status(_ptr(ws), _stream(stream))
+
+
+# ---- around the FF block: norms and the residual stream, the paged cache, attention over it ---------------------
+_TORCH_DTYPE = {DT_F32: torch.float32, DT_BF16: torch.bfloat16}
+
+
+def _dtype(v):
+    return DTYPE_BY_NAME[v] if isinstance(v, str) else int(v)
+
+
+def _rows(t, n, heads, d, dtype, what):
+    """Token stride of an [n, heads, d] (or [n, heads * d]) tensor whose tokens are rows of heads * d
+    consecutive entries."""
+    st = t.stride()
+    inner = st[1:] == (d, 1) and t.shape[1:] == (heads, d) if t.dim() == 3 else t.dim() == 2 and st[1] == 1 and t.shape[1] == heads * d
+    if not inner or t.shape[0] < n or t.dtype != _TORCH_DTYPE[dtype]:
+        raise ValueError(f"{what}: expected {_TORCH_DTYPE[dtype]} [{n}, {heads}, {d}] with the heads of a token in one "
+                         f"row, got {t.dtype} {tuple(t.shape)} with strides {st}")
+    return st[0] if t.shape[0] > 1 else heads * d
+
+
+def make_norm_desc(d, dtype, res_dtype=None, pre="rms", post="none", eps=1e-6, weight_offset=0.0, res_scale=1.0, out_scale=1.0,
+                   gate_act="linear"):
+    return NormDesc(int(d), _dtype(dtype), _dtype(dtype if res_dtype is None else res_dtype), NORM_BY_NAME[pre], NORM_BY_NAME[post],
+                    GATE_BY_NAME[gate_act], float(eps), float(weight_offset), float(res_scale), float(out_scale))
+
+
+def make_norm_weights(pre_w=None, pre_b=None, post_w=None, post_b=None):
+    w = NormWeights(_ptr(pre_w), _ptr(pre_b), _ptr(post_w), _ptr(post_b))
+    w._keep = (pre_w, pre_b, post_w, post_b)
+    return w
+
+
+def _norm_rows(t, desc, dtype, T, what):
+    if t.dim() != 2 or t.shape[0] != T or t.shape[1] != desc.d or t.stride(1) != 1 or t.dtype != _TORCH_DTYPE[dtype]:
+        raise ValueError(f"{what}: expected {_TORCH_DTYPE[dtype]} [{T}, {desc.d}] with consecutive entries, got {t.dtype} "
+                         f"{tuple(t.shape)} with strides {t.stride()}")
+    return t.stride(0) if T > 1 else desc.d
+
+
+def griffin_norm_residual(desc, weights, res, res_out, h, y=None, gate=None, stream=None):
+    """res_out = a res + c act(gate) * post_norm(y), h = pre_norm(res_out) for the rows of res [T, d].  y, gate, res_out
+    and h may be None (see include/griffin_ff.h); gate is [d] or [T, d]."""
+    T = res.shape[0]
+    if T == 0:
+        return
+    ld = [0, 0, _norm_rows(res, desc, desc.res_dtype, T, "res"), 0, 0]
+    if y is not None:
+        ld[0] = _norm_rows(y, desc, desc.dtype, T, "y")
+    if gate is not None:
+        ld[1] = _norm_rows(gate, desc, desc.dtype, T, "gate") if gate.dim() == 2 else \
+            _norm_rows(gate[None], desc, desc.dtype, 1, "gate") * 0
+    if res_out is not None:
+        ld[3] = _norm_rows(res_out, desc, desc.res_dtype, T, "res_out")
+    if h is not None:
+        ld[4] = _norm_rows(h, desc, desc.dtype, T, "h")
+    _check(load().griffin_norm_residual(C.byref(desc), C.byref(weights), T, _ptr(y), ld[0], _ptr(gate), ld[1], _ptr(res), ld[2],
+                                        _ptr(res_out), ld[3], _ptr(h), ld[4], _stream(stream)), "griffin_norm_residual")
+
+
+def make_attn_desc(n_q_heads, n_kv_heads, head_dim, page_size, dtype, scale=None):
+    return AttnDesc(int(n_q_heads), int(n_kv_heads), int(head_dim), int(page_size), _dtype(dtype),
+                    float(head_dim ** -0.5 if scale is None else scale))
+
+
+def make_kv_cache(k, v):
+    """A paged cache from two tensors [n_pages, n_kv_heads, page_size, head_dim] of the same strides (any, as long as the
+    entries of a head are consecutive: pages laid out [page_size, n_kv_heads, head_dim] go in as a transposed view)."""
+    if k.shape != v.shape or k.stride() != v.stride() or k.dim() != 4 or k.stride(3) != 1 or k.dtype != v.dtype:
+        raise ValueError(f"k and v must be alike, [pages, heads, tokens, head_dim]: got {k.dtype} {tuple(k.shape)} {k.stride()}, "
+                         f"{v.dtype} {tuple(v.shape)} {v.stride()}")
+    c = KVCache(_ptr(k), _ptr(v), k.shape[0], k.stride(0), k.stride(1), k.stride(2))
+    c._keep = (k, v)
+    return c
+
+
+def make_attn_batch(q_start, seq_len, page_table, n_tokens, prefix_pages=None, prefix_len=0):
+    """The tokens of a call.  q_start [n_seq + 1], seq_len [n_seq], page_table [n_seq, pages], prefix_pages: int32 on the
+    device, read when the call runs (so the same batch serves every step of a generation whose lengths are counted up on
+    the device); n_tokens, prefix_len: host numbers."""
+    for name, t in (("q_start", q_start), ("seq_len", seq_len), ("page_table", page_table), ("prefix_pages", prefix_pages)):
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
+            raise ValueError(f"{name}: expected contiguous int32, got {t.dtype}")
+    n_seq = seq_len.shape[0]
+    if q_start.shape != (n_seq + 1,) or page_table.dim() != 2 or page_table.shape[0] != n_seq:
+        raise ValueError(f"q_start {tuple(q_start.shape)}, seq_len {tuple(seq_len.shape)}, page_table {tuple(page_table.shape)}")
+    b = AttnBatch(n_seq, int(n_tokens), _ptr(q_start), _ptr(seq_len), _ptr(page_table),
+                  page_table.shape[1], int(prefix_len), _ptr(prefix_pages))
+    b._keep = (q_start, seq_len, page_table, prefix_pages)
+    return b
+
+
+def make_rope(table, style="half"):
+    """Rotation by the rows of `table` [n_pos, rot_dim], fp32: rot_dim/2 cosines, then the sines."""
+    if table.dim() != 2 or table.dtype != torch.float32 or not table.is_contiguous():
+        raise ValueError(f"expected contiguous float32 [n_pos, rot_dim], got {table.dtype} {tuple(table.shape)}")
+    r = Rope(_ptr(table), table.shape[0], table.shape[1], ROPE_BY_NAME[style])
+    r._keep = table
+    return r
+
+
+def rope_table(n_pos, rot_dim, theta=10000.0, device=None):
+    """cos and sin of p * theta^(-2j / rot_dim), angles in float64."""
+    freq = float(theta) ** (-torch.arange(rot_dim // 2, dtype=torch.float64) * 2 / rot_dim)
+    a = torch.arange(n_pos, dtype=torch.float64)[:, None] * freq
+    return torch.cat((a.cos(), a.sin()), 1).float().to(device)
+
+
+def griffin_kv_append(desc, batch, cache, rope, q, k, v, q_out, ws=None, stream=None):
+    """New keys and values [n_tokens, n_kv_heads, head_dim] into the cache, keys and queries rotated; q and q_out may be
+    None, q_out may be q."""
+    n, hq, hk, d = batch.n_tokens, desc.n_q_heads, desc.n_kv_heads, desc.head_dim
+    ld_q = 0 if q is None else _rows(q, n, hq, d, desc.dtype, "q")
+    ld_o = 0 if q_out is None else _rows(q_out, n, hq, d, desc.dtype, "q_out")
+    _check(load().griffin_kv_append(C.byref(desc), C.byref(batch), C.byref(cache), None if rope is None else C.byref(rope),
+                                    _ptr(q), ld_q, _ptr(k), _rows(k, n, hk, d, desc.dtype, "k"), _ptr(v),
+                                    _rows(v, n, hk, d, desc.dtype, "v"), _ptr(q_out), ld_o, _ptr(ws), _stream(stream)),
+           "griffin_kv_append")
+
+
+def griffin_attn_workspace_bytes(desc, n_tokens_max, n_seq_max):
+    return load().griffin_attn_workspace_bytes(C.byref(desc), int(n_tokens_max), int(n_seq_max))
+
+
+def alloc_attn_workspace(desc, n_tokens_max, n_seq_max, device, stream=None):
+    n = griffin_attn_workspace_bytes(desc, n_tokens_max, n_seq_max)
+    if n == 0:
+        raise GriffinError(ERR_INVALID_ARG, "griffin_attn_workspace_bytes")
+    ws = torch.empty((n,), device=device, dtype=torch.uint8)
+    griffin_workspace_init(ws, stream)
+    return ws
+
+
+def griffin_attn_prefix(desc, batch, cache, q, out, ws, stream=None):
+    """Attention of the batch's new tokens over the shared prefix and their own sequences; q, out [n_tokens, n_q_heads,
+    head_dim]."""
+    n, hq, d = batch.n_tokens, desc.n_q_heads, desc.head_dim
+    _check(load().griffin_attn_prefix(C.byref(desc), C.byref(batch), C.byref(cache), _ptr(q), _rows(q, n, hq, d, desc.dtype, "q"),
+                                      _ptr(out), _rows(out, n, hq, d, desc.dtype, "out"), _ptr(ws), ws.numel(), _stream(stream)),
+           "griffin_attn_prefix")

@@ -1,0 +1,74 @@
+// griffin_attn_prefix on the host: the plan's sizes, the scratch, the two launches.
+#include <math.h>
+
+#include "attn.h"
+#include "attn_join.cuh"
+
+namespace griffin {
+
+constexpr int ATTN_MAX_GRID = 148;  // CTAs at most (one per SM of a B200)
+
+static AttnShape shape_of(const griffin_attn_desc *desc) {
+    (void)desc;
+    return attn_simt_shape();
+}
+
+struct AttnScratch {
+    size_t own_off, pre_off, cta_off, total;  // the bases are at 0
+    long long own_rows;
+};
+// (every size grows with n_tokens and n_seq, so a workspace for the largest call serves the others)
+static AttnScratch attn_scratch(const griffin_attn_desc *desc, const AttnShape &sh, long long n_tokens, long long n_seq) {
+    AttnScratch s;
+    const size_t row = (size_t)(desc->head_dim + 2) * sizeof(float), streams = sh.alt ? 2 : 1;
+    const long long by_token = n_tokens * desc->n_q_heads, by_seq = n_seq * desc->n_kv_heads * 128;
+    s.own_rows = by_token < by_seq ? by_token : by_seq;
+    s.own_off = ((size_t)(n_seq + 1) * 8 + 255) / 256 * 256;
+    s.pre_off = s.own_off + streams * s.own_rows * row;
+    s.cta_off = s.pre_off + (n_seq > 1 ? streams * s.own_rows * row : 0);
+    s.total = s.cta_off + (size_t)ATTN_MAX_GRID * 2 * (2 * sh.tile_rows) * row;
+    return s;
+}
+
+size_t attn_scratch_bytes(const griffin_attn_desc *desc, int n_tokens, int n_seq) {
+    return attn_scratch(desc, shape_of(desc), n_tokens, n_seq).total;
+}
+
+griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
+                                  const griffin_kv_cache *cache, const void *q, int64_t ld_q, void *out, int64_t ld_out,
+                                  uint8_t *scratch, void *ws, cudaStream_t stream) {
+    const int sms = device_sm_count();
+    if (sms <= 0) return GRIFFIN_ERR_CUDA;
+    const AttnShape sh = shape_of(desc);
+    AttnPlan p{};
+    p.q_start = batch->q_start; p.seq_len = batch->seq_len; p.page_table = batch->page_table;
+    p.prefix_pages = batch->prefix_pages;
+    p.n_seq = batch->n_seq; p.n_tokens = batch->n_tokens; p.table_stride = batch->table_stride;
+    p.prefix_len = batch->prefix_len; p.n_pages = cache->n_pages;
+    while ((1 << p.page_shift) < desc->page_size) ++p.page_shift;
+    p.hq = desc->n_q_heads; p.hkv = desc->n_kv_heads; p.group = p.hq / p.hkv; p.d = desc->head_dim;
+    p.fused = attn_fused(p.n_seq, p.n_tokens, p.group, p.prefix_len);
+    p.by_token = attn_by_token(p.n_seq, p.n_tokens, p.group);
+    p.alt = sh.alt;
+    p.tile_tokens = sh.tile_rows / p.group;
+    p.tiles_per_block = sh.tiles_per_block;
+    p.block_tokens = p.tile_tokens * p.tiles_per_block;
+    p.kt = sh.kt;
+    p.prefix_tiles = ceil_div(p.prefix_len, p.kt);
+    p.prefix_blocks = p.fused ? 0 : ceil_div(p.n_tokens, p.block_tokens);
+    p.grid = sms < ATTN_MAX_GRID ? sms : ATTN_MAX_GRID;
+    p.scale_log2 = desc->scale * 1.4426950408889634f;
+    p.ws = ws;
+    const AttnScratch s = attn_scratch(desc, sh, p.n_tokens, p.n_seq);
+    p.bases = reinterpret_cast<long long *>(scratch);
+    p.own = reinterpret_cast<float *>(scratch + s.own_off);
+    p.pre = reinterpret_cast<float *>(scratch + s.pre_off);
+    p.cta = reinterpret_cast<float *>(scratch + s.cta_off);
+    p.own_rows = s.own_rows;
+    p.cta_rows = 2 * sh.tile_rows;
+    const AttnData x{q, cache->k, cache->v, out, ld_q, ld_out, cache->stride_page, cache->stride_head, cache->stride_token};
+    const griffin_status st = launch_attn_simt(p, x, desc->dtype, stream);
+    return st != GRIFFIN_OK ? st : launch_attn_join(p, desc->dtype, out, ld_out, stream);
+}
+
+}  // namespace griffin

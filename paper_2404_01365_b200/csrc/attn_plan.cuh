@@ -1,0 +1,219 @@
+// How one griffin_attn_prefix call is cut up, shared by the attention kernels and the joining kernel.
+//
+// A JOB is a block of query rows under one key head (row = token * group + query head of the group) and the
+// keys that they see; its work is counted in TILES of KT keys.  All jobs' tiles, laid end to end, are dealt
+// out in equal shares to G CTAs (one per SM, or one per tile where there are fewer): CTA c takes tiles [c W / G, (c+1) W / G).  So every SM has
+// the same number of tiles to within one, however ragged the lengths, without any word from the host about
+// them; a share that ends inside a job leaves a PARTIAL (running maximum m, sum l, unnormalised output, all
+// fp32), and the joining kernel adds a row's partials in the order of the keys.
+//
+// Order of the jobs: first those of the shared prefix (by key head, then row block over all the call's
+// tokens), then sequence by sequence its own keys (by key head, then row block).  When the call is FUSED
+// (see attn_fused) there are no prefix jobs and every job walks the prefix's tiles before its own.
+//
+// A block is `tiles_per_block` row tiles of `tile_rows` rows.  With ALT, a block that fits in one row tile
+// is worked on by two groups of warps that take its key tiles in turn, each with its own m, l and output:
+// two partials (streams 0 and 1) per segment.
+#pragma once
+
+#include "common.cuh"
+
+namespace griffin {
+
+struct AttnPlan {
+    const int *q_start, *seq_len, *page_table, *prefix_pages;
+    int n_seq, n_tokens, table_stride, prefix_len, n_pages;
+    int page_shift;
+    int hq, hkv, group, d;
+    int fused, alt, by_token;  // by_token: how partials by row are numbered (attn_part_row)
+    int tile_tokens;       // tokens per row tile
+    int tiles_per_block;   // row tiles per block
+    int block_tokens;      // tile_tokens * tiles_per_block
+    int kt;                // keys per tile
+    int prefix_tiles;      // ceil(prefix_len / kt)
+    int prefix_blocks;     // row blocks per key head of the prefix jobs (0 when fused or without a prefix)
+    int grid;
+    float scale_log2;      // scale * log2(e): logits in units of log2
+    void *ws;
+    // scratch (see attn_scratch)
+    long long *bases;      // [n_seq + 1]: first own tile of each sequence; the last entry is W
+    float *own, *pre;      // partials by row: [2 streams][rows]: m and l, then the outputs
+    float *cta;            // partials by CTA: [grid][2: continued from before / going on behind][2 * tile_rows]
+    long long own_rows;
+    int cta_rows;          // 2 * tile_rows
+};
+
+// Rows of one partial array: (m, l) pairs for all rows, then D outputs for all rows.
+__host__ __device__ inline float *part_ml(float *base, long long row) { return base + 2 * row; }
+__host__ __device__ inline float *part_o(float *base, long long rows, long long row, int d) { return base + 2 * rows + row * d; }
+
+// Whether the call's rows are fewer than 128 per sequence and key head.
+__host__ __device__ inline bool attn_by_token(int n_seq, int n_tokens, int group) {
+    return (long long)n_tokens * group <= (long long)n_seq * 128;
+}
+
+// Whether each sequence walks the prefix itself.  Read once for the batch, the prefix costs two partials per
+// row; read by each sequence it costs its bytes n_seq times.  With 128 rows or more per sequence and key head
+// the second reading is no longer what bounds the call (the matrix unit's tiles are full either way), and
+// nothing has to be joined.
+__host__ __device__ inline bool attn_fused(int n_seq, int n_tokens, int group, int prefix_len) {
+    return n_seq == 1 || prefix_len == 0 || !attn_by_token(n_seq, n_tokens, group);
+}
+
+__host__ __device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+struct AttnSeq {
+    int q0, nq, len;  // first new token, how many, own tokens
+};
+// The sequence's lengths, held to what the arrays can hold.
+__device__ __forceinline__ AttnSeq attn_seq(const AttnPlan &p, int s) {
+    AttnSeq r;
+    int a = __ldg(p.q_start + s), b = __ldg(p.q_start + s + 1), len = __ldg(p.seq_len + s);
+    const long long cap = (long long)p.table_stride << p.page_shift;
+    const bool bad = a < 0 || b < a || b > p.n_tokens || len < 0 || len > cap;
+    a = min(max(a, 0), p.n_tokens);
+    b = min(max(b, a), p.n_tokens);
+    if (bad) raise_status(p.ws, DEV_STATUS_BAD_INDEX, 41);
+    r.q0 = a;
+    r.nq = b - a;
+    r.len = (int)min((long long)max(len, 0), cap);
+    return r;
+}
+// Key tiles of row block b of a sequence: the prefix's (fused) and its own up to the last row's place.
+__device__ __forceinline__ int attn_block_tiles(const AttnPlan &p, const AttnSeq &q, int b) {
+    const int last = q.len - q.nq + min(q.nq, (b + 1) * p.block_tokens);  // own tokens that the block's last row sees
+    return (p.fused ? p.prefix_tiles : 0) + ceil_div(max(last, 0), p.kt);
+}
+
+// CTAs that have work (every one of them at least a tile), first tile of CTA c, and the CTA that has tile g.
+__host__ __device__ inline int attn_ctas(long long W, int grid) { return W < grid ? (int)W : grid; }
+__host__ __device__ inline long long attn_share(long long W, int G, int c) { return (long long)c * W / G; }
+__host__ __device__ inline int attn_cta_of(long long W, int G, long long g) { return (int)(((g + 1) * G - 1) / W); }
+
+struct AttnJob {
+    long long g0, g1;     // its tiles
+    int seq;              // -1: prefix job
+    int head;             // key head
+    int tok0, n_tok;      // its rows' tokens
+    int block;            // row block of its sequence
+    int seen0;            // own tokens that the first of them sees (the next one sees one more)
+    int rows;             // n_tok * group
+    int own_len;          // own tokens of the sequence that any row sees
+    bool alt;
+};
+
+__device__ __forceinline__ AttnJob attn_prefix_job(const AttnPlan &p, int head, int b) {
+    AttnJob j;
+    j.seq = -1;
+    j.head = head;
+    j.block = b;
+    j.tok0 = b * p.block_tokens;
+    j.n_tok = min(p.block_tokens, p.n_tokens - j.tok0);
+    j.g0 = (long long)(head * p.prefix_blocks + b) * p.prefix_tiles;
+    j.g1 = j.g0 + p.prefix_tiles;
+    j.seen0 = 0;
+    j.own_len = 0;
+    j.rows = j.n_tok * p.group;
+    j.alt = p.alt && j.n_tok <= p.tile_tokens;
+    return j;
+}
+
+__device__ __forceinline__ AttnJob attn_own_job(const AttnPlan &p, const AttnSeq &q, int s, int head, int b, long long g0) {
+    AttnJob j;
+    j.g0 = g0;
+    j.g1 = g0 + attn_block_tiles(p, q, b);
+    j.seq = s;
+    j.head = head;
+    j.block = b;
+    j.tok0 = q.q0 + b * p.block_tokens;
+    j.n_tok = min(p.block_tokens, q.nq - b * p.block_tokens);
+    j.seen0 = q.len - q.nq + b * p.block_tokens + 1;
+    j.own_len = max(j.seen0 + j.n_tok - 1, 0);
+    j.rows = j.n_tok * p.group;
+    j.alt = p.alt && j.n_tok <= p.tile_tokens;
+    return j;
+}
+
+// Own key tiles of a sequence under one key head.
+__device__ __forceinline__ long long attn_seq_tiles(const AttnPlan &p, const AttnSeq &q) {
+    long long n = 0;
+    for (int b = 0; b * p.block_tokens < q.nq; ++b) n += attn_block_tiles(p, q, b);
+    return n;
+}
+
+// First tile of every sequence into bases[0 .. n_seq] (shared memory), by all threads of the CTA; bases[n_seq] is
+// the number of tiles of the call.  The first CTA also leaves them in the scratch for the joining kernel.
+__device__ __forceinline__ void attn_scan(const AttnPlan &p, long long *bases) {
+    const int lane = threadIdx.x & 31;
+    for (int s = threadIdx.x; s < p.n_seq; s += blockDim.x) bases[s] = attn_seq_tiles(p, attn_seq(p, s)) * p.hkv;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        long long sum = (long long)p.hkv * p.prefix_blocks * p.prefix_tiles;
+        for (int s0 = 0; s0 < p.n_seq; s0 += 32) {
+            const int s = s0 + lane;
+            const long long mine = s < p.n_seq ? bases[s] : 0;
+            long long upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long v = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            if (s < p.n_seq) bases[s] = sum + upto - mine;
+            sum += __shfl_sync(0xffffffffu, upto, 31);
+        }
+        if (lane == 0) bases[p.n_seq] = sum;
+    }
+    __syncthreads();
+    if (blockIdx.x == 0)
+        for (int s = threadIdx.x; s <= p.n_seq; s += blockDim.x) p.bases[s] = bases[s];
+}
+
+// The job that has tile g (one exists: g < bases[n_seq]).
+__device__ __forceinline__ AttnJob attn_find(const AttnPlan &p, const long long *bases, long long g) {
+    if (g < bases[0]) {
+        const int hb = (int)(g / p.prefix_tiles);
+        return attn_prefix_job(p, hb / p.prefix_blocks, hb % p.prefix_blocks);
+    }
+    int lo = 0, hi = p.n_seq;  // bases[lo] <= g < bases[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (bases[mid] <= g) lo = mid; else hi = mid;
+    }
+    const AttnSeq q = attn_seq(p, lo);
+    const long long per_head = (bases[lo + 1] - bases[lo]) / p.hkv;
+    const int head = (int)((g - bases[lo]) / per_head);
+    long long at = bases[lo] + head * per_head;
+    int b = 0;
+    for (;; ++b) {
+        const int n = attn_block_tiles(p, q, b);
+        if (g < at + n) break;
+        at += n;
+    }
+    return attn_own_job(p, q, lo, head, b, at);
+}
+// The job behind j, whose first tile is j.g1 < bases[n_seq].
+__device__ __forceinline__ AttnJob attn_next(const AttnPlan &p, const long long *bases, const AttnJob &j) {
+    if (j.seq >= 0) {
+        const AttnSeq q = attn_seq(p, j.seq);
+        if ((j.block + 1) * p.block_tokens < q.nq) return attn_own_job(p, q, j.seq, j.head, j.block + 1, j.g1);
+    }
+    return attn_find(p, bases, j.g1);
+}
+
+// Whether a whole job's result goes straight to the output (no other partial of its rows exists).
+__device__ __forceinline__ bool attn_direct(const AttnPlan &p, const AttnJob &j, bool whole) {
+    return whole && !j.alt && p.fused;
+}
+// Row of `own` / `pre` for row r of a job.  Either every row (token and query head) has a place, or, where that
+// is less, 128 rows of every sequence and key head: then only one-tile blocks are kept there, of which a
+// sequence has one at most.  (A call that is not fused is by token: that is the same comparison.)
+__device__ __forceinline__ long long attn_part_row(const AttnPlan &p, const AttnJob &j, int r) {
+    if (!p.by_token) return (long long)(j.seq * p.hkv + j.head) * 128 + r;
+    return (long long)(j.tok0 + r / p.group) * p.hq + j.head * p.group + r % p.group;
+}
+
+// Where the first segment of a job (the one with its first tile) leaves its partials: by row, or with the
+// CTA when a block of several row tiles is cut in a fused call.
+__device__ __forceinline__ bool attn_first_by_row(const AttnPlan &p, const AttnJob &j) { return j.alt || !p.fused; }
+
+}  // namespace griffin
