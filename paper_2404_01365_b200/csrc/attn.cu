@@ -9,8 +9,7 @@ namespace griffin {
 constexpr int ATTN_MAX_GRID = 148;  // CTAs at most (one per SM of a B200)
 
 static AttnShape shape_of(const griffin_attn_desc *desc) {
-    (void)desc;
-    return attn_simt_shape();
+    return desc->dtype == GRIFFIN_DT_F32 ? attn_simt_shape() : attn_tc_shape(desc->head_dim);
 }
 
 struct AttnScratch {
@@ -22,7 +21,7 @@ static AttnScratch attn_scratch(const griffin_attn_desc *desc, const AttnShape &
     AttnScratch s;
     const size_t row = (size_t)(desc->head_dim + 2) * sizeof(float), streams = sh.alt ? 2 : 1;
     const long long by_token = n_tokens * desc->n_q_heads, by_seq = n_seq * desc->n_kv_heads * 128;
-    s.own_rows = by_token < by_seq ? by_token : by_seq;
+    s.own_rows = ((by_token < by_seq ? by_token : by_seq) + 3) / 4 * 4;  // (16-byte alignment of what follows the rows)
     s.own_off = ((size_t)(n_seq + 1) * 8 + 255) / 256 * 256;
     s.pre_off = s.own_off + streams * s.own_rows * row;
     s.cta_off = s.pre_off + (n_seq > 1 ? streams * s.own_rows * row : 0);
@@ -67,7 +66,7 @@ griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_a
     p.own_rows = s.own_rows;
     p.cta_rows = 2 * sh.tile_rows;
     const AttnData x{q, cache->k, cache->v, out, ld_q, ld_out, cache->stride_page, cache->stride_head, cache->stride_token};
-    const griffin_status st = launch_attn_simt(p, x, desc->dtype, stream);
+    const griffin_status st = desc->dtype == GRIFFIN_DT_F32 ? launch_attn_simt(p, x, stream) : launch_attn_tc(p, x, stream);
     return st != GRIFFIN_OK ? st : launch_attn_join(p, desc->dtype, out, ld_out, stream);
 }
 

@@ -18,6 +18,8 @@ struct AttnShape {
 };
 
 AttnShape attn_simt_shape();
-griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, int dtype, cudaStream_t stream);
+AttnShape attn_tc_shape(int head_dim);
+griffin_status launch_attn_tc(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // bf16
+griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // fp32
 
 }  // namespace griffin

@@ -1,4 +1,4 @@
-// Attention over the shared prefix and each sequence's own keys, on the plain fp32 pipes:
+// Attention over the shared prefix and each sequence's own keys, fp32 storage, on the plain fp32 pipes:
 //   S = scale Q K^T, masked by place;  m' = max(m, max S);  P = 2^(S - m');
 //   l = l 2^(m - m') + sum P;  O = O 2^(m - m') + P V        (S in units of log2, all fp32)
 // one CTA of 256 threads per SM, each with its share of the call's key tiles (attn_plan.cuh).  Keys and
@@ -17,7 +17,7 @@ template <int DP> constexpr size_t simt_smem(int n_seq) {
 }
 
 // DP: the head's width rounded up to 64, 128 or 256; entries from D on are zeros in shared memory.
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_constant__ AttnPlan p,
                                                                  const __grid_constant__ AttnData x) {
     constexpr int LD = DP + 4, NE = DP / 64;  // NE: groups of 4 outputs of a thread, 64 apart
@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_co
             const int r = i / (DP / 8), e = i % (DP / 8) * 8;
             float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (r < j.rows && e < p.d)
-                load8<T>(x.q, (j.tok0 + r / p.group) * x.ld_q + (j.head * p.group + r % p.group) * p.d + e, f);
+                load8<float>(x.q, (j.tok0 + r / p.group) * x.ld_q + (j.head * p.group + r % p.group) * p.d + e, f);
             store8<float>(sq, r * LD + e, f);
         }
         if (tid < SIMT_ROWS) {
@@ -75,8 +75,8 @@ __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_co
                     if (page >= 0 && page < p.n_pages) {
                         const long long at = page * x.stride_page + j.head * x.stride_head +
                                              (key & ((1 << p.page_shift) - 1)) * x.stride_token + e;
-                        load8<T>(x.k, at, fk);
-                        load8<T>(x.v, at, fv);
+                        load8<float>(x.k, at, fk);
+                        load8<float>(x.v, at, fv);
                     } else {
                         raise_status(p.ws, DEV_STATUS_BAD_INDEX, 42);
                     }
@@ -168,13 +168,12 @@ __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_co
             const float m = sm[r], l = sl[r];
             if (direct) {
                 const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
-                T *const to = static_cast<T *>(x.out) + (j.tok0 + r / p.group) * x.ld_out + (j.head * p.group + r % p.group) * p.d;
+                float *const to = static_cast<float *>(x.out) + (j.tok0 + r / p.group) * x.ld_out + (j.head * p.group + r % p.group) * p.d;
 #pragma unroll
                 for (int b = 0; b < NE; ++b)
-                    if (b * 64 + tx * 4 < p.d) {
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) to[b * 64 + tx * 4 + c] = Elem<T>::from_float(o[a][b][c] * inv);
-                    }
+                    if (b * 64 + tx * 4 < p.d)
+                        *reinterpret_cast<float4 *>(to + b * 64 + tx * 4) =
+                            make_float4(o[a][b][0] * inv, o[a][b][1] * inv, o[a][b][2] * inv, o[a][b][3] * inv);
             } else {
                 const PartPlace at = attn_place(p, j, first, 0, r);
                 if (tx == 0) *reinterpret_cast<float2 *>(at.ml) = make_float2(m, l);
@@ -189,32 +188,22 @@ __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_co
     }
 }
 
-template <typename T> static const void *simt_kernel(int d, size_t (**smem)(int)) {
-    if (d <= 64) {
-        *smem = simt_smem<64>;
-        return reinterpret_cast<const void *>(attn_simt_kernel<T, 64>);
-    }
-    if (d <= 128) {
-        *smem = simt_smem<128>;
-        return reinterpret_cast<const void *>(attn_simt_kernel<T, 128>);
-    }
-    *smem = simt_smem<256>;
-    return reinterpret_cast<const void *>(attn_simt_kernel<T, 256>);
-}
-
 AttnShape attn_simt_shape() { return {SIMT_ROWS, 1, SIMT_KT, 0}; }
 
-griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, int dtype, cudaStream_t stream) {
-    AttnPlan p = plan;
-    AttnData x = data;
-    size_t (*smem_of)(int);
-    const void *fn = dtype == GRIFFIN_DT_F32 ? simt_kernel<float>(p.d, &smem_of) : simt_kernel<__nv_bfloat16>(p.d, &smem_of);
-    const size_t smem = smem_of(p.n_seq);
+template <int DP> static griffin_status launch_dp(AttnPlan p, AttnData x, cudaStream_t stream) {
+    const void *fn = reinterpret_cast<const void *>(attn_simt_kernel<DP>);
+    const size_t smem = simt_smem<DP>(p.n_seq);
     if (ensure_dynamic_smem(fn, smem) != cudaSuccess) return GRIFFIN_ERR_CUDA;
     void *args[] = {&p, &x};
     return launch_maybe_overlapped(fn, dim3(p.grid), dim3(SIMT_THREADS), smem, stream, true, args) == cudaSuccess
                ? GRIFFIN_OK
                : GRIFFIN_ERR_CUDA;
+}
+
+griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, cudaStream_t stream) {
+    if (plan.d <= 64) return launch_dp<64>(plan, data, stream);
+    if (plan.d <= 128) return launch_dp<128>(plan, data, stream);
+    return launch_dp<256>(plan, data, stream);
 }
 
 }  // namespace griffin
