@@ -45,15 +45,17 @@ griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_a
     p.n_seq = batch->n_seq; p.n_tokens = batch->n_tokens; p.table_stride = batch->table_stride;
     p.prefix_len = batch->prefix_len; p.n_pages = cache->n_pages;
     while ((1 << p.page_shift) < desc->page_size) ++p.page_shift;
-    p.hq = desc->n_q_heads; p.hkv = desc->n_kv_heads; p.group = p.hq / p.hkv; p.d = desc->head_dim;
+    p.hq = desc->n_q_heads; p.hkv = desc->n_kv_heads; p.group = p.hq / p.hkv;
+    p.group_inv = (65536u + p.group - 1) / p.group;
+    p.d = desc->head_dim;
     p.fused = attn_fused(p.n_seq, p.n_tokens, p.group, p.prefix_len);
     p.by_token = attn_by_token(p.n_seq, p.n_tokens, p.group);
     p.alt = sh.alt;
     p.tile_tokens = sh.tile_rows / p.group;
     p.tiles_per_block = sh.tiles_per_block;
     p.block_tokens = p.tile_tokens * p.tiles_per_block;
-    p.kt = sh.kt;
-    p.prefix_tiles = ceil_div(p.prefix_len, p.kt);
+    while ((1 << p.kt_shift) < sh.kt) ++p.kt_shift;
+    p.prefix_tiles = ceil_div(p.prefix_len, sh.kt);
     p.prefix_blocks = p.fused ? 0 : ceil_div(p.n_tokens, p.block_tokens);
     p.grid = sms < ATTN_MAX_GRID ? sms : ATTN_MAX_GRID;
     p.scale_log2 = desc->scale * 1.4426950408889634f;

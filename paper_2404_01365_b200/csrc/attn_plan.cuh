@@ -2,7 +2,7 @@
 //
 // A JOB is a block of query rows under one key head (row = token * group + query head of the group) and the
 // keys that they see; its work is counted in TILES of KT keys.  All jobs' tiles, laid end to end, are dealt
-// out in equal shares to G CTAs (one per SM, or one per tile where there are fewer): CTA c takes tiles [c W / G, (c+1) W / G).  So every SM has
+// out in equal shares to G CTAs (one per SM, or one per tile where there are fewer): W / G each, the first W mod G of them one more.  So every SM has
 // the same number of tiles to within one, however ragged the lengths, without any word from the host about
 // them; a share that ends inside a job leaves a PARTIAL (running maximum m, sum l, unnormalised output, all
 // fp32), and the joining kernel adds a row's partials in the order of the keys.
@@ -29,8 +29,9 @@ struct AttnPlan {
     int tile_tokens;       // tokens per row tile
     int tiles_per_block;   // row tiles per block
     int block_tokens;      // tile_tokens * tiles_per_block
-    int kt;                // keys per tile
-    int prefix_tiles;      // ceil(prefix_len / kt)
+    int kt_shift;          // keys per tile: 1 << kt_shift
+    uint32_t group_inv;    // ceil(2^16 / group): x / group = x * group_inv >> 16 for x * group < 2^16
+    int prefix_tiles;      // ceil(prefix_len / keys per tile)
     int prefix_blocks;     // row blocks per key head of the prefix jobs (0 when fused or without a prefix)
     int grid;
     float scale_log2;      // scale * log2(e): logits in units of log2
@@ -60,7 +61,17 @@ __host__ __device__ inline bool attn_fused(int n_seq, int n_tokens, int group, i
     return n_seq == 1 || prefix_len == 0 || !attn_by_token(n_seq, n_tokens, group);
 }
 
+// row (of a block) / query heads per key head
+__device__ __forceinline__ int attn_row_token(const AttnPlan &p, int row) { return (int)(((uint32_t)row * p.group_inv) >> 16); }
+
+// Quotient of non-negative numbers that nearly always fit in 32 bits (a 64-bit division is a long routine).
+__host__ __device__ inline long long attn_div(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 __host__ __device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+static __device__ __noinline__ void attn_bad(void *ws, int where) { raise_status(ws, DEV_STATUS_BAD_INDEX, where); }
 
 struct AttnSeq {
     int q0, nq, len;  // first new token, how many, own tokens
@@ -73,7 +84,7 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnPlan &p, int s) {
     const bool bad = a < 0 || b < a || b > p.n_tokens || len < 0 || len > cap;
     a = min(max(a, 0), p.n_tokens);
     b = min(max(b, a), p.n_tokens);
-    if (bad) raise_status(p.ws, DEV_STATUS_BAD_INDEX, 41);
+    if (bad) attn_bad(p.ws, 41);
     r.q0 = a;
     r.nq = b - a;
     r.len = (int)min((long long)max(len, 0), cap);
@@ -82,24 +93,35 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnPlan &p, int s) {
 // Key tiles of row block b of a sequence: the prefix's (fused) and its own up to the last row's place.
 __device__ __forceinline__ int attn_block_tiles(const AttnPlan &p, const AttnSeq &q, int b) {
     const int last = q.len - q.nq + min(q.nq, (b + 1) * p.block_tokens);  // own tokens that the block's last row sees
-    return (p.fused ? p.prefix_tiles : 0) + ceil_div(max(last, 0), p.kt);
+    return (p.fused ? p.prefix_tiles : 0) + ((max(last, 0) + (1 << p.kt_shift) - 1) >> p.kt_shift);
 }
 
-// CTAs that have work (every one of them at least a tile), first tile of CTA c, and the CTA that has tile g.
+// CTAs that have work (every one of them at least a tile), first tile of CTA c, and the CTA that has tile g: the
+// first W mod G CTAs have a tile more than the others.
 __host__ __device__ inline int attn_ctas(long long W, int grid) { return W < grid ? (int)W : grid; }
-__host__ __device__ inline long long attn_share(long long W, int G, int c) { return (long long)c * W / G; }
-__host__ __device__ inline int attn_cta_of(long long W, int G, long long g) { return (int)(((g + 1) * G - 1) / W); }
+__host__ __device__ inline long long attn_share(long long W, int G, int c) {
+    const long long q = attn_div(W, G), r = W - q * G;
+    return c * q + (c < r ? c : r);
+}
+__host__ __device__ inline int attn_cta_of(long long W, int G, long long g) {
+    const long long q = attn_div(W, G), r = W - q * G, lead = r * (q + 1);
+    return (int)(g < lead ? attn_div(g, q + 1) : r + attn_div(g - lead, q));
+}
 
-struct AttnJob {
-    long long g0, g1;     // its tiles
+// What says where a job's partials are.
+struct PartJob {
     int seq;              // -1: prefix job
     int head;             // key head
-    int tok0, n_tok;      // its rows' tokens
+    int tok0;             // first token of its rows
+    bool alt;
+};
+struct AttnJob : PartJob {
+    long long g0, g1;     // its tiles
+    int n_tok;            // its rows' tokens
     int block;            // row block of its sequence
     int seen0;            // own tokens that the first of them sees (the next one sees one more)
     int rows;             // n_tok * group
     int own_len;          // own tokens of the sequence that any row sees
-    bool alt;
 };
 
 __device__ __forceinline__ AttnJob attn_prefix_job(const AttnPlan &p, int head, int b) {
@@ -135,8 +157,9 @@ __device__ __forceinline__ AttnJob attn_own_job(const AttnPlan &p, const AttnSeq
 }
 
 // Own key tiles of a sequence under one key head.
-__device__ __forceinline__ long long attn_seq_tiles(const AttnPlan &p, const AttnSeq &q) {
+static __device__ __noinline__ long long attn_seq_tiles(const AttnPlan &p, const AttnSeq &q) {
     long long n = 0;
+#pragma unroll 1
     for (int b = 0; b * p.block_tokens < q.nq; ++b) n += attn_block_tiles(p, q, b);
     return n;
 }
@@ -168,10 +191,11 @@ __device__ __forceinline__ void attn_scan(const AttnPlan &p, long long *bases) {
         for (int s = threadIdx.x; s <= p.n_seq; s += blockDim.x) p.bases[s] = bases[s];
 }
 
+// (Not inlined: the schedule's code would otherwise be most of a kernel's, and instruction fetches its time.)
 // The job that has tile g (one exists: g < bases[n_seq]).
-__device__ __forceinline__ AttnJob attn_find(const AttnPlan &p, const long long *bases, long long g) {
+static __device__ __noinline__ AttnJob attn_find(const AttnPlan &p, const long long *bases, long long g) {
     if (g < bases[0]) {
-        const int hb = (int)(g / p.prefix_tiles);
+        const int hb = (int)attn_div(g, p.prefix_tiles);
         return attn_prefix_job(p, hb / p.prefix_blocks, hb % p.prefix_blocks);
     }
     int lo = 0, hi = p.n_seq;  // bases[lo] <= g < bases[hi]
@@ -180,10 +204,11 @@ __device__ __forceinline__ AttnJob attn_find(const AttnPlan &p, const long long 
         if (bases[mid] <= g) lo = mid; else hi = mid;
     }
     const AttnSeq q = attn_seq(p, lo);
-    const long long per_head = (bases[lo + 1] - bases[lo]) / p.hkv;
-    const int head = (int)((g - bases[lo]) / per_head);
+    const long long per_head = attn_div(bases[lo + 1] - bases[lo], p.hkv);
+    const int head = (int)attn_div(g - bases[lo], per_head);
     long long at = bases[lo] + head * per_head;
     int b = 0;
+#pragma unroll 1
     for (;; ++b) {
         const int n = attn_block_tiles(p, q, b);
         if (g < at + n) break;
@@ -192,12 +217,25 @@ __device__ __forceinline__ AttnJob attn_find(const AttnPlan &p, const long long 
     return attn_own_job(p, q, lo, head, b, at);
 }
 // The job behind j, whose first tile is j.g1 < bases[n_seq].
-__device__ __forceinline__ AttnJob attn_next(const AttnPlan &p, const long long *bases, const AttnJob &j) {
-    if (j.seq >= 0) {
-        const AttnSeq q = attn_seq(p, j.seq);
-        if ((j.block + 1) * p.block_tokens < q.nq) return attn_own_job(p, q, j.seq, j.head, j.block + 1, j.g1);
+static __device__ __noinline__ AttnJob attn_next(const AttnPlan &p, const long long *bases, const AttnJob &j) {
+    int s = j.seq, head = j.head, b = j.block + 1;
+    if (s < 0) {
+        if (j.g1 < bases[0]) return b < p.prefix_blocks ? attn_prefix_job(p, head, b) : attn_prefix_job(p, head + 1, 0);
+        s = 0;
+        head = b = 0;
+        while (bases[s + 1] == bases[s]) ++s;
     }
-    return attn_find(p, bases, j.g1);
+    AttnSeq q = attn_seq(p, s);
+    if (b * p.block_tokens >= q.nq) {
+        b = 0;
+        if (++head == p.hkv) {
+            head = 0;
+            do ++s; while (bases[s + 1] == bases[s]);
+            q = attn_seq(p, s);
+        }
+    }
+    while (attn_block_tiles(p, q, b) == 0) ++b;  // (only in front of blocks that have some)
+    return attn_own_job(p, q, s, head, b, j.g1);
 }
 
 // Whether a whole job's result goes straight to the output (no other partial of its rows exists).
@@ -207,13 +245,13 @@ __device__ __forceinline__ bool attn_direct(const AttnPlan &p, const AttnJob &j,
 // Row of `own` / `pre` for row r of a job.  Either every row (token and query head) has a place, or, where that
 // is less, 128 rows of every sequence and key head: then only one-tile blocks are kept there, of which a
 // sequence has one at most.  (A call that is not fused is by token: that is the same comparison.)
-__device__ __forceinline__ long long attn_part_row(const AttnPlan &p, const AttnJob &j, int r) {
+__device__ __forceinline__ long long attn_part_row(const AttnPlan &p, const PartJob &j, int r) {
     if (!p.by_token) return (long long)(j.seq * p.hkv + j.head) * 128 + r;
-    return (long long)(j.tok0 + r / p.group) * p.hq + j.head * p.group + r % p.group;
+    return (long long)(j.tok0 + attn_row_token(p, r)) * p.hq + j.head * p.group + (r - attn_row_token(p, r) * p.group);
 }
 
 // Where the first segment of a job (the one with its first tile) leaves its partials: by row, or with the
 // CTA when a block of several row tiles is cut in a fused call.
-__device__ __forceinline__ bool attn_first_by_row(const AttnPlan &p, const AttnJob &j) { return j.alt || !p.fused; }
+__device__ __forceinline__ bool attn_first_by_row(const AttnPlan &p, const PartJob &j) { return j.alt || !p.fused; }
 
 }  // namespace griffin

@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_co
             const int r = i / (DP / 8), e = i % (DP / 8) * 8;
             float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (r < j.rows && e < p.d)
-                load8<float>(x.q, (j.tok0 + r / p.group) * x.ld_q + (j.head * p.group + r % p.group) * p.d + e, f);
+                load8<float>(x.q, (j.tok0 + attn_row_token(p, r)) * x.ld_q + (j.head * p.group + r - attn_row_token(p, r) * p.group) * p.d + e, f);
             store8<float>(sq, r * LD + e, f);
         }
         if (tid < SIMT_ROWS) {
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_co
             }
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
-                const int r = ty * 4 + a, seen = in_prefix ? len : min(len, j.seen0 + r / p.group);
+                const int r = ty * 4 + a, seen = in_prefix ? len : min(len, j.seen0 + attn_row_token(p, r));
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
                     ss[r * (SIMT_KT + 1) + tx + 16 * b] = k0 + tx + 16 * b < seen ? s[a][b] * p.scale_log2 : -INFINITY;
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_co
             const float m = sm[r], l = sl[r];
             if (direct) {
                 const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
-                float *const to = static_cast<float *>(x.out) + (j.tok0 + r / p.group) * x.ld_out + (j.head * p.group + r % p.group) * p.d;
+                float *const to = static_cast<float *>(x.out) + (j.tok0 + attn_row_token(p, r)) * x.ld_out + (j.head * p.group + r - attn_row_token(p, r) * p.group) * p.d;
 #pragma unroll
                 for (int b = 0; b < NE; ++b)
                     if (b * 64 + tx * 4 < p.d)

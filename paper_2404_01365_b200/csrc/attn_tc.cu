@@ -7,6 +7,8 @@
 //   warp 0      TMA producer: query tiles and, page by page, key and value tiles (128-byte swizzle) into a ring
 //   warp 1      MMA issuer: one thread issues tcgen05.mma; it also owns the TMEM allocation
 //   warp 2      clears the rows of a value tile that no key stands for (0 * NaN would reach the sum)
+//   warp 3      scheduler: walks the share, segment by segment (a segment: what the share has of one job), and
+//               hands descriptions of the segments to the others through a ring in shared memory
 //   warps 4-7, 8-11   two softmax groups, a row per thread: S from TMEM, P (bf16) back to TMEM over S,
 //               and at the end of a segment O to the output or the partials
 // The work is a sequence of UNITS (one row tile times one key tile).  Unit U belongs to softmax group U & 1,
@@ -22,7 +24,7 @@
 // Every wait is bounded; after a give-up the CTA still frees its TMEM before it returns.
 #include "attn.h"
 #include "attn_join.cuh"
-#include "tc_common.cuh"
+#include "tmem_wide.cuh"
 
 namespace griffin {
 
@@ -37,7 +39,7 @@ template <int DP> struct AtcCfg {
     static constexpr int O_COL = 2 * KT;                  // TMEM columns: S/P 0, S/P 1, O (0, 1)
     static constexpr int MAX_SLOTS = DP == 64 ? 10 : 5;
 };
-constexpr int ATC_BARS = 2 * 10 + 10 + 4 + 6;  // kv full/empty, v_ok, q full/empty, s_full, p_ready, o_full
+constexpr int ATC_BARS = 2 * 10 + 10 + 4 + 6 + 2 * 4;  // kv full/empty, v_ok, q full/empty, s_full, p_ready, o_full, seg full/empty
 
 struct AtcMaps {
     CUtensorMap q, k, v;
@@ -105,51 +107,117 @@ __device__ __forceinline__ float fast_exp2(float x) {
     return y;
 }
 
-// A wait of a whole warp: all its lanes go on, or none.
-__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort, void *ws, int where) {
-    return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort, ws, where));
+__device__ __forceinline__ void prefetch_tensormap(const CUtensorMap *map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// two fp32 lanes in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(d)
+        : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
+    return *reinterpret_cast<float2 *>(&d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
+    return *reinterpret_cast<float2 *>(&d);
+}
+// Keys from `lim` on are not seen.
+__device__ __forceinline__ void mask_keys(float (&s)[64], int lim) {
+#pragma unroll
+    for (int i = 0; i < 64; ++i) s[i] = i < lim ? s[i] : -INFINITY;
 }
 
-// Walks a CTA's share, segment by segment (a segment: what the share has of one job).
-struct SegWalk {
-    AttnJob j;
-    long long g, stop, end;
-    __device__ __forceinline__ void start(const AttnPlan &p, const long long *bases, long long g0, long long g_end) {
-        g = g0;
-        end = g_end;
-        j = attn_find(p, bases, g0);
-        stop = min(end, j.g1);
+// The bounded wait with its slow path in one place: the loops below stay small enough for the instruction cache
+// (with everything inlined the kernel was 128 KB of code and spent half its time fetching it).
+static __device__ __noinline__ bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort, void *ws, int where) {
+    return wait_or_abort(bar, parity, abort, ws, where);
+}
+__device__ __forceinline__ bool wait_bar(uint64_t *bar, uint32_t parity, volatile int *abort, void *ws, int where) {
+    return mbar_try_wait(bar, parity) || mbar_try_wait(bar, parity) || wait_slow(bar, parity, abort, ws, where);
+}
+// A wait of a whole warp: all its lanes go on, or none.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort, void *ws, int where) {
+    return __all_sync(0xffffffffu, wait_bar(bar, parity, abort, ws, where));
+}
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e != 0;
+}
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+
+// Place in a ring of barriers, and the parity that a wait for this round's completion takes.
+struct Ring {
+    uint32_t slot, parity;
+    __device__ __forceinline__ void step(uint32_t by, uint32_t n) {  // by <= n
+        slot += by;
+        if (slot >= n) {
+            slot -= n;
+            parity ^= 1u;
+        }
     }
-    __device__ __forceinline__ bool next(const AttnPlan &p, const long long *bases) {
-        if (stop >= end) return false;
-        g = stop;
-        j = attn_next(p, bases, j);
-        stop = min(end, j.g1);
-        return true;
-    }
-    __device__ __forceinline__ int tiles() const { return (int)(stop - g); }
-    __device__ __forceinline__ int first_tile() const { return (int)(g - j.g0); }
-    __device__ __forceinline__ bool from_start() const { return g == j.g0; }
-    __device__ __forceinline__ bool whole() const { return g == j.g0 && stop == j.g1; }
 };
+
+// A segment, as the scheduler hands it on.
+struct __align__(16) Segment {
+    int t0, n;            // first key tile (of the job's) and how many; n = 0: the share is done
+    int pre_tiles;        // the job's tiles of the prefix; the others are the sequence's own
+    int head, seq, tok0, rows, seen0, own_len;
+    int alt, direct, first;
+};
+constexpr int ATC_SEGS = 4;
+
 // One key tile of a job: where its keys are and how many there are.
 struct KeyTile {
-    const int *pages;
     int k0, len;  // first key; keys behind `len` are not there
     bool prefix;
 };
-__device__ __forceinline__ KeyTile key_tile(const AttnPlan &p, const AttnJob &j, int t) {
-    const int pre = j.seq < 0 || p.fused ? p.prefix_tiles : 0;
+__device__ __forceinline__ KeyTile key_tile(const AttnPlan &p, const Segment &s, int t) {
     KeyTile k;
-    k.prefix = t < pre;
-    k.k0 = (k.prefix ? t : t - pre) * p.kt;
-    k.len = k.prefix ? p.prefix_len : j.own_len;
-    k.pages = k.prefix ? p.prefix_pages : p.page_table + (long long)j.seq * p.table_stride;
+    k.prefix = t < s.pre_tiles;
+    k.k0 = (k.prefix ? t : t - s.pre_tiles) << p.kt_shift;
+    k.len = k.prefix ? p.prefix_len : s.own_len;
     return k;
 }
 
+// A reader's place in the ring of segments.
+struct SegReader {
+    uint32_t slot, parity;
+    uint64_t *full, *empty;
+    const Segment *ring;
+    // the next segment, into s; false: a wait gave up.  s.n == 0: there is none.
+    __device__ __forceinline__ bool get(Segment &s, volatile int *abort, void *ws, int where) {
+        if (!wait_bar(&full[slot], parity, abort, ws, where)) return false;
+        s = ring[slot];
+        return true;
+    }
+    __device__ __forceinline__ void step() {
+        if (++slot == ATC_SEGS) {
+            slot = 0;
+            parity ^= 1u;
+        }
+    }
+    // once a reader (a warp, or the issuer with its later look) has copied the segment
+    __device__ __forceinline__ void release() { mbar_arrive(&empty[slot]); }
+    // get by a whole warp, which then gives the place back
+    __device__ __forceinline__ bool take(Segment &s, volatile int *abort, void *ws, int where) {
+        const bool ok = __all_sync(0xffffffffu, get(s, abort, ws, where));
+        if (ok && (threadIdx.x & 31) == 0) release();
+        step();
+        return ok;
+    }
+};
+
 template <int DP>
-__global__ void __launch_bounds__(ATC_THREADS) attn_tc_kernel(const __grid_constant__ AtcMaps maps,
+__global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_constant__ AtcMaps maps,
                                                               const __grid_constant__ AtcParams prm) {
     using Cfg = AtcCfg<DP>;
     constexpr int KT = Cfg::KT, NS = Cfg::NS, CB = Cfg::CB;
@@ -161,13 +229,16 @@ __global__ void __launch_bounds__(ATC_THREADS) attn_tc_kernel(const __grid_const
     const int n_slots = prm.n_slots;
     uint64_t *const bars = reinterpret_cast<uint64_t *>(s_kv + n_slots * Cfg::KV_BYTES);
     uint64_t *const kv_full = bars, *const kv_empty = bars + 10, *const v_ok = bars + 20, *const q_full = bars + 30,
-                   *const q_empty = bars + 32, *const s_full = bars + 34, *const p_ready = bars + 36, *const o_full = bars + 38;
-    uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(bars + ATC_BARS);
+                   *const q_empty = bars + 32, *const s_full = bars + 34, *const p_ready = bars + 36, *const o_full = bars + 38,
+                   *const seg_full = bars + 40, *const seg_empty = bars + 44;
+    Segment *const segs = reinterpret_cast<Segment *>(bars + ATC_BARS);
+    uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(segs + ATC_SEGS);
     volatile int *const abort = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    long long *const bases = reinterpret_cast<long long *>(bars + ATC_BARS + 1);
+    long long *const bases = reinterpret_cast<long long *>(tmem_slot + 2);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_launch_dependents();
+    if (tid < 3) prefetch_tensormap(tid == 0 ? &maps.q : tid == 1 ? &maps.k : &maps.v);
     if (tid == 0) {
         for (int i = 0; i < n_slots; ++i) {
             mbar_init(&kv_full[i], 1);
@@ -180,6 +251,10 @@ __global__ void __launch_bounds__(ATC_THREADS) attn_tc_kernel(const __grid_const
             mbar_init(&s_full[i], 1);
             mbar_init(&p_ready[i], 4);  // one arrival per warp of the group
             mbar_init(&o_full[i], 1);
+        }
+        for (int i = 0; i < ATC_SEGS; ++i) {
+            mbar_init(&seg_full[i], 1);
+            mbar_init(&seg_empty[i], 3 + 4 * NS);  // producer, issuer, value warp, softmax warps
         }
         *abort = 0;
         mbar_fence_init();
@@ -194,34 +269,33 @@ __global__ void __launch_bounds__(ATC_THREADS) attn_tc_kernel(const __grid_const
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = *tmem_slot;
-    const long long g0 = attn_share(W, G, blockIdx.x), g_end = attn_share(W, G, blockIdx.x + 1);
+    SegReader seg{0, 0, seg_full, seg_empty, segs};
 
     if (warp == 0) {
         // ---------------- TMA producer ----------------
-        SegWalk w;
-        w.start(p, bases, g0, g_end);
-        uint32_t kv = 0, nq = 0;  // ring slots and query buffers handed out so far
+        Segment w;
+        uint32_t kv_n = 0, nq = 0;  // ring slots and query buffers handed out so far
+        Ring kv{0, 0};
         bool ok = true;
         const int per_tile = KT / prm.box_rows;  // boxes per 64-entry block
-        do {
-            const int q_tiles = NS == 2 && !w.j.alt ? 2 : 1;
+        while (ok && (ok = seg.take(w, abort, p.ws, 49)) && w.n > 0) {
+            const int q_tiles = NS == 2 && !w.alt ? 2 : 1;
             for (int r = 0; r < q_tiles && ok; ++r, ++nq) {
                 const int b = nq % NS;
                 if (nq >= NS) ok = warp_wait(&q_empty[b], (nq / NS - 1) & 1, abort, p.ws, 50);
                 if (ok && lane == 0) {
                     mbar_arrive_expect_tx(&q_full[b], CB * prm.q_box_bytes);
                     for (int c = 0; c < CB; ++c)
-                        tma_load_3d(s_q + b * Cfg::Q_BYTES + c * (ATC_ROWS * 128), &maps.q, c * 64, w.j.head * p.group,
-                                    w.j.tok0 + r * p.tile_tokens, &q_full[b]);
+                        tma_load_3d(s_q + b * Cfg::Q_BYTES + c * (ATC_ROWS * 128), &maps.q, c * 64, w.head * p.group,
+                                    w.tok0 + r * p.tile_tokens, &q_full[b]);
                 }
             }
-            const int t0 = w.first_tile(), n = w.tiles();
-            for (int t = 0; t < n && ok; ++t) {
-                const KeyTile k = key_tile(p, w.j, t0 + t);
-                for (int which = 0; which < 2 && ok; ++which, ++kv) {
-                    const int slot = kv % n_slots;
-                    if (kv >= (uint32_t)n_slots) ok = warp_wait(&kv_empty[slot], (kv / n_slots - 1) & 1, abort, p.ws, 51);
-                    if (!ok) break;
+            for (int t = 0; t < w.n && ok; ++t) {
+                const KeyTile k = key_tile(p, w, w.t0 + t);
+                const int *const pages = k.prefix ? p.prefix_pages : p.page_table + (long long)w.seq * p.table_stride;
+                for (int which = 0; which < 2; ++which) {
+                    const uint32_t slot = kv.slot;
+                    if (kv_n >= (uint32_t)n_slots && !(ok = warp_wait(&kv_empty[slot], kv.parity ^ 1u, abort, p.ws, 51))) break;
                     if (lane == 0) mbar_arrive_expect_tx(&kv_full[slot], Cfg::KV_BYTES);
                     __syncwarp();
                     for (int i = lane; i < per_tile * CB; i += 32) {
@@ -229,23 +303,25 @@ __global__ void __launch_bounds__(ATC_THREADS) attn_tc_kernel(const __grid_const
                         // a box behind the last key: a page that is not there reads as zeros
                         int page = p.n_pages;
                         if (key < k.len) {
-                            page = __ldg(k.pages + (key >> p.page_shift));
+                            page = __ldg(pages + (key >> p.page_shift));
                             if (page < 0 || page >= p.n_pages) {
-                                raise_status(p.ws, DEV_STATUS_BAD_INDEX, 42);
+                                attn_bad(p.ws, 42);
                                 page = p.n_pages;
                             }
                         }
                         tma_load_4d(s_kv + slot * Cfg::KV_BYTES + c * (KT * 128) + r * prm.box_rows * 128, which ? &maps.v : &maps.k,
-                                    c * 64, key & ((1 << p.page_shift) - 1), w.j.head, page, &kv_full[slot]);
+                                    c * 64, key & ((1 << p.page_shift) - 1), w.head, page, &kv_full[slot]);
                     }
                     __syncwarp();
+                    kv.step(1, n_slots);
+                    ++kv_n;
                 }
             }
-        } while (ok && w.next(p, bases));
+        }
         // stay until every copy that was started has landed
         if (lane == 0) {
             const long long t_0 = clock64();
-            for (uint32_t i = kv > (uint32_t)n_slots ? kv - n_slots : 0; i < kv; ++i)
+            for (uint32_t i = kv_n > (uint32_t)n_slots ? kv_n - n_slots : 0; i < kv_n; ++i)
                 while (!mbar_try_wait(&kv_full[i % n_slots], (i / n_slots) & 1))
                     if (clock64() - t_0 > WAIT_LIMIT_CYCLES) break;
             for (uint32_t i = nq > (uint32_t)NS ? nq - NS : 0; i < nq; ++i)
@@ -254,80 +330,99 @@ __global__ void __launch_bounds__(ATC_THREADS) attn_tc_kernel(const __grid_const
         }
     } else if (warp == 1) {
         // ---------------- MMA issuer ----------------
-        if (lane == 0) {
-            constexpr uint32_t ID_QK = umma_idesc(ATC_ROWS, KT), ID_PV = umma_idesc(ATC_ROWS, DP) | (1u << 16);
-            SegWalk a, b;  // where S = Q K^T stands, and where P V
-            a.start(p, bases, g0, g_end);
-            b = a;
-            bool a_more = true, ok = true;
-            uint32_t ua = 0, Ua = 0, kva = 0, qa = 0;  // a's unit in its segment, unit of the CTA, first ring slot and query buffer of the segment
-            uint32_t ub = 0, kvb = 0;
-            const auto units = [](const SegWalk &w) { return (uint32_t)w.tiles() * (NS == 2 && !w.j.alt ? 2u : 1u); };
-
-            const auto issue_qk = [&]() -> bool {
-                const bool dual = NS == 2 && !a.j.alt;
-                const uint32_t n = units(a), t = dual ? ua >> 1 : ua, qi = qa + (dual ? ua & 1 : 0), qb = qi % NS;
-                const uint32_t slot = (kva + 2 * t) % n_slots;
-                if (ua < (dual ? 2u : 1u) && !wait_or_abort(&q_full[qb], (qi / NS) & 1, abort, p.ws, 52)) return false;
-                if (!wait_or_abort(&kv_full[slot], ((kva + 2 * t) / n_slots) & 1, abort, p.ws, 53)) return false;
+        // (the whole warp walks, one lane issues: the operands stay in uniform registers)
+        constexpr uint32_t ID_QK = umma_idesc(ATC_ROWS, KT), ID_PV = umma_idesc(ATC_ROWS, DP) | (1u << 16);
+        // Where S = Q K^T stands (a) and where P V (b): unit in its segment, units in it, whether blocks of two row tiles.
+        SegReader seg_b = seg;
+        bool a_dual = false, b_dual = false;
+        uint32_t a_n = 0, b_n = 0, a_u = 0, b_u = 0;
+        uint32_t a_U = 0, b_U = 0, qi = 0;  // units of the CTA; first query buffer of a's segment
+        Ring ka{0, 0}, vb{1, 0}, okb{0, 0}; // ring places of the next key tile, of the next value tile, and the latter's v_ok
+        const uint64_t q_desc = smem_desc_sw128(s_q, 0), k_desc = smem_desc_sw128(s_kv, 0), v_desc = smem_desc_mn_sw128(s_kv, 0, KT * 128);
+        const auto next_segment = [&](SegReader &r, uint32_t &n, bool &dual, bool last_reader) -> bool {
+            if (!warp_wait(&r.full[r.slot], r.parity, abort, p.ws, 48)) return false;
+            const Segment &s = r.ring[r.slot];
+            dual = NS == 2 && uniform(s.alt) == 0;
+            n = uniform(s.n) << (dual ? 1 : 0);
+            __syncwarp();
+            if (last_reader && elect_one()) r.release();
+            r.step();
+            return true;
+        };
+        bool ok = next_segment(seg, a_n, a_dual, false) && next_segment(seg_b, b_n, b_dual, true);
+        uint32_t ahead = 0;  // units whose S has been issued and P V not: two in front of every P V
+        while (ok && b_n > 0) {
+            if (ahead < 2 && a_n > 0) {
+                const uint32_t q_at = qi + (a_dual ? a_u & 1 : 0), qb = NS == 2 ? q_at & 1 : 0;
+                if (a_u < (a_dual ? 2u : 1u) && !(ok = warp_wait(&q_full[qb], (NS == 2 ? q_at >> 1 : q_at) & 1, abort, p.ws, 52))) break;
+                if (!(ok = warp_wait(&kv_full[ka.slot], ka.parity, abort, p.ws, 53))) break;
                 tc_fence_after_sync();
-                const uint8_t *const q = s_q + qb * Cfg::Q_BYTES, *const k = s_kv + slot * Cfg::KV_BYTES;
-                const uint32_t d = tmem + (Ua & 1) * KT;
+                const uint64_t q = q_desc + (uint64_t)(qb * (Cfg::Q_BYTES >> 4)), k = k_desc + (uint64_t)(ka.slot * (Cfg::KV_BYTES >> 4));
+                const uint32_t d = tmem + (a_U & 1) * KT;
+                const bool k_done = !a_dual || (a_u & 1), q_done = a_u + (a_dual ? 2 : 1) >= a_n;
+                if (elect_one()) {
 #pragma unroll
-                for (int kk = 0; kk < DP / 16; ++kk)
-                    umma_bf16(d, smem_desc_sw128(q + (kk >> 2) * (ATC_ROWS * 128), kk & 3),
-                              smem_desc_sw128(k + (kk >> 2) * (KT * 128), kk & 3), ID_QK, kk > 0);
-                umma_commit(&s_full[Ua & 1]);
-                if (!dual || (ua & 1)) umma_commit(&kv_empty[slot]);
-                if (ua + (dual ? 2 : 1) >= n) umma_commit(&q_empty[qb]);
-                ++Ua;
-                if (++ua == n) {
-                    qa += dual ? 2 : 1;
-                    kva += 2 * a.tiles();
-                    ua = 0;
-                    a_more = a.next(p, bases);
+                    for (int kk = 0; kk < DP / 16; ++kk)
+                        umma_bf16(d, q + (uint64_t)(((kk >> 2) * (ATC_ROWS * 128) + (kk & 3) * 32) >> 4),
+                                  k + (uint64_t)(((kk >> 2) * (KT * 128) + (kk & 3) * 32) >> 4), ID_QK, kk > 0);
+                    umma_commit(&s_full[a_U & 1]);
+                    if (k_done) umma_commit(&kv_empty[ka.slot]);
+                    if (q_done) umma_commit(&q_empty[qb]);
                 }
-                return true;
-            };
-            ok = issue_qk() && (!a_more || issue_qk());
-            bool b_more = true;
-            for (uint32_t U = 0; ok && b_more; ++U) {
-                const bool dual = NS == 2 && !b.j.alt;
-                const uint32_t n = units(b), t = dual ? ub >> 1 : ub, vi = kvb + 2 * t + 1, slot = vi % n_slots, vt = vi >> 1;
-                if (!wait_or_abort(&kv_full[slot], (vi / n_slots) & 1, abort, p.ws, 54)) break;
-                if (!wait_or_abort(&v_ok[vt % n_slots], (vt / n_slots) & 1, abort, p.ws, 54)) break;
-                if (!wait_or_abort(&p_ready[U & 1], (U >> 1) & 1, abort, p.ws, 55)) break;
-                tc_fence_after_sync();
-                const uint32_t o = NS == 2 ? U & 1 : 0;
-                const uint8_t *const v = s_kv + slot * Cfg::KV_BYTES;
+                __syncwarp();
+                if (k_done) ka.step(2, n_slots);
+                ++a_U;
+                ++ahead;
+                if (++a_u == a_n) {
+                    qi += a_dual ? 2 : 1;
+                    a_u = 0;
+                    ok = next_segment(seg, a_n, a_dual, false);
+                }
+                continue;
+            }
+            if (!warp_wait(&kv_full[vb.slot], vb.parity, abort, p.ws, 54)) break;
+            if (!warp_wait(&v_ok[okb.slot], okb.parity, abort, p.ws, 54)) break;
+            if (!warp_wait(&p_ready[b_U & 1], (b_U >> 1) & 1, abort, p.ws, 55)) break;
+            tc_fence_after_sync();
+            const uint32_t o = NS == 2 ? b_U & 1 : 0, d = tmem + Cfg::O_COL + o * DP, pt = tmem + (b_U & 1) * KT;
+            const uint64_t v = v_desc + (uint64_t)(vb.slot * (Cfg::KV_BYTES >> 4));
+            const uint32_t add = b_u >= NS;
+            const bool v_done = !b_dual || (b_u & 1);
+            if (elect_one()) {
 #pragma unroll
-                for (int kk = 0; kk < KT / 16; ++kk)
-                    umma_bf16_ts(tmem + Cfg::O_COL + o * DP, tmem + (U & 1) * KT + kk * 8, smem_desc_mn_sw128(v, kk, KT * 128),
-                                 ID_PV, ub >= NS || kk > 0);
-                if (!dual || (ub & 1)) umma_commit(&kv_empty[slot]);
-                if (NS == 1 || ub + 2 >= n) umma_commit(&o_full[o]);
-                if (a_more) ok = issue_qk();
-                if (++ub == n) {
-                    kvb += 2 * b.tiles();
-                    ub = 0;
-                    b_more = b.next(p, bases);
-                }
+                for (int kk = 0; kk < KT / 16; ++kk) umma_bf16_ts(d, pt + kk * 8, v + (uint64_t)(kk * (2048 >> 4)), ID_PV, kk > 0 ? 1 : add);
+                if (v_done) umma_commit(&kv_empty[vb.slot]);
+                if (NS == 1 || b_u + 2 >= b_n) umma_commit(&o_full[o]);
+            }
+            __syncwarp();
+            if (v_done) {
+                vb.step(2, n_slots);
+                okb.step(1, n_slots);
+            }
+            --ahead;
+            ++b_U;
+            if (++b_u == b_n) {
+                b_u = 0;
+                ok = next_segment(seg_b, b_n, b_dual, true);
             }
         }
     } else if (warp == 2) {
         // ---------------- value tiles: rows that no key stands for become zeros ----------------
-        SegWalk w;
-        w.start(p, bases, g0, g_end);
-        uint32_t vt = 0;
+        Segment w;
+        // (It waits for the key tiles too: a wait for a slot's n-th filling may only begin when the one before has been
+        // seen, or the parity of an older one passes for it.)
+        Ring kv{0, 0}, done{0, 0};
         bool ok = true;
-        do {
-            const int t0 = w.first_tile(), n = w.tiles();
-            for (int t = 0; t < n && ok; ++t, ++vt) {
-                const KeyTile k = key_tile(p, w.j, t0 + t);
-                const uint32_t vi = 2 * vt + 1, slot = vi % n_slots;
-                ok = warp_wait(&kv_full[slot], (vi / n_slots) & 1, abort, p.ws, 56);
+        while (ok && (ok = seg.take(w, abort, p.ws, 47)) && w.n > 0) {
+            for (int t = 0; t < w.n && ok; ++t, done.step(1, n_slots)) {
+                const KeyTile k = key_tile(p, w, w.t0 + t);
+                if (!(ok = warp_wait(&kv_full[kv.slot], kv.parity, abort, p.ws, 56))) break;
+                kv.step(1, n_slots);
+                const uint32_t slot = kv.slot;
+                if (!(ok = warp_wait(&kv_full[slot], kv.parity, abort, p.ws, 56))) break;
+                kv.step(1, n_slots);
                 const int valid = k.len - k.k0;
-                if (ok && valid < KT) {
+                if (valid < KT) {
                     for (int i = lane; i < (KT - valid) * 8 * CB; i += 32) {
                         const int c = i % CB, r = valid + i / CB / 8, e = i / CB % 8;
                         *reinterpret_cast<uint4 *>(s_kv + slot * Cfg::KV_BYTES + c * (KT * 128) + r * 128 + e * 16) = make_uint4(0, 0, 0, 0);
@@ -335,35 +430,64 @@ __global__ void __launch_bounds__(ATC_THREADS) attn_tc_kernel(const __grid_const
                     fence_proxy_async_smem();
                 }
                 __syncwarp();
-                if (ok && lane == 0) mbar_arrive(&v_ok[vt % n_slots]);
+                if (lane == 0) mbar_arrive(&v_ok[done.slot]);
             }
-        } while (ok && w.next(p, bases));
+        }
+    } else if (warp == 3) {
+        // ---------------- scheduler ----------------
+        if (lane == 0) {
+            long long g = attn_share(W, G, blockIdx.x);
+            const long long g_end = attn_share(W, G, blockIdx.x + 1);
+            AttnJob j = attn_find(p, bases, g);
+            for (uint32_t k = 0;; ++k) {
+                const uint32_t slot = k % ATC_SEGS;
+                if (k >= ATC_SEGS && !wait_bar(&seg_empty[slot], (k / ATC_SEGS - 1) & 1, abort, p.ws, 46)) break;
+                const long long stop = min(g_end, j.g1);
+                Segment s;
+                s.t0 = (int)(g - j.g0);
+                s.n = (int)(stop - g);
+                s.pre_tiles = j.seq < 0 || p.fused ? p.prefix_tiles : 0;
+                s.head = j.head;
+                s.seq = j.seq;
+                s.tok0 = j.tok0;
+                s.rows = j.rows;
+                s.seen0 = j.seen0;
+                s.own_len = j.own_len;
+                s.alt = j.alt;
+                s.first = g == j.g0;
+                s.direct = attn_direct(p, j, s.first && stop == j.g1);
+                segs[slot] = s;
+                mbar_arrive(&seg_full[slot]);
+                if (s.n == 0) break;
+                g = stop;
+                if (g < g_end) j = attn_next(p, bases, j);
+                else j.g1 = g;  // the last description: no tiles
+            }
+        }
     } else if (warp >= 4 && (NS == 2 || warp < 8)) {
         // ---------------- softmax ----------------
         const uint32_t grp = (warp - 4) >> 2;
         const int wr = (warp & 3) * 32;                            // the group's rows of this warp: wr .. wr + 31
         const uint32_t lanes = tmem + ((uint32_t)wr << 16);
         const int tile_rows = p.tile_tokens * p.group;
-        SegWalk w;
-        w.start(p, bases, g0, g_end);
+        Segment j;
         uint32_t U0 = 0, n_o = 0;  // units before this segment; segments finished by this group
         bool ok = true;
-        do {
-            const AttnJob &j = w.j;
+        while (ok && (ok = seg.take(j, abort, p.ws, 45)) && j.n > 0) {
             const bool dual = NS == 2 && !j.alt;
-            const uint32_t n = (uint32_t)w.tiles() * (dual ? 2u : 1u);
+            const uint32_t n = (uint32_t)j.n << (dual ? 1 : 0);
             uint32_t u = NS == 2 ? (U0 ^ grp) & 1 : 0;             // the group's first unit
-            const int t0 = w.first_tile(), row0 = dual ? (int)u * tile_rows : 0, r = wr + lane, row = row0 + r;
+            const int row0 = dual ? (int)u * tile_rows : 0, r = wr + lane, row = row0 + r;
             const bool valid = r < tile_rows && row < j.rows;
             const bool warp_on = wr < tile_rows && row0 + wr < j.rows;
-            const int tok = row / p.group, own_seen = j.seen0 + tok;
+            const int tok = attn_row_token(p, row), own_seen = j.seen0 + tok;
             const int stream = j.alt ? (int)u : 0;
             const bool has = u < n;
             float m = -INFINITY, l = 0.f;
             bool started = false;
             for (; u < n && ok; u += NS) {
                 const uint32_t U = U0 + u, buf = U & 1;
-                const KeyTile k = key_tile(p, j, t0 + (int)(dual ? u >> 1 : u));
+                const KeyTile k = key_tile(p, j, j.t0 + (int)(dual ? u >> 1 : u));
                 ok = warp_wait(&s_full[buf], (U >> 1) & 1, abort, p.ws, 57);
                 if (!ok) break;
                 tc_fence_after_sync();
@@ -371,19 +495,18 @@ __global__ void __launch_bounds__(ATC_THREADS) attn_tc_kernel(const __grid_const
                     const uint32_t ts = lanes + buf * KT;
                     const int lim = (k.prefix ? k.len : min(k.len, own_seen)) - k.k0;   // keys of the tile that the row sees
                     const bool masked = __any_sync(0xffffffffu, lim < KT);
-                    float mx = -INFINITY;
+                    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+                    for (int c = 0; c < KT; c += 64) {
+                        float s[64];
+                        tmem_ld64(ts + c, s);
+                        if (masked) mask_keys(s, lim - c);
 #pragma unroll
-                    for (int c = 0; c < KT; c += 32) {
-                        float s[32];
-                        tmem_ld32(ts + c, s);
-                        if (masked) {
+                        for (int i = 0; i < 64; i += 8)
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) mx = fmaxf(mx, c + i < lim ? s[i] : -INFINITY);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) mx = fmaxf(mx, s[i]);
-                        }
+                            for (int e = 0; e < 4; ++e) mx4[e] = max3(mx4[e], s[i + e], s[i + 4 + e]);
                     }
+                    float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
                     mx *= p.scale_log2;
                     // the maximum moves only when 2^(c S - m) could grow too large (or there is none yet)
                     const bool move = mx > m + ATC_SLACK || (m == -INFINITY && mx > m);
@@ -408,27 +531,30 @@ __global__ void __launch_bounds__(ATC_THREADS) attn_tc_kernel(const __grid_const
                         }
                     }
                     const float off = m == -INFINITY ? 0.f : m;
-                    float sum = 0.f;
+                    const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), off2 = make_float2(-off, -off);
+                    float2 sum[4] = {};
+#pragma unroll 1
+                    for (int c = 0; c < KT; c += 64) {
+                        float s[64];
+                        tmem_ld64(ts + c, s);
+                        if (masked) mask_keys(s, lim - c);   // 2^-inf = 0
 #pragma unroll
-                    for (int c = 0; c < KT; c += 32) {
-                        float s[32];
-                        tmem_ld32(ts + c, s);
-                        uint32_t pk[16];
-                        float e[32];
+                        for (int h = 0; h < 64; h += 32) {
+                            uint32_t pk[16];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            e[i] = fast_exp2(fmaf(s[i], p.scale_log2, -off));
-                            if (masked && c + i >= lim) e[i] = 0.f;
-                            sum += e[i];
+                            for (int i = 0; i < 16; ++i) {
+                                float2 e = fma2(make_float2(s[h + 2 * i], s[h + 2 * i + 1]), scale2, off2);
+                                e.x = fast_exp2(e.x);
+                                e.y = fast_exp2(e.y);
+                                sum[i & 3] = add2(sum[i & 3], e);
+                                const __nv_bfloat162 x = __floats2bfloat162_rn(e.x, e.y);
+                                pk[i] = *reinterpret_cast<const uint32_t *>(&x);
+                            }
+                            tmem_st16(ts + (c + h) / 2, pk);
                         }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const __nv_bfloat162 h = __floats2bfloat162_rn(e[2 * i], e[2 * i + 1]);
-                            pk[i] = *reinterpret_cast<const uint32_t *>(&h);
-                        }
-                        tmem_st16(ts + c / 2, pk);
                     }
-                    l += sum;
+                    const float2 s4 = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+                    l += s4.x + s4.y;
                     started = true;
                     tmem_wait_st();
                 }
@@ -443,10 +569,10 @@ __global__ void __launch_bounds__(ATC_THREADS) attn_tc_kernel(const __grid_const
                 if (ok && warp_on) {
                     tc_fence_after_sync();
                     const uint32_t to = lanes + Cfg::O_COL + (NS == 2 ? grp : 0) * DP;
-                    if (attn_direct(p, j, w.whole())) {
+                    if (j.direct) {
                         const float inv = l == 0.f ? 0.f : 1.0f / l;
                         __nv_bfloat16 *const dst = static_cast<__nv_bfloat16 *>(prm.out) + (j.tok0 + tok) * prm.ld_out +
-                                                   (j.head * p.group + row % p.group) * p.d;
+                                                   (j.head * p.group + row - tok * p.group) * p.d;
 #pragma unroll 1
                         for (int c = 0; c < DP; c += 32) {
                             float o[32];
@@ -468,7 +594,7 @@ __global__ void __launch_bounds__(ATC_THREADS) attn_tc_kernel(const __grid_const
                     } else {
                         PartPlace at{nullptr, nullptr};
                         if (valid) {
-                            at = attn_place(p, j, w.from_start(), stream, row);
+                            at = attn_place(p, PartJob{j.seq, j.head, j.tok0, j.alt != 0}, j.first != 0, stream, row);
                             *reinterpret_cast<float2 *>(at.ml) = make_float2(m, l);
                         }
 #pragma unroll 1
@@ -489,10 +615,10 @@ __global__ void __launch_bounds__(ATC_THREADS) attn_tc_kernel(const __grid_const
                     tc_fence_before_sync();
                 }
             } else if (ok && valid && j.alt) {  // a segment of one tile leaves the other stream empty
-                *reinterpret_cast<float2 *>(attn_place(p, j, w.from_start(), stream, row).ml) = make_float2(-INFINITY, 0.f);
+                *reinterpret_cast<float2 *>(attn_place(p, PartJob{j.seq, j.head, j.tok0, j.alt != 0}, j.first != 0, stream, row).ml) = make_float2(-INFINITY, 0.f);
             }
             U0 += n;
-        } while (ok && w.next(p, bases));
+        }
     }
 
     // ---------------- teardown: everybody meets, the allocating warp frees TMEM ----------------
@@ -535,7 +661,7 @@ template <int DP> static griffin_status launch_dp(const AttnPlan &plan, const At
             return GRIFFIN_ERR_UNSUPPORTED;  // (strides that the copy engine does not take)
     }
     // as many ring slots as fit beside the list of the sequences' first tiles
-    const size_t tail = ATC_BARS * 8 + 8 + ((size_t)plan.n_seq + 1) * 8, fixed = 1024 + Cfg::NS * Cfg::Q_BYTES + tail;
+    const size_t tail = ATC_BARS * 8 + ATC_SEGS * sizeof(Segment) + 8 + ((size_t)plan.n_seq + 1) * 8, fixed = 1024 + Cfg::NS * Cfg::Q_BYTES + tail;
     prm.n_slots = (int)((232448 - fixed) / Cfg::KV_BYTES);
     if (prm.n_slots > Cfg::MAX_SLOTS) prm.n_slots = Cfg::MAX_SLOTS;
     const size_t smem = fixed + (size_t)prm.n_slots * Cfg::KV_BYTES;
