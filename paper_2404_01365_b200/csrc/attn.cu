@@ -13,7 +13,7 @@ static AttnShape shape_of(const griffin_attn_desc *desc) {
 }
 
 struct AttnScratch {
-    size_t own_off, pre_off, cta_off, total;  // the bases are at 0
+    size_t cuts_off, own_off, pre_off, cta_off, total;  // the bases are at 0
     long long own_rows;
 };
 // (every size grows with n_tokens and n_seq, so a workspace for the largest call serves the others)
@@ -22,7 +22,8 @@ static AttnScratch attn_scratch(const griffin_attn_desc *desc, const AttnShape &
     const size_t row = (size_t)(desc->head_dim + 2) * sizeof(float), streams = sh.alt ? 2 : 1;
     const long long by_token = n_tokens * desc->n_q_heads, by_seq = n_seq * desc->n_kv_heads * 128;
     s.own_rows = ((by_token < by_seq ? by_token : by_seq) + 3) / 4 * 4;  // (16-byte alignment of what follows the rows)
-    s.own_off = ((size_t)(n_seq + 1) * 8 + 255) / 256 * 256;
+    s.cuts_off = ((size_t)(n_seq + 1) * 4 + 255) / 256 * 256;
+    s.own_off = s.cuts_off + ATTN_MAX_GRID * sizeof(CutJob);
     s.pre_off = s.own_off + streams * s.own_rows * row;
     s.cta_off = s.pre_off + (n_seq > 1 ? streams * s.own_rows * row : 0);
     s.total = s.cta_off + (size_t)ATTN_MAX_GRID * 2 * (2 * sh.tile_rows) * row;
@@ -61,7 +62,8 @@ griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_a
     p.scale_log2 = desc->scale * 1.4426950408889634f;
     p.ws = ws;
     const AttnScratch s = attn_scratch(desc, sh, p.n_tokens, p.n_seq);
-    p.bases = reinterpret_cast<long long *>(scratch);
+    p.bases = reinterpret_cast<int *>(scratch);
+    p.cuts = reinterpret_cast<CutJob *>(scratch + s.cuts_off);
     p.own = reinterpret_cast<float *>(scratch + s.own_off);
     p.pre = reinterpret_cast<float *>(scratch + s.pre_off);
     p.cta = reinterpret_cast<float *>(scratch + s.cta_off);

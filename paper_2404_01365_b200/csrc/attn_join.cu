@@ -1,36 +1,33 @@
 // Joins the partials of rows whose keys were worked on in more than one place: with M = max m_i,
 //   out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i,
 // the partials in the order of their keys (prefix, then own).  Rows that the attention kernel finished itself are
-// left alone; rows that see nothing get zeros.
+// left alone; rows that see nothing get zeros.  Bound by latency: the list of a row's partials, their m and l,
+// their outputs are three dependent trips to L2; 32 partials travel in one of each.
 #include "attn_join.cuh"
 #include "layer.h"
 
 namespace griffin {
 
 constexpr int JOIN_THREADS = 128;
+constexpr int JOIN_ROWS = 16;  // rows of a cut block that one CTA joins
 
-// The partials of one job: n segments on CTAs c0, c0 + 1, ..., `streams` of each.
+// The partials of one job: n of them on CTAs c0, c0 + 1, ..., `streams` of each.
 struct JobParts {
-    AttnJob job;
+    PartJob job;
     int c0, streams, n;
 };
-static __device__ __noinline__ JobParts job_parts(const AttnPlan &p, const AttnJob &j, long long W) {
-    JobParts r;
-    r.job = j;
-    r.streams = j.alt ? 2 : 1;
-    r.c0 = 0;
-    r.n = 0;
+__device__ __forceinline__ JobParts job_parts(const AttnPlan &p, const AttnShares &sh, const AttnJob &j) {
+    JobParts r{j, 0, j.alt ? 2 : 1, 0};
     if (j.g1 > j.g0) {
-        const int G = attn_ctas(W, p.grid);
-        r.c0 = attn_cta_of(W, G, j.g0);
-        r.n = (attn_cta_of(W, G, j.g1 - 1) - r.c0 + 1) * r.streams;
+        r.c0 = sh.cta_of(j.g0);
+        r.n = (sh.cta_of(j.g1 - 1) - r.c0 + 1) * r.streams;
     }
     return r;
 }
 __device__ __forceinline__ PartPlace part_place(const AttnPlan &p, const JobParts &a, int i, int r) {
     const int stream = a.streams == 2 ? i & 1 : 0, c = a.c0 + (a.streams == 2 ? i >> 1 : i);
-    if (c == a.c0) return attn_first_by_row(p, a.job) ? attn_place_row(p, a.job, stream, r) : attn_place_cta(p, c, 1, r);
-    return attn_place_cta(p, c, 0, a.job.alt ? stream * (p.cta_rows >> 1) + r : r);
+    if (c == a.c0 && attn_first_by_row(p, a.job)) return attn_place_row(p, a.job, stream, r);
+    return attn_place_cta(p, c, c == a.c0 ? 1 : 0, a.streams == 2 ? stream * (p.cta_rows >> 1) + r : r);
 }
 
 template <typename T> __device__ __forceinline__ void store_row4(T *to, const float (&f)[4]) {
@@ -42,171 +39,190 @@ template <typename T> __device__ __forceinline__ void store_row4(T *to, const fl
     }
 }
 
-struct JoinShared {
-    float ml[4][2];
-    float o[4][256];
-};
-
-// Rows r0 .. r1 of one job.  `wpr` warps share a row (4, 2 or 1: more when there are fewer rows), each taking a
-// stretch of its partials; their sums are added in order through shared memory.
-template <typename T>
-__device__ __noinline__ void join_rows(const AttnPlan &p, const JobParts &a, long long W, int r0, int r1, T *out, long long ld_out,
-                                          JoinShared &sh) {
+// CTAs 0 .. by_row - 1: jobs whose partials are kept by row: in a fused call the last row block of each sequence and
+// key head (no other has just one row tile) and the blocks that see nothing, else every row block.  The others
+// (fused calls): the blocks that were cut, JOIN_ROWS rows each.
+// NV: 128-entry pieces of a row (a lane has 4 entries of each).
+template <typename T, int NV>
+__global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ AttnPlan p, T *__restrict__ out,
+                                                                 long long ld_out, int by_row) {
+    __shared__ float sh_ml[4][2], sh_o[4][NV * 128];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int wpr = r1 - r0 >= 3 ? 1 : r1 - r0 == 2 ? 2 : 4, sub = warp % wpr;
-    for (int rb = r0; rb < r1; rb += 4 / wpr) {
-        const int r = rb + warp / wpr;
-        const bool on = r < r1;
-        float M = -INFINITY, sum = 0.f, acc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-        const int rt = attn_row_token(p, r), tok = a.job.tok0 + rt, head = a.job.head * p.group + r - rt * p.group;
-        if (on) {
-            JobParts pre = a;
-            int rp = 0;
-            pre.n = 0;
-            if (p.prefix_blocks > 0) {
-                const int bp = tok / p.block_tokens;
-                pre = job_parts(p, attn_prefix_job(p, a.job.head, bp), W);
-                rp = (tok - bp * p.block_tokens) * p.group + r - rt * p.group;
+    pdl_launch_dependents();
+    pdl_wait_prior_grids();
+    const AttnShares sh(p.bases[p.n_seq], p.grid);
+    JobParts a;
+    AttnSeq q{};
+    int r0 = 0, r1 = 0, head = 0, seq = 0, n_blocks = 0, b = 0;
+    bool cut = false;
+    if ((int)blockIdx.x >= by_row) {
+        const int chunks = p.cta_rows / JOIN_ROWS, c = (int)(blockIdx.x - by_row) / chunks;
+        if (c >= sh.G) return;
+        const CutJob j = p.cuts[c];
+        r0 = (int)(blockIdx.x - by_row) % chunks * JOIN_ROWS;
+        r1 = min(j.rows, r0 + JOIN_ROWS);
+        if (r0 >= r1) return;
+        a = JobParts{PartJob{0, j.head, j.tok0, false}, j.c0, 1, c - j.c0 + 1};
+        cut = true;
+    } else {
+        const int bx = (int)((uint32_t)blockIdx.x / (uint32_t)p.hkv);
+        head = blockIdx.x - bx * p.hkv;
+        seq = bx;
+        if (!p.fused) {
+            // Sequence s owns the block numbers from q_start[s] / block_tokens + s on: at least as many as it has blocks.
+            seq = -1;
+            for (int s0 = 0; s0 < p.n_seq; s0 += JOIN_THREADS) {
+                const int s = s0 + threadIdx.x;
+                seq += __syncthreads_count(s < p.n_seq && __ldg(p.q_start + s) / p.block_tokens + s <= bx);
             }
-            const int n = pre.n + a.n, per = (n + wpr - 1) / wpr, i0 = sub * per, i1 = min(n, i0 + per);
-            for (int ib = i0; ib < i1; ib += 32) {   // a lane per partial for m, l and the place of the outputs
-                const int i = ib + lane;
-                PartPlace at{nullptr, nullptr};
-                float2 ml = make_float2(-INFINITY, 0.f);
-                if (i < i1) {
-                    at = i < pre.n ? part_place(p, pre, i, rp) : part_place(p, a, i - pre.n, r);
-                    ml = *reinterpret_cast<const float2 *>(at.ml);
+            if (seq < 0) return;
+            b = bx - (__ldg(p.q_start + seq) / p.block_tokens + seq);
+        }
+        q = attn_seq(p, seq);
+        n_blocks = ceil_div(q.nq, p.block_tokens);
+        if (b >= n_blocks) return;
+    }
+#pragma unroll 1
+    for (;;) {
+        if (!cut) {
+            // this job's place among the tiles: behind those of the heads and blocks before it
+            const int base = p.bases[seq], per_head = (int)((uint32_t)(p.bases[seq + 1] - base) / (uint32_t)p.hkv);
+            if (p.fused && attn_block_tiles(p, q, b) > 0) b = n_blocks - 1;
+            int g0 = base + (head + 1) * per_head;
+#pragma unroll 1
+            for (int k = n_blocks - 1; k >= b; --k) g0 -= attn_block_tiles(p, q, k);
+            const AttnJob j = attn_own_job(p, q, seq, head, b, g0);
+            a = job_parts(p, sh, j);
+            r1 = j.rows;
+            if (p.fused && j.g1 > j.g0 && !j.alt) return;  // finished by the attention kernel, or cut
+        }
+        // Each row is joined by `wpr` warps (more when there are fewer rows), each taking a stretch of its partials; their
+        // sums are added in order through shared memory.
+        const int wpr = r1 - r0 >= 3 ? 1 : r1 - r0 == 2 ? 2 : 4, sub = warp % wpr;
+#pragma unroll 1
+        for (int rb = r0; rb < r1; rb += 4 / wpr) {
+            const int r = rb + warp / wpr;
+            const bool on = r < r1;
+            const int rt = attn_row_token(p, r), tok = a.job.tok0 + rt, hq = a.job.head * p.group + r - rt * p.group;
+            float M = -INFINITY, sum = 0.f, acc[NV][4] = {};
+            if (on) {
+                JobParts pre = a;
+                int rp = 0;
+                pre.n = 0;
+                if (p.prefix_blocks > 0) {
+                    const int bp = tok / p.block_tokens;
+                    pre = job_parts(p, sh, attn_prefix_job(p, a.job.head, bp));
+                    rp = (tok - bp * p.block_tokens) * p.group + r - rt * p.group;
                 }
-                float mb = ml.x;
+                const int n = pre.n + a.n, per = (n + wpr - 1) / wpr, i0 = sub * per, i1 = min(n, i0 + per);
+#pragma unroll 1
+                for (int ib = i0; ib < i1; ib += 32) {  // a lane per partial for m, l and the place of the outputs
+                    const int i = ib + lane;
+                    PartPlace at{nullptr, nullptr};
+                    float2 ml = make_float2(-INFINITY, 0.f);
+                    if (i < i1) {
+                        const bool of_prefix = i < pre.n;
+                        at = part_place(p, of_prefix ? pre : a, of_prefix ? i : i - pre.n, of_prefix ? rp : r);
+                        ml = *reinterpret_cast<const float2 *>(at.ml);
+                    }
+                    float mb = ml.x;
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, o));
-                const float m_new = fmaxf(M, mb), f = m_new == -INFINITY ? 0.f : exp2f(M - m_new);
-                const float wgt = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m_new);
-                M = m_new;
-                sum *= f;
+                    for (int o = 16; o > 0; o >>= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, o));
+                    const float m_new = fmaxf(M, mb), f = m_new == -INFINITY ? 0.f : exp2f(M - m_new);
+                    // (a part in which the row sees nothing leaves no output)
+                    const float wgt = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m_new);
+                    if (wgt == 0.f) at.o = nullptr;
+                    M = m_new;
+                    sum = sum * f + warp_sum(wgt * ml.y);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) acc[k >> 2][k & 3] *= f;
-                const int cnt = min(32, i1 - ib);
-#pragma unroll 4
-                for (int q = 0; q < cnt; ++q) {
-                    const float w = __shfl_sync(0xffffffffu, wgt, q), l = __shfl_sync(0xffffffffu, ml.y, q);
-                    const float *src = reinterpret_cast<const float *>(
-                        __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(at.o), q));
-                    if (w == 0.f) continue;   // a part in which the row sees nothing leaves no output
-                    sum = fmaf(w, l, sum);
+                    for (int k = 0; k < NV; ++k)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int e = (k * 32 + lane) * 4;
-                        if (e >= p.d) continue;
-                        const float4 o = __ldcg(reinterpret_cast<const float4 *>(src + e));
-                        acc[k][0] = fmaf(w, o.x, acc[k][0]);
-                        acc[k][1] = fmaf(w, o.y, acc[k][1]);
-                        acc[k][2] = fmaf(w, o.z, acc[k][2]);
-                        acc[k][3] = fmaf(w, o.w, acc[k][3]);
+                        for (int c = 0; c < 4; ++c) acc[k][c] *= f;
+                    const int cnt = min(32, i1 - ib);
+#pragma unroll 1
+                    for (int s = 0; s < cnt; s += 4) {
+                        float4 o[4][NV];
+                        float w[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {   // (lanes beyond cnt hold no part)
+                            w[u] = __shfl_sync(0xffffffffu, wgt, (s + u) & 31);
+                            const float *src = reinterpret_cast<const float *>(
+                                __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(at.o), (s + u) & 31));
+#pragma unroll
+                            for (int k = 0; k < NV; ++k) {
+                                const int e = (k * 32 + lane) * 4;
+                                o[u][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                                if (src != nullptr && s + u < cnt && e < p.d) o[u][k] = *reinterpret_cast<const float4 *>(src + e);
+                            }
+                        }
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+#pragma unroll
+                            for (int k = 0; k < NV; ++k) {
+                                acc[k][0] = fmaf(w[u], o[u][k].x, acc[k][0]);
+                                acc[k][1] = fmaf(w[u], o[u][k].y, acc[k][1]);
+                                acc[k][2] = fmaf(w[u], o[u][k].z, acc[k][2]);
+                                acc[k][3] = fmaf(w[u], o[u][k].w, acc[k][3]);
+                            }
                     }
                 }
             }
-        }
-        if (wpr > 1) {
-            if (lane == 0) {
-                sh.ml[warp][0] = M;
-                sh.ml[warp][1] = sum;
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) sh.o[warp][(k * 32 + lane) * 4 + c] = acc[k][c];
-            __syncthreads();
-            if (sub == 0 && on) {
-                float m_all = M;
-                for (int s = 1; s < wpr; ++s) m_all = fmaxf(m_all, sh.ml[warp + s][0]);
-                float f = m_all == -INFINITY ? 0.f : exp2f(M - m_all);
-                sum *= f;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) acc[k >> 2][k & 3] *= f;
-                for (int s = 1; s < wpr; ++s) {
-                    f = m_all == -INFINITY ? 0.f : exp2f(sh.ml[warp + s][0] - m_all);
-                    sum = fmaf(f, sh.ml[warp + s][1], sum);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) acc[k >> 2][k & 3] = fmaf(f, sh.o[warp + s][((k >> 2) * 32 + lane) * 4 + (k & 3)], acc[k >> 2][k & 3]);
+            if (wpr > 1) {
+                if (lane == 0) {
+                    sh_ml[warp][0] = M;
+                    sh_ml[warp][1] = sum;
                 }
-                M = m_all;
-            }
-            __syncthreads();
-        }
-        if (on && sub == 0) {
-            const float inv = M == -INFINITY ? 0.f : 1.0f / sum;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int e = (k * 32 + lane) * 4;
-                if (e >= p.d) continue;
-                const float f[4] = {acc[k][0] * inv, acc[k][1] * inv, acc[k][2] * inv, acc[k][3] * inv};
-                store_row4<T>(out + tok * ld_out + head * p.d + e, f);
+                for (int k = 0; k < NV; ++k)
+                    *reinterpret_cast<float4 *>(&sh_o[warp][(k * 32 + lane) * 4]) = make_float4(acc[k][0], acc[k][1], acc[k][2], acc[k][3]);
+                __syncthreads();
+                if (sub == 0 && on) {
+                    float m_all = M;
+                    for (int s = 1; s < wpr; ++s) m_all = fmaxf(m_all, sh_ml[warp + s][0]);
+                    float own_sum = sum, own[NV][4];
+#pragma unroll
+                    for (int k = 0; k < NV; ++k)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) own[k][c] = acc[k][c], acc[k][c] = 0.f;
+                    sum = 0.f;
+#pragma unroll 1
+                    for (int s = 0; s < wpr; ++s) {
+                        const float ms = s == 0 ? M : sh_ml[warp + s][0], f = ms == -INFINITY ? 0.f : exp2f(ms - m_all);
+                        sum = fmaf(f, s == 0 ? own_sum : sh_ml[warp + s][1], sum);
+#pragma unroll
+                        for (int k = 0; k < NV; ++k)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+                                acc[k][c] = fmaf(f, s == 0 ? own[k][c] : sh_o[warp + s][(k * 32 + lane) * 4 + c], acc[k][c]);
+                    }
+                    M = m_all;
+                }
+                __syncthreads();
+            }
+            if (on && sub == 0) {
+                const float inv = M == -INFINITY ? 0.f : 1.0f / sum;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    const int e = (k * 32 + lane) * 4;
+                    const float f[4] = {acc[k][0] * inv, acc[k][1] * inv, acc[k][2] * inv, acc[k][3] * inv};
+                    if (e < p.d) store_row4<T>(out + tok * ld_out + hq * p.d + e, f);
+                }
             }
         }
+        // (blocks that see nothing come first, and in front of the last one)
+        if (cut || !p.fused || ++b >= n_blocks) return;
     }
-}
-
-constexpr int JOIN_ROWS = 16;  // rows of a cut block that one CTA joins
-
-// CTAs 0 .. by_row: jobs whose partials are kept by row: in a fused call the last row block of each sequence and key
-// head (no other has just one row tile), else every row block.  The others (fused calls): the jobs that are
-// cut at a CTA's first tile, JOIN_ROWS rows each.
-template <typename T>
-__global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ AttnPlan p, T *__restrict__ out,
-                                                                 long long ld_out, int by_row) {
-    __shared__ JoinShared sh;
-    pdl_launch_dependents();
-    pdl_wait_prior_grids();
-    const long long W = p.bases[p.n_seq];
-    const int G = attn_ctas(W, p.grid);
-    if ((int)blockIdx.x >= by_row) {
-        const int chunks = p.cta_rows / JOIN_ROWS, c = (blockIdx.x - by_row) / chunks, r0 = (blockIdx.x - by_row) % chunks * JOIN_ROWS;
-        if (c >= G) return;
-        const long long g = attn_share(W, G, c);
-        const AttnJob j = attn_find(p, p.bases, g);
-        // (the CTA with the job's last tile: every cut job is met once)
-        if (g == j.g0 || attn_first_by_row(p, j) || attn_share(W, G, c + 1) < j.g1 || r0 >= j.rows) return;
-        join_rows<T>(p, job_parts(p, j, W), W, r0, min(j.rows, r0 + JOIN_ROWS), out, ld_out, sh);
-        return;
-    }
-    const int head = blockIdx.x % p.hkv, bx = blockIdx.x / p.hkv;
-    if (p.fused) {
-        const AttnSeq q = attn_seq(p, bx);
-        const int n_blocks = ceil_div(q.nq, p.block_tokens);
-        const long long per_head = attn_div(p.bases[bx + 1] - p.bases[bx], p.hkv), g1 = p.bases[bx] + (head + 1) * per_head;
-        for (int b = 0; b < n_blocks && attn_block_tiles(p, q, b) == 0; ++b) {  // rows that see nothing
-            const AttnJob j = attn_own_job(p, q, bx, head, b, g1);
-            join_rows<T>(p, job_parts(p, j, W), W, 0, j.rows, out, ld_out, sh);
-        }
-        if (n_blocks == 0) return;
-        const int n = attn_block_tiles(p, q, n_blocks - 1);
-        const AttnJob j = attn_own_job(p, q, bx, head, n_blocks - 1, g1 - n);
-        if (n > 0 && j.alt) join_rows<T>(p, job_parts(p, j, W), W, 0, j.rows, out, ld_out, sh);
-        return;
-    }
-    // Sequence s owns the block numbers from q_start[s] / block_tokens + s on: at least as many as it has blocks.
-    int seq = -1;
-    for (int s0 = 0; s0 < p.n_seq; s0 += JOIN_THREADS) {
-        const int s = s0 + threadIdx.x;
-        seq += __syncthreads_count(s < p.n_seq && __ldg(p.q_start + s) / p.block_tokens + s <= bx);
-    }
-    if (seq < 0) return;
-    const AttnSeq q = attn_seq(p, seq);
-    const int b = bx - (__ldg(p.q_start + seq) / p.block_tokens + seq);
-    if (b * p.block_tokens >= q.nq) return;
-    long long g0 = p.bases[seq] + head * attn_div(p.bases[seq + 1] - p.bases[seq], p.hkv);
-    for (int k = 0; k < b; ++k) g0 += attn_block_tiles(p, q, k);
-    const AttnJob j = attn_own_job(p, q, seq, head, b, g0);
-    join_rows<T>(p, job_parts(p, j, W), W, 0, j.rows, out, ld_out, sh);
 }
 
 griffin_status launch_attn_join(const AttnPlan &plan, int dtype, void *out, long long ld_out, cudaStream_t stream) {
     AttnPlan p = plan;
     int by_row = p.hkv * (p.fused ? p.n_seq : p.n_seq + p.n_tokens / p.block_tokens);
-    const int cut = p.fused ? p.grid * (p.cta_rows / JOIN_ROWS) : 0;
-    const void *fn = dtype == GRIFFIN_DT_F32 ? reinterpret_cast<const void *>(attn_join_kernel<float>)
-                                             : reinterpret_cast<const void *>(attn_join_kernel<__nv_bfloat16>);
+    // (with no more tokens than a row tile takes, no block has several; a kernel without streams cuts those too)
+    const int cut = p.fused && (!p.alt || p.n_tokens > p.tile_tokens) ? p.grid * (p.cta_rows / JOIN_ROWS) : 0;
+    const void *fn = dtype == GRIFFIN_DT_F32 ? (p.d <= 128 ? reinterpret_cast<const void *>(attn_join_kernel<float, 1>)
+                                                           : reinterpret_cast<const void *>(attn_join_kernel<float, 2>))
+                                             : (p.d <= 128 ? reinterpret_cast<const void *>(attn_join_kernel<__nv_bfloat16, 1>)
+                                                           : reinterpret_cast<const void *>(attn_join_kernel<__nv_bfloat16, 2>));
     void *args[] = {&p, &out, &ld_out, &by_row};
     return launch_maybe_overlapped(fn, dim3(by_row + cut), dim3(JOIN_THREADS), 0, stream, true, args) == cudaSuccess ? GRIFFIN_OK
                                                                                                                      : GRIFFIN_ERR_CUDA;

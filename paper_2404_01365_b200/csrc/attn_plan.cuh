@@ -37,7 +37,8 @@ struct AttnPlan {
     float scale_log2;      // scale * log2(e): logits in units of log2
     void *ws;
     // scratch (see attn_scratch)
-    long long *bases;      // [n_seq + 1]: first own tile of each sequence; the last entry is W
+    int *bases;            // [n_seq + 1]: first own tile of each sequence; the last entry is W
+    struct CutJob *cuts;   // [grid]: the cut block that ends in the CTA's first segment, for the joining kernel
     float *own, *pre;      // partials by row: [2 streams][rows]: m and l, then the outputs
     float *cta;            // partials by CTA: [grid][2: continued from before / going on behind][2 * tile_rows]
     long long own_rows;
@@ -63,11 +64,6 @@ __host__ __device__ inline bool attn_fused(int n_seq, int n_tokens, int group, i
 
 // row (of a block) / query heads per key head
 __device__ __forceinline__ int attn_row_token(const AttnPlan &p, int row) { return (int)(((uint32_t)row * p.group_inv) >> 16); }
-
-// Quotient of non-negative numbers that nearly always fit in 32 bits (a 64-bit division is a long routine).
-__host__ __device__ inline long long attn_div(long long a, long long b) {
-    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
-}
 
 __host__ __device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
@@ -96,17 +92,21 @@ __device__ __forceinline__ int attn_block_tiles(const AttnPlan &p, const AttnSeq
     return (p.fused ? p.prefix_tiles : 0) + ((max(last, 0) + (1 << p.kt_shift) - 1) >> p.kt_shift);
 }
 
-// CTAs that have work (every one of them at least a tile), first tile of CTA c, and the CTA that has tile g: the
-// first W mod G CTAs have a tile more than the others.
-__host__ __device__ inline int attn_ctas(long long W, int grid) { return W < grid ? (int)W : grid; }
-__host__ __device__ inline long long attn_share(long long W, int G, int c) {
-    const long long q = attn_div(W, G), r = W - q * G;
-    return c * q + (c < r ? c : r);
-}
-__host__ __device__ inline int attn_cta_of(long long W, int G, long long g) {
-    const long long q = attn_div(W, G), r = W - q * G, lead = r * (q + 1);
-    return (int)(g < lead ? attn_div(g, q + 1) : r + attn_div(g - lead, q));
-}
+// The shares: G CTAs have work (every one of them at least a tile), the first `more` of them each a tile more.
+struct AttnShares {
+    int W, G, each, more;
+    __device__ __forceinline__ AttnShares(int W_, int grid) : W(W_), G(W_ < grid ? W_ : grid), each(0), more(0) {
+        if (G > 0) {
+            each = (int)((uint32_t)W / (uint32_t)G);
+            more = W - each * G;
+        }
+    }
+    __device__ __forceinline__ int first(int c) const { return c * each + min(c, more); }   // first tile of CTA c
+    __device__ __forceinline__ int cta_of(int g) const {                                    // the CTA that has tile g
+        const int lead = more * (each + 1);
+        return g < lead ? (int)((uint32_t)g / (uint32_t)(each + 1)) : more + (int)((uint32_t)(g - lead) / (uint32_t)each);
+    }
+};
 
 // What says where a job's partials are.
 struct PartJob {
@@ -116,7 +116,7 @@ struct PartJob {
     bool alt;
 };
 struct AttnJob : PartJob {
-    long long g0, g1;     // its tiles
+    int g0, g1;           // its tiles
     int n_tok;            // its rows' tokens
     int block;            // row block of its sequence
     int seen0;            // own tokens that the first of them sees (the next one sees one more)
@@ -131,7 +131,7 @@ __device__ __forceinline__ AttnJob attn_prefix_job(const AttnPlan &p, int head, 
     j.block = b;
     j.tok0 = b * p.block_tokens;
     j.n_tok = min(p.block_tokens, p.n_tokens - j.tok0);
-    j.g0 = (long long)(head * p.prefix_blocks + b) * p.prefix_tiles;
+    j.g0 = (head * p.prefix_blocks + b) * p.prefix_tiles;
     j.g1 = j.g0 + p.prefix_tiles;
     j.seen0 = 0;
     j.own_len = 0;
@@ -140,7 +140,7 @@ __device__ __forceinline__ AttnJob attn_prefix_job(const AttnPlan &p, int head, 
     return j;
 }
 
-__device__ __forceinline__ AttnJob attn_own_job(const AttnPlan &p, const AttnSeq &q, int s, int head, int b, long long g0) {
+__device__ __forceinline__ AttnJob attn_own_job(const AttnPlan &p, const AttnSeq &q, int s, int head, int b, int g0) {
     AttnJob j;
     j.g0 = g0;
     j.g1 = g0 + attn_block_tiles(p, q, b);
@@ -166,25 +166,37 @@ static __device__ __noinline__ long long attn_seq_tiles(const AttnPlan &p, const
 
 // First tile of every sequence into bases[0 .. n_seq] (shared memory), by all threads of the CTA; bases[n_seq] is
 // the number of tiles of the call.  The first CTA also leaves them in the scratch for the joining kernel.
-__device__ __forceinline__ void attn_scan(const AttnPlan &p, long long *bases) {
+// A call of 2^31 tiles or more (10^14 bytes of keys) is not run: no tiles, and the status word is raised.
+__device__ __forceinline__ void attn_scan(const AttnPlan &p, int *bases) {
     const int lane = threadIdx.x & 31;
-    for (int s = threadIdx.x; s < p.n_seq; s += blockDim.x) bases[s] = attn_seq_tiles(p, attn_seq(p, s)) * p.hkv;
+    const long long most = 1ll << 31;
+    for (int s = threadIdx.x; s < p.n_seq; s += blockDim.x) {
+        const long long n = attn_seq_tiles(p, attn_seq(p, s)) * p.hkv;
+        bases[s] = n < most ? (int)n : -1;
+    }
     __syncthreads();
     if (threadIdx.x < 32) {
         long long sum = (long long)p.hkv * p.prefix_blocks * p.prefix_tiles;
+        bool bad = false;
+#pragma unroll 1
         for (int s0 = 0; s0 < p.n_seq; s0 += 32) {
             const int s = s0 + lane;
             const long long mine = s < p.n_seq ? bases[s] : 0;
+            bad |= mine < 0;
             long long upto = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const long long v = __shfl_up_sync(0xffffffffu, upto, o);
                 if (lane >= o) upto += v;
             }
-            if (s < p.n_seq) bases[s] = sum + upto - mine;
+            if (s < p.n_seq) bases[s] = (int)(sum + upto - mine);
             sum += __shfl_sync(0xffffffffu, upto, 31);
         }
-        if (lane == 0) bases[p.n_seq] = sum;
+        bad = __any_sync(0xffffffffu, bad) || sum >= most;
+        if (lane == 0) {
+            bases[p.n_seq] = bad ? 0 : (int)sum;
+            if (bad) attn_bad(p.ws, 43);
+        }
     }
     __syncthreads();
     if (blockIdx.x == 0)
@@ -193,21 +205,21 @@ __device__ __forceinline__ void attn_scan(const AttnPlan &p, long long *bases) {
 
 // (Not inlined: the schedule's code would otherwise be most of a kernel's, and instruction fetches its time.)
 // The job that has tile g (one exists: g < bases[n_seq]).
-static __device__ __noinline__ AttnJob attn_find(const AttnPlan &p, const long long *bases, long long g) {
+static __device__ __noinline__ AttnJob attn_find(const AttnPlan &p, const int *bases, int g) {
     if (g < bases[0]) {
-        const int hb = (int)attn_div(g, p.prefix_tiles);
-        return attn_prefix_job(p, hb / p.prefix_blocks, hb % p.prefix_blocks);
+        const int hb = (int)((uint32_t)g / (uint32_t)p.prefix_tiles), head = (int)((uint32_t)hb / (uint32_t)p.prefix_blocks);
+        return attn_prefix_job(p, head, hb - head * p.prefix_blocks);
     }
     int lo = 0, hi = p.n_seq;  // bases[lo] <= g < bases[hi]
+#pragma unroll 1
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (bases[mid] <= g) lo = mid; else hi = mid;
     }
     const AttnSeq q = attn_seq(p, lo);
-    const long long per_head = attn_div(bases[lo + 1] - bases[lo], p.hkv);
-    const int head = (int)attn_div(g - bases[lo], per_head);
-    long long at = bases[lo] + head * per_head;
-    int b = 0;
+    const int per_head = (int)((uint32_t)(bases[lo + 1] - bases[lo]) / (uint32_t)p.hkv);
+    const int head = (int)((uint32_t)(g - bases[lo]) / (uint32_t)per_head);
+    int at = bases[lo] + head * per_head, b = 0;
 #pragma unroll 1
     for (;; ++b) {
         const int n = attn_block_tiles(p, q, b);
@@ -217,7 +229,7 @@ static __device__ __noinline__ AttnJob attn_find(const AttnPlan &p, const long l
     return attn_own_job(p, q, lo, head, b, at);
 }
 // The job behind j, whose first tile is j.g1 < bases[n_seq].
-static __device__ __noinline__ AttnJob attn_next(const AttnPlan &p, const long long *bases, const AttnJob &j) {
+static __device__ __noinline__ AttnJob attn_next(const AttnPlan &p, const int *bases, const AttnJob &j) {
     int s = j.seq, head = j.head, b = j.block + 1;
     if (s < 0) {
         if (j.g1 < bases[0]) return b < p.prefix_blocks ? attn_prefix_job(p, head, b) : attn_prefix_job(p, head + 1, 0);
@@ -253,5 +265,14 @@ __device__ __forceinline__ long long attn_part_row(const AttnPlan &p, const Part
 // Where the first segment of a job (the one with its first tile) leaves its partials: by row, or with the
 // CTA when a block of several row tiles is cut in a fused call.
 __device__ __forceinline__ bool attn_first_by_row(const AttnPlan &p, const PartJob &j) { return j.alt || !p.fused; }
+
+// A block of several row tiles that was cut in a fused call, noted by the CTA that has its last tile.
+struct __align__(16) CutJob {
+    int head, tok0, rows, c0;   // rows 0: none; c0: the CTA with its first tile
+};
+__device__ __forceinline__ void attn_note_cut(const AttnPlan &p, const AttnShares &sh, const AttnJob &j, int g, int stop) {
+    const bool cut = g > j.g0 && stop == j.g1 && !attn_first_by_row(p, j);
+    p.cuts[blockIdx.x] = CutJob{j.head, j.tok0, cut ? j.rows : 0, cut ? sh.cta_of(j.g0) : 0};
+}
 
 }  // namespace griffin

@@ -13,7 +13,7 @@ constexpr int SIMT_ROWS = 64, SIMT_KT = 32, SIMT_THREADS = 256;
 
 template <int DP> constexpr size_t simt_smem(int n_seq) {
     return (size_t)(SIMT_ROWS + 2 * SIMT_KT) * (DP + 4) * 4 + SIMT_ROWS * (SIMT_KT + 1) * 4 + 3 * SIMT_ROWS * 4 +
-           ((size_t)n_seq + 1) * 8 + 16;
+           ((size_t)n_seq + 1) * 4;
 }
 
 // DP: the head's width rounded up to 64, 128 or 256; entries from D on are zeros in shared memory.
@@ -24,20 +24,20 @@ __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_co
     extern __shared__ __align__(16) uint8_t smem_raw[];
     float *const sq = reinterpret_cast<float *>(smem_raw), *const sk = sq + SIMT_ROWS * LD, *const sv = sk + SIMT_KT * LD;
     float *const ss = sv + SIMT_KT * LD, *const sm = ss + SIMT_ROWS * (SIMT_KT + 1), *const sl = sm + SIMT_ROWS, *const sf = sl + SIMT_ROWS;
-    long long *const bases = reinterpret_cast<long long *>((reinterpret_cast<uintptr_t>(sf + SIMT_ROWS) + 7) & ~uintptr_t(7));
+    int *const bases = reinterpret_cast<int *>(sf + SIMT_ROWS);
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
 
     pdl_launch_dependents();
     pdl_wait_prior_grids();
     attn_scan(p, bases);
-    const long long W = bases[p.n_seq];
-    const int G = attn_ctas(W, p.grid);
-    if ((int)blockIdx.x >= G) return;
-    long long g = attn_share(W, G, blockIdx.x);
-    const long long g_end = attn_share(W, G, blockIdx.x + 1);
+    const AttnShares shares(bases[p.n_seq], p.grid);
+    if ((int)blockIdx.x >= shares.G) return;
+    int g = shares.first(blockIdx.x);
+    const int g_end = shares.first(blockIdx.x + 1);
     AttnJob j = attn_find(p, bases, g);
+    if (tid == 0) attn_note_cut(p, shares, j, g, min(g_end, j.g1));
     for (;;) {
-        const long long stop = min(g_end, j.g1);
+        const int stop = min(g_end, j.g1);
         const bool first = g == j.g0, whole = first && stop == j.g1;
         const int pre_tiles = j.seq < 0 || p.fused ? p.prefix_tiles : 0;
         __syncthreads();  // the segment before is done with shared memory
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_co
                 for (int c = 0; c < 4; ++c) o[a][b][c] = 0.f;
 
         for (; g < stop; ++g) {
-            const int t = (int)(g - j.g0);
+            const int t = g - j.g0;
             const bool in_prefix = t < pre_tiles;
             const int k0 = (in_prefix ? t : t - pre_tiles) * SIMT_KT;       // first key of the tile
             const int len = in_prefix ? p.prefix_len : j.own_len;          // keys behind this are not there

@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
     Segment *const segs = reinterpret_cast<Segment *>(bars + ATC_BARS);
     uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(segs + ATC_SEGS);
     volatile int *const abort = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    long long *const bases = reinterpret_cast<long long *>(tmem_slot + 2);
+    int *const bases = reinterpret_cast<int *>(tmem_slot + 2);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_launch_dependents();
@@ -261,9 +261,8 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
     }
     pdl_wait_prior_grids();
     attn_scan(p, bases);
-    const long long W = bases[p.n_seq];
-    const int G = attn_ctas(W, p.grid);
-    if ((int)blockIdx.x >= G) return;
+    const AttnShares shares(bases[p.n_seq], p.grid);
+    if ((int)blockIdx.x >= shares.G) return;
     if (warp == 1) tmem_alloc(tmem_slot, 512);
     tc_fence_before_sync();
     __syncthreads();
@@ -436,16 +435,17 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
     } else if (warp == 3) {
         // ---------------- scheduler ----------------
         if (lane == 0) {
-            long long g = attn_share(W, G, blockIdx.x);
-            const long long g_end = attn_share(W, G, blockIdx.x + 1);
+            int g = shares.first(blockIdx.x);
+            const int g_end = shares.first(blockIdx.x + 1);
             AttnJob j = attn_find(p, bases, g);
+            attn_note_cut(p, shares, j, g, min(g_end, j.g1));
             for (uint32_t k = 0;; ++k) {
                 const uint32_t slot = k % ATC_SEGS;
                 if (k >= ATC_SEGS && !wait_bar(&seg_empty[slot], (k / ATC_SEGS - 1) & 1, abort, p.ws, 46)) break;
-                const long long stop = min(g_end, j.g1);
+                const int stop = min(g_end, j.g1);
                 Segment s;
-                s.t0 = (int)(g - j.g0);
-                s.n = (int)(stop - g);
+                s.t0 = g - j.g0;
+                s.n = stop - g;
                 s.pre_tiles = j.seq < 0 || p.fused ? p.prefix_tiles : 0;
                 s.head = j.head;
                 s.seq = j.seq;
@@ -661,7 +661,7 @@ template <int DP> static griffin_status launch_dp(const AttnPlan &plan, const At
             return GRIFFIN_ERR_UNSUPPORTED;  // (strides that the copy engine does not take)
     }
     // as many ring slots as fit beside the list of the sequences' first tiles
-    const size_t tail = ATC_BARS * 8 + ATC_SEGS * sizeof(Segment) + 8 + ((size_t)plan.n_seq + 1) * 8, fixed = 1024 + Cfg::NS * Cfg::Q_BYTES + tail;
+    const size_t tail = ATC_BARS * 8 + ATC_SEGS * sizeof(Segment) + 8 + ((size_t)plan.n_seq + 1) * 4, fixed = 1024 + Cfg::NS * Cfg::Q_BYTES + tail;
     prm.n_slots = (int)((232448 - fixed) / Cfg::KV_BYTES);
     if (prm.n_slots > Cfg::MAX_SLOTS) prm.n_slots = Cfg::MAX_SLOTS;
     const size_t smem = fixed + (size_t)prm.n_slots * Cfg::KV_BYTES;
