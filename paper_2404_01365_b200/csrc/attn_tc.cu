@@ -81,22 +81,22 @@ __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, i
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
         : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
-        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"::
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
-    uint32_t r[16];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[h * 16 + i]);
-        tmem_st16(taddr + h * 16, r);
-    }
+// 32 bytes, a whole sector, in one store (the partials' rows start on 32-byte boundaries)
+__device__ __forceinline__ void store_8f(float *to, const float *v) {
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+                 "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                 : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_proxy_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -128,6 +128,43 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
     return *reinterpret_cast<float2 *>(&d);
 }
+// 2^x of both lanes on the FMA and integer pipes, x >= -120 after clamping: n = the integer next to x (by adding
+// 1.5 * 2^23), f = x - n, a cubic for 2^f on [-1/2, 1/2] (its own minimax fit, relative error 7.5e-5: a fiftieth of
+// the rounding of P to bf16 that follows), n into the exponent.
+__device__ __forceinline__ float2 poly_exp2(float2 x) {
+    const float2 magic = make_float2(12582912.f, 12582912.f), neg = make_float2(-12582912.f, -12582912.f);
+    x.x = fmaxf(x.x, -120.f);
+    x.y = fmaxf(x.y, -120.f);
+    const float2 n = add2(x, magic), back = add2(n, neg);
+    const float2 f = fma2(back, make_float2(-1.f, -1.f), x);
+    float2 y = fma2(f, make_float2(0.0551716685295105f, 0.0551716685295105f), make_float2(0.2426111251115799f, 0.2426111251115799f));
+    y = fma2(y, f, make_float2(0.6932609677314758f, 0.6932609677314758f));
+    y = fma2(y, f, make_float2(0.9999280571937561f, 0.9999280571937561f));
+    y.x = __int_as_float(__float_as_int(y.x) + (__float_as_int(n.x) << 23));
+    y.y = __int_as_float(__float_as_int(y.y) + (__float_as_int(n.y) << 23));
+    return y;
+}
+// P of 64 keys: 2^(c S - m), summed in fp32 and packed to bf16.  POLY of every 8 pairs go through poly_exp2: the
+// special-function unit gives 16 results a clock and SM, and 32768 of them per tile would take as long as the
+// four products of the tile do.
+constexpr int ATC_POLY = 3;
+template <int POLY>
+__device__ __forceinline__ void exp_pairs(const float (&s)[64], float2 scale2, float2 off2, float2 (&sum)[4], uint32_t (&pk)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        float2 e = fma2(make_float2(s[2 * i], s[2 * i + 1]), scale2, off2);
+        if ((i * 3 & 7) < POLY) {
+            e = poly_exp2(e);
+        } else {
+            e.x = fast_exp2(e.x);
+            e.y = fast_exp2(e.y);
+        }
+        sum[i & 3] = add2(sum[i & 3], e);
+        const __nv_bfloat162 x = __floats2bfloat162_rn(e.x, e.y);
+        pk[i] = *reinterpret_cast<const uint32_t *>(&x);
+    }
+}
+
 // Keys from `lim` on are not seen.
 __device__ __forceinline__ void mask_keys(float (&s)[64], int lim) {
 #pragma unroll
@@ -140,7 +177,7 @@ static __device__ __noinline__ bool wait_slow(uint64_t *bar, uint32_t parity, vo
     return wait_or_abort(bar, parity, abort, ws, where);
 }
 __device__ __forceinline__ bool wait_bar(uint64_t *bar, uint32_t parity, volatile int *abort, void *ws, int where) {
-    return mbar_try_wait(bar, parity) || mbar_try_wait(bar, parity) || wait_slow(bar, parity, abort, ws, where);
+    return mbar_try_wait(bar, parity) || wait_slow(bar, parity, abort, ws, where);
 }
 // A wait of a whole warp: all its lanes go on, or none.
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort, void *ws, int where) {
@@ -297,6 +334,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                     if (kv_n >= (uint32_t)n_slots && !(ok = warp_wait(&kv_empty[slot], kv.parity ^ 1u, abort, p.ws, 51))) break;
                     if (lane == 0) mbar_arrive_expect_tx(&kv_full[slot], Cfg::KV_BYTES);
                     __syncwarp();
+#pragma unroll 1
                     for (int i = lane; i < per_tile * CB; i += 32) {
                         const int r = i / CB, c = i % CB, key = k.k0 + r * prm.box_rows;
                         // a box behind the last key: a page that is not there reads as zeros
@@ -336,7 +374,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
         bool a_dual = false, b_dual = false;
         uint32_t a_n = 0, b_n = 0, a_u = 0, b_u = 0;
         uint32_t a_U = 0, b_U = 0, qi = 0;  // units of the CTA; first query buffer of a's segment
-        Ring ka{0, 0}, vb{1, 0}, okb{0, 0}; // ring places of the next key tile, of the next value tile, and the latter's v_ok
+        Ring ka{0, 0}, vb{1, 0}, okb{0, 0};  // ring places of the next key tile, of the next value tile, and the latter's v_ok
         const uint64_t q_desc = smem_desc_sw128(s_q, 0), k_desc = smem_desc_sw128(s_kv, 0), v_desc = smem_desc_mn_sw128(s_kv, 0, KT * 128);
         const auto next_segment = [&](SegReader &r, uint32_t &n, bool &dual, bool last_reader) -> bool {
             if (!warp_wait(&r.full[r.slot], r.parity, abort, p.ws, 48)) return false;
@@ -379,7 +417,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                 }
                 continue;
             }
-            if (!warp_wait(&kv_full[vb.slot], vb.parity, abort, p.ws, 54)) break;
+            // (the value warp has seen the tile arrive)
             if (!warp_wait(&v_ok[okb.slot], okb.parity, abort, p.ws, 54)) break;
             if (!warp_wait(&p_ready[b_U & 1], (b_U >> 1) & 1, abort, p.ws, 55)) break;
             tc_fence_after_sync();
@@ -422,6 +460,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                 kv.step(1, n_slots);
                 const int valid = k.len - k.k0;
                 if (valid < KT) {
+#pragma unroll 1
                     for (int i = lane; i < (KT - valid) * 8 * CB; i += 32) {
                         const int c = i % CB, r = valid + i / CB / 8, e = i / CB % 8;
                         *reinterpret_cast<uint4 *>(s_kv + slot * Cfg::KV_BYTES + c * (KT * 128) + r * 128 + e * 16) = make_uint4(0, 0, 0, 0);
@@ -523,10 +562,11 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
 #pragma unroll 1
                             for (int c = 0; c < DP; c += 32) {
                                 float o[32];
+                                uint32_t scaled[32];
                                 tmem_ld32(to + c, o);
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] *= f;
-                                tmem_st32(to + c, o);
+                                for (int i = 0; i < 32; ++i) scaled[i] = __float_as_uint(o[i] * f);
+                                tmem_st32(to + c, scaled);
                             }
                         }
                     }
@@ -537,21 +577,14 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                     for (int c = 0; c < KT; c += 64) {
                         float s[64];
                         tmem_ld64(ts + c, s);
-                        if (masked) mask_keys(s, lim - c);   // 2^-inf = 0
-#pragma unroll
-                        for (int h = 0; h < 64; h += 32) {
-                            uint32_t pk[16];
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                float2 e = fma2(make_float2(s[h + 2 * i], s[h + 2 * i + 1]), scale2, off2);
-                                e.x = fast_exp2(e.x);
-                                e.y = fast_exp2(e.y);
-                                sum[i & 3] = add2(sum[i & 3], e);
-                                const __nv_bfloat162 x = __floats2bfloat162_rn(e.x, e.y);
-                                pk[i] = *reinterpret_cast<const uint32_t *>(&x);
-                            }
-                            tmem_st16(ts + (c + h) / 2, pk);
+                        uint32_t pk[32];
+                        if (masked) {
+                            mask_keys(s, lim - c);   // 2^-inf = 0
+                            exp_pairs<0>(s, scale2, off2, sum, pk);
+                        } else {
+                            exp_pairs<ATC_POLY>(s, scale2, off2, sum, pk);
                         }
+                        tmem_st32(ts + c / 2, pk);
                     }
                     const float2 s4 = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
                     l += s4.x + s4.y;
@@ -580,14 +613,13 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                             if (valid) {
 #pragma unroll
                                 for (int i = 0; i < 32; i += 8) {
-                                    if (c + i >= p.d) break;
                                     uint32_t h[4];
 #pragma unroll
                                     for (int e = 0; e < 4; ++e) {
                                         const __nv_bfloat162 x = __floats2bfloat162_rn(o[i + 2 * e] * inv, o[i + 2 * e + 1] * inv);
                                         h[e] = *reinterpret_cast<const uint32_t *>(&x);
                                     }
-                                    *reinterpret_cast<uint4 *>(dst + c + i) = make_uint4(h[0], h[1], h[2], h[3]);
+                                    if (c + i < p.d) *reinterpret_cast<uint4 *>(dst + c + i) = make_uint4(h[0], h[1], h[2], h[3]);
                                 }
                             }
                         }
@@ -604,10 +636,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                             if (valid) {
 #pragma unroll
                                 for (int i = 0; i < 32; i += 8) {
-                                    if (c + i >= p.d) break;
-                                    float2 *const dst = reinterpret_cast<float2 *>(at.o + c + i);
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) dst[e] = make_float2(o[i + 2 * e], o[i + 2 * e + 1]);
+                                    if (c + i < p.d) store_8f(at.o + c + i, o + i);
                                 }
                             }
                         }
