@@ -22,7 +22,7 @@ static AttnScratch attn_scratch(const griffin_attn_desc *desc, const AttnShape &
     const size_t row = (size_t)(desc->head_dim + 2) * sizeof(float), streams = sh.alt ? 2 : 1;
     const long long by_token = n_tokens * desc->n_q_heads, by_seq = n_seq * desc->n_kv_heads * 128;
     s.own_rows = ((by_token < by_seq ? by_token : by_seq) + 3) / 4 * 4;  // (16-byte alignment of what follows the rows)
-    s.cuts_off = ((size_t)(n_seq + 1) * 4 + 255) / 256 * 256;
+    s.cuts_off = ((size_t)(n_seq + 3) * 4 + 255) / 256 * 256;
     s.own_off = s.cuts_off + ATTN_MAX_GRID * sizeof(CutJob);
     s.pre_off = s.own_off + streams * s.own_rows * row;
     s.cta_off = s.pre_off + (n_seq > 1 ? streams * s.own_rows * row : 0);
@@ -61,6 +61,8 @@ griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_a
     p.grid = sms < ATTN_MAX_GRID ? sms : ATTN_MAX_GRID;
     p.scale_log2 = desc->scale * 1.4426950408889634f;
     p.ws = ws;
+    p.may_queue = p.fused && desc->dtype == GRIFFIN_DT_BF16;
+    p.queue = &static_cast<WsHeader *>(ws)->queue_attn;
     const AttnScratch s = attn_scratch(desc, sh, p.n_tokens, p.n_seq);
     p.bases = reinterpret_cast<int *>(scratch);
     p.cuts = reinterpret_cast<CutJob *>(scratch + s.cuts_off);

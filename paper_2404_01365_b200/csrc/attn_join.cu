@@ -50,14 +50,16 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     pdl_launch_dependents();
     pdl_wait_prior_grids();
-    const AttnShares sh(p.bases[p.n_seq], p.grid);
+    const AttnTotals tot = attn_totals(p, p.bases);
+    if (tot.queued && blockIdx.x == 0 && threadIdx.x == 0) *p.queue = 0;
+    const AttnShares sh(tot.W, p.grid);
     JobParts a;
     AttnSeq q{};
     int r0 = 0, r1 = 0, head = 0, seq = 0, n_blocks = 0, b = 0;
     bool cut = false;
     if ((int)blockIdx.x >= by_row) {
         const int chunks = p.cta_rows / JOIN_ROWS, c = (int)(blockIdx.x - by_row) / chunks;
-        if (c >= sh.G) return;
+        if (c >= sh.G || tot.queued) return;
         const CutJob j = p.cuts[c];
         r0 = (int)(blockIdx.x - by_row) % chunks * JOIN_ROWS;
         r1 = min(j.rows, r0 + JOIN_ROWS);
@@ -89,12 +91,11 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
             const int base = p.bases[seq], per_head = (int)((uint32_t)(p.bases[seq + 1] - base) / (uint32_t)p.hkv);
             if (p.fused && attn_block_tiles(p, q, b) > 0) b = n_blocks - 1;
             int g0 = base + (head + 1) * per_head;
-#pragma unroll 1
-            for (int k = n_blocks - 1; k >= b; --k) g0 -= attn_block_tiles(p, q, k);
+            g0 -= (int)attn_sum_tiles(p, q, b, n_blocks);
             const AttnJob j = attn_own_job(p, q, seq, head, b, g0);
             a = job_parts(p, sh, j);
             r1 = j.rows;
-            if (p.fused && j.g1 > j.g0 && !j.alt) return;  // finished by the attention kernel, or cut
+            if (p.fused && j.g1 > j.g0 && (!j.alt || tot.queued)) return;  // finished by the attention kernel, or cut
         }
         // Each row is joined by `wpr` warps (more when there are fewer rows), each taking a stretch of its partials; their
         // sums are added in order through shared memory.

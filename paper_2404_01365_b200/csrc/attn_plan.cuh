@@ -25,6 +25,7 @@ struct AttnPlan {
     int n_seq, n_tokens, table_stride, prefix_len, n_pages;
     int page_shift;
     int hq, hkv, group, d;
+    int may_queue;         // whether the kernel takes jobs from a queue (and the call is fused)
     int fused, alt, by_token;  // by_token: how partials by row are numbered (attn_part_row)
     int tile_tokens;       // tokens per row tile
     int tiles_per_block;   // row tiles per block
@@ -37,7 +38,8 @@ struct AttnPlan {
     float scale_log2;      // scale * log2(e): logits in units of log2
     void *ws;
     // scratch (see attn_scratch)
-    int *bases;            // [n_seq + 1]: first own tile of each sequence; the last entry is W
+    int *bases;            // [n_seq + 3]: first own tile of each sequence, W, jobs, longest job
+    unsigned int *queue;   // how many jobs of a queued call have been taken (in the workspace's header; 0 between calls)
     struct CutJob *cuts;   // [grid]: the cut block that ends in the CTA's first segment, for the joining kernel
     float *own, *pre;      // partials by row: [2 streams][rows]: m and l, then the outputs
     float *cta;            // partials by CTA: [grid][2: continued from before / going on behind][2 * tile_rows]
@@ -156,33 +158,65 @@ __device__ __forceinline__ AttnJob attn_own_job(const AttnPlan &p, const AttnSeq
     return j;
 }
 
-// Own key tiles of a sequence under one key head.
-static __device__ __noinline__ long long attn_seq_tiles(const AttnPlan &p, const AttnSeq &q) {
+// Sum over blocks b0 .. b1 - 1 of a sequence of their key tiles, by a whole warp.
+__device__ __forceinline__ long long attn_sum_tiles(const AttnPlan &p, const AttnSeq &q, int b0, int b1) {
     long long n = 0;
 #pragma unroll 1
-    for (int b = 0; b * p.block_tokens < q.nq; ++b) n += attn_block_tiles(p, q, b);
+    for (int b = b0 + (threadIdx.x & 31); b < b1; b += 32) n += attn_block_tiles(p, q, b);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
     return n;
 }
 
+// What the CTAs know of a call after the scan.
+struct AttnTotals {
+    int W;         // tiles
+    int jobs;      // of the sequences
+    bool queued;   // whether jobs are handed out whole, from a queue
+};
+constexpr int ATTN_QUEUE_JOBS = 3;   // jobs per CTA from which a call is queued
+
 // First tile of every sequence into bases[0 .. n_seq] (shared memory), by all threads of the CTA; bases[n_seq] is
-// the number of tiles of the call.  The first CTA also leaves them in the scratch for the joining kernel.
-// A call of 2^31 tiles or more (10^14 bytes of keys) is not run: no tiles, and the status word is raised.
+// the number of tiles of the call, and the two entries behind it say how many jobs there are and how long the longest is.
+// The first CTA also leaves them in the scratch for the joining kernel.  A call of 2^31 tiles or more (10^14
+// bytes of keys) is not run: no tiles, and the status word is raised.
 __device__ __forceinline__ void attn_scan(const AttnPlan &p, int *bases) {
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const long long most = 1ll << 31;
+    // sequences of one row block (steps of a generation): a thread each; the others: a warp each
+#pragma unroll 1
     for (int s = threadIdx.x; s < p.n_seq; s += blockDim.x) {
-        const long long n = attn_seq_tiles(p, attn_seq(p, s)) * p.hkv;
-        bases[s] = n < most ? (int)n : -1;
+        const AttnSeq q = attn_seq(p, s);
+        if (q.nq <= p.block_tokens) {
+            const long long n = q.nq > 0 ? (long long)attn_block_tiles(p, q, 0) * p.hkv : 0;
+            bases[s] = n < most ? (int)n : -1;
+        }
+    }
+    if (p.n_tokens > p.block_tokens) {
+#pragma unroll 1
+        for (int s = warp; s < p.n_seq; s += warps) {
+            const AttnSeq q = attn_seq(p, s);
+            if (q.nq <= p.block_tokens) continue;
+            const long long n = attn_sum_tiles(p, q, 0, ceil_div(q.nq, p.block_tokens)) * p.hkv;
+            if (lane == 0) bases[s] = n < most ? (int)n : -1;
+        }
     }
     __syncthreads();
-    if (threadIdx.x < 32) {
+    if (warp == 0) {
         long long sum = (long long)p.hkv * p.prefix_blocks * p.prefix_tiles;
         bool bad = false;
+        int jobs = 0, longest = 0;
 #pragma unroll 1
         for (int s0 = 0; s0 < p.n_seq; s0 += 32) {
             const int s = s0 + lane;
             const long long mine = s < p.n_seq ? bases[s] : 0;
             bad |= mine < 0;
+            if (mine > 0 && p.n_tokens > p.block_tokens) {  // (a call of one row block has nothing to queue)
+                const AttnSeq q = attn_seq(p, s);
+                const int nb = ceil_div(q.nq, p.block_tokens);
+                jobs += nb;
+                longest = max(longest, attn_block_tiles(p, q, nb - 1));
+            }
             long long upto = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -193,18 +227,36 @@ __device__ __forceinline__ void attn_scan(const AttnPlan &p, int *bases) {
             sum += __shfl_sync(0xffffffffu, upto, 31);
         }
         bad = __any_sync(0xffffffffu, bad) || sum >= most;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            jobs += __shfl_xor_sync(0xffffffffu, jobs, o);
+            longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
+        }
         if (lane == 0) {
             bases[p.n_seq] = bad ? 0 : (int)sum;
+            bases[p.n_seq + 1] = jobs * p.hkv;
+            bases[p.n_seq + 2] = longest;
             if (bad) attn_bad(p.ws, 43);
         }
     }
     __syncthreads();
     if (blockIdx.x == 0)
-        for (int s = threadIdx.x; s <= p.n_seq; s += blockDim.x) p.bases[s] = bases[s];
+        for (int s = threadIdx.x; s <= p.n_seq + 2; s += blockDim.x) p.bases[s] = bases[s];
+}
+// Whether a call's jobs are handed out whole.  Cut shares are even to a tile, but every cut costs two partials of a
+// block, written and read again (a 4096-token prompt of 32 heads: 20 of 200 us).  With several jobs per CTA and none of
+// them longer than a fair share, taking whole jobs from a queue, the longest of a sequence first, comes within a short
+// job of even.  Only fused calls: the others have partials to join anyway.
+__device__ __forceinline__ AttnTotals attn_totals(const AttnPlan &p, const int *bases) {
+    AttnTotals t;
+    t.W = bases[p.n_seq];
+    t.jobs = bases[p.n_seq + 1];
+    t.queued = p.may_queue && t.jobs >= ATTN_QUEUE_JOBS * p.grid && (long long)bases[p.n_seq + 2] * p.grid <= t.W;
+    return t;
 }
 
 // (Not inlined: the schedule's code would otherwise be most of a kernel's, and instruction fetches its time.)
-// The job that has tile g (one exists: g < bases[n_seq]).
+// The job that has tile g (one exists: g < bases[n_seq]); by a whole warp.
 static __device__ __noinline__ AttnJob attn_find(const AttnPlan &p, const int *bases, int g) {
     if (g < bases[0]) {
         const int hb = (int)((uint32_t)g / (uint32_t)p.prefix_tiles), head = (int)((uint32_t)hb / (uint32_t)p.prefix_blocks);
@@ -219,14 +271,41 @@ static __device__ __noinline__ AttnJob attn_find(const AttnPlan &p, const int *b
     const AttnSeq q = attn_seq(p, lo);
     const int per_head = (int)((uint32_t)(bases[lo + 1] - bases[lo]) / (uint32_t)p.hkv);
     const int head = (int)((uint32_t)(g - bases[lo]) / (uint32_t)per_head);
-    int at = bases[lo] + head * per_head, b = 0;
+    const int lane = threadIdx.x & 31;
+    int at = bases[lo] + head * per_head;
 #pragma unroll 1
-    for (;; ++b) {
-        const int n = attn_block_tiles(p, q, b);
-        if (g < at + n) break;
-        at += n;
+    for (int b0 = 0;; b0 += 32) {   // 32 blocks at a time
+        const int b = b0 + lane, n = b * p.block_tokens < q.nq ? attn_block_tiles(p, q, b) : 0;
+        int upto = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const unsigned here = __ballot_sync(0xffffffffu, g < at + upto);
+        if (here != 0) {
+            const int first = __ffs(here) - 1;
+            return attn_own_job(p, q, lo, head, b0 + first, at + __shfl_sync(0xffffffffu, upto - n, first));
+        }
+        at += __shfl_sync(0xffffffffu, upto, 31);
     }
-    return attn_own_job(p, q, lo, head, b, at);
+}
+// Job i of a queued call: sequence by sequence, its row blocks from the last (the longest) to the first, each under
+// every key head.
+static __device__ __noinline__ AttnJob attn_queued(const AttnPlan &p, int i) {
+    int s = -1, nb = 0;
+    AttnSeq q{};
+#pragma unroll 1
+    for (;;) {
+        do q = attn_seq(p, ++s); while (q.nq == 0 || attn_block_tiles(p, q, (q.nq - 1) / p.block_tokens) == 0);
+        nb = ceil_div(q.nq, p.block_tokens);
+        if (i < nb * p.hkv) break;
+        i -= nb * p.hkv;
+    }
+    const int k = (int)((uint32_t)i / (uint32_t)p.hkv);
+    AttnJob j = attn_own_job(p, q, s, i - k * p.hkv, nb - 1 - k, 0);
+    j.alt = false;   // (its result is not joined with another)
+    return j;
 }
 // The job behind j, whose first tile is j.g1 < bases[n_seq].
 static __device__ __noinline__ AttnJob attn_next(const AttnPlan &p, const int *bases, const AttnJob &j) {

@@ -13,7 +13,7 @@ constexpr int SIMT_ROWS = 64, SIMT_KT = 32, SIMT_THREADS = 256;
 
 template <int DP> constexpr size_t simt_smem(int n_seq) {
     return (size_t)(SIMT_ROWS + 2 * SIMT_KT) * (DP + 4) * 4 + SIMT_ROWS * (SIMT_KT + 1) * 4 + 3 * SIMT_ROWS * 4 +
-           ((size_t)n_seq + 1) * 4;
+           ((size_t)n_seq + 3) * 4;
 }
 
 // DP: the head's width rounded up to 64, 128 or 256; entries from D on are zeros in shared memory.

@@ -4,25 +4,22 @@
 //   l += sum P;  O += P V;  when m grows by more than 2^8 can hold, O and l are scaled by 2^(m_old - m_new)
 //
 // One persistent CTA per SM, each with its share of the call's key tiles (attn_plan.cuh), 384 threads:
-//   warp 0      TMA: query tiles and, page by page, key and value tiles (128-byte swizzle) into a ring
-//   warp 1      MMA issuer; it also owns the TMEM allocation
-//   warp 2      sees the tiles arrive and clears the rows of a value tile that no key stands for (0 * NaN would reach
-//               the sum)
-//   warp 3      walks the share, segment by segment (a segment: what the share has of one job), and hands descriptions
-//               of the segments to the others through a ring in shared memory
+//   warp 0      TMA producer: query tiles and, page by page, key and value tiles (128-byte swizzle) into a ring
+//   warp 1      MMA issuer: one thread issues tcgen05.mma; it also owns the TMEM allocation
+//   warp 2      clears the rows of a value tile that no key stands for (0 * NaN would reach the sum)
+//   warp 3      scheduler: walks the share, segment by segment (a segment: what the share has of one job), and
+//               hands descriptions of the segments to the others through a ring in shared memory
 //   warps 4-7, 8-11   two softmax groups, a row per thread: S from TMEM, P (bf16) back to TMEM over S,
 //               and at the end of a segment O to the output or the partials
-// The work is a sequence of UNITS (one row tile times one key tile).  Unit U belongs to group U & 1, which has
-// its own S/P columns and (heads of up to 128 entries) its own O columns.  A block of two row tiles meets each key
-// tile with two units; a block of one row tile gives its key tiles to the two groups in turn, and the two O are
-// joined with the other partials.  The issuer runs S = Q K^T two units ahead of P V: one group's softmax runs
-// under the other's products.  (An issuer for each group was slower: the groups then fall into step, softmax with
-// softmax and product with product.)  Heads wider than 128 fill the O columns with one accumulator; then one
-// group does all units, with the same two S buffers.
+// The work is a sequence of UNITS (one row tile times one key tile).  Unit U belongs to softmax group U & 1,
+// which has its own S/P columns and (heads of up to 128 entries) its own O columns.  A block of two row
+// tiles meets each key tile with two units; a block of one row tile gives its key tiles to the two groups in
+// turn, and the two O are joined with the other partials.  The issuer runs S = Q K^T two units ahead of P V, so
+// one group's softmax runs under the other's products.  Heads wider than 128 fill the O columns with one
+// accumulator; then one group does all units, with the same two S buffers.
 //
-// MMAs of one thread complete in the order of issue, and tcgen05.commit covers all before it: with two
-// accumulators, S of a group's next unit is issued behind P V of its last, so its barrier also says that P V has
-// read P and updated O.
+// MMAs of one thread complete in the order of issue, and tcgen05.commit covers all before it: S of unit U + 2
+// is issued behind P V of unit U, so its barrier also says that P V of unit U has read P and updated O.
 //
 // Every wait is bounded; after a give-up the CTA still frees its TMEM before it returns.
 #include "attn.h"
@@ -39,13 +36,10 @@ template <int DP> struct AtcCfg {
     static constexpr int NS = DP == 256 ? 1 : 2;          // O accumulators
     static constexpr int CB = DP / 64;                    // 64-entry column blocks (128 swizzled bytes per row)
     static constexpr int Q_BYTES = ATC_ROWS * DP * 2, KV_BYTES = KT * DP * 2;
-    static constexpr int O_COL = 2 * KT;                  // TMEM columns: S/P 0, S/P 1, O (0, 1); P of 64 keys over the first half of their S
+    static constexpr int O_COL = 2 * KT;                  // TMEM columns: S/P 0, S/P 1, O (0, 1)
     static constexpr int MAX_SLOTS = DP == 64 ? 10 : 5;
 };
-constexpr int ATC_SEGS = 4;   // ring of segment descriptions
-// barriers, by number
-constexpr int B_KV_FULL = 0, B_KV_EMPTY = 10, B_Q_FULL = 20, B_Q_EMPTY = 22, B_S_FULL = 24, B_P_READY = 26, B_O_FULL = 28,
-              B_SEG_FULL = 30, B_SEG_EMPTY = B_SEG_FULL + ATC_SEGS, B_V_OK = B_SEG_EMPTY + ATC_SEGS, ATC_BARS = B_V_OK + 10;
+constexpr int ATC_BARS = 2 * 10 + 10 + 4 + 6 + 2 * 4 + 2;  // kv full/empty, v_ok, q full/empty, s_full, p_ready, o_full, seg full/empty, seg wanted
 
 struct AtcMaps {
     CUtensorMap q, k, v;
@@ -59,9 +53,9 @@ struct AtcParams {
 
 // Value tiles are read with their entries (not their keys) consecutive: swizzled blocks of 64 entries x 8 keys,
 // 1024 bytes from 8 keys to the next, `block` bytes from 64 entries to the next.
-// (stepping 16 keys adds 2048 bytes to the start address)
-__device__ __forceinline__ uint64_t smem_desc_mn_sw128(const void *tile, uint32_t block) {
-    return (uint64_t)((smem_u32(tile) >> 4) & 0x3FFFu) | ((uint64_t)(block >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+__device__ __forceinline__ uint64_t smem_desc_mn_sw128(const void *tile, int k16, uint32_t block) {
+    const uint32_t addr = smem_u32(tile) + (uint32_t)k16 * 2048u;
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(block >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
 // D[tmem] (+)= A[tmem] * B[smem]
 __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
@@ -73,18 +67,18 @@ __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, u
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, int x, int y, int z, uint64_t *bar) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
-            dst),
-        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+            smem_u32(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
         : "memory");
 }
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar) {
+__device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, int x, int y, int z, int w, uint64_t *bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-            dst),
-        "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+            smem_u32(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
         : "memory");
 }
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
@@ -116,10 +110,9 @@ __device__ __forceinline__ float fast_exp2(float x) {
 __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
-// the largest of three, NaN if there is one
-__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+__device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
-    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
 // two fp32 lanes in one instruction
@@ -151,122 +144,44 @@ __device__ __forceinline__ float2 poly_exp2(float2 x) {
     y.y = __int_as_float(__float_as_int(y.y) + (__float_as_int(n.y) << 23));
     return y;
 }
-// P of 64 keys: 2^(c S - m), summed in fp32 and packed to bf16.  ATC_POLY of every 8 pairs go through poly_exp2: the
+// P of 64 keys: 2^(c S - m), summed in fp32 and packed to bf16.  POLY of every 8 pairs go through poly_exp2: the
 // special-function unit gives 16 results a clock and SM, and 32768 of them per tile would take as long as the
-// four products of the tile do.  (A key that is not seen comes out as 2^-120 there, not 0: a row that sees nothing
-// at all is known by its m.)
-constexpr int ATC_POLY = 4;
-__device__ __forceinline__ void exp_pairs(const float (&s)[64], float2 scale2, float2 off2, float2 (&sum)[2], uint32_t (&pk)[32]) {
+// four products of the tile do.
+constexpr int ATC_POLY = 3;
+template <int POLY>
+__device__ __forceinline__ void exp_pairs(const float (&s)[64], float2 scale2, float2 off2, float2 (&sum)[4], uint32_t (&pk)[32]) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
         float2 e = fma2(make_float2(s[2 * i], s[2 * i + 1]), scale2, off2);
-        if ((i * 3 & 7) < ATC_POLY) {
+        if ((i * 3 & 7) < POLY) {
             e = poly_exp2(e);
         } else {
             e.x = fast_exp2(e.x);
             e.y = fast_exp2(e.y);
         }
-        sum[i & 1] = add2(sum[i & 1], e);
+        sum[i & 3] = add2(sum[i & 3], e);
         const __nv_bfloat162 x = __floats2bfloat162_rn(e.x, e.y);
         pk[i] = *reinterpret_cast<const uint32_t *>(&x);
     }
 }
-// What is not part of every tile's loop is kept out of line: the loops of all warps together have to fit in the SM's
-// instruction cache (measured: with the whole row of 128 in one stretch of code, a prompt took a fifth longer).
-//
-// Keys from `lim` on are not seen: -inf in their places of S, whatever is there.
-template <int KT> static __device__ __noinline__ void mask_tile(uint32_t ts, int lim) {
-#pragma unroll 1
-    for (int c = 0; c < KT; c += 32) {
-        float s[32];
-        uint32_t r[32];
-        tmem_ld32(ts + c, s);
+
+// Keys from `lim` on are not seen.
+__device__ __forceinline__ void mask_keys(float (&s)[64], int lim) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(c + i < lim ? s[i] : -INFINITY);
-        tmem_st32(ts + c, r);
-    }
-    tmem_wait_st();
-}
-template <int DP> static __device__ __noinline__ void scale_out(uint32_t to, float f) {
-#pragma unroll 1
-    for (int c = 0; c < DP; c += 32) {
-        float o[32];
-        uint32_t r[32];
-        tmem_ld32(to + c, o);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(o[i] * f);
-        tmem_st32(to + c, r);
-    }
-}
-// A row of O: times `scale` and rounded to dst, or as it is to the partials (dst NULL); nothing where on is false.
-template <int DP>
-static __device__ __noinline__ void write_out(uint32_t to, int d, bool on, float scale, __nv_bfloat16 *dst, float *part) {
-#pragma unroll 1
-    for (int c = 0; c < DP; c += 32) {
-        float o[32];
-        tmem_ld32(to + c, o);
-        if (!on) continue;
-#pragma unroll
-        for (int i = 0; i < 32; i += 8) {
-            if (c + i >= d) continue;
-            if (dst != nullptr) {
-                uint32_t h[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const __nv_bfloat162 x = __floats2bfloat162_rn(o[i + 2 * e] * scale, o[i + 2 * e + 1] * scale);
-                    h[e] = *reinterpret_cast<const uint32_t *>(&x);
-                }
-                *reinterpret_cast<uint4 *>(dst + c + i) = make_uint4(h[0], h[1], h[2], h[3]);
-            } else {
-                store_8f(part + c + i, o + i);
-            }
-        }
-    }
+    for (int i = 0; i < 64; ++i) s[i] = i < lim ? s[i] : -INFINITY;
 }
 
-// Barriers by their shared-memory address: the issuers' instructions between two products are what their chains wait for.
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void commit_to(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-// What every wait needs when it does not succeed at once.
-struct WaitCtx {
-    volatile int *abort;
-    void *ws;
-};
-// The bounded wait's slow path, in one place: the loops below stay small enough for the instruction cache
+// The bounded wait with its slow path in one place: the loops below stay small enough for the instruction cache
 // (with everything inlined the kernel was 128 KB of code and spent half its time fetching it).
-static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int *abort, void *ws, int where) {
-    const long long t0 = clock64();
-    for (;;) {
-#pragma unroll 1
-        for (int i = 0; i < 4096; ++i)
-            if (bar_try(bar, parity)) return true;
-        if (*abort) return false;
-        if (clock64() - t0 > WAIT_LIMIT_CYCLES) {
-            *abort = 1;
-            raise_status(ws, DEV_STATUS_TIMEOUT, where);
-            return false;
-        }
-    }
+static __device__ __noinline__ bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort, void *ws, int where) {
+    return wait_or_abort(bar, parity, abort, ws, where);
+}
+__device__ __forceinline__ bool wait_bar(uint64_t *bar, uint32_t parity, volatile int *abort, void *ws, int where) {
+    return mbar_try_wait(bar, parity) || wait_slow(bar, parity, abort, ws, where);
 }
 // A wait of a whole warp: all its lanes go on, or none.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const WaitCtx &c, int where) {
-    return __all_sync(0xffffffffu, bar_try(bar, parity) || wait_slow(bar, parity, c.abort, c.ws, where));
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort, void *ws, int where) {
+    return __all_sync(0xffffffffu, wait_bar(bar, parity, abort, ws, where));
 }
 // One lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {
@@ -276,9 +191,7 @@ __device__ __forceinline__ bool elect_one() {
 }
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
 
-// Place in a ring of barriers, and the parity that a wait for this round's completion takes.  (A wait for a barrier's
-// n-th completion may only begin when the one before has been seen, or the parity of an older one passes for it: every
-// reader of a ring waits at each of its places in turn.)
+// Place in a ring of barriers, and the parity that a wait for this round's completion takes.
 struct Ring {
     uint32_t slot, parity;
     __device__ __forceinline__ void step(uint32_t by, uint32_t n) {  // by <= n
@@ -290,13 +203,14 @@ struct Ring {
     }
 };
 
-// A segment, as warp 3 hands it on.
+// A segment, as the scheduler hands it on.
 struct __align__(16) Segment {
     int t0, n;            // first key tile (of the job's) and how many; n = 0: the share is done
     int pre_tiles;        // the job's tiles of the prefix; the others are the sequence's own
     int head, seq, tok0, rows, seen0, own_len;
     int alt, direct, first;
 };
+constexpr int ATC_SEGS = 4;
 
 // One key tile of a job: where its keys are and how many there are.
 struct KeyTile {
@@ -313,19 +227,29 @@ __device__ __forceinline__ KeyTile key_tile(const AttnPlan &p, const Segment &s,
 
 // A reader's place in the ring of segments.
 struct SegReader {
-    uint32_t slot, parity, bars;
+    uint32_t slot, parity;
+    uint64_t *full, *empty;
     const Segment *ring;
-    // the next segment, copied by a whole warp, which then gives its place back; false: a wait gave up.  n = 0: there is none
-    __device__ __forceinline__ bool take(Segment &s, const WaitCtx &c, int where) {
-        if (!warp_wait(bars + (B_SEG_FULL + slot) * 8, parity, c, where)) return false;
+    // the next segment, into s; false: a wait gave up.  s.n == 0: there is none.
+    __device__ __forceinline__ bool get(Segment &s, volatile int *abort, void *ws, int where) {
+        if (!wait_bar(&full[slot], parity, abort, ws, where)) return false;
         s = ring[slot];
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) bar_arrive(bars + (B_SEG_EMPTY + slot) * 8);
+        return true;
+    }
+    __device__ __forceinline__ void step() {
         if (++slot == ATC_SEGS) {
             slot = 0;
             parity ^= 1u;
         }
-        return true;
+    }
+    // once a reader (a warp, or the issuer with its later look) has copied the segment
+    __device__ __forceinline__ void release() { mbar_arrive(&empty[slot]); }
+    // get by a whole warp, which then gives the place back
+    __device__ __forceinline__ bool take(Segment &s, volatile int *abort, void *ws, int where) {
+        const bool ok = __all_sync(0xffffffffu, get(s, abort, ws, where));
+        if (ok && (threadIdx.x & 31) == 0) release();
+        step();
+        return ok;
     }
 };
 
@@ -340,68 +264,78 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
     uint8_t *const s_q = base;                                  // NS query tiles
     uint8_t *const s_kv = base + NS * Cfg::Q_BYTES;             // ring of key and value tiles
     const int n_slots = prm.n_slots;
-    uint64_t *const bar_mem = reinterpret_cast<uint64_t *>(s_kv + n_slots * Cfg::KV_BYTES);
-    Segment *const segs = reinterpret_cast<Segment *>(bar_mem + ATC_BARS);
+    uint64_t *const bars = reinterpret_cast<uint64_t *>(s_kv + n_slots * Cfg::KV_BYTES);
+    uint64_t *const kv_full = bars, *const kv_empty = bars + 10, *const v_ok = bars + 20, *const q_full = bars + 30,
+                   *const q_empty = bars + 32, *const s_full = bars + 34, *const p_ready = bars + 36, *const o_full = bars + 38,
+                   *const seg_full = bars + 40, *const seg_empty = bars + 44, *const seg_want = bars + 48;
+    Segment *const segs = reinterpret_cast<Segment *>(bars + ATC_BARS);
     uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(segs + ATC_SEGS);
-    const WaitCtx ctx{reinterpret_cast<volatile int *>(tmem_slot + 1), p.ws};
+    volatile int *const abort = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int *const bases = reinterpret_cast<int *>(tmem_slot + 2);
-    const uint32_t bars = smem_u32(bar_mem);
-    const auto bar = [bars](int b, uint32_t i) { return bars + (b + i) * 8; };
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_launch_dependents();
     if (tid < 3) prefetch_tensormap(tid == 0 ? &maps.q : tid == 1 ? &maps.k : &maps.v);
     if (tid == 0) {
-#pragma unroll 1
-        for (int i = 0; i < ATC_BARS; ++i) {
-            int n = 1;
-            if (i >= B_P_READY && i < B_O_FULL) n = 4;                   // the group's warps
-            else if (i >= B_SEG_EMPTY && i < B_V_OK) n = 3 + 4 * NS;      // warps 0 to 2, softmax warps
-            mbar_init(bar_mem + i, n);
+        for (int i = 0; i < n_slots; ++i) {
+            mbar_init(&kv_full[i], 1);
+            mbar_init(&kv_empty[i], 1);
+            mbar_init(&v_ok[i], 1);
         }
-        *ctx.abort = 0;
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&q_full[i], 1);
+            mbar_init(&q_empty[i], 1);
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_ready[i], 4);  // one arrival per warp of the group
+            mbar_init(&o_full[i], 1);
+        }
+        for (int i = 0; i < ATC_SEGS; ++i) {
+            mbar_init(&seg_full[i], 1);
+            mbar_init(&seg_empty[i], 3 + 4 * NS);  // producer, issuer, value warp, softmax warps
+        }
+        mbar_init(seg_want, 1);
+        *abort = 0;
         mbar_fence_init();
     }
     pdl_wait_prior_grids();
     attn_scan(p, bases);
-    const AttnShares shares(bases[p.n_seq], p.grid);
+    const AttnTotals totals = attn_totals(p, bases);
+    const AttnShares shares(totals.W, p.grid);
     if ((int)blockIdx.x >= shares.G) return;
     if (warp == 1) tmem_alloc(tmem_slot, 512);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = *tmem_slot;
-    SegReader seg{0, 0, bars, segs};
+    SegReader seg{0, 0, seg_full, seg_empty, segs};
 
     if (warp == 0) {
-        // ---------------- loads ----------------
+        // ---------------- TMA producer ----------------
+        Segment w;
         uint32_t kv_n = 0, nq = 0;  // ring slots and query buffers handed out so far
         Ring kv{0, 0};
-        Segment w;
         bool ok = true;
         const int per_tile = KT / prm.box_rows;  // boxes per 64-entry block
-        const uint32_t q_at = smem_u32(s_q), kv_at = smem_u32(s_kv);
-        while (ok && (ok = seg.take(w, ctx, 49)) && w.n > 0) {
+        if (lane == 0) mbar_arrive(seg_want);
+        while (ok && (ok = seg.take(w, abort, p.ws, 49)) && w.n > 0) {
             const int q_tiles = NS == 2 && !w.alt ? 2 : 1;
             for (int r = 0; r < q_tiles && ok; ++r, ++nq) {
-                const uint32_t b = nq % NS;
-                if (nq >= NS && !(ok = warp_wait(bar(B_Q_EMPTY, b), (nq / NS - 1) & 1, ctx, 50))) break;
-                if (lane == 0) {
-                    bar_expect(bar(B_Q_FULL, b), CB * prm.q_box_bytes);
-#pragma unroll 1
+                const int b = nq % NS;
+                if (nq >= NS) ok = warp_wait(&q_empty[b], (nq / NS - 1) & 1, abort, p.ws, 50);
+                if (ok && lane == 0) {
+                    mbar_arrive_expect_tx(&q_full[b], CB * prm.q_box_bytes);
                     for (int c = 0; c < CB; ++c)
-                        tma_load_3d(q_at + b * Cfg::Q_BYTES + c * (ATC_ROWS * 128), &maps.q, c * 64, w.head * p.group,
-                                    w.tok0 + r * p.tile_tokens, bar(B_Q_FULL, b));
+                        tma_load_3d(s_q + b * Cfg::Q_BYTES + c * (ATC_ROWS * 128), &maps.q, c * 64, w.head * p.group,
+                                    w.tok0 + r * p.tile_tokens, &q_full[b]);
                 }
             }
             for (int t = 0; t < w.n && ok; ++t) {
                 const KeyTile k = key_tile(p, w, w.t0 + t);
                 const int *const pages = k.prefix ? p.prefix_pages : p.page_table + (long long)w.seq * p.table_stride;
-#pragma unroll 1
                 for (int which = 0; which < 2; ++which) {
-                    const uint32_t full = bar(B_KV_FULL, kv.slot), dst = kv_at + kv.slot * Cfg::KV_BYTES;
-                    if (kv_n >= (uint32_t)n_slots && !(ok = warp_wait(bar(B_KV_EMPTY, kv.slot), kv.parity ^ 1u, ctx, 51))) break;
-                    if (lane == 0) bar_expect(full, Cfg::KV_BYTES);
+                    const uint32_t slot = kv.slot;
+                    if (kv_n >= (uint32_t)n_slots && !(ok = warp_wait(&kv_empty[slot], kv.parity ^ 1u, abort, p.ws, 51))) break;
+                    if (lane == 0) mbar_arrive_expect_tx(&kv_full[slot], Cfg::KV_BYTES);
                     __syncwarp();
 #pragma unroll 1
                     for (int i = lane; i < per_tile * CB; i += 32) {
@@ -415,23 +349,24 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                                 page = p.n_pages;
                             }
                         }
-                        tma_load_4d(dst + c * (KT * 128) + r * prm.box_rows * 128, which ? &maps.v : &maps.k, c * 64,
-                                    key & ((1 << p.page_shift) - 1), w.head, page, full);
+                        tma_load_4d(s_kv + slot * Cfg::KV_BYTES + c * (KT * 128) + r * prm.box_rows * 128, which ? &maps.v : &maps.k,
+                                    c * 64, key & ((1 << p.page_shift) - 1), w.head, page, &kv_full[slot]);
                     }
                     __syncwarp();
                     kv.step(1, n_slots);
                     ++kv_n;
                 }
             }
+            if (lane == 0) mbar_arrive(seg_want);
         }
         // stay until every copy that was started has landed
         if (lane == 0) {
             const long long t_0 = clock64();
             for (uint32_t i = kv_n > (uint32_t)n_slots ? kv_n - n_slots : 0; i < kv_n; ++i)
-                while (!bar_try(bar(B_KV_FULL, i % n_slots), (i / n_slots) & 1))
+                while (!mbar_try_wait(&kv_full[i % n_slots], (i / n_slots) & 1))
                     if (clock64() - t_0 > WAIT_LIMIT_CYCLES) break;
             for (uint32_t i = nq > (uint32_t)NS ? nq - NS : 0; i < nq; ++i)
-                while (!bar_try(bar(B_Q_FULL, i % NS), (i / NS) & 1))
+                while (!mbar_try_wait(&q_full[i % NS], (i / NS) & 1))
                     if (clock64() - t_0 > WAIT_LIMIT_CYCLES) break;
         }
     } else if (warp == 1) {
@@ -439,43 +374,41 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
         // (the whole warp walks, one lane issues: the operands stay in uniform registers)
         constexpr uint32_t ID_QK = umma_idesc(ATC_ROWS, KT), ID_PV = umma_idesc(ATC_ROWS, DP) | (1u << 16);
         // Where S = Q K^T stands (a) and where P V (b): unit in its segment, units in it, whether blocks of two row tiles.
-        uint32_t a_seg = 0, a_par = 0, b_seg = 0, b_par = 0, a_n = 0, b_n = 0, a_u = 0, b_u = 0;
-        uint32_t a_U = 0, b_U = 0, qi = 0;   // units of the CTA; first query tile of a's segment
+        SegReader seg_b = seg;
         bool a_dual = false, b_dual = false;
-        Ring ka{0, 0}, vb{1, 0}, okb{0, 0};  // ring places of the next key tile, of the next value tile, and the latter's B_V_OK
-        const uint64_t q_desc = smem_desc_sw128(s_q, 0), k_desc = smem_desc_sw128(s_kv, 0), v_desc = smem_desc_mn_sw128(s_kv, KT * 128);
-        const auto next_segment = [&](uint32_t &place, uint32_t &par, uint32_t &n, bool &dual, bool last_reader) -> bool {
-            if (!warp_wait(bar(B_SEG_FULL, place), par, ctx, 48)) return false;
-            const Segment &s = segs[place];
+        uint32_t a_n = 0, b_n = 0, a_u = 0, b_u = 0;
+        uint32_t a_U = 0, b_U = 0, qi = 0;  // units of the CTA; first query buffer of a's segment
+        Ring ka{0, 0}, vb{1, 0}, okb{0, 0};  // ring places of the next key tile, of the next value tile, and the latter's v_ok
+        const uint64_t q_desc = smem_desc_sw128(s_q, 0), k_desc = smem_desc_sw128(s_kv, 0), v_desc = smem_desc_mn_sw128(s_kv, 0, KT * 128);
+        const auto next_segment = [&](SegReader &r, uint32_t &n, bool &dual, bool last_reader) -> bool {
+            if (!warp_wait(&r.full[r.slot], r.parity, abort, p.ws, 48)) return false;
+            const Segment &s = r.ring[r.slot];
             dual = NS == 2 && uniform(s.alt) == 0;
             n = uniform(s.n) << (dual ? 1 : 0);
             __syncwarp();
-            if (last_reader && lane == 0) bar_arrive(bar(B_SEG_EMPTY, place));
-            if (++place == ATC_SEGS) {
-                place = 0;
-                par ^= 1u;
-            }
+            if (last_reader && elect_one()) r.release();
+            r.step();
             return true;
         };
-        bool ok = next_segment(a_seg, a_par, a_n, a_dual, false) && next_segment(b_seg, b_par, b_n, b_dual, true);
+        bool ok = next_segment(seg, a_n, a_dual, false) && next_segment(seg_b, b_n, b_dual, true);
         uint32_t ahead = 0;  // units whose S has been issued and P V not: two in front of every P V
         while (ok && b_n > 0) {
             if (ahead < 2 && a_n > 0) {
                 const uint32_t q_at = qi + (a_dual ? a_u & 1 : 0), qb = NS == 2 ? q_at & 1 : 0;
-                if (a_u < (a_dual ? 2u : 1u) && !(ok = warp_wait(bar(B_Q_FULL, qb), (NS == 2 ? q_at >> 1 : q_at) & 1, ctx, 52))) break;
-                if (!(ok = warp_wait(bar(B_KV_FULL, ka.slot), ka.parity, ctx, 53))) break;
+                if (a_u < (a_dual ? 2u : 1u) && !(ok = warp_wait(&q_full[qb], (NS == 2 ? q_at >> 1 : q_at) & 1, abort, p.ws, 52))) break;
+                if (!(ok = warp_wait(&kv_full[ka.slot], ka.parity, abort, p.ws, 53))) break;
                 tc_fence_after_sync();
                 const uint64_t q = q_desc + (uint64_t)(qb * (Cfg::Q_BYTES >> 4)), k = k_desc + (uint64_t)(ka.slot * (Cfg::KV_BYTES >> 4));
-                const uint32_t buf = a_U & 1, d = tmem + buf * KT;
+                const uint32_t d = tmem + (a_U & 1) * KT;
                 const bool k_done = !a_dual || (a_u & 1), q_done = a_u + (a_dual ? 2 : 1) >= a_n;
                 if (elect_one()) {
 #pragma unroll
                     for (int kk = 0; kk < DP / 16; ++kk)
                         umma_bf16(d, q + (uint64_t)(((kk >> 2) * (ATC_ROWS * 128) + (kk & 3) * 32) >> 4),
                                   k + (uint64_t)(((kk >> 2) * (KT * 128) + (kk & 3) * 32) >> 4), ID_QK, kk > 0);
-                    commit_to(bar(B_S_FULL, buf));
-                    if (k_done) commit_to(bar(B_KV_EMPTY, ka.slot));
-                    if (q_done) commit_to(bar(B_Q_EMPTY, qb));
+                    umma_commit(&s_full[a_U & 1]);
+                    if (k_done) umma_commit(&kv_empty[ka.slot]);
+                    if (q_done) umma_commit(&q_empty[qb]);
                 }
                 __syncwarp();
                 if (k_done) ka.step(2, n_slots);
@@ -484,23 +417,23 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                 if (++a_u == a_n) {
                     qi += a_dual ? 2 : 1;
                     a_u = 0;
-                    ok = next_segment(a_seg, a_par, a_n, a_dual, false);
+                    ok = next_segment(seg, a_n, a_dual, false);
                 }
                 continue;
             }
-            const uint32_t buf = b_U & 1, o = NS == 2 ? buf : 0;
-            // (warp 2 has seen the tile arrive)
-            if (!warp_wait(bar(B_V_OK, okb.slot), okb.parity, ctx, 54)) break;
-            if (!warp_wait(bar(B_P_READY, buf), (b_U >> 1) & 1, ctx, 55)) break;
+            // (the value warp has seen the tile arrive)
+            if (!warp_wait(&v_ok[okb.slot], okb.parity, abort, p.ws, 54)) break;
+            if (!warp_wait(&p_ready[b_U & 1], (b_U >> 1) & 1, abort, p.ws, 55)) break;
             tc_fence_after_sync();
-            const uint32_t d = tmem + Cfg::O_COL + o * DP, pt = tmem + buf * KT, add = b_u >= NS;
+            const uint32_t o = NS == 2 ? b_U & 1 : 0, d = tmem + Cfg::O_COL + o * DP, pt = tmem + (b_U & 1) * KT;
             const uint64_t v = v_desc + (uint64_t)(vb.slot * (Cfg::KV_BYTES >> 4));
+            const uint32_t add = b_u >= NS;
             const bool v_done = !b_dual || (b_u & 1);
             if (elect_one()) {
 #pragma unroll
-                for (int kk = 0; kk < KT / 16; ++kk) umma_bf16_ts(d, pt + (kk >> 2) * 64 + (kk & 3) * 8, v + (uint64_t)(kk * (2048 >> 4)), ID_PV, kk > 0 ? 1 : add);
-                if (v_done) commit_to(bar(B_KV_EMPTY, vb.slot));
-                if (NS == 1 || b_u + 2 >= b_n) commit_to(bar(B_O_FULL, o));
+                for (int kk = 0; kk < KT / 16; ++kk) umma_bf16_ts(d, pt + kk * 8, v + (uint64_t)(kk * (2048 >> 4)), ID_PV, kk > 0 ? 1 : add);
+                if (v_done) umma_commit(&kv_empty[vb.slot]);
+                if (NS == 1 || b_u + 2 >= b_n) umma_commit(&o_full[o]);
             }
             __syncwarp();
             if (v_done) {
@@ -511,70 +444,85 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
             ++b_U;
             if (++b_u == b_n) {
                 b_u = 0;
-                ok = next_segment(b_seg, b_par, b_n, b_dual, true);
+                ok = next_segment(seg_b, b_n, b_dual, true);
             }
         }
     } else if (warp == 2) {
         // ---------------- value tiles: rows that no key stands for become zeros ----------------
         Segment w;
+        // (It waits for the key tiles too: a wait for a slot's n-th filling may only begin when the one before has been
+        // seen, or the parity of an older one passes for it.)
         Ring kv{0, 0}, done{0, 0};
         bool ok = true;
-        while (ok && (ok = seg.take(w, ctx, 47)) && w.n > 0) {
-#pragma unroll 1
-            for (int t = 0; t < w.n && ok; ++t) {
+        while (ok && (ok = seg.take(w, abort, p.ws, 47)) && w.n > 0) {
+            for (int t = 0; t < w.n && ok; ++t, done.step(1, n_slots)) {
                 const KeyTile k = key_tile(p, w, w.t0 + t);
-                if (!(ok = warp_wait(bar(B_KV_FULL, kv.slot), kv.parity, ctx, 56))) break;
+                if (!(ok = warp_wait(&kv_full[kv.slot], kv.parity, abort, p.ws, 56))) break;
                 kv.step(1, n_slots);
-                if (!(ok = warp_wait(bar(B_KV_FULL, kv.slot), kv.parity, ctx, 56))) break;
+                const uint32_t slot = kv.slot;
+                if (!(ok = warp_wait(&kv_full[slot], kv.parity, abort, p.ws, 56))) break;
+                kv.step(1, n_slots);
                 const int valid = k.len - k.k0;
                 if (valid < KT) {
-                    uint8_t *const tile = s_kv + kv.slot * Cfg::KV_BYTES;
 #pragma unroll 1
                     for (int i = lane; i < (KT - valid) * 8 * CB; i += 32) {
                         const int c = i % CB, r = valid + i / CB / 8, e = i / CB % 8;
-                        *reinterpret_cast<uint4 *>(tile + c * (KT * 128) + r * 128 + e * 16) = make_uint4(0, 0, 0, 0);
+                        *reinterpret_cast<uint4 *>(s_kv + slot * Cfg::KV_BYTES + c * (KT * 128) + r * 128 + e * 16) = make_uint4(0, 0, 0, 0);
                     }
                     fence_proxy_async_smem();
-                    __syncwarp();
                 }
-                if (lane == 0) bar_arrive(bar(B_V_OK, done.slot));
-                kv.step(1, n_slots);
-                done.step(1, n_slots);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&v_ok[done.slot]);
             }
         }
     } else if (warp == 3) {
-        // ---------------- schedule ----------------
+        // ---------------- scheduler ----------------
+        int g = shares.first(blockIdx.x);
+        const int g_end = shares.first(blockIdx.x + 1);
+        AttnJob j;
+        bool more = true;
+        if (!totals.queued) {
+            j = attn_find(p, bases, g);
+            if (lane == 0) attn_note_cut(p, shares, j, g, min(g_end, j.g1));
+        }
         if (lane == 0) {
-            int g = shares.first(blockIdx.x);
-            const int g_end = shares.first(blockIdx.x + 1);
-            AttnJob j = attn_find(p, bases, g);
-            attn_note_cut(p, shares, j, g, min(g_end, j.g1));
-            Ring sg{0, 0};
+            Ring at{0, 0};
             for (uint32_t k = 0;; ++k) {
-                if (k >= ATC_SEGS && !bar_try(bar(B_SEG_EMPTY, sg.slot), sg.parity ^ 1u) &&
-                    !wait_slow(bar(B_SEG_EMPTY, sg.slot), sg.parity ^ 1u, ctx.abort, ctx.ws, 46))
-                    break;
-                const int stop = min(g_end, j.g1);
-                Segment w;
-                w.t0 = g - j.g0;
-                w.n = stop - g;
-                w.pre_tiles = j.seq < 0 || p.fused ? p.prefix_tiles : 0;
-                w.head = j.head;
-                w.seq = j.seq;
-                w.tok0 = j.tok0;
-                w.rows = j.rows;
-                w.seen0 = j.seen0;
-                w.own_len = j.own_len;
-                w.alt = j.alt;
-                w.first = g == j.g0;
-                w.direct = attn_direct(p, j, w.first && stop == j.g1);
-                segs[sg.slot] = w;
-                bar_arrive(bar(B_SEG_FULL, sg.slot));
-                if (w.n == 0) break;
-                sg.step(1, ATC_SEGS);
-                g = stop;
-                if (g < g_end) j = attn_next(p, bases, j);
-                else j.g1 = g;  // the last description: no tiles
+                if (k >= ATC_SEGS && !wait_bar(&seg_empty[at.slot], at.parity ^ 1u, abort, p.ws, 46)) break;
+                if (totals.queued) {
+                    // the next job of the queue, once the copies of the one before have been asked for
+                    if (!wait_bar(seg_want, k & 1, abort, p.ws, 44)) break;
+                    do {
+                        const int i = (int)atomicAdd(p.queue, 1u);
+                        more = i < totals.jobs;
+                        if (!more) break;
+                        j = attn_queued(p, i);
+                        g = j.g0;
+                    } while (j.g1 == j.g0);   // (blocks that see nothing are the joining kernel's)
+                }
+                const int stop = totals.queued ? j.g1 : min(g_end, j.g1);
+                Segment s;
+                s.t0 = g - j.g0;
+                s.n = more ? stop - g : 0;
+                s.pre_tiles = j.seq < 0 || p.fused ? p.prefix_tiles : 0;
+                s.head = j.head;
+                s.seq = j.seq;
+                s.tok0 = j.tok0;
+                s.rows = j.rows;
+                s.seen0 = j.seen0;
+                s.own_len = j.own_len;
+                s.alt = j.alt;
+                s.first = g == j.g0;
+                s.direct = attn_direct(p, j, s.first && stop == j.g1);
+                segs[at.slot] = s;
+                mbar_arrive(&seg_full[at.slot]);
+                if (!more) break;
+                at.step(1, ATC_SEGS);
+                if (!totals.queued) {
+                    g = stop;
+                    more = g < g_end;
+                    if (more) j = attn_next(p, bases, j);
+                }
             }
         }
     } else if (warp >= 4 && (NS == 2 || warp < 8)) {
@@ -586,7 +534,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
         Segment j;
         uint32_t U0 = 0, n_o = 0;  // units before this segment; segments finished by this group
         bool ok = true;
-        while (ok && (ok = seg.take(j, ctx, 45)) && j.n > 0) {
+        while (ok && (ok = seg.take(j, abort, p.ws, 45)) && j.n > 0) {
             const bool dual = NS == 2 && !j.alt;
             const uint32_t n = (uint32_t)j.n << (dual ? 1 : 0);
             uint32_t u = NS == 2 ? (U0 ^ grp) & 1 : 0;             // the group's first unit
@@ -601,25 +549,26 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
             for (; u < n && ok; u += NS) {
                 const uint32_t U = U0 + u, buf = U & 1;
                 const KeyTile k = key_tile(p, j, j.t0 + (int)(dual ? u >> 1 : u));
-                bool o_seen = u == 0;   // (one accumulator: whether P V of the unit before is known to be done)
-                ok = warp_wait(bar(B_S_FULL, buf), (U >> 1) & 1, ctx, 57);
+                ok = warp_wait(&s_full[buf], (U >> 1) & 1, abort, p.ws, 57);
                 if (!ok) break;
                 tc_fence_after_sync();
                 if (warp_on) {
                     const uint32_t ts = lanes + buf * KT;
                     const int lim = (k.prefix ? k.len : min(k.len, own_seen)) - k.k0;   // keys of the tile that the row sees
-                    if (__any_sync(0xffffffffu, lim < KT)) mask_tile<KT>(ts, lim);
-                    float s[64], mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    const bool masked = __any_sync(0xffffffffu, lim < KT);
+                    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
                     for (int c = 0; c < KT; c += 64) {
+                        float s[64];
                         tmem_ld64(ts + c, s);
+                        if (masked) mask_keys(s, lim - c);
 #pragma unroll
                         for (int i = 0; i < 64; i += 8)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) mx4[e] = max3_nan(mx4[e], s[i + e], s[i + 4 + e]);
+                            for (int e = 0; e < 4; ++e) mx4[e] = max3(mx4[e], s[i + e], s[i + 4 + e]);
                     }
-                    const float mx = max3_nan(max3_nan(mx4[0], mx4[1], mx4[2]), mx4[3], -INFINITY) * p.scale_log2;
-                    if (mx != -INFINITY) l += mx - mx;   // a NaN or an infinity among the logits makes the row NaN
+                    float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+                    mx *= p.scale_log2;
                     // the maximum moves only when 2^(c S - m) could grow too large (or there is none yet)
                     const bool move = mx > m + ATC_SLACK || (m == -INFINITY && mx > m);
                     if (__any_sync(0xffffffffu, move)) {
@@ -629,57 +578,91 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                         if (started) {
                             // (one accumulator: S of this unit was issued before P V of the last one, so its barrier
                             // does not cover it)
-                            if (NS == 1) {
-                                if (!(ok = warp_wait(bar(B_O_FULL, 0), (U - 1) & 1, ctx, 59))) break;
-                                o_seen = true;
-                                tc_fence_after_sync();
+                            if (NS == 1 && !(ok = warp_wait(&o_full[0], (U - 1) & 1, abort, p.ws, 59))) break;
+                            tc_fence_after_sync();
+                            const uint32_t to = lanes + Cfg::O_COL + (NS == 2 ? buf : 0) * DP;
+#pragma unroll 1
+                            for (int c = 0; c < DP; c += 32) {
+                                float o[32];
+                                uint32_t scaled[32];
+                                tmem_ld32(to + c, o);
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) scaled[i] = __float_as_uint(o[i] * f);
+                                tmem_st32(to + c, scaled);
                             }
-                            scale_out<DP>(lanes + Cfg::O_COL + (NS == 2 ? buf : 0) * DP, f);
                         }
                     }
                     const float off = m == -INFINITY ? 0.f : m;
                     const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), off2 = make_float2(-off, -off);
-                    float2 sum[2] = {};
-                    // (the last 64 keys first: they are still here; the count is hidden from the compiler, and the loop
-                    // in this form, so that its body is laid out once)
-                    int c = KT - 64;
-                    asm volatile("" : "+r"(c));
+                    float2 sum[4] = {};
 #pragma unroll 1
-                    do {
+                    for (int c = 0; c < KT; c += 64) {
+                        float s[64];
+                        tmem_ld64(ts + c, s);
                         uint32_t pk[32];
-                        if (c != KT - 64) tmem_ld64(ts + c, s);
-                        exp_pairs(s, scale2, off2, sum, pk);
-                        tmem_st32(ts + c, pk);
-                        c -= 64;
-                    } while (c >= 0);
-                    const float2 both = add2(sum[0], sum[1]);
-                    l += both.x + both.y;
+                        if (masked) {
+                            mask_keys(s, lim - c);   // 2^-inf = 0
+                            exp_pairs<0>(s, scale2, off2, sum, pk);
+                        } else {
+                            exp_pairs<ATC_POLY>(s, scale2, off2, sum, pk);
+                        }
+                        tmem_st32(ts + c / 2, pk);
+                    }
+                    const float2 s4 = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+                    l += s4.x + s4.y;
                     started = true;
                     tmem_wait_st();
                 }
-                if (NS == 1 && !o_seen && !(ok = warp_wait(bar(B_O_FULL, 0), (U - 1) & 1, ctx, 59))) break;
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) bar_arrive(bar(B_P_READY, buf));
+                if (lane == 0) mbar_arrive(&p_ready[buf]);
             }
             // the segment's result
             if (ok && has) {
-                ok = warp_wait(bar(B_O_FULL, NS == 2 ? grp : 0), (NS == 2 ? n_o : U0 + n - 1) & 1, ctx, 58);
+                ok = warp_wait(&o_full[NS == 2 ? grp : 0], (NS == 2 ? n_o : U0 + n - 1) & 1, abort, p.ws, 58);
                 ++n_o;
                 if (ok && warp_on) {
                     tc_fence_after_sync();
                     const uint32_t to = lanes + Cfg::O_COL + (NS == 2 ? grp : 0) * DP;
-                    __nv_bfloat16 *dst = nullptr;
-                    float *part = nullptr;
                     if (j.direct) {
-                        dst = static_cast<__nv_bfloat16 *>(prm.out) + (j.tok0 + tok) * prm.ld_out +
-                              (j.head * p.group + row - tok * p.group) * p.d;
-                    } else if (valid) {
-                        const PartPlace at = attn_place(p, PartJob{j.seq, j.head, j.tok0, j.alt != 0}, j.first != 0, stream, row);
-                        *reinterpret_cast<float2 *>(at.ml) = make_float2(m, l);
-                        part = at.o;
+                        const float inv = l == 0.f ? 0.f : 1.0f / l;
+                        __nv_bfloat16 *const dst = static_cast<__nv_bfloat16 *>(prm.out) + (j.tok0 + tok) * prm.ld_out +
+                                                   (j.head * p.group + row - tok * p.group) * p.d;
+#pragma unroll 1
+                        for (int c = 0; c < DP; c += 32) {
+                            float o[32];
+                            tmem_ld32(to + c, o);
+                            if (valid) {
+#pragma unroll
+                                for (int i = 0; i < 32; i += 8) {
+                                    uint32_t h[4];
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        const __nv_bfloat162 x = __floats2bfloat162_rn(o[i + 2 * e] * inv, o[i + 2 * e + 1] * inv);
+                                        h[e] = *reinterpret_cast<const uint32_t *>(&x);
+                                    }
+                                    if (c + i < p.d) *reinterpret_cast<uint4 *>(dst + c + i) = make_uint4(h[0], h[1], h[2], h[3]);
+                                }
+                            }
+                        }
+                    } else {
+                        PartPlace at{nullptr, nullptr};
+                        if (valid) {
+                            at = attn_place(p, PartJob{j.seq, j.head, j.tok0, j.alt != 0}, j.first != 0, stream, row);
+                            *reinterpret_cast<float2 *>(at.ml) = make_float2(m, l);
+                        }
+#pragma unroll 1
+                        for (int c = 0; c < DP; c += 32) {
+                            float o[32];
+                            tmem_ld32(to + c, o);
+                            if (valid) {
+#pragma unroll
+                                for (int i = 0; i < 32; i += 8) {
+                                    if (c + i < p.d) store_8f(at.o + c + i, o + i);
+                                }
+                            }
+                        }
                     }
-                    write_out<DP>(to, p.d, valid, m == -INFINITY ? 0.f : 1.0f / l, dst, part);
                     tc_fence_before_sync();
                 }
             } else if (ok && valid && j.alt) {  // a segment of one tile leaves the other stream empty
@@ -729,7 +712,7 @@ template <int DP> static griffin_status launch_dp(const AttnPlan &plan, const At
             return GRIFFIN_ERR_UNSUPPORTED;  // (strides that the copy engine does not take)
     }
     // as many ring slots as fit beside the list of the sequences' first tiles
-    const size_t tail = ATC_BARS * 8 + ATC_SEGS * sizeof(Segment) + 8 + ((size_t)plan.n_seq + 1) * 4, fixed = 1024 + Cfg::NS * Cfg::Q_BYTES + tail;
+    const size_t tail = ATC_BARS * 8 + ATC_SEGS * sizeof(Segment) + 8 + ((size_t)plan.n_seq + 3) * 4, fixed = 1024 + Cfg::NS * Cfg::Q_BYTES + tail;
     prm.n_slots = (int)((232448 - fixed) / Cfg::KV_BYTES);
     if (prm.n_slots > Cfg::MAX_SLOTS) prm.n_slots = Cfg::MAX_SLOTS;
     const size_t smem = fixed + (size_t)prm.n_slots * Cfg::KV_BYTES;

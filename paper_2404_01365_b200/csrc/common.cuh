@@ -27,6 +27,7 @@ struct WsHeader {
     unsigned int meet_idx;   // ... and of the index-direct one
     unsigned int meet_stream;  // ... and of the register-streaming one
     unsigned int pool_stream;  // that kernel's count of claims on its pool of pairs (runs round once per call)
+    unsigned int queue_attn;   // jobs taken by the attention kernel (0 again after each call)
 };
 
 __device__ __forceinline__ void raise_status(void *ws, int status, int detail) {
