@@ -549,6 +549,9 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
             for (; u < n && ok; u += NS) {
                 const uint32_t U = U0 + u, buf = U & 1;
                 const KeyTile k = key_tile(p, j, j.t0 + (int)(dual ? u >> 1 : u));
+                // (one accumulator: whether P V of the unit before is known to be done; every one is waited for in turn, or
+                // a later wait would take the parity of an older one)
+                bool o_seen = u == 0;
                 ok = warp_wait(&s_full[buf], (U >> 1) & 1, abort, p.ws, 57);
                 if (!ok) break;
                 tc_fence_after_sync();
@@ -578,7 +581,10 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                         if (started) {
                             // (one accumulator: S of this unit was issued before P V of the last one, so its barrier
                             // does not cover it)
-                            if (NS == 1 && !(ok = warp_wait(&o_full[0], (U - 1) & 1, abort, p.ws, 59))) break;
+                            if (NS == 1) {
+                                if (!(ok = warp_wait(&o_full[0], (U - 1) & 1, abort, p.ws, 59))) break;
+                                o_seen = true;
+                            }
                             tc_fence_after_sync();
                             const uint32_t to = lanes + Cfg::O_COL + (NS == 2 ? buf : 0) * DP;
 #pragma unroll 1
@@ -613,6 +619,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                     started = true;
                     tmem_wait_st();
                 }
+                if (NS == 1 && !o_seen && !(ok = warp_wait(&o_full[0], (U - 1) & 1, abort, p.ws, 59))) break;
                 tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&p_ready[buf]);
