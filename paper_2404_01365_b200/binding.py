@@ -168,10 +168,16 @@ def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
+# (current_stream() builds a Stream object, 3 us; its handle alone is a tenth of a microsecond)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return C.c_void_p(stream.cuda_stream)
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def _check(st, what):
@@ -347,12 +353,15 @@ def _dtype(v):
 def _rows(t, n, heads, d, dtype, what):
     """Token stride of an [n, heads, d] (or [n, heads * d]) tensor whose tokens are rows of heads * d
     consecutive entries."""
-    st = t.stride()
-    inner = st[1:] == (d, 1) and t.shape[1:] == (heads, d) if t.dim() == 3 else t.dim() == 2 and st[1] == 1 and t.shape[1] == heads * d
-    if not inner or t.shape[0] < n or t.dtype != _TORCH_DTYPE[dtype]:
+    st, shape = t.stride(), t.shape
+    if len(st) == 3:
+        ok = shape[1] == heads and shape[2] == d and st[2] == 1 and st[1] == d
+    else:
+        ok = len(st) == 2 and shape[1] == heads * d and st[1] == 1
+    if not ok or shape[0] < n or t.dtype != _TORCH_DTYPE[dtype]:
         raise ValueError(f"{what}: expected {_TORCH_DTYPE[dtype]} [{n}, {heads}, {d}] with the heads of a token in one "
-                         f"row, got {t.dtype} {tuple(t.shape)} with strides {st}")
-    return st[0] if t.shape[0] > 1 else heads * d
+                         f"row, got {t.dtype} {tuple(shape)} with strides {st}")
+    return st[0] if shape[0] > 1 else heads * d
 
 
 def make_norm_desc(d, dtype, res_dtype=None, pre="rms", post="none", eps=1e-6, weight_offset=0.0, res_scale=1.0, out_scale=1.0,
@@ -367,31 +376,40 @@ def make_norm_weights(pre_w=None, pre_b=None, post_w=None, post_b=None):
     return w
 
 
-def _norm_rows(t, desc, dtype, T, what):
-    if t.dim() != 2 or t.shape[0] != T or t.shape[1] != desc.d or t.stride(1) != 1 or t.dtype != _TORCH_DTYPE[dtype]:
-        raise ValueError(f"{what}: expected {_TORCH_DTYPE[dtype]} [{T}, {desc.d}] with consecutive entries, got {t.dtype} "
-                         f"{tuple(t.shape)} with strides {t.stride()}")
-    return t.stride(0) if T > 1 else desc.d
+def _norm_rows(t, d, dtype, T, what):
+    st, shape = t.stride(), t.shape
+    if len(st) != 2 or shape[0] != T or shape[1] != d or st[1] != 1 or t.dtype != dtype:
+        raise ValueError(f"{what}: expected {dtype} [{T}, {d}] with consecutive entries, got {t.dtype} {tuple(shape)} with "
+                         f"strides {st}")
+    return st[0] if T > 1 else d
 
 
 def griffin_norm_residual(desc, weights, res, res_out, h, y=None, gate=None, stream=None):
     """res_out = a res + c act(gate) * post_norm(y), h = pre_norm(res_out) for the rows of res [T, d].  y, gate, res_out
     and h may be None (see include/griffin_ff.h); gate is [d] or [T, d]."""
-    T = res.shape[0]
+    T, d = res.shape[0], desc.d
     if T == 0:
         return
-    ld = [0, 0, _norm_rows(res, desc, desc.res_dtype, T, "res"), 0, 0]
+    dt, rdt = _TORCH_DTYPE[desc.dtype], _TORCH_DTYPE[desc.res_dtype]
+    y_p = g_p = ro_p = h_p = None
+    ld_y = ld_g = ld_ro = ld_h = 0
+    ld_r = _norm_rows(res, d, rdt, T, "res")
     if y is not None:
-        ld[0] = _norm_rows(y, desc, desc.dtype, T, "y")
+        ld_y, y_p = _norm_rows(y, d, dt, T, "y"), y.data_ptr()
     if gate is not None:
-        ld[1] = _norm_rows(gate, desc, desc.dtype, T, "gate") if gate.dim() == 2 else \
-            _norm_rows(gate[None], desc, desc.dtype, 1, "gate") * 0
+        g_p = gate.data_ptr()
+        if gate.dim() == 2:
+            ld_g = _norm_rows(gate, d, dt, T, "gate")
+        else:
+            _norm_rows(gate[None], d, dt, 1, "gate")
     if res_out is not None:
-        ld[3] = _norm_rows(res_out, desc, desc.res_dtype, T, "res_out")
+        ld_ro, ro_p = _norm_rows(res_out, d, rdt, T, "res_out"), res_out.data_ptr()
     if h is not None:
-        ld[4] = _norm_rows(h, desc, desc.dtype, T, "h")
-    _check(load().griffin_norm_residual(C.byref(desc), C.byref(weights), T, _ptr(y), ld[0], _ptr(gate), ld[1], _ptr(res), ld[2],
-                                        _ptr(res_out), ld[3], _ptr(h), ld[4], _stream(stream)), "griffin_norm_residual")
+        ld_h, h_p = _norm_rows(h, d, dt, T, "h"), h.data_ptr()
+    st = load().griffin_norm_residual(C.byref(desc), C.byref(weights), T, y_p, ld_y, g_p, ld_g, res.data_ptr(), ld_r, ro_p, ld_ro,
+                                      h_p, ld_h, _stream(stream))
+    if st != OK:
+        raise GriffinError(st, "griffin_norm_residual")
 
 
 def make_attn_desc(n_q_heads, n_kv_heads, head_dim, page_size, dtype, scale=None):
@@ -445,13 +463,18 @@ def rope_table(n_pos, rot_dim, theta=10000.0, device=None):
 def griffin_kv_append(desc, batch, cache, rope, q, k, v, q_out, ws=None, stream=None):
     """New keys and values [n_tokens, n_kv_heads, head_dim] into the cache, keys and queries rotated; q and q_out may be
     None, q_out may be q."""
-    n, hq, hk, d = batch.n_tokens, desc.n_q_heads, desc.n_kv_heads, desc.head_dim
-    ld_q = 0 if q is None else _rows(q, n, hq, d, desc.dtype, "q")
-    ld_o = 0 if q_out is None else _rows(q_out, n, hq, d, desc.dtype, "q_out")
-    _check(load().griffin_kv_append(C.byref(desc), C.byref(batch), C.byref(cache), None if rope is None else C.byref(rope),
-                                    _ptr(q), ld_q, _ptr(k), _rows(k, n, hk, d, desc.dtype, "k"), _ptr(v),
-                                    _rows(v, n, hk, d, desc.dtype, "v"), _ptr(q_out), ld_o, _ptr(ws), _stream(stream)),
-           "griffin_kv_append")
+    n, hq, hk, d, dt = batch.n_tokens, desc.n_q_heads, desc.n_kv_heads, desc.head_dim, desc.dtype
+    q_p = o_p = None
+    ld_q = ld_o = 0
+    if q is not None:
+        ld_q, q_p = _rows(q, n, hq, d, dt, "q"), q.data_ptr()
+    if q_out is not None:
+        ld_o, o_p = _rows(q_out, n, hq, d, dt, "q_out"), q_out.data_ptr()
+    st = load().griffin_kv_append(C.byref(desc), C.byref(batch), C.byref(cache), None if rope is None else C.byref(rope), q_p, ld_q,
+                                  k.data_ptr(), _rows(k, n, hk, d, dt, "k"), v.data_ptr(), _rows(v, n, hk, d, dt, "v"), o_p, ld_o,
+                                  None if ws is None else ws.data_ptr(), _stream(stream))
+    if st != OK:
+        raise GriffinError(st, "griffin_kv_append")
 
 
 def griffin_attn_workspace_bytes(desc, n_tokens_max, n_seq_max):
@@ -470,7 +493,8 @@ def alloc_attn_workspace(desc, n_tokens_max, n_seq_max, device, stream=None):
 def griffin_attn_prefix(desc, batch, cache, q, out, ws, stream=None):
     """Attention of the batch's new tokens over the shared prefix and their own sequences; q, out [n_tokens, n_q_heads,
     head_dim]."""
-    n, hq, d = batch.n_tokens, desc.n_q_heads, desc.head_dim
-    _check(load().griffin_attn_prefix(C.byref(desc), C.byref(batch), C.byref(cache), _ptr(q), _rows(q, n, hq, d, desc.dtype, "q"),
-                                      _ptr(out), _rows(out, n, hq, d, desc.dtype, "out"), _ptr(ws), ws.numel(), _stream(stream)),
-           "griffin_attn_prefix")
+    n, hq, d, dt = batch.n_tokens, desc.n_q_heads, desc.head_dim, desc.dtype
+    st = load().griffin_attn_prefix(C.byref(desc), C.byref(batch), C.byref(cache), q.data_ptr(), _rows(q, n, hq, d, dt, "q"),
+                                    out.data_ptr(), _rows(out, n, hq, d, dt, "out"), ws.data_ptr(), ws.numel(), _stream(stream))
+    if st != OK:
+        raise GriffinError(st, "griffin_attn_prefix")
