@@ -14,7 +14,7 @@ struct NormParams {
     const void *y, *gate, *res, *pre_w, *pre_b, *post_w, *post_b;
     void *res_out, *h;
     long long ld_y, ld_gate, ld_res, ld_res_out, ld_h;
-    int T, d, pre, post, gate_act;
+    int T, d, pre, post, gate_act, wide;  // wide: every row of y, gate, res, res_out and h starts on a 32-byte boundary
     float eps, w0, res_scale, out_scale;
 };
 
@@ -81,7 +81,7 @@ __device__ __forceinline__ float gate_value(int act, float t) {
 
 // T: storage of y, h, gate, weights; R: of the residual stream.
 template <typename T, typename R, int VPT, bool WARP_ROW>
-__global__ void __launch_bounds__(WARP_ROW ? 128 : 512) norm_residual_kernel(const __grid_constant__ NormParams p) {
+__global__ void __launch_bounds__(WARP_ROW ? 128 : 512, WARP_ROW ? 8 : VPT == 1 ? 4 : VPT == 2 ? 2 : 1) norm_residual_kernel(const __grid_constant__ NormParams p) {
     __shared__ float red[4][32];
     const int row = WARP_ROW ? blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
     const int v0 = WARP_ROW ? threadIdx.x & 31 : threadIdx.x, step = WARP_ROW ? 32 : blockDim.x;
@@ -97,8 +97,8 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : 512) norm_residual_kernel(con
 #pragma unroll
         for (int i = 0; i < 8; ++i) r[k][i] = u[k][i] = 0.f;
         if (v >= nv) continue;
-        load8<R>(p.res, row * p.ld_res + v * 8, r[k]);
-        if (p.y != nullptr) load8<T>(p.y, row * p.ld_y + v * 8, u[k]);
+        load8<R>(p.res, row * p.ld_res + v * 8, r[k], p.wide);
+        if (p.y != nullptr) load8<T>(p.y, row * p.ld_y + v * 8, u[k], p.wide);
     }
     if (p.y != nullptr && p.post != GRIFFIN_NORM_NONE)
         norm_row<T, VPT, WARP_ROW>(u, p.post, p.post_w, p.post_b, p, v0, step, &red[0]);
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : 512) norm_residual_kernel(con
         if (v >= nv) continue;
         if (p.y != nullptr && p.gate != nullptr) {
             float g[8];
-            load8<T>(p.gate, row * p.ld_gate + v * 8, g);
+            load8<T>(p.gate, row * p.ld_gate + v * 8, g, p.wide);
 #pragma unroll
             for (int i = 0; i < 8; ++i) u[k][i] *= gate_value(p.gate_act, g[i]);
         }
@@ -119,14 +119,14 @@ __global__ void __launch_bounds__(WARP_ROW ? 128 : 512) norm_residual_kernel(con
 #pragma unroll
             for (int i = 0; i < 8; ++i) r[k][i] *= p.res_scale;
         }
-        if (p.res_out != nullptr) store8<R>(p.res_out, row * p.ld_res_out + v * 8, r[k]);
+        if (p.res_out != nullptr) store8<R>(p.res_out, row * p.ld_res_out + v * 8, r[k], p.wide);
     }
     if (p.h == nullptr) return;
     if (p.pre != GRIFFIN_NORM_NONE) norm_row<T, VPT, WARP_ROW>(r, p.pre, p.pre_w, p.pre_b, p, v0, step, &red[2]);
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
         const int v = v0 + k * step;
-        if (v < nv) store8<T>(p.h, row * p.ld_h + v * 8, r[k]);
+        if (v < nv) store8<T>(p.h, row * p.ld_h + v * 8, r[k], p.wide);
     }
 }
 
@@ -154,6 +154,10 @@ griffin_status launch_norm_residual(const griffin_norm_desc *desc, const griffin
     p.pre_w = w->pre_w; p.pre_b = w->pre_b; p.post_w = w->post_w; p.post_b = w->post_b;
     p.ld_y = ld_y; p.ld_gate = ld_gate; p.ld_res = ld_res; p.ld_res_out = ld_res_out; p.ld_h = ld_h;
     p.T = T; p.d = desc->d; p.pre = desc->pre_norm; p.post = desc->post_norm; p.gate_act = desc->gate_act;
+    const auto on32 = [](const void *q, int64_t ld, int bytes) { return (reinterpret_cast<uintptr_t>(q) & 31) == 0 && ld * bytes % 32 == 0; };
+    const int eb = desc->dtype == GRIFFIN_DT_F32 ? 4 : 2, rb = desc->res_dtype == GRIFFIN_DT_F32 ? 4 : 2;
+    // (a pointer that is not there is on every boundary)
+    p.wide = on32(y, ld_y, eb) && on32(gate, ld_gate, eb) && on32(res, ld_res, rb) && on32(res_out, ld_res_out, rb) && on32(h, ld_h, eb);
     p.eps = desc->eps; p.w0 = desc->weight_offset; p.res_scale = desc->res_scale; p.out_scale = desc->out_scale;
     int threads, rows;
     const void *fn = desc->dtype == GRIFFIN_DT_F32       ? norm_kernel<float, float>(desc->d >> 3, &threads, &rows)

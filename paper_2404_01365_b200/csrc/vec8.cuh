@@ -31,4 +31,28 @@ template <typename T> __device__ __forceinline__ void store8(void *base, long lo
     }
 }
 
+// The same where the caller knows whether the address is on a 32-byte boundary: then fp32 takes one access as well.
+template <typename T> __device__ __forceinline__ void load8(const void *base, long long at, float (&f)[8], bool wide) {
+    if constexpr (sizeof(T) == 4) {
+        if (wide) {
+            asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7])
+                         : "l"(static_cast<const T *>(base) + at));
+            return;
+        }
+    }
+    load8<T>(base, at, f);
+}
+template <typename T> __device__ __forceinline__ void store8(void *base, long long at, const float (&f)[8], bool wide) {
+    if constexpr (sizeof(T) == 4) {
+        if (wide) {
+            asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(static_cast<T *>(base) + at), "f"(f[0]),
+                         "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7])
+                         : "memory");
+            return;
+        }
+    }
+    store8<T>(base, at, f);
+}
+
 }  // namespace griffin
