@@ -1,9 +1,13 @@
 // New tokens into the paged cache, keys and queries rotated by their positions on the way:
 //   (x, y) -> (x cos - y sin, x sin + y cos), the angle's cosine and sine read from an fp32 table.
 //
-// One pass over q, k and v: each thread takes 16 entries of a head at a time, which are the two halves of
-// 8 pairs (HALF: 8 entries at j and 8 at j + rot/2; PAIRS: 16 neighbours), 16 entries behind the rotated
-// part, or 16 of v.  Both ends of a pair are in one thread, so q may be turned in place.
+// One pass over q, k and v.  A thread takes one piece of one head, of TPC tokens: the two halves
+// of 8 pairs (HALF: 8 entries at j and 8 at j + rot/2; PAIRS: 16 neighbours), or 16 entries that do not turn (behind the
+// rotated part, or of v).  Both ends of a pair are in one thread, so q may be turned in place.
+//
+// A token's place takes three dependent trips to L2 (sequence, length, page) and its angles a fourth: the CTA takes
+// them for its TPC tokens together (with more than one, the angles through shared memory: every head wants the
+// same ones), while the data of all the tokens is on the way.
 #include "common.cuh"
 #include "layer.h"
 #include "vec8.cuh"
@@ -17,107 +21,150 @@ struct AppendParams {
     const int *q_start, *seq_len, *page_table;
     void *ws;
     long long ld_q, ld_k, ld_v, ld_q_out, stride_page, stride_head, stride_token;
-    int n_seq, n_pages, table_stride, prefix_len, page_shift;
-    int hq, hkv, d, rot, n_pos, style, groups_qk, groups_v;  // groups: 16-entry pieces of one head
+    int n_tokens, n_seq, n_pages, table_stride, prefix_len, page_shift;
+    int hq, hkv, d, rot, n_pos, style;
 };
 
 constexpr int APPEND_THREADS = 128;
 
-template <typename T>
+template <typename T> struct Piece {  // a thread's two times 8 entries, as they lie in memory
+    uint4 v[sizeof(T)];               // (bf16: one 16-byte word for 8 entries; fp32: two)
+};
+template <typename T> __device__ __forceinline__ void load_half(Piece<T> &p, int half, const T *at) {
+    constexpr int N = sizeof(T) / 2;
+#pragma unroll
+    for (int i = 0; i < N; ++i) p.v[half * N + i] = reinterpret_cast<const uint4 *>(at)[i];
+}
+template <typename T> __device__ __forceinline__ void store_half(const Piece<T> &p, int half, T *at) {
+    constexpr int N = sizeof(T) / 2;
+#pragma unroll
+    for (int i = 0; i < N; ++i) reinterpret_cast<uint4 *>(at)[i] = p.v[half * N + i];
+}
+template <typename T> __device__ __forceinline__ void get_half(const Piece<T> &p, int half, float (&f)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        Elem<__nv_bfloat16>::unpack(p.v[half], f);
+    } else {
+        const uint4 a = p.v[2 * half], b = p.v[2 * half + 1];
+        f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y); f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
+        f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y); f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
+    }
+}
+
+template <typename T, int TPC>
 __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const __grid_constant__ AppendParams p) {
-    const int t = blockIdx.x;
+    __shared__ long long s_at[TPC];   // the tokens' places in the cache, in elements; -1: none; -2: behind the last sequence
+    __shared__ int s_pos[TPC];
+    __shared__ __align__(16) float s_table[TPC][TPC > 1 ? 256 : 4];
+    const int t0 = blockIdx.x * TPC, pieces = (p.d + 15) >> 4, per_round = APPEND_THREADS / pieces;  // heads side by side
+    const int slot = threadIdx.x / pieces, piece = threadIdx.x - slot * pieces, turned = p.rot >> 4;
+    const int hq = p.q != nullptr ? p.hq : 0, h = blockIdx.y * per_round + slot;
+    const bool on = slot < per_round && h < hq + 2 * p.hkv, is_v = h >= hq + p.hkv, is_q = h < hq;   // heads: q, k, v
+    const bool turn = on && !is_v && piece < turned;
+    const int e0 = turn && p.style == GRIFFIN_ROPE_HALF ? piece * 8 : piece * 16;
+    const int e1 = turn && p.style == GRIFFIN_ROPE_HALF ? (p.rot >> 1) + piece * 8 : piece * 16 + 8;
+    const bool two = e1 < p.d;        // (the last piece of a head may be one of 8)
+    const T *const src = static_cast<const T *>(is_q ? p.q : is_v ? p.v : p.k) + (is_q ? h : is_v ? h - hq - p.hkv : h - hq) * p.d;
+    const long long ld = is_q ? p.ld_q : is_v ? p.ld_v : p.ld_k;
     pdl_launch_dependents();
     pdl_wait_prior_grids();
-    // the token's sequence: how many sequences end at or before it (empty ones included)
-    int seq = 0;
-    for (int s0 = 0; s0 < p.n_seq; s0 += APPEND_THREADS) {
-        const int s = s0 + threadIdx.x;
-        seq += __syncthreads_count(s < p.n_seq && __ldg(p.q_start + s + 1) <= t);
-    }
-    if (seq >= p.n_seq) return;  // a row behind the last sequence
-    const int i = __ldg(p.seq_len + seq) - (__ldg(p.q_start + seq + 1) - t);
-    const int pos = p.prefix_len + i;
-    long long at = -1;  // the token's place in the cache, in elements; -1: it has none
-    if (i >= 0) {
-        const int col = i >> p.page_shift;
-        const int page = col < p.table_stride ? __ldg(p.page_table + (long long)seq * p.table_stride + col) : -1;
-        if (page >= 0 && page < p.n_pages && (p.rot == 0 || pos < p.n_pos))
-            at = page * p.stride_page + (i & ((1 << p.page_shift) - 1)) * p.stride_token;
-        else if (threadIdx.x == 0 && blockIdx.y == 0)
-            raise_status(p.ws, DEV_STATUS_BAD_INDEX, 40);
-    }
 
-    const int hq = p.q != nullptr ? p.hq : 0;
-    const int n_qk = (hq + p.hkv) * p.groups_qk, n = n_qk + p.hkv * p.groups_v;
-    for (int it = blockIdx.y * APPEND_THREADS + threadIdx.x; it < n; it += gridDim.y * APPEND_THREADS) {
-        const bool is_v = it >= n_qk;
-        const int per = is_v ? p.groups_v : p.groups_qk, j = is_v ? it - n_qk : it;
-        int head = j / per;
-        const int piece = j - head * per;
-        const void *src;
-        void *dst;
-        long long from, to;
-        bool to_q = false;
-        if (is_v) {
-            src = p.v; from = t * p.ld_v + head * p.d;
-            dst = p.v_cache; to = at + head * p.stride_head;
-        } else if (head < hq) {
-            src = p.q; from = t * p.ld_q + head * p.d;
-            dst = p.q_out; to = t * p.ld_q_out + head * p.d;
-            to_q = true;
-        } else {
-            head -= hq;
-            src = p.k; from = t * p.ld_k + head * p.d;
-            dst = p.k_cache; to = at + head * p.stride_head;
+    Piece<T> x[TPC];
+#pragma unroll
+    for (int u = 0; u < TPC; ++u)
+        if (on && t0 + u < p.n_tokens) {
+            load_half<T>(x[u], 0, src + (t0 + u) * ld + e0);
+            if (two) load_half<T>(x[u], 1, src + (t0 + u) * ld + e1);
         }
-        if (!to_q && at < 0) continue;
-        const int turned = is_v ? 0 : p.rot >> 4;  // pieces of the head that turn
-        float a[8], b[8];
-        if (piece < turned) {
-            const int e0 = p.style == GRIFFIN_ROPE_HALF ? piece * 8 : piece * 16;
-            const int e1 = p.style == GRIFFIN_ROPE_HALF ? (p.rot >> 1) + piece * 8 : piece * 16 + 8;
-            load8<T>(src, from + e0, a);
-            load8<T>(src, from + e1, b);
-            if (at >= 0) {
-                float c[8], s[8];
-                const float *row = p.table + (long long)pos * p.rot + piece * 8;
-                load8<float>(row, 0, c);
-                load8<float>(row, p.rot >> 1, s);
-                if (p.style == GRIFFIN_ROPE_HALF) {
+    // the first token's sequence: how many sequences end at or before it (empty ones included)
+    int seq = 0;
+    if (p.n_seq > 1) {
+        for (int s0 = 0; s0 < p.n_seq; s0 += APPEND_THREADS) {
+            const int s = s0 + threadIdx.x;
+            seq += __syncthreads_count(s < p.n_seq && __ldg(p.q_start + s + 1) <= t0);
+        }
+    }
+    if (threadIdx.x < TPC) {
+        const int t = t0 + threadIdx.x;
+        while (seq < p.n_seq && __ldg(p.q_start + seq + 1) <= t) ++seq;
+        long long at = -2;
+        int pos = 0;
+        if (seq < p.n_seq && t < p.n_tokens) {
+            const int k = __ldg(p.seq_len + seq) - (__ldg(p.q_start + seq + 1) - t);   // index among its own tokens
+            at = -1;
+            pos = p.prefix_len + k;
+            if (k >= 0) {
+                const int col = k >> p.page_shift;
+                const int page = col < p.table_stride ? __ldg(p.page_table + (long long)seq * p.table_stride + col) : -1;
+                if (page >= 0 && page < p.n_pages && (p.rot == 0 || pos < p.n_pos))
+                    at = page * p.stride_page + (k & ((1 << p.page_shift) - 1)) * p.stride_token;
+                else if (blockIdx.y == 0)
+                    raise_status(p.ws, DEV_STATUS_BAD_INDEX, 40);
+            }
+        }
+        s_at[threadIdx.x] = at;
+        s_pos[threadIdx.x] = pos;
+    }
+    __syncthreads();
+    if (TPC > 1 && p.rot > 0) {
+        const int quads = p.rot >> 2;
+        for (int i = threadIdx.x; i < TPC * quads; i += APPEND_THREADS) {
+            const int u = i / quads, e = (i - u * quads) * 4;
+            if (s_at[u] >= 0)
+                *reinterpret_cast<float4 *>(&s_table[u][e]) = __ldg(reinterpret_cast<const float4 *>(p.table + (long long)s_pos[u] * p.rot + e));
+        }
+        __syncthreads();
+    }
+    if (!on) return;
+    T *const cache = static_cast<T *>(is_v ? p.v_cache : p.k_cache) + (is_v ? h - hq - p.hkv : h - hq) * p.stride_head;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float x = a[e], y = b[e];
-                        a[e] = x * c[e] - y * s[e];
-                        b[e] = x * s[e] + y * c[e];
-                    }
-                } else {
+    for (int u = 0; u < TPC; ++u) {
+        const long long at = s_at[u];
+        if (at == -2) return;
+        const int t = t0 + u;
+        if (at < 0) {   // padding, or a token that could not be placed
+            if (!is_q) continue;
 #pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const float x0 = a[e], y0 = a[e + 1], x1 = b[e], y1 = b[e + 1];
-                        a[e] = x0 * c[e >> 1] - y0 * s[e >> 1];
-                        a[e + 1] = x0 * s[e >> 1] + y0 * c[e >> 1];
-                        b[e] = x1 * c[4 + (e >> 1)] - y1 * s[4 + (e >> 1)];
-                        b[e + 1] = x1 * s[4 + (e >> 1)] + y1 * c[4 + (e >> 1)];
-                    }
+            for (int i = 0; i < (int)sizeof(T); ++i) x[u].v[i] = make_uint4(0, 0, 0, 0);
+        } else if (turn) {
+            float a[8], b[8], c[8], s[8];
+            const float *const row = TPC > 1 ? s_table[u] : p.table + (long long)s_pos[u] * p.rot;
+            load8<float>(row, piece * 8, c);
+            load8<float>(row, (p.rot >> 1) + piece * 8, s);
+            get_half<T>(x[u], 0, a);
+            get_half<T>(x[u], 1, b);
+            if (p.style == GRIFFIN_ROPE_HALF) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = a[e], w = b[e];
+                    a[e] = v * c[e] - w * s[e];
+                    b[e] = v * s[e] + w * c[e];
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) a[e] = b[e] = 0.f;  // padding, or a token that could not be placed
-            }
-            store8<T>(dst, to + e0, a);
-            store8<T>(dst, to + e1, b);
-        } else {
-            const int e0 = (is_v ? 0 : p.rot) + (piece - turned) * 16, n8 = e0 + 8 < p.d ? 2 : 1;
-            for (int h = 0; h < n8; ++h) {
-                load8<T>(src, from + e0 + h * 8, a);
-                if (at < 0) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) a[e] = 0.f;
+                for (int e = 0; e < 8; e += 2) {
+                    const float v0 = a[e], w0 = a[e + 1], v1 = b[e], w1 = b[e + 1];
+                    a[e] = v0 * c[e >> 1] - w0 * s[e >> 1];
+                    a[e + 1] = v0 * s[e >> 1] + w0 * c[e >> 1];
+                    b[e] = v1 * c[4 + (e >> 1)] - w1 * s[4 + (e >> 1)];
+                    b[e + 1] = v1 * s[4 + (e >> 1)] + w1 * c[4 + (e >> 1)];
                 }
-                store8<T>(dst, to + e0 + h * 8, a);
             }
+            T *const dst = is_q ? static_cast<T *>(p.q_out) + t * p.ld_q_out + h * p.d : cache + at;
+            store8<T>(dst, e0, a);
+            store8<T>(dst, e1, b);
+            continue;
         }
+        T *const dst = is_q ? static_cast<T *>(p.q_out) + t * p.ld_q_out + h * p.d : cache + at;
+        store_half<T>(x[u], 0, dst + e0);
+        if (two) store_half<T>(x[u], 1, dst + e1);
     }
+}
+
+// (800 tokens of 16 heads of 80, fp32: 4.5 us one by one, 5.3 in pairs; 4096 tokens of 48 heads of 128, bf16: 21.3 us one by one,
+// 20.5 in pairs, 21.0 and 23.7 by four and eight: a copy of the same bytes takes 16)
+constexpr int APPEND_TOKENS = 2;
+template <typename T> static const void *append_kernel(bool many) {
+    return many ? reinterpret_cast<const void *>(kv_append_kernel<T, APPEND_TOKENS>) : reinterpret_cast<const void *>(kv_append_kernel<T, 1>);
 }
 
 griffin_status launch_kv_append(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
@@ -130,25 +177,21 @@ griffin_status launch_kv_append(const griffin_attn_desc *desc, const griffin_att
     p.ws = ws;
     p.ld_q = ld_q; p.ld_k = ld_k; p.ld_v = ld_v; p.ld_q_out = ld_q_out;
     p.stride_page = cache->stride_page; p.stride_head = cache->stride_head; p.stride_token = cache->stride_token;
-    p.n_seq = batch->n_seq; p.n_pages = cache->n_pages; p.table_stride = batch->table_stride; p.prefix_len = batch->prefix_len;
+    p.n_tokens = batch->n_tokens; p.n_seq = batch->n_seq; p.n_pages = cache->n_pages; p.table_stride = batch->table_stride; p.prefix_len = batch->prefix_len;
     while ((1 << p.page_shift) < desc->page_size) ++p.page_shift;
     p.hq = desc->n_q_heads; p.hkv = desc->n_kv_heads; p.d = desc->head_dim;
     if (rope != nullptr) {
         p.table = rope->table; p.rot = rope->rot_dim; p.n_pos = rope->n_pos; p.style = rope->style;
     }
-    p.groups_qk = (p.rot >> 4) + (p.d - p.rot + 15) / 16;
-    p.groups_v = (p.d + 15) / 16;
-    const int n = ((q != nullptr ? p.hq : 0) + p.hkv) * p.groups_qk + p.hkv * p.groups_v;
-    // the pieces of one token on several CTAs while the tokens alone do not fill the device, else three
-    // pieces per thread
+    // several tokens per CTA once there are enough for all SMs
     const int sms = device_sm_count();
     if (sms <= 0) return GRIFFIN_ERR_CUDA;
-    const int full = (n + APPEND_THREADS - 1) / APPEND_THREADS;
-    const int y = batch->n_tokens >= 4 * sms ? (full + 2) / 3 : full;
-    const void *fn = desc->dtype == GRIFFIN_DT_F32 ? reinterpret_cast<const void *>(kv_append_kernel<float>)
-                                                   : reinterpret_cast<const void *>(kv_append_kernel<__nv_bfloat16>);
+    const bool many = batch->n_tokens >= 16 * sms;
+    const int per_round = APPEND_THREADS / ((p.d + 15) / 16), tpc = many ? APPEND_TOKENS : 1;
+    const int x = (batch->n_tokens + tpc - 1) / tpc, y = ((q != nullptr ? p.hq : 0) + 2 * p.hkv + per_round - 1) / per_round;
+    const void *fn = desc->dtype == GRIFFIN_DT_F32 ? append_kernel<float>(many) : append_kernel<__nv_bfloat16>(many);
     void *args[] = {&p};
-    return launch_maybe_overlapped(fn, dim3(batch->n_tokens, y), dim3(APPEND_THREADS), 0, stream, true, args) == cudaSuccess
+    return launch_maybe_overlapped(fn, dim3(x, y), dim3(APPEND_THREADS), 0, stream, true, args) == cudaSuccess
                ? GRIFFIN_OK
                : GRIFFIN_ERR_CUDA;
 }
