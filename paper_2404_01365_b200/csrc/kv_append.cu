@@ -83,28 +83,32 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const __grid_
             seq += __syncthreads_count(s < p.n_seq && __ldg(p.q_start + s + 1) <= t0);
         }
     }
-    if (threadIdx.x < TPC) {
-        const int t = t0 + threadIdx.x;
-        while (seq < p.n_seq && __ldg(p.q_start + seq + 1) <= t) ++seq;
-        long long at = -2;
-        int pos = 0;
+    // a token's place and position (with one token every thread looks them up for itself)
+    long long at1 = -2;
+    int pos1 = 0;
+    if (TPC == 1 || threadIdx.x < TPC) {
+        const int t = TPC == 1 ? t0 : t0 + threadIdx.x;
+        if (TPC > 1 || p.n_seq == 1)  // (otherwise the count above was this token's)
+            while (seq < p.n_seq && __ldg(p.q_start + seq + 1) <= t) ++seq;
         if (seq < p.n_seq && t < p.n_tokens) {
             const int k = __ldg(p.seq_len + seq) - (__ldg(p.q_start + seq + 1) - t);   // index among its own tokens
-            at = -1;
-            pos = p.prefix_len + k;
+            at1 = -1;
+            pos1 = p.prefix_len + k;
             if (k >= 0) {
                 const int col = k >> p.page_shift;
                 const int page = col < p.table_stride ? __ldg(p.page_table + (long long)seq * p.table_stride + col) : -1;
-                if (page >= 0 && page < p.n_pages && (p.rot == 0 || pos < p.n_pos))
-                    at = page * p.stride_page + (k & ((1 << p.page_shift) - 1)) * p.stride_token;
-                else if (blockIdx.y == 0)
+                if (page >= 0 && page < p.n_pages && (p.rot == 0 || pos1 < p.n_pos))
+                    at1 = page * p.stride_page + (k & ((1 << p.page_shift) - 1)) * p.stride_token;
+                else if (blockIdx.y == 0 && threadIdx.x < TPC)
                     raise_status(p.ws, DEV_STATUS_BAD_INDEX, 40);
             }
         }
-        s_at[threadIdx.x] = at;
-        s_pos[threadIdx.x] = pos;
+        if (TPC > 1) {
+            s_at[threadIdx.x] = at1;
+            s_pos[threadIdx.x] = pos1;
+        }
     }
-    __syncthreads();
+    if (TPC > 1) __syncthreads();
     if (TPC > 1 && p.rot > 0) {
         const int quads = p.rot >> 2;
         for (int i = threadIdx.x; i < TPC * quads; i += APPEND_THREADS) {
@@ -118,7 +122,7 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const __grid_
     T *const cache = static_cast<T *>(is_v ? p.v_cache : p.k_cache) + (is_v ? h - hq - p.hkv : h - hq) * p.stride_head;
 #pragma unroll
     for (int u = 0; u < TPC; ++u) {
-        const long long at = s_at[u];
+        const long long at = TPC > 1 ? s_at[u] : at1;
         if (at == -2) return;
         const int t = t0 + u;
         if (at < 0) {   // padding, or a token that could not be placed
@@ -127,7 +131,7 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const __grid_
             for (int i = 0; i < (int)sizeof(T); ++i) x[u].v[i] = make_uint4(0, 0, 0, 0);
         } else if (turn) {
             float a[8], b[8], c[8], s[8];
-            const float *const row = TPC > 1 ? s_table[u] : p.table + (long long)s_pos[u] * p.rot;
+            const float *const row = TPC > 1 ? s_table[u] : p.table + (long long)pos1 * p.rot;
             load8<float>(row, piece * 8, c);
             load8<float>(row, (p.rot >> 1) + piece * 8, s);
             get_half<T>(x[u], 0, a);
@@ -160,7 +164,7 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const __grid_
     }
 }
 
-// (800 tokens of 16 heads of 80, fp32: 4.5 us one by one, 5.3 in pairs; 4096 tokens of 48 heads of 128, bf16: 21.3 us one by one,
+// (800 tokens of 16 heads of 80, fp32: 5.4 us one by one, 6.3 in pairs; 4096 tokens of 48 heads of 128, bf16: 21.3 us one by one,
 // 20.5 in pairs, 21.0 and 23.7 by four and eight: a copy of the same bytes takes 16)
 constexpr int APPEND_TOKENS = 2;
 template <typename T> static const void *append_kernel(bool many) {
