@@ -9,7 +9,7 @@ namespace griffin {
 constexpr int ATTN_MAX_GRID = 148;  // CTAs at most (one per SM of a B200)
 
 static AttnShape shape_of(const griffin_attn_desc *desc) {
-    return desc->dtype == GRIFFIN_DT_F32 ? attn_simt_shape() : attn_tc_shape(desc->head_dim);
+    return desc->dtype == GRIFFIN_DT_F32 ? attn_simt_shape(desc->head_dim) : attn_tc_shape(desc->head_dim);
 }
 
 struct AttnScratch {

@@ -17,7 +17,7 @@ struct AttnShape {
     int tile_rows, tiles_per_block, kt, alt;
 };
 
-AttnShape attn_simt_shape();
+AttnShape attn_simt_shape(int head_dim);
 AttnShape attn_tc_shape(int head_dim);
 griffin_status launch_attn_tc(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // bf16
 griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // fp32

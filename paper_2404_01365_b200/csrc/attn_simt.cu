@@ -1,31 +1,205 @@
 // Attention over the shared prefix and each sequence's own keys, fp32 storage, on the plain fp32 pipes:
 //   S = scale Q K^T, masked by place;  m' = max(m, max S);  P = 2^(S - m');
 //   l = l 2^(m - m') + sum P;  O = O 2^(m - m') + P V        (S in units of log2, all fp32)
-// one CTA of 256 threads per SM, each with its share of the call's key tiles (attn_plan.cuh).  Keys and
-// values behind what any row of the block sees are read as zeros, whatever the cache holds there.
+// one CTA of 256 threads per SM, each with its share of the call's key tiles (attn_plan.cuh).
+//
+// A half warp has A neighbouring rows and walks the whole tile: keys tx, tx + 16, ... of S, entries 4 tx .. of O.  So
+// the softmax stays in registers (four shuffles a row), and P goes through shared memory within its own warp; the CTA
+// meets once a tile, for the keys and values.  Those come by cp.async, the next tile's behind the present one's
+// products, and their pages are looked up a tile ahead.  Keys and values behind what any row of the block sees are
+// read as zeros, whatever the cache holds there.
 #include "attn.h"
 #include "attn_join.cuh"
 #include "vec8.cuh"
 
 namespace griffin {
 
-constexpr int SIMT_ROWS = 64, SIMT_KT = 32, SIMT_THREADS = 256;
+constexpr int SIMT_ROWS = 64, SIMT_THREADS = 256;
 
-template <int DP> constexpr size_t simt_smem(int n_seq) {
-    return (size_t)(SIMT_ROWS + 2 * SIMT_KT) * (DP + 4) * 4 + SIMT_ROWS * (SIMT_KT + 1) * 4 + 3 * SIMT_ROWS * 4 +
-           ((size_t)n_seq + 3) * 4;
+// DP: the head's width rounded up to 64, 128 or 256.
+template <int DP> struct SimtCfg {
+    static constexpr int KT = DP == 256 ? 32 : 64;                 // keys per tile: two tiles fit beside the queries
+    static constexpr int LD = DP + 4;                              // (rows 16 bytes apart in the banks)
+    static constexpr int TILE = KT * LD;                           // keys or values of a tile
+    static constexpr int LDP = KT + 4;
+    static constexpr int PASSES = KT * (DP / 4) / SIMT_THREADS;    // 16-byte pieces per thread, keys as values
+    static size_t smem(int n_seq) { return (SIMT_ROWS * LD + 4 * TILE + SIMT_ROWS * LDP + (size_t)n_seq + 3) * 4; }
+};
+
+__device__ __forceinline__ void copy16(float *dst, const float *src, bool there) {   // zeros where nothing is there
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
+                 "r"(there ? 16 : 0)
+                 : "memory");
+}
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
 }
 
-// DP: the head's width rounded up to 64, 128 or 256; entries from D on are zeros in shared memory.
+// The tiles of one segment, by which the kernel and its loads find keys.
+struct SimtKeys {
+    const int *own_pages;
+    int pre_tiles, own_len, t0, n, head;
+};
+template <int DP> __device__ __forceinline__ void tile_pages(const AttnPlan &p, const SimtKeys &s, int t, int (&page)[SimtCfg<DP>::PASSES]) {
+    const bool pre = t < s.pre_tiles;
+    const int k0 = (pre ? t : t - s.pre_tiles) * SimtCfg<DP>::KT, len = pre ? p.prefix_len : s.own_len;
+    const int *const pages = pre ? p.prefix_pages : s.own_pages;
+#pragma unroll
+    for (int i = 0; i < SimtCfg<DP>::PASSES; ++i) {
+        const int key = k0 + (threadIdx.x + i * SIMT_THREADS) / (DP / 4);
+        page[i] = key < len ? __ldg(pages + (key >> p.page_shift)) : -1;
+    }
+}
+template <int DP>
+__device__ __forceinline__ void tile_copy(const AttnPlan &p, const AttnData &x, const SimtKeys &s, int t,
+                                          const int (&page)[SimtCfg<DP>::PASSES], float *sk, float *sv) {
+    const bool pre = t < s.pre_tiles;
+    const int k0 = (pre ? t : t - s.pre_tiles) * SimtCfg<DP>::KT, len = pre ? p.prefix_len : s.own_len;
+    const float *const k = static_cast<const float *>(x.k), *const v = static_cast<const float *>(x.v);
+#pragma unroll
+    for (int i = 0; i < SimtCfg<DP>::PASSES; ++i) {
+        const int c = threadIdx.x + i * SIMT_THREADS, r = c / (DP / 4), e = c % (DP / 4) * 4, key = k0 + r;
+        if (e >= p.d) continue;
+        const bool there = key < len && page[i] >= 0 && page[i] < p.n_pages;
+        if (key < len && !there) raise_status(p.ws, DEV_STATUS_BAD_INDEX, 42);
+        const long long at = there ? page[i] * x.stride_page + s.head * x.stride_head + (key & ((1 << p.page_shift) - 1)) * x.stride_token + e : 0;
+        copy16(sk + r * SimtCfg<DP>::LD + e, k + at, there);
+        copy16(sv + r * SimtCfg<DP>::LD + e, v + at, there);
+    }
+}
+
+// The rows of one segment, A to a half warp.  page: of the segment's first tile.
+template <int DP, int A>
+__device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &x, const AttnJob &j, const SimtKeys &keys, bool first,
+                                             bool whole, float *sq, float *skv, float *sp, int (&page)[SimtCfg<DP>::PASSES]) {
+    using Cfg = SimtCfg<DP>;
+    constexpr int KT = Cfg::KT, LD = Cfg::LD, LDP = Cfg::LDP, NK = KT / 16, NE = DP / 64;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const bool on = (ty & ~1) * A < j.rows;       // any row of the warp
+    float o[A][NE][4] = {}, m[A], l[A];
+#pragma unroll
+    for (int a = 0; a < A; ++a) m[a] = -INFINITY, l[a] = 0.f;
+    tile_copy<DP>(p, x, keys, keys.t0, page, skv, skv + Cfg::TILE);
+    if (keys.n > 1) tile_pages<DP>(p, keys, keys.t0 + 1, page);
+#pragma unroll 1
+    for (int i = 0; i < keys.n; ++i) {
+        const int t = keys.t0 + i;
+        const float *const sk = skv + (i & 1) * 2 * Cfg::TILE, *const sv = sk + Cfg::TILE;
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();   // this tile has come; the one before is done with
+        if (i + 1 < keys.n) {
+            float *const next = skv + (i + 1 & 1) * 2 * Cfg::TILE;
+            tile_copy<DP>(p, x, keys, t + 1, page, next, next + Cfg::TILE);
+            if (i + 2 < keys.n) tile_pages<DP>(p, keys, t + 2, page);
+        }
+        if (!on) continue;
+        float s[A][NK] = {};
+#pragma unroll 4
+        for (int e = 0; e < p.d; e += 4) {
+            float4 q[A];
+#pragma unroll
+            for (int a = 0; a < A; ++a) q[a] = *reinterpret_cast<const float4 *>(sq + (ty * A + a) * LD + e);
+#pragma unroll
+            for (int b = 0; b < NK; ++b) {
+                const float4 k = *reinterpret_cast<const float4 *>(sk + (tx + 16 * b) * LD + e);
+#pragma unroll
+                for (int a = 0; a < A; ++a)
+                    s[a][b] = fmaf(q[a].x, k.x, fmaf(q[a].y, k.y, fmaf(q[a].z, k.z, fmaf(q[a].w, k.w, s[a][b]))));
+            }
+        }
+        const bool pre = t < keys.pre_tiles;
+        const int k0 = (pre ? t : t - keys.pre_tiles) * KT;
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+            const int seen = pre ? p.prefix_len : min(keys.own_len, j.seen0 + attn_row_token(p, ty * A + a));
+            float mx = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < NK; ++b) {
+                s[a][b] = k0 + tx + 16 * b < seen ? s[a][b] * p.scale_log2 : -INFINITY;
+                mx = max_nan(mx, s[a][b]);
+            }
+#pragma unroll
+            for (int w = 1; w < 16; w *= 2) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+            float f = 1.f;
+            if (!(mx <= m[a])) {   // (a logit that is NaN or infinite makes the row NaN: mx - mx)
+                f = exp2f(m[a] - mx);
+                l[a] = l[a] * f + (mx - mx);
+                m[a] = mx == mx ? mx : INFINITY;
+            }
+            const float base = m[a] == -INFINITY ? 0.f : m[a];
+            float sum = 0.f;
+#pragma unroll
+            for (int b = 0; b < NK; ++b) {
+                const float e = exp2f(s[a][b] - base);
+                sp[(ty * A + a) * LDP + tx + 16 * b] = e;
+                sum += e;
+            }
+#pragma unroll
+            for (int w = 1; w < 16; w *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+            l[a] += sum;
+#pragma unroll
+            for (int b = 0; b < NE; ++b)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) o[a][b][c] *= f;
+        }
+        __syncwarp();
+#pragma unroll 2
+        for (int k = 0; k < KT; k += 4) {
+            float4 w[A];
+#pragma unroll
+            for (int a = 0; a < A; ++a) w[a] = *reinterpret_cast<const float4 *>(sp + (ty * A + a) * LDP + k);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int b = 0; b < NE; ++b) {
+                    const float4 v = *reinterpret_cast<const float4 *>(sv + (k + u) * LD + b * 64 + tx * 4);
+#pragma unroll
+                    for (int a = 0; a < A; ++a) {
+                        const float f = u == 0 ? w[a].x : u == 1 ? w[a].y : u == 2 ? w[a].z : w[a].w;
+                        o[a][b][0] = fmaf(f, v.x, o[a][b][0]);
+                        o[a][b][1] = fmaf(f, v.y, o[a][b][1]);
+                        o[a][b][2] = fmaf(f, v.z, o[a][b][2]);
+                        o[a][b][3] = fmaf(f, v.w, o[a][b][3]);
+                    }
+                }
+        }
+        __syncwarp();
+    }
+    // the segment's result
+    const bool direct = attn_direct(p, j, whole);
+#pragma unroll
+    for (int a = 0; a < A; ++a) {
+        const int r = ty * A + a;
+        if (r >= j.rows) continue;
+        float *to;
+        float inv = 1.f;
+        if (direct) {
+            const int tok = attn_row_token(p, r);
+            inv = m[a] == -INFINITY ? 0.f : 1.0f / l[a];
+            to = static_cast<float *>(x.out) + (j.tok0 + tok) * x.ld_out + (j.head * p.group + r - tok * p.group) * p.d;
+        } else {
+            const PartPlace at = attn_place(p, j, first, 0, r);
+            if (tx == 0) *reinterpret_cast<float2 *>(at.ml) = make_float2(m[a], l[a]);
+            to = at.o;
+        }
+#pragma unroll
+        for (int b = 0; b < NE; ++b)
+            if (b * 64 + tx * 4 < p.d)
+                *reinterpret_cast<float4 *>(to + b * 64 + tx * 4) =
+                    make_float4(o[a][b][0] * inv, o[a][b][1] * inv, o[a][b][2] * inv, o[a][b][3] * inv);
+    }
+}
+
 template <int DP>
 __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_constant__ AttnPlan p,
                                                                  const __grid_constant__ AttnData x) {
-    constexpr int LD = DP + 4, NE = DP / 64;  // NE: groups of 4 outputs of a thread, 64 apart
+    using Cfg = SimtCfg<DP>;
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    float *const sq = reinterpret_cast<float *>(smem_raw), *const sk = sq + SIMT_ROWS * LD, *const sv = sk + SIMT_KT * LD;
-    float *const ss = sv + SIMT_KT * LD, *const sm = ss + SIMT_ROWS * (SIMT_KT + 1), *const sl = sm + SIMT_ROWS, *const sf = sl + SIMT_ROWS;
-    int *const bases = reinterpret_cast<int *>(sf + SIMT_ROWS);
-    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    float *const sq = reinterpret_cast<float *>(smem_raw), *const skv = sq + SIMT_ROWS * Cfg::LD, *const sp = skv + 4 * Cfg::TILE;
+    int *const bases = reinterpret_cast<int *>(sp + SIMT_ROWS * Cfg::LDP);
+    const int tid = threadIdx.x;
 
     pdl_launch_dependents();
     pdl_wait_prior_grids();
@@ -39,160 +213,31 @@ __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_co
     for (;;) {
         const int stop = min(g_end, j.g1);
         const bool first = g == j.g0, whole = first && stop == j.g1;
-        const int pre_tiles = j.seq < 0 || p.fused ? p.prefix_tiles : 0;
-        __syncthreads();  // the segment before is done with shared memory
-        for (int i = tid; i < SIMT_ROWS * (DP / 8); i += SIMT_THREADS) {
-            const int r = i / (DP / 8), e = i % (DP / 8) * 8;
-            float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (r < j.rows && e < p.d)
-                load8<float>(x.q, (j.tok0 + attn_row_token(p, r)) * x.ld_q + (j.head * p.group + r - attn_row_token(p, r) * p.group) * p.d + e, f);
-            store8<float>(sq, r * LD + e, f);
+        const SimtKeys keys{p.page_table + (long long)j.seq * p.table_stride, j.seq < 0 || p.fused ? p.prefix_tiles : 0, j.own_len,
+                            g - j.g0, stop - g, j.head};
+        int page[Cfg::PASSES];
+        tile_pages<DP>(p, keys, keys.t0, page);
+        for (int i = tid; i < j.rows * (DP / 4); i += SIMT_THREADS) {
+            const int r = i / (DP / 4), e = i % (DP / 4) * 4, tok = attn_row_token(p, r);
+            if (e < p.d)
+                copy16(sq + r * Cfg::LD + e,
+                       static_cast<const float *>(x.q) + (j.tok0 + tok) * x.ld_q + (j.head * p.group + r - tok * p.group) * p.d + e, true);
         }
-        if (tid < SIMT_ROWS) {
-            sm[tid] = -INFINITY;
-            sl[tid] = 0.f;
-        }
-        float o[4][NE][4];
-#pragma unroll
-        for (int a = 0; a < 4; ++a)
-#pragma unroll
-            for (int b = 0; b < NE; ++b)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) o[a][b][c] = 0.f;
-
-        for (; g < stop; ++g) {
-            const int t = g - j.g0;
-            const bool in_prefix = t < pre_tiles;
-            const int k0 = (in_prefix ? t : t - pre_tiles) * SIMT_KT;       // first key of the tile
-            const int len = in_prefix ? p.prefix_len : j.own_len;          // keys behind this are not there
-            const int *const pages = in_prefix ? p.prefix_pages : p.page_table + (long long)j.seq * p.table_stride;
-            __syncthreads();  // the tile before is done with
-            for (int i = tid; i < SIMT_KT * (DP / 8); i += SIMT_THREADS) {
-                const int r = i / (DP / 8), e = i % (DP / 8) * 8, key = k0 + r;
-                float fk[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, fv[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                if (key < len && e < p.d) {
-                    const int page = __ldg(pages + (key >> p.page_shift));
-                    if (page >= 0 && page < p.n_pages) {
-                        const long long at = page * x.stride_page + j.head * x.stride_head +
-                                             (key & ((1 << p.page_shift) - 1)) * x.stride_token + e;
-                        load8<float>(x.k, at, fk);
-                        load8<float>(x.v, at, fv);
-                    } else {
-                        raise_status(p.ws, DEV_STATUS_BAD_INDEX, 42);
-                    }
-                }
-                store8<float>(sk, r * LD + e, fk);
-                store8<float>(sv, r * LD + e, fv);
-            }
-            __syncthreads();
-            // S: rows 4 ty .., keys tx and tx + 16
-            float s[4][2] = {};
-#pragma unroll 4
-            for (int e = 0; e < DP; e += 4) {
-                const float4 b0 = *reinterpret_cast<const float4 *>(sk + tx * LD + e);
-                const float4 b1 = *reinterpret_cast<const float4 *>(sk + (tx + 16) * LD + e);
-#pragma unroll
-                for (int a = 0; a < 4; ++a) {
-                    const float4 q = *reinterpret_cast<const float4 *>(sq + (ty * 4 + a) * LD + e);
-                    s[a][0] = fmaf(q.x, b0.x, fmaf(q.y, b0.y, fmaf(q.z, b0.z, fmaf(q.w, b0.w, s[a][0]))));
-                    s[a][1] = fmaf(q.x, b1.x, fmaf(q.y, b1.y, fmaf(q.z, b1.z, fmaf(q.w, b1.w, s[a][1]))));
-                }
-            }
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                const int r = ty * 4 + a, seen = in_prefix ? len : min(len, j.seen0 + attn_row_token(p, r));
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-                    ss[r * (SIMT_KT + 1) + tx + 16 * b] = k0 + tx + 16 * b < seen ? s[a][b] * p.scale_log2 : -INFINITY;
-            }
-            __syncthreads();
-            {   // running maximum and sum: four neighbouring threads per row
-                const int r = tid >> 2, c0 = (tid & 3) * (SIMT_KT / 4);
-                float *const row = ss + r * (SIMT_KT + 1) + c0;
-                float mx = row[0];
-#pragma unroll
-                for (int c = 1; c < SIMT_KT / 4; ++c) mx = fmaxf(mx, row[c]);
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                const float m_old = sm[r], m_new = fmaxf(m_old, mx), base = m_new == -INFINITY ? 0.f : m_new;
-                float sum = 0.f;
-#pragma unroll
-                for (int c = 0; c < SIMT_KT / 4; ++c) {
-                    const float e = exp2f(row[c] - base);
-                    row[c] = e;
-                    sum += e;
-                }
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                const float f = exp2f(m_old - base);  // 0 while nothing was seen
-                if ((tid & 3) == 0) {
-                    sm[r] = m_new;
-                    sl[r] = sl[r] * f + sum;
-                    sf[r] = f;
-                }
-            }
-            __syncthreads();
-            // O: rows 4 ty .., entries 4 tx .. and 64 further
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                const float f = sf[ty * 4 + a];
-#pragma unroll
-                for (int b = 0; b < NE; ++b)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) o[a][b][c] *= f;
-            }
-#pragma unroll 4
-            for (int k = 0; k < SIMT_KT; ++k) {
-                float w[4];
-#pragma unroll
-                for (int a = 0; a < 4; ++a) w[a] = ss[(ty * 4 + a) * (SIMT_KT + 1) + k];
-#pragma unroll
-                for (int b = 0; b < NE; ++b) {
-                    const float4 v = *reinterpret_cast<const float4 *>(sv + k * LD + b * 64 + tx * 4);
-#pragma unroll
-                    for (int a = 0; a < 4; ++a) {
-                        o[a][b][0] = fmaf(w[a], v.x, o[a][b][0]);
-                        o[a][b][1] = fmaf(w[a], v.y, o[a][b][1]);
-                        o[a][b][2] = fmaf(w[a], v.z, o[a][b][2]);
-                        o[a][b][3] = fmaf(w[a], v.w, o[a][b][3]);
-                    }
-                }
-            }
-        }
-        // the segment's result
-        const bool direct = attn_direct(p, j, whole);
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            const int r = ty * 4 + a;
-            if (r >= j.rows) continue;
-            const float m = sm[r], l = sl[r];
-            if (direct) {
-                const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
-                float *const to = static_cast<float *>(x.out) + (j.tok0 + attn_row_token(p, r)) * x.ld_out + (j.head * p.group + r - attn_row_token(p, r) * p.group) * p.d;
-#pragma unroll
-                for (int b = 0; b < NE; ++b)
-                    if (b * 64 + tx * 4 < p.d)
-                        *reinterpret_cast<float4 *>(to + b * 64 + tx * 4) =
-                            make_float4(o[a][b][0] * inv, o[a][b][1] * inv, o[a][b][2] * inv, o[a][b][3] * inv);
-            } else {
-                const PartPlace at = attn_place(p, j, first, 0, r);
-                if (tx == 0) *reinterpret_cast<float2 *>(at.ml) = make_float2(m, l);
-#pragma unroll
-                for (int b = 0; b < NE; ++b)
-                    if (b * 64 + tx * 4 < p.d)
-                        *reinterpret_cast<float4 *>(at.o + b * 64 + tx * 4) = make_float4(o[a][b][0], o[a][b][1], o[a][b][2], o[a][b][3]);
-            }
-        }
+        if (j.rows <= 16) simt_segment<DP, 1>(p, x, j, keys, first, whole, sq, skv, sp, page);
+        else if (j.rows <= 32) simt_segment<DP, 2>(p, x, j, keys, first, whole, sq, skv, sp, page);
+        else simt_segment<DP, 4>(p, x, j, keys, first, whole, sq, skv, sp, page);
+        g = stop;
         if (g >= g_end) return;
         j = attn_next(p, bases, j);
+        __syncthreads();  // the segment before is done with shared memory
     }
 }
 
-AttnShape attn_simt_shape() { return {SIMT_ROWS, 1, SIMT_KT, 0}; }
+AttnShape attn_simt_shape(int head_dim) { return {SIMT_ROWS, 1, head_dim <= 128 ? SimtCfg<64>::KT : SimtCfg<256>::KT, 0}; }
 
 template <int DP> static griffin_status launch_dp(AttnPlan p, AttnData x, cudaStream_t stream) {
     const void *fn = reinterpret_cast<const void *>(attn_simt_kernel<DP>);
-    const size_t smem = simt_smem<DP>(p.n_seq);
+    const size_t smem = SimtCfg<DP>::smem(p.n_seq);
     if (ensure_dynamic_smem(fn, smem) != cudaSuccess) return GRIFFIN_ERR_CUDA;
     void *args[] = {&p, &x};
     return launch_maybe_overlapped(fn, dim3(p.grid), dim3(SIMT_THREADS), smem, stream, true, args) == cudaSuccess
