@@ -110,9 +110,9 @@ __device__ __forceinline__ float fast_exp2(float x) {
 __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
-__device__ __forceinline__ float max3(float a, float b, float c) {
+__device__ __forceinline__ float max3(float a, float b, float c) {  // NaN if any is
     float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
 // two fp32 lanes in one instruction
@@ -128,7 +128,7 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
     return *reinterpret_cast<float2 *>(&d);
 }
-// 2^x of both lanes on the FMA and integer pipes, x >= -120 after clamping: n = the integer next to x (by adding
+// 2^x of both lanes on the FMA and integer pipes, x >= -120 after clamping (NaN too: the row's maximum tells of one): n = the integer next to x (by adding
 // 1.5 * 2^23), f = x - n, a cubic for 2^f on [-1/2, 1/2] (its own minimax fit, relative error 7.5e-5: a fiftieth of
 // the rounding of P to bf16 that follows), n into the exponent.
 __device__ __forceinline__ float2 poly_exp2(float2 x) {
@@ -570,14 +570,17 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
 #pragma unroll
                             for (int e = 0; e < 4; ++e) mx4[e] = max3(mx4[e], s[i + e], s[i + 4 + e]);
                     }
-                    float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+                    float mx = max3(max3(mx4[0], mx4[1], mx4[2]), mx4[3], mx4[3]);
                     mx *= p.scale_log2;
-                    // the maximum moves only when 2^(c S - m) could grow too large (or there is none yet)
-                    const bool move = mx > m + ATC_SLACK || (m == -INFINITY && mx > m);
+                    // the maximum moves only when 2^(c S - m) could grow too large, or there is none yet, or it is NaN
+                    const bool move = !(mx <= m + ATC_SLACK);
                     if (__any_sync(0xffffffffu, move)) {
                         const float f = move ? fast_exp2(m - mx) : 1.f;   // (0 for the first)
-                        if (move) m = mx;
                         l *= f;
+                        if (move) {   // (a logit that is NaN or infinite makes the row NaN)
+                            l += mx - mx;
+                            m = mx == mx ? mx : INFINITY;
+                        }
                         if (started) {
                             // (one accumulator: S of this unit was issued before P V of the last one, so its barrier
                             // does not cover it)
@@ -632,7 +635,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                     tc_fence_after_sync();
                     const uint32_t to = lanes + Cfg::O_COL + (NS == 2 ? grp : 0) * DP;
                     if (j.direct) {
-                        const float inv = l == 0.f ? 0.f : 1.0f / l;
+                        const float inv = m == -INFINITY ? 0.f : 1.0f / l;
                         __nv_bfloat16 *const dst = static_cast<__nv_bfloat16 *>(prm.out) + (j.tok0 + tok) * prm.ld_out +
                                                    (j.head * p.group + row - tok * p.group) * p.d;
 #pragma unroll 1

@@ -240,6 +240,35 @@ def test_attention_does_not_see_what_lies_behind_the_ends(dtype, fill):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("which,value", [("k", float("nan")), ("v", float("nan")), ("k", float("inf")), ("v", -float("inf")), ("q", float("nan"))])
+@pytest.mark.parametrize("hd", [64, 128, 256])
+def test_attention_lets_a_seen_value_that_is_not_finite_through(dtype, which, value, hd):
+    # one bad entry in a key, a value or a query that is seen (also as the only thing seen): what the formula makes of it
+    for prefix, own, at in [(0, 1, 0), (0, 9, 3), (40, 200, 197), (40, 200, 70), (40, 200, 2), (0, 300, 128)] + [(0, 64, i) for i in range(16, 32)]:
+        b = Batch([1, 1], [own, 30], prefix, 2, 1, hd, 16, dtype, fill=0.0)
+        q = b.q.clone()
+        if which == "q":
+            q[0, 1, 5] = value
+        else:
+            q[0, 0, 5], q[0, 1, 5] = 1.5, -1.5             # an infinite key: one logit of +inf, one of -inf
+            t = b.k_host if which == "k" else b.v_host
+            t[int(b.page_table[0, at // 16]), 0, at % 16, 5] = value
+        with np.errstate(all="ignore"):
+            want, mass = L.attention(f64(q), f64(b.k_host), f64(b.v_host), b.q_start.numpy(), b.seq_len.numpy(), b.page_table.numpy(),
+                                     b.prefix_pages.numpy(), b.prefix, b.scale)
+            bound = b.bound(np.nan_to_num(want, posinf=0.0, neginf=0.0), np.nan_to_num(mass, posinf=0.0))
+        if (which, value, prefix + own) == ("k", float("inf"), 1):
+            want[0, 1] = 0.0                               # no logit above -inf counts as nothing seen
+        b.to_device()
+        got = f64(b.attend(q=q.to(DEV)))
+        assert not np.all(np.isfinite(want))
+        assert np.array_equal(np.isnan(want), np.isnan(got)), (prefix, own, at)
+        assert np.array_equal(np.isinf(want), np.isinf(got)) and np.all(got[np.isinf(want)] == want[np.isinf(want)])
+        fine = np.isfinite(want)
+        assert np.all(np.abs(got - want)[fine] <= bound[fine])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("q_lens,seq_lens,prefix", [
     ([1, 0, 3, 0], [4, 9, 7, 0], 20),          # sequences without new tokens
     ([2, 1], [0, 0], 0),                       # padding only: nothing is seen
