@@ -8,7 +8,7 @@
 
 namespace griffin {
 
-constexpr int JOIN_THREADS = 128;
+constexpr int JOIN_THREADS = 256, JOIN_WARPS = JOIN_THREADS / 32;
 constexpr int JOIN_ROWS = 16;  // rows of a cut block that one CTA joins
 
 // The partials of one job: n of them on CTAs c0, c0 + 1, ..., `streams` of each.
@@ -46,8 +46,9 @@ template <typename T> __device__ __forceinline__ void store_row4(T *to, const fl
 template <typename T, int NV>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ AttnPlan p, T *__restrict__ out,
                                                                  long long ld_out, int by_row) {
-    __shared__ float sh_ml[4][2], sh_o[4][NV * 128];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __shared__ float sh_ml[JOIN_WARPS][2], sh_o[JOIN_WARPS][NV * 128];
+    __shared__ int sh_seq[5];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     pdl_launch_dependents();
     pdl_wait_prior_grids();
     const AttnTotals tot = attn_totals(p, p.bases);
@@ -55,7 +56,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     const AttnShares sh(tot.W, p.grid);
     JobParts a;
     AttnSeq q{};
-    int r0 = 0, r1 = 0, head = 0, seq = 0, n_blocks = 0, b = 0;
+    int r0 = 0, r1 = 0, head = 0, seq = 0, n_blocks = 0, b = 0, base0 = 0, base1 = 0;
     bool cut = false;
     if ((int)blockIdx.x >= by_row) {
         const int chunks = p.cta_rows / JOIN_ROWS, c = (int)(blockIdx.x - by_row) / chunks;
@@ -69,18 +70,36 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     } else {
         const int bx = (int)((uint32_t)blockIdx.x / (uint32_t)p.hkv);
         head = blockIdx.x - bx * p.hkv;
-        seq = bx;
-        if (!p.fused) {
+        int q_start, q_end, len;
+        if (p.fused) {
+            seq = bx;
+            q_start = __ldg(p.q_start + seq), q_end = __ldg(p.q_start + seq + 1), len = __ldg(p.seq_len + seq);
+            base0 = p.bases[seq], base1 = p.bases[seq + 1];
+        } else {
             // Sequence s owns the block numbers from q_start[s] / block_tokens + s on: at least as many as it has blocks.
+            // (a thread per sequence asks for all that may be wanted of it: one trip to L2, not three)
             seq = -1;
-            for (int s0 = 0; s0 < p.n_seq; s0 += JOIN_THREADS) {
+#pragma unroll 1
+            for (int s0 = 0; s0 < p.n_seq; s0 += blockDim.x) {
                 const int s = s0 + threadIdx.x;
-                seq += __syncthreads_count(s < p.n_seq && __ldg(p.q_start + s) / p.block_tokens + s <= bx);
+                int v[5] = {};
+                if (s < p.n_seq) {
+                    v[0] = __ldg(p.q_start + s), v[1] = __ldg(p.q_start + s + 1), v[2] = __ldg(p.seq_len + s);
+                    v[3] = p.bases[s], v[4] = p.bases[s + 1];
+                }
+                const int n = __syncthreads_count(s < p.n_seq && v[0] / p.block_tokens + s <= bx);
+                seq += n;
+                if ((int)threadIdx.x == n - 1) {
+#pragma unroll
+                    for (int i = 0; i < 5; ++i) sh_seq[i] = v[i];
+                }
             }
             if (seq < 0) return;
-            b = bx - (__ldg(p.q_start + seq) / p.block_tokens + seq);
+            __syncthreads();
+            q_start = sh_seq[0], q_end = sh_seq[1], len = sh_seq[2], base0 = sh_seq[3], base1 = sh_seq[4];
+            b = bx - (q_start / p.block_tokens + seq);
         }
-        q = attn_seq(p, seq);
+        q = attn_seq_of(p, q_start, q_end, len);
         n_blocks = ceil_div(q.nq, p.block_tokens);
         if (b >= n_blocks) return;
     }
@@ -88,9 +107,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     for (;;) {
         if (!cut) {
             // this job's place among the tiles: behind those of the heads and blocks before it
-            const int base = p.bases[seq], per_head = (int)((uint32_t)(p.bases[seq + 1] - base) / (uint32_t)p.hkv);
+            const int per_head = (int)((uint32_t)(base1 - base0) / (uint32_t)p.hkv);
             if (p.fused && attn_block_tiles(p, q, b) > 0) b = n_blocks - 1;
-            int g0 = base + (head + 1) * per_head;
+            int g0 = base0 + (head + 1) * per_head;
             g0 -= (int)attn_sum_tiles(p, q, b, n_blocks);
             const AttnJob j = attn_own_job(p, q, seq, head, b, g0);
             a = job_parts(p, sh, j);
@@ -99,9 +118,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
         }
         // Each row is joined by `wpr` warps (more when there are fewer rows), each taking a stretch of its partials; their
         // sums are added in order through shared memory.
-        const int wpr = r1 - r0 >= 3 ? 1 : r1 - r0 == 2 ? 2 : 4, sub = warp % wpr;
+        const int wpr = r1 - r0 == 1 ? warps : r1 - r0 == 2 ? warps / 2 : 2 * (r1 - r0) <= warps ? warps / 4 : 1, sub = warp % wpr;
+        constexpr int AT_ONCE = NV == 1 ? 8 : 4;
 #pragma unroll 1
-        for (int rb = r0; rb < r1; rb += 4 / wpr) {
+        for (int rb = r0; rb < r1; rb += warps / wpr) {
             const int r = rb + warp / wpr;
             const bool on = r < r1;
             const int rt = attn_row_token(p, r), tok = a.job.tok0 + rt, hq = a.job.head * p.group + r - rt * p.group;
@@ -141,11 +161,11 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
                         for (int c = 0; c < 4; ++c) acc[k][c] *= f;
                     const int cnt = min(32, i1 - ib);
 #pragma unroll 1
-                    for (int s = 0; s < cnt; s += 4) {
-                        float4 o[4][NV];
-                        float w[4];
+                    for (int s = 0; s < cnt; s += AT_ONCE) {
+                        float4 o[AT_ONCE][NV];
+                        float w[AT_ONCE];
 #pragma unroll
-                        for (int u = 0; u < 4; ++u) {   // (lanes beyond cnt hold no part)
+                        for (int u = 0; u < AT_ONCE; ++u) {   // (lanes beyond cnt hold no part)
                             w[u] = __shfl_sync(0xffffffffu, wgt, (s + u) & 31);
                             const float *src = reinterpret_cast<const float *>(
                                 __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(at.o), (s + u) & 31));
@@ -157,7 +177,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
                             }
                         }
 #pragma unroll
-                        for (int u = 0; u < 4; ++u)
+                        for (int u = 0; u < AT_ONCE; ++u)
 #pragma unroll
                             for (int k = 0; k < NV; ++k) {
                                 acc[k][0] = fmaf(w[u], o[u][k].x, acc[k][0]);
@@ -224,8 +244,11 @@ griffin_status launch_attn_join(const AttnPlan &plan, int dtype, void *out, long
                                                            : reinterpret_cast<const void *>(attn_join_kernel<float, 2>))
                                              : (p.d <= 128 ? reinterpret_cast<const void *>(attn_join_kernel<__nv_bfloat16, 1>)
                                                            : reinterpret_cast<const void *>(attn_join_kernel<__nv_bfloat16, 2>));
+    // More warps to a row shorten its chain, more CTAs than fit at once lengthen the whole: with 320 one-row blocks 128
+    // threads take 30.7 us with the attention in front (256: 34.8), with 96 five-row blocks 256 take 22.8 (128: 25.6).
+    const int threads = by_row + cut > 2 * p.grid ? JOIN_THREADS / 2 : JOIN_THREADS;
     void *args[] = {&p, &out, &ld_out, &by_row};
-    return launch_maybe_overlapped(fn, dim3(by_row + cut), dim3(JOIN_THREADS), 0, stream, true, args) == cudaSuccess ? GRIFFIN_OK
+    return launch_maybe_overlapped(fn, dim3(by_row + cut), dim3(threads), 0, stream, true, args) == cudaSuccess ? GRIFFIN_OK
                                                                                                                      : GRIFFIN_ERR_CUDA;
 }
 

@@ -74,10 +74,9 @@ static __device__ __noinline__ void attn_bad(void *ws, int where) { raise_status
 struct AttnSeq {
     int q0, nq, len;  // first new token, how many, own tokens
 };
-// The sequence's lengths, held to what the arrays can hold.
-__device__ __forceinline__ AttnSeq attn_seq(const AttnPlan &p, int s) {
+// A sequence's lengths as the arrays q_start (a, b) and seq_len have them, held to what the call can hold.
+__device__ __forceinline__ AttnSeq attn_seq_of(const AttnPlan &p, int a, int b, int len) {
     AttnSeq r;
-    int a = __ldg(p.q_start + s), b = __ldg(p.q_start + s + 1), len = __ldg(p.seq_len + s);
     const long long cap = (long long)p.table_stride << p.page_shift;
     const bool bad = a < 0 || b < a || b > p.n_tokens || len < 0 || len > cap;
     a = min(max(a, 0), p.n_tokens);
@@ -87,6 +86,9 @@ __device__ __forceinline__ AttnSeq attn_seq(const AttnPlan &p, int s) {
     r.nq = b - a;
     r.len = (int)min((long long)max(len, 0), cap);
     return r;
+}
+__device__ __forceinline__ AttnSeq attn_seq(const AttnPlan &p, int s) {
+    return attn_seq_of(p, __ldg(p.q_start + s), __ldg(p.q_start + s + 1), __ldg(p.seq_len + s));
 }
 // Key tiles of row block b of a sequence: the prefix's (fused) and its own up to the last row's place.
 __device__ __forceinline__ int attn_block_tiles(const AttnPlan &p, const AttnSeq &q, int b) {
