@@ -8,8 +8,20 @@ namespace griffin {
 
 constexpr int ATTN_MAX_GRID = 148;  // CTAs at most (one per SM of a B200)
 
-static AttnShape shape_of(const griffin_attn_desc *desc) {
-    return desc->dtype == GRIFFIN_DT_F32 ? attn_simt_shape(desc->head_dim) : attn_tc_shape(desc->head_dim);
+// Whether the kernel for blocks of 8 rows (attn_few.cu) takes a call rather than the tcgen05 one: its sequences' rows fit
+// one such block on average, those of a shared prefix do, and a CTA has about two of the sequences' blocks at most.
+// Both sides, us a pass, few / tcgen05: 1 sequence of 32 heads behind 512 tokens 12.4 / 14.5, behind 20000 60.4 / 64.9;
+// 32 query heads over 8 behind 2048 11.4 / 15.2; 8 sequences of 32 heads behind 2048 (256 blocks) 25.7 / 26.8, of 40 heads
+// (320 blocks) 31.5 / 30.5; 64 sequences of 32 heads of their own (2048 blocks) 90 / 83: the end of a block costs this
+// kernel more.
+static bool attn_few(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
+    const long long rows = (long long)batch->n_tokens * (desc->n_q_heads / desc->n_kv_heads);
+    return desc->dtype == GRIFFIN_DT_BF16 && desc->n_q_heads <= 8 * desc->n_kv_heads && rows <= 8ll * batch->n_seq &&
+           (batch->n_seq == 1 || batch->prefix_len == 0 || rows <= 8) && batch->n_seq * desc->n_kv_heads <= 2 * ATTN_MAX_GRID;
+}
+static AttnShape shape_of(const griffin_attn_desc *desc, bool few) {
+    if (desc->dtype == GRIFFIN_DT_F32) return attn_simt_shape(desc->head_dim);
+    return few ? attn_few_shape(desc->head_dim) : attn_tc_shape(desc->head_dim);
 }
 
 struct AttnScratch {
@@ -31,7 +43,8 @@ static AttnScratch attn_scratch(const griffin_attn_desc *desc, const AttnShape &
 }
 
 size_t attn_scratch_bytes(const griffin_attn_desc *desc, int n_tokens, int n_seq) {
-    return attn_scratch(desc, shape_of(desc), n_tokens, n_seq).total;
+    const size_t a = attn_scratch(desc, shape_of(desc, false), n_tokens, n_seq).total, b = attn_scratch(desc, shape_of(desc, true), n_tokens, n_seq).total;
+    return a > b ? a : b;
 }
 
 griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
@@ -39,7 +52,8 @@ griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_a
                                   uint8_t *scratch, void *ws, cudaStream_t stream) {
     const int sms = device_sm_count();
     if (sms <= 0) return GRIFFIN_ERR_CUDA;
-    const AttnShape sh = shape_of(desc);
+    const bool few = attn_few(desc, batch);
+    const AttnShape sh = shape_of(desc, few);
     AttnPlan p{};
     p.q_start = batch->q_start; p.seq_len = batch->seq_len; p.page_table = batch->page_table;
     p.prefix_pages = batch->prefix_pages;
@@ -61,7 +75,7 @@ griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_a
     p.grid = sms < ATTN_MAX_GRID ? sms : ATTN_MAX_GRID;
     p.scale_log2 = desc->scale * 1.4426950408889634f;
     p.ws = ws;
-    p.may_queue = p.fused && desc->dtype == GRIFFIN_DT_BF16;
+    p.may_queue = p.fused && desc->dtype == GRIFFIN_DT_BF16 && !few;
     p.queue = &static_cast<WsHeader *>(ws)->queue_attn;
     const AttnScratch s = attn_scratch(desc, sh, p.n_tokens, p.n_seq);
     p.bases = reinterpret_cast<int *>(scratch);
@@ -72,7 +86,9 @@ griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_a
     p.own_rows = s.own_rows;
     p.cta_rows = 2 * sh.tile_rows;
     const AttnData x{q, cache->k, cache->v, out, ld_q, ld_out, cache->stride_page, cache->stride_head, cache->stride_token};
-    const griffin_status st = desc->dtype == GRIFFIN_DT_F32 ? launch_attn_simt(p, x, stream) : launch_attn_tc(p, x, stream);
+    const griffin_status st = desc->dtype == GRIFFIN_DT_F32 ? launch_attn_simt(p, x, stream)
+                              : few                         ? launch_attn_few(p, x, stream)
+                                                            : launch_attn_tc(p, x, stream);
     return st != GRIFFIN_OK ? st : launch_attn_join(p, desc->dtype, out, ld_out, stream);
 }
 

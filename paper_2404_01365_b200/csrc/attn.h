@@ -17,9 +17,28 @@ struct AttnShape {
     int tile_rows, tiles_per_block, kt, alt;
 };
 
+// 2^x to about 2^-22, 0 for -inf
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// NaN if either is
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+// 16 bytes to shared memory, asynchronously; zeros where nothing is there
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+
 AttnShape attn_simt_shape(int head_dim);
 AttnShape attn_tc_shape(int head_dim);
+AttnShape attn_few_shape(int head_dim);
 griffin_status launch_attn_tc(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // bf16
+griffin_status launch_attn_few(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // bf16, few rows
 griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // fp32
 
 }  // namespace griffin

@@ -26,17 +26,6 @@ template <int DP> struct SimtCfg {
     static size_t smem(int n_seq) { return (SIMT_ROWS * LD + 4 * TILE + SIMT_ROWS * LDP + (size_t)n_seq + 3) * 4; }
 };
 
-__device__ __forceinline__ void copy16(float *dst, const float *src, bool there) {   // zeros where nothing is there
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
-                 "r"(there ? 16 : 0)
-                 : "memory");
-}
-__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
-    float d;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-    return d;
-}
-
 // The tiles of one segment, by which the kernel and its loads find keys.
 struct SimtKeys {
     const int *own_pages;
@@ -65,8 +54,8 @@ __device__ __forceinline__ void tile_copy(const AttnPlan &p, const AttnData &x, 
         const bool there = key < len && page[i] >= 0 && page[i] < p.n_pages;
         if (key < len && !there) raise_status(p.ws, DEV_STATUS_BAD_INDEX, 42);
         const long long at = there ? page[i] * x.stride_page + s.head * x.stride_head + (key & ((1 << p.page_shift) - 1)) * x.stride_token + e : 0;
-        copy16(sk + r * SimtCfg<DP>::LD + e, k + at, there);
-        copy16(sv + r * SimtCfg<DP>::LD + e, v + at, there);
+        copy16(smem_u32(sk + r * SimtCfg<DP>::LD + e), k + at, there);
+        copy16(smem_u32(sv + r * SimtCfg<DP>::LD + e), v + at, there);
     }
 }
 
@@ -220,7 +209,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_co
         for (int i = tid; i < j.rows * (DP / 4); i += SIMT_THREADS) {
             const int r = i / (DP / 4), e = i % (DP / 4) * 4, tok = attn_row_token(p, r);
             if (e < p.d)
-                copy16(sq + r * Cfg::LD + e,
+                copy16(smem_u32(sq + r * Cfg::LD + e),
                        static_cast<const float *>(x.q) + (j.tok0 + tok) * x.ld_q + (j.head * p.group + r - tok * p.group) * p.d + e, true);
         }
         if (j.rows <= 16) simt_segment<DP, 1>(p, x, j, keys, first, whole, sq, skv, sp, page);

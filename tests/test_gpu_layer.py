@@ -242,15 +242,16 @@ def test_attention_does_not_see_what_lies_behind_the_ends(dtype, fill):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("which,value", [("k", float("nan")), ("v", float("nan")), ("k", float("inf")), ("v", -float("inf")), ("q", float("nan"))])
 @pytest.mark.parametrize("hd", [64, 128, 256])
-def test_attention_lets_a_seen_value_that_is_not_finite_through(dtype, which, value, hd):
+@pytest.mark.parametrize("hq", [2, 10])
+def test_attention_lets_a_seen_value_that_is_not_finite_through(dtype, which, value, hd, hq):
     # one bad entry in a key, a value or a query that is seen (also as the only thing seen): what the formula makes of it
     for prefix, own, at in [(0, 1, 0), (0, 9, 3), (40, 200, 197), (40, 200, 70), (40, 200, 2), (0, 300, 128)] + [(0, 64, i) for i in range(16, 32)]:
-        b = Batch([1, 1], [own, 30], prefix, 2, 1, hd, 16, dtype, fill=0.0)
+        b = Batch([1, 1], [own, 30], prefix, hq, 1, hd, 16, dtype, fill=0.0)
         q = b.q.clone()
         if which == "q":
             q[0, 1, 5] = value
         else:
-            q[0, 0, 5], q[0, 1, 5] = 1.5, -1.5             # an infinite key: one logit of +inf, one of -inf
+            q[0, ::2, 5], q[0, 1::2, 5] = 1.5, -1.5         # an infinite key: logits of +inf and of -inf
             t = b.k_host if which == "k" else b.v_host
             t[int(b.page_table[0, at // 16]), 0, at % 16, 5] = value
         with np.errstate(all="ignore"):
@@ -258,14 +259,14 @@ def test_attention_lets_a_seen_value_that_is_not_finite_through(dtype, which, va
                                      b.prefix_pages.numpy(), b.prefix, b.scale)
             bound = b.bound(np.nan_to_num(want, posinf=0.0, neginf=0.0), np.nan_to_num(mass, posinf=0.0))
         if (which, value, prefix + own) == ("k", float("inf"), 1):
-            want[0, 1] = 0.0                               # no logit above -inf counts as nothing seen
+            want[0, 1::2] = 0.0                            # no logit above -inf counts as nothing seen
         b.to_device()
         got = f64(b.attend(q=q.to(DEV)))
         assert not np.all(np.isfinite(want))
         assert np.array_equal(np.isnan(want), np.isnan(got)), (prefix, own, at)
         assert np.array_equal(np.isinf(want), np.isinf(got)) and np.all(got[np.isinf(want)] == want[np.isinf(want)])
         fine = np.isfinite(want)
-        assert np.all(np.abs(got - want)[fine] <= bound[fine])
+        assert np.all(np.abs(got[fine] - want[fine]) <= bound[fine])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -282,6 +283,33 @@ def test_attention_lets_a_seen_value_that_is_not_finite_through(dtype, which, va
 def test_attention_ragged_batches(dtype, q_lens, seq_lens, prefix):
     check_attention(Batch(q_lens, seq_lens, prefix, 4, 2, 64, 16, dtype, extra_rows=2))
     check_attention(Batch(q_lens, seq_lens, prefix, 3, 1, 128, 16, dtype))
+
+
+@pytest.mark.parametrize("hq,hkv,hd", [(2, 2, 64), (4, 2, 72), (8, 1, 128), (3, 1, 200), (2, 1, 256)])
+@pytest.mark.parametrize("page,layout", [(8, "hnd"), (8, "nhd"), (16, "hnd"), (128, "nhd")])
+def test_attention_of_a_few_rows(hq, hkv, hd, page, layout):
+    # up to 8 rows a block (the kernel for single tokens), the bounds of that, and calls of more behind the same lengths
+    group = hq // hkv
+    most = 8 // group
+    for q_lens, seq_lens, prefix in [([1], [1], 0), ([1], [700], 0), ([most], [333], 90), ([most + 1], [333], 90), ([most, 0], [130, 5], 0),
+                                     ([most - most // 2, most // 2], [17, 129], 300), ([most, 1], [17, 129], 300), ([1, 1], [0, 3], 0),
+                                     ([3 * most, 1, 1], [3 * most + 5, 40, 16], 0), ([most, 1], [most - 1, 64], 0)]:
+        check_attention(Batch(q_lens, seq_lens, prefix, hq, hkv, hd, page, "bf16", layout=layout))
+
+
+def test_attention_of_few_rows_and_many_blocks():
+    # 296 blocks of sequences are the most that the kernel for single tokens takes
+    for n in (74, 75):
+        check_attention(Batch([1] * n, [(31 * i) % 190 for i in range(n)], 0, 8, 4, 64, 16, "bf16"), rows={0, 1, 7, n - 2, n - 1})
+    check_attention(Batch([1] * 8, [(31 * i) % 190 + 1 for i in range(8)], 1100, 37, 37, 64, 16, "bf16"), rows={0, 7})
+    check_attention(Batch([1] * 8, [(31 * i) % 190 + 1 for i in range(8)], 1100, 38, 38, 64, 16, "bf16"), rows={0, 7})
+
+
+@pytest.mark.parametrize("fill", [float("nan"), float("inf"), -float("inf"), 3e38])
+def test_attention_of_more_rows_does_not_see_what_lies_behind_the_ends(fill):
+    check_attention(Batch([4, 2, 3], [5, 70, 129], 37, 4, 2, 64, 64, "bf16", fill=fill))
+    check_attention(Batch([4, 2, 3], [5, 70, 129], 37, 2, 1, 256, 32, "bf16", fill=fill))
+    check_attention(Batch([9], [40], 37, 2, 2, 128, 16, "bf16", fill=fill))
 
 
 def test_attention_of_many_sequences():
