@@ -1,9 +1,9 @@
 // Attention over the shared prefix and each sequence's own keys, fp32 storage, on the plain fp32 pipes:
 //   S = scale Q K^T, masked by place;  m' = max(m, max S);  P = 2^(S - m');
 //   l = l 2^(m - m') + sum P;  O = O 2^(m - m') + P V        (S in units of log2, all fp32)
-// one CTA of 256 threads per SM, each with its share of the call's key tiles (attn_plan.cuh).
+// one CTA per SM, each with its share of the call's key tiles (attn_plan.cuh).
 //
-// A half warp has A neighbouring rows and walks the whole tile: keys tx, tx + 16, ... of S, entries 4 tx .. of O.  So
+// A half warp has up to A rows, HALVES apart, and walks the whole tile: keys tx, tx + 16, ... of S, entries 4 tx .. of O.  So
 // the softmax stays in registers (four shuffles a row), and P goes through shared memory within its own warp; the CTA
 // meets once a tile, for the keys and values.  Those come by cp.async, the next tile's behind the present one's
 // products, and their pages are looked up a tile ahead.  Keys and values behind what any row of the block sees are
@@ -14,15 +14,18 @@
 
 namespace griffin {
 
-constexpr int SIMT_ROWS = 64, SIMT_THREADS = 256;
+constexpr int SIMT_ROWS = 64;
 
 // DP: the head's width rounded up to 64, 128 or 256.
 template <int DP> struct SimtCfg {
+    // 16 warps keep the pipes busier than 8 (1000 causal tokens of 8 64-wide heads over 2: 72 us, 8 warps 87); 256-wide heads
+    // would read shared memory too often with so few rows to a warp (33 steps behind 3189 tokens of 16 heads: 199 us, 145)
+    static constexpr int THREADS = DP == 256 ? 256 : 512, HALVES = THREADS / 16;
     static constexpr int KT = DP == 256 ? 32 : 64;                 // keys per tile: two tiles fit beside the queries
     static constexpr int LD = DP + 4;                              // (rows 16 bytes apart in the banks)
     static constexpr int TILE = KT * LD;                           // keys or values of a tile
     static constexpr int LDP = KT + 4;
-    static constexpr int PASSES = KT * (DP / 4) / SIMT_THREADS;    // 16-byte pieces per thread, keys as values
+    static constexpr int PASSES = KT * (DP / 4) / THREADS;    // 16-byte pieces per thread, keys as values
     static size_t smem(int n_seq) { return (SIMT_ROWS * LD + 4 * TILE + SIMT_ROWS * LDP + (size_t)n_seq + 3) * 4; }
 };
 
@@ -37,7 +40,7 @@ template <int DP> __device__ __forceinline__ void tile_pages(const AttnPlan &p, 
     const int *const pages = pre ? p.prefix_pages : s.own_pages;
 #pragma unroll
     for (int i = 0; i < SimtCfg<DP>::PASSES; ++i) {
-        const int key = k0 + (threadIdx.x + i * SIMT_THREADS) / (DP / 4);
+        const int key = k0 + (threadIdx.x + i * SimtCfg<DP>::THREADS) / (DP / 4);
         page[i] = key < len ? __ldg(pages + (key >> p.page_shift)) : -1;
     }
 }
@@ -49,7 +52,7 @@ __device__ __forceinline__ void tile_copy(const AttnPlan &p, const AttnData &x, 
     const float *const k = static_cast<const float *>(x.k), *const v = static_cast<const float *>(x.v);
 #pragma unroll
     for (int i = 0; i < SimtCfg<DP>::PASSES; ++i) {
-        const int c = threadIdx.x + i * SIMT_THREADS, r = c / (DP / 4), e = c % (DP / 4) * 4, key = k0 + r;
+        const int c = threadIdx.x + i * SimtCfg<DP>::THREADS, r = c / (DP / 4), e = c % (DP / 4) * 4, key = k0 + r;
         if (e >= p.d) continue;
         const bool there = key < len && page[i] >= 0 && page[i] < p.n_pages;
         if (key < len && !there) raise_status(p.ws, DEV_STATUS_BAD_INDEX, 42);
@@ -66,8 +69,9 @@ __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &
     using Cfg = SimtCfg<DP>;
     constexpr int KT = Cfg::KT, LD = Cfg::LD, LDP = Cfg::LDP, NK = KT / 16, NE = DP / 64;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const bool on = (ty & ~1) * A < j.rows;       // any row of the warp
-    float o[A][NE][4] = {}, m[A], l[A];
+    const bool on = (ty & ~1) < j.rows;       // any row of the warp
+    float2 o[A][NE][2] = {};
+    float m[A], l[A];
 #pragma unroll
     for (int a = 0; a < A; ++a) m[a] = -INFINITY, l[a] = 0.f;
     tile_copy<DP>(p, x, keys, keys.t0, page, skv, skv + Cfg::TILE);
@@ -84,29 +88,32 @@ __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &
             if (i + 2 < keys.n) tile_pages<DP>(p, keys, t + 2, page);
         }
         if (!on) continue;
-        float s[A][NK] = {};
+        float2 s2[A][NK] = {};   // sums over the even and the odd entries
 #pragma unroll 4
         for (int e = 0; e < p.d; e += 4) {
             float4 q[A];
 #pragma unroll
-            for (int a = 0; a < A; ++a) q[a] = *reinterpret_cast<const float4 *>(sq + (ty * A + a) * LD + e);
+            for (int a = 0; a < A; ++a) q[a] = *reinterpret_cast<const float4 *>(sq + (ty + Cfg::HALVES * a) * LD + e);
 #pragma unroll
             for (int b = 0; b < NK; ++b) {
                 const float4 k = *reinterpret_cast<const float4 *>(sk + (tx + 16 * b) * LD + e);
 #pragma unroll
-                for (int a = 0; a < A; ++a)
-                    s[a][b] = fmaf(q[a].x, k.x, fmaf(q[a].y, k.y, fmaf(q[a].z, k.z, fmaf(q[a].w, k.w, s[a][b]))));
+                for (int a = 0; a < A; ++a) {
+                    s2[a][b] = fma2(make_float2(q[a].x, q[a].y), make_float2(k.x, k.y), s2[a][b]);
+                    s2[a][b] = fma2(make_float2(q[a].z, q[a].w), make_float2(k.z, k.w), s2[a][b]);
+                }
             }
         }
+        float s[A][NK];
         const bool pre = t < keys.pre_tiles;
         const int k0 = (pre ? t : t - keys.pre_tiles) * KT;
 #pragma unroll
         for (int a = 0; a < A; ++a) {
-            const int seen = pre ? p.prefix_len : min(keys.own_len, j.seen0 + attn_row_token(p, ty * A + a));
+            const int seen = pre ? p.prefix_len : min(keys.own_len, j.seen0 + attn_row_token(p, ty + Cfg::HALVES * a));
             float mx = -INFINITY;
 #pragma unroll
             for (int b = 0; b < NK; ++b) {
-                s[a][b] = k0 + tx + 16 * b < seen ? s[a][b] * p.scale_log2 : -INFINITY;
+                s[a][b] = k0 + tx + 16 * b < seen ? (s2[a][b].x + s2[a][b].y) * p.scale_log2 : -INFINITY;
                 mx = max_nan(mx, s[a][b]);
             }
 #pragma unroll
@@ -122,7 +129,7 @@ __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &
 #pragma unroll
             for (int b = 0; b < NK; ++b) {
                 const float e = exp2f(s[a][b] - base);
-                sp[(ty * A + a) * LDP + tx + 16 * b] = e;
+                sp[(ty + Cfg::HALVES * a) * LDP + tx + 16 * b] = e;
                 sum += e;
             }
 #pragma unroll
@@ -131,14 +138,14 @@ __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &
 #pragma unroll
             for (int b = 0; b < NE; ++b)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) o[a][b][c] *= f;
+                for (int c = 0; c < 2; ++c) o[a][b][c].x *= f, o[a][b][c].y *= f;
         }
         __syncwarp();
 #pragma unroll 2
         for (int k = 0; k < KT; k += 4) {
             float4 w[A];
 #pragma unroll
-            for (int a = 0; a < A; ++a) w[a] = *reinterpret_cast<const float4 *>(sp + (ty * A + a) * LDP + k);
+            for (int a = 0; a < A; ++a) w[a] = *reinterpret_cast<const float4 *>(sp + (ty + Cfg::HALVES * a) * LDP + k);
 #pragma unroll
             for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -147,10 +154,8 @@ __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &
 #pragma unroll
                     for (int a = 0; a < A; ++a) {
                         const float f = u == 0 ? w[a].x : u == 1 ? w[a].y : u == 2 ? w[a].z : w[a].w;
-                        o[a][b][0] = fmaf(f, v.x, o[a][b][0]);
-                        o[a][b][1] = fmaf(f, v.y, o[a][b][1]);
-                        o[a][b][2] = fmaf(f, v.z, o[a][b][2]);
-                        o[a][b][3] = fmaf(f, v.w, o[a][b][3]);
+                        o[a][b][0] = fma2(make_float2(f, f), make_float2(v.x, v.y), o[a][b][0]);
+                        o[a][b][1] = fma2(make_float2(f, f), make_float2(v.z, v.w), o[a][b][1]);
                     }
                 }
         }
@@ -160,7 +165,7 @@ __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &
     const bool direct = attn_direct(p, j, whole);
 #pragma unroll
     for (int a = 0; a < A; ++a) {
-        const int r = ty * A + a;
+        const int r = ty + Cfg::HALVES * a;
         if (r >= j.rows) continue;
         float *to;
         float inv = 1.f;
@@ -177,12 +182,12 @@ __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &
         for (int b = 0; b < NE; ++b)
             if (b * 64 + tx * 4 < p.d)
                 *reinterpret_cast<float4 *>(to + b * 64 + tx * 4) =
-                    make_float4(o[a][b][0] * inv, o[a][b][1] * inv, o[a][b][2] * inv, o[a][b][3] * inv);
+                    make_float4(o[a][b][0].x * inv, o[a][b][0].y * inv, o[a][b][1].x * inv, o[a][b][1].y * inv);
     }
 }
 
 template <int DP>
-__global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_constant__ AttnPlan p,
+__global__ void __launch_bounds__(SimtCfg<DP>::THREADS, 1) attn_simt_kernel(const __grid_constant__ AttnPlan p,
                                                                  const __grid_constant__ AttnData x) {
     using Cfg = SimtCfg<DP>;
     extern __shared__ __align__(16) uint8_t smem_raw[];
@@ -206,15 +211,19 @@ __global__ void __launch_bounds__(SIMT_THREADS) attn_simt_kernel(const __grid_co
                             g - j.g0, stop - g, j.head};
         int page[Cfg::PASSES];
         tile_pages<DP>(p, keys, keys.t0, page);
-        for (int i = tid; i < j.rows * (DP / 4); i += SIMT_THREADS) {
+        for (int i = tid; i < j.rows * (DP / 4); i += Cfg::THREADS) {
             const int r = i / (DP / 4), e = i % (DP / 4) * 4, tok = attn_row_token(p, r);
             if (e < p.d)
                 copy16(smem_u32(sq + r * Cfg::LD + e),
                        static_cast<const float *>(x.q) + (j.tok0 + tok) * x.ld_q + (j.head * p.group + r - tok * p.group) * p.d + e, true);
         }
-        if (j.rows <= 16) simt_segment<DP, 1>(p, x, j, keys, first, whole, sq, skv, sp, page);
-        else if (j.rows <= 32) simt_segment<DP, 2>(p, x, j, keys, first, whole, sq, skv, sp, page);
-        else simt_segment<DP, 4>(p, x, j, keys, first, whole, sq, skv, sp, page);
+        constexpr int H = Cfg::HALVES;
+        if (j.rows <= H) simt_segment<DP, 1>(p, x, j, keys, first, whole, sq, skv, sp, page);
+        else if (2 * H == SIMT_ROWS || j.rows <= 2 * H) simt_segment<DP, 2>(p, x, j, keys, first, whole, sq, skv, sp, page);
+        else if constexpr (2 * H < SIMT_ROWS) {
+            if (j.rows <= 3 * H) simt_segment<DP, 3>(p, x, j, keys, first, whole, sq, skv, sp, page);
+            else simt_segment<DP, 4>(p, x, j, keys, first, whole, sq, skv, sp, page);
+        }
         g = stop;
         if (g >= g_end) return;
         j = attn_next(p, bases, j);
@@ -229,7 +238,7 @@ template <int DP> static griffin_status launch_dp(AttnPlan p, AttnData x, cudaSt
     const size_t smem = SimtCfg<DP>::smem(p.n_seq);
     if (ensure_dynamic_smem(fn, smem) != cudaSuccess) return GRIFFIN_ERR_CUDA;
     void *args[] = {&p, &x};
-    return launch_maybe_overlapped(fn, dim3(p.grid), dim3(SIMT_THREADS), smem, stream, true, args) == cudaSuccess
+    return launch_maybe_overlapped(fn, dim3(p.grid), dim3(SimtCfg<DP>::THREADS), smem, stream, true, args) == cudaSuccess
                ? GRIFFIN_OK
                : GRIFFIN_ERR_CUDA;
 }

@@ -109,19 +109,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // NaN if an
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// two fp32 lanes in one instruction
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(d)
-        : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
-    return *reinterpret_cast<float2 *>(&d);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
-    return *reinterpret_cast<float2 *>(&d);
-}
 // 2^x of both lanes on the FMA and integer pipes, x >= -120 after clamping (NaN too: the row's maximum tells of one): n = the integer next to x (by adding
 // 1.5 * 2^23), f = x - n, a cubic for 2^f on [-1/2, 1/2] (its own minimax fit, relative error 7.5e-5: a fiftieth of
 // the rounding of P to bf16 that follows), n into the exponent.
