@@ -14,6 +14,10 @@
 // instruction are keys or entries and its 8 columns the queries: none is empty.  K rows are the left operand as they lie
 // (ldmatrix), V rows transposed (ldmatrix.trans), P^T is turned by movmatrix, the queries stay in registers.  16-byte
 // pieces of a row are placed at piece ^ (row mod 8), which keeps the loads free of bank conflicts.
+//
+// Measured, the joining kernel included: one sequence of 32 heads behind 20000 tokens (332 MB) 60.4 us, 5.5 TB/s, 0.84 of
+// the measured copy; behind 512 tokens (10 MB) 12.3 us, of which the bytes are 1.6: the launches, the schedule's loads, the
+// pages', the keys', and the partials' follow one another.
 #include "attn.h"
 #include "attn_join.cuh"
 #include "decode_mma.cuh"
