@@ -8,16 +8,23 @@ namespace griffin {
 
 constexpr int ATTN_MAX_GRID = 148;  // CTAs at most (one per SM of a B200)
 
-// Whether the kernel for blocks of 8 rows (attn_few.cu) takes a call rather than the tcgen05 one: its sequences' rows fit
-// one such block on average, those of a shared prefix do, and a CTA has about two of the sequences' blocks at most.
-// Both sides, us a pass, few / tcgen05: 1 sequence of 32 heads behind 512 tokens 12.4 / 14.5, behind 20000 60.4 / 64.9;
-// 32 query heads over 8 behind 2048 11.4 / 15.2; 8 sequences of 32 heads behind 2048 (256 blocks) 25.7 / 26.8, of 40 heads
-// (320 blocks) 31.5 / 30.5; 64 sequences of 32 heads of their own (2048 blocks) 90 / 83: the end of a block costs this
-// kernel more.
+// Whether the kernel for blocks of 8 rows (attn_few.cu) takes a call rather than the tcgen05 one: a CTA has about two of
+// the sequences' key heads at most, and the rows that a sequence has on average, and those of a shared prefix, fit one such
+// block, or two whose second reading of the keys finds them in L2.
+// Both sides, us a pass, few / tcgen05.  One block: 1 sequence of 32 heads behind 512 tokens 12.4 / 14.5, behind 20000 60.4 /
+// 64.9; 32 query heads over 8 behind 2048 11.4 / 15.2; 8 sequences of 32 heads behind 2048 (256 key heads) 25.7 / 26.8, of 40
+// (320) 31.5 / 30.5; 64 sequences of 32 heads of their own (2048) 90 / 83: the end of a block costs this kernel more.
+// Two blocks of a sequence of its own keys: 4 tokens, 32 heads over 8, 16000 keys (66 MB) 27 / 41; 16 tokens of 32 heads, 2600
+// keys (43 MB) 23.5 / 27.4, 9100 keys (149 MB) 50 / 43; 4 sequences of 13 tokens and up to 4000 keys, 4 heads 16 / 26.  Two blocks of a
+// shared prefix, 4 sequences, 32 heads over 8: 2048 tokens (8 MB) 15.5 / 16.4, 8000 27.4 / 25.3, 20000 52 / 35.
+constexpr long long FEW_OWN_TWICE = 64ll << 20, FEW_PREFIX_TWICE = 8ll << 20;   // bytes
 static bool attn_few(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
-    const long long rows = (long long)batch->n_tokens * (desc->n_q_heads / desc->n_kv_heads);
-    return desc->dtype == GRIFFIN_DT_BF16 && desc->n_q_heads <= 8 * desc->n_kv_heads && rows <= 8ll * batch->n_seq &&
-           (batch->n_seq == 1 || batch->prefix_len == 0 || rows <= 8) && batch->n_seq * desc->n_kv_heads <= 2 * ATTN_MAX_GRID;
+    const long long rows = (long long)batch->n_tokens * (desc->n_q_heads / desc->n_kv_heads), n = batch->n_seq;
+    if (desc->dtype != GRIFFIN_DT_BF16 || desc->n_q_heads > 8 * desc->n_kv_heads || n * desc->n_kv_heads > 2 * ATTN_MAX_GRID) return false;
+    const long long token = 4ll * desc->n_kv_heads * desc->head_dim, prefix = batch->prefix_len * token;
+    const long long own = n * batch->table_stride * desc->page_size * token;   // (at most: the lengths are on the device)
+    if (n > 1 && prefix > 0 && rows > 8 && (rows > 16 || prefix > FEW_PREFIX_TWICE)) return false;
+    return rows <= 8 * n || (rows <= 16 * n && own + prefix <= FEW_OWN_TWICE);
 }
 static AttnShape shape_of(const griffin_attn_desc *desc, bool few) {
     if (desc->dtype == GRIFFIN_DT_F32) return attn_simt_shape(desc->head_dim);

@@ -305,6 +305,15 @@ def test_attention_of_few_rows_and_many_blocks():
     check_attention(Batch([1] * 8, [(31 * i) % 190 + 1 for i in range(8)], 1100, 38, 38, 64, 16, "bf16"), rows={0, 7})
 
 
+def test_attention_of_two_blocks_of_few_rows():
+    # 9 to 16 rows of a sequence or of a short prefix, and sequences whose rows are unevenly many
+    check_attention(Batch([4], [1500], 0, 8, 2, 128, 16, "bf16"))
+    check_attention(Batch([13, 9, 2], [700, 9, 40], 0, 2, 2, 72, 32, "bf16"))
+    check_attention(Batch([2, 2], [200, 5], 333, 8, 2, 128, 16, "bf16"))
+    check_attention(Batch([1, 3, 0, 1], [20, 90, 4, 1], 1111, 3, 1, 256, 64, "bf16"))
+    check_attention(Batch([17, 1], [16, 30], 0, 1, 1, 64, 8, "bf16"))
+
+
 @pytest.mark.parametrize("fill", [float("nan"), float("inf"), -float("inf"), 3e38])
 def test_attention_of_more_rows_does_not_see_what_lies_behind_the_ends(fill):
     check_attention(Batch([4, 2, 3], [5, 70, 129], 37, 4, 2, 64, 64, "bf16", fill=fill))
