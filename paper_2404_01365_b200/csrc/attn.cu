@@ -11,13 +11,13 @@ constexpr int ATTN_MAX_GRID = 148;  // CTAs at most (one per SM of a B200)
 // Whether the kernel for blocks of 8 rows (attn_few.cu) takes a call rather than the tcgen05 one: a CTA has about two of
 // the sequences' key heads at most, and the rows that a sequence has on average, and those of a shared prefix, fit one such
 // block, or two whose second reading of the keys finds them in L2.
-// Both sides, us a pass, few / tcgen05.  One block: 1 sequence of 32 heads behind 512 tokens 12.4 / 14.5, behind 20000 60.4 /
-// 64.9; 32 query heads over 8 behind 2048 11.4 / 15.2; 8 sequences of 32 heads behind 2048 (256 key heads) 25.7 / 26.8, of 40
-// (320) 31.5 / 30.5; 64 sequences of 32 heads of their own (2048) 90 / 83: the end of a block costs this kernel more.
-// Two blocks of a sequence of its own keys: 4 tokens, 32 heads over 8, 16000 keys (66 MB) 27 / 41; 16 tokens of 32 heads, 2600
-// keys (43 MB) 23.5 / 27.4, 9100 keys (149 MB) 50 / 43; 4 sequences of 13 tokens and up to 4000 keys, 4 heads 16 / 26.  Two blocks of a
-// shared prefix, 4 sequences, 32 heads over 8: 2048 tokens (8 MB) 15.5 / 16.4, 8000 27.4 / 25.3, 20000 52 / 35.
-constexpr long long FEW_OWN_TWICE = 64ll << 20, FEW_PREFIX_TWICE = 8ll << 20;   // bytes
+// Both sides, us a pass, few / tcgen05.  One block: 1 sequence of 32 heads behind 512 tokens 12.4 / 14.6, behind 20000 61.3 /
+// 65.2; 32 query heads over 8 behind 2048 11.4 / 14.2; 8 sequences of 32 heads behind 2048 (256 key heads) 25.8 / 27.1, of 40
+// (320) 31.5 / 30.6; 64 sequences of 32 heads of their own (2048) 90 / 83: the end of a block costs this kernel more.
+// Two blocks of a sequence's keys: 4 sequences of 16 tokens of 8 heads 11.7 / 14.6; 4 tokens, 32 heads over 8, 9000 keys (37 MB)
+// 20.9 / 21.8, 16000 (66 MB) 27.6 / 26.5; 16 tokens of 32 heads, 2600 keys (43 MB) 23.4 / 22.7.  Two blocks of a shared prefix: 2
+// sequences of 2 tokens, 16 heads over 4, 3000 tokens (6 MB) 12.4 / 14.9; 4 sequences, 32 over 8, 2048 (8 MB) 15.2 / 15.1.
+constexpr long long FEW_OWN_TWICE = 36ll << 20, FEW_PREFIX_TWICE = 7ll << 20;   // bytes
 static bool attn_few(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
     const long long rows = (long long)batch->n_tokens * (desc->n_q_heads / desc->n_kv_heads), n = batch->n_seq;
     if (desc->dtype != GRIFFIN_DT_BF16 || desc->n_q_heads > 8 * desc->n_kv_heads || n * desc->n_kv_heads > 2 * ATTN_MAX_GRID) return false;

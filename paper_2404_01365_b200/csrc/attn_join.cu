@@ -41,13 +41,13 @@ template <typename T> __device__ __forceinline__ void store_row4(T *to, const fl
     }
 }
 
-// CTAs 0 .. by_row - 1: jobs whose partials are kept by row: in a fused call the last row block of each sequence and
+// CTAs 0 .. by_row * split - 1, `split` of them to a job: jobs whose partials are kept by row: in a fused call the last row block of each sequence and
 // key head (no other has just one row tile) and the blocks that see nothing, else every row block.  The others
 // (fused calls): the blocks that were cut, JOIN_ROWS rows each.
 // NV: 128-entry pieces of a row (a lane has 4 entries of each).
 template <typename T, int NV>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ AttnPlan p, T *__restrict__ out,
-                                                                 long long ld_out, int by_row) {
+                                                                 long long ld_out, int by_row, int split) {
     __shared__ float sh_ml[JOIN_WARPS][2], sh_o[JOIN_WARPS][NV * 128];
     __shared__ int sh_seq[5];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -60,18 +60,19 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     AttnSeq q{};
     int r0 = 0, r1 = 0, head = 0, seq = 0, n_blocks = 0, b = 0, base0 = 0, base1 = 0;
     bool cut = false;
-    if ((int)blockIdx.x >= by_row) {
-        const int chunks = p.cta_rows / JOIN_ROWS, c = (int)(blockIdx.x - by_row) / chunks;
+    const int id = (int)((uint32_t)blockIdx.x / (uint32_t)split), part = blockIdx.x - id * split;
+    if (id >= by_row) {
+        const int at = blockIdx.x - by_row * split, chunks = p.cta_rows / JOIN_ROWS, c = at / chunks;
         if (c >= sh.G || tot.queued) return;
         const CutJob j = p.cuts[c];
-        r0 = (int)(blockIdx.x - by_row) % chunks * JOIN_ROWS;
+        r0 = at % chunks * JOIN_ROWS;
         r1 = min(j.rows, r0 + JOIN_ROWS);
         if (r0 >= r1) return;
         a = JobParts{PartJob{0, j.head, j.tok0, false}, j.c0, 1, c - j.c0 + 1};
         cut = true;
     } else {
-        const int bx = (int)((uint32_t)blockIdx.x / (uint32_t)p.hkv);
-        head = blockIdx.x - bx * p.hkv;
+        const int bx = (int)((uint32_t)id / (uint32_t)p.hkv);
+        head = id - bx * p.hkv;
         int q_start, q_end, len;
         if (p.fused) {
             seq = bx;
@@ -115,7 +116,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
             g0 -= (int)attn_sum_tiles(p, q, b, n_blocks);
             const AttnJob j = attn_own_job(p, q, seq, head, b, g0);
             a = job_parts(p, sh, j);
-            r1 = j.rows;
+            const int per = (j.rows + split - 1) / split;   // this CTA's rows of the job
+            r0 = part * per;
+            r1 = min(j.rows, r0 + per);
             if (p.fused && j.g1 > j.g0 && (!j.alt || tot.queued)) return;  // finished by the attention kernel, or cut
         }
         // Each row is joined by `wpr` warps (more when there are fewer rows), each taking a stretch of its partials; their
@@ -248,9 +251,14 @@ griffin_status launch_attn_join(const AttnPlan &plan, int dtype, void *out, long
                                                            : reinterpret_cast<const void *>(attn_join_kernel<__nv_bfloat16, 2>));
     // More warps to a row shorten its chain, more CTAs than fit at once lengthen the whole: with 320 one-row blocks 128
     // threads take 30.7 us with the attention in front (256: 34.8), with 96 five-row blocks 256 take 22.8 (128: 25.6).
-    const int threads = by_row + cut > 2 * p.grid ? JOIN_THREADS / 2 : JOIN_THREADS;
-    void *args[] = {&p, &out, &ld_out, &by_row};
-    return launch_maybe_overlapped(fn, dim3(by_row + cut), dim3(threads), 0, stream, true, args) == cudaSuccess ? GRIFFIN_OK
+    // Jobs of several rows go to several CTAs while there are fewer CTAs than fit at once (8 tokens of one sequence, 32 heads
+    // over 8, behind 9000: 52.7 -> 22.1 us), unless the jobs by row are the rare ones (a prompt's last block).
+    const bool rows_here = !p.fused || (p.alt && p.n_tokens <= p.n_seq * p.tile_tokens);
+    const int most = (p.n_tokens < p.block_tokens ? p.n_tokens : p.block_tokens) * p.group, room = 2 * p.grid / by_row;
+    int split = room < 1 || !rows_here ? 1 : room < most ? room : most;
+    const int threads = by_row * split + cut > 2 * p.grid ? JOIN_THREADS / 2 : JOIN_THREADS;
+    void *args[] = {&p, &out, &ld_out, &by_row, &split};
+    return launch_maybe_overlapped(fn, dim3(by_row * split + cut), dim3(threads), 0, stream, true, args) == cudaSuccess ? GRIFFIN_OK
                                                                                                                      : GRIFFIN_ERR_CUDA;
 }
 
