@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
     if (tid == 0) {
         for (int i = 0; i < n_slots; ++i) {
             mbar_init(&kv_full[i], 1);
-            mbar_init(&kv_empty[i], 1);
+            mbar_init(&kv_empty[i], 2);   // the products that read it, and the value warp
             mbar_init(&v_ok[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -438,13 +438,15 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
         // ---------------- value tiles: rows that no key stands for become zeros ----------------
         Segment w;
         // (It waits for the key tiles too: a wait for a slot's n-th filling may only begin when the one before has been
-        // seen, or the parity of an older one passes for it.)
+        // seen, or the parity of an older one passes for it.  And no slot is filled again before it has looked: a filling
+        // that it missed would leave it waiting for one that needs its own word.)
         Ring kv{0, 0}, done{0, 0};
         bool ok = true;
         while (ok && (ok = seg.take(w, abort, p.ws, 47)) && w.n > 0) {
             for (int t = 0; t < w.n && ok; ++t, done.step(1, n_slots)) {
                 const KeyTile k = key_tile(p, w, w.t0 + t);
                 if (!(ok = warp_wait(&kv_full[kv.slot], kv.parity, abort, p.ws, 56))) break;
+                if (lane == 0) mbar_arrive(&kv_empty[kv.slot]);
                 kv.step(1, n_slots);
                 const uint32_t slot = kv.slot;
                 if (!(ok = warp_wait(&kv_full[slot], kv.parity, abort, p.ws, 56))) break;
@@ -459,7 +461,10 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                     fence_proxy_async_smem();
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&v_ok[done.slot]);
+                if (lane == 0) {
+                    mbar_arrive(&v_ok[done.slot]);
+                    mbar_arrive(&kv_empty[slot]);
+                }
             }
         }
     } else if (warp == 3) {
