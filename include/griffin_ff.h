@@ -409,8 +409,8 @@ typedef struct {
  * values are in pages prefix_pages[0 ..]; behind it each has tokens of its own, in pages
  * page_table[s * table_stride ..].  The call's new tokens are rows of q (k, v): those of sequence s
  * are rows q_start[s] .. q_start[s+1]-1, and they are the LAST of its seq_len[s] own tokens.
- * The arrays are on the device; the counts are host values (n_tokens: rows of q; rows from
- * q_start[n_seq] on are left alone). */
+ * The arrays are on the device; the counts are host values (n_tokens: rows of q; rows in front of
+ * q_start[0] and from q_start[n_seq] on belong to no sequence and are left alone). */
 typedef struct {
     int32_t n_seq, n_tokens;
     const int32_t *q_start;       /* [n_seq + 1], ascending                                     */

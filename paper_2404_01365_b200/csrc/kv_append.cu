@@ -55,7 +55,7 @@ template <typename T> __device__ __forceinline__ void get_half(const Piece<T> &p
 
 template <typename T, int TPC>
 __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const __grid_constant__ AppendParams p) {
-    __shared__ long long s_at[TPC];   // the tokens' places in the cache, in elements; -1: none; -2: behind the last sequence
+    __shared__ long long s_at[TPC];   // the tokens' places in the cache, in elements; -1: none; -2: of no sequence
     __shared__ int s_pos[TPC];
     __shared__ __align__(16) float s_table[TPC][TPC > 1 ? 256 : 4];
     const int t0 = blockIdx.x * TPC, pieces = (p.d + 15) >> 4, per_round = APPEND_THREADS / pieces;  // heads side by side
@@ -93,8 +93,14 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const __grid_
         const int t = TPC == 1 ? t0 : t0 + threadIdx.x;
         if (TPC > 1 || p.n_seq == 1)  // (otherwise the count above was this token's)
             while (seq < p.n_seq && __ldg(p.q_start + seq + 1) <= t) ++seq;
+        int first = t + 1, end = 0, len = 0;   // (three loads in one trip)
         if (seq < p.n_seq && t < p.n_tokens) {
-            const int k = __ldg(p.seq_len + seq) - (__ldg(p.q_start + seq + 1) - t);   // index among its own tokens
+            first = __ldg(p.q_start + seq);
+            end = __ldg(p.q_start + seq + 1);
+            len = __ldg(p.seq_len + seq);
+        }
+        if (t >= first) {   // (rows in front of the first sequence's, as those behind the last one's, belong to none)
+            const int k = len - (end - t);   // index among its own tokens
             at1 = -1;
             pos1 = p.prefix_len + k;
             if (k >= 0) {
@@ -126,7 +132,7 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const __grid_
 #pragma unroll
     for (int u = 0; u < TPC; ++u) {
         const long long at = TPC > 1 ? s_at[u] : at1;
-        if (at == -2) return;
+        if (at == -2) continue;
         const int t = t0 + u;
         if (at < 0) {   // padding, or a token that could not be placed
             if (!is_q) continue;

@@ -1,0 +1,62 @@
+"""The operators around the FF block at the edges of what their arguments may say: rows of no sequence, workspaces and
+lengths at their limits, arrays out of order."""
+import numpy as np
+import pytest
+import torch
+
+from layer_util import Batch, f64
+from oracle import layer_oracle as L
+from paper_2404_01365_b200 import binding as G
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def behind(lead, q_lens, seq_lens, *args, **kw):
+    """A batch whose first sequence's rows begin at `lead`: a slice of a larger batch's arrays."""
+    b = Batch([lead] + q_lens, [0] + seq_lens, *args, **kw)
+    b.q_start, b.seq_len, b.page_table = b.q_start[1:].clone(), b.seq_len[1:].clone(), b.page_table[1:].clone()
+    return b
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lead,q_lens,seq_lens", [(4, [1, 1], [100, 50]), (1, [3], [40]), (3, [0, 2, 5], [30, 9, 5]),
+                                                  (7, [2400], [2400]), (2400, [3, 1], [2500, 1])])
+def test_append_leaves_rows_in_front_of_the_first_sequence_alone(dtype, lead, q_lens, seq_lens):
+    b = behind(lead, q_lens, seq_lens, 21, 2, 1, 64, 16, dtype, extra_rows=2).to_device()
+    table = G.rope_table(b.prefix + max(seq_lens) + 1, 64, device=DEV)
+    q_out = torch.full((b.T, b.hq, b.hd), 33.0, dtype=b.dt, device=DEV)
+    old_k, old_v = b.kc.clone(), b.vc.clone()
+    G.griffin_kv_append(b.desc, b.batch, b.cache, G.make_rope(table), b.q.to(DEV), b.k.to(DEV), b.v.to(DEV), q_out, b.ws)
+    assert G.griffin_check_device_status(b.ws) == G.OK
+    n = int(b.q_start[-1])
+    assert torch.all(q_out[:lead] == 33.0) and torch.all(q_out[n:] == 33.0), "rows of no sequence were written"
+    want_k, want_v, want_q = L.kv_append(f64(old_k), f64(old_v), b.q_start.numpy(), b.seq_len.numpy(), b.page_table.numpy(), b.prefix,
+                                         f64(b.q), f64(b.k), f64(b.v), f64(table))
+    touched = np.zeros(want_k.shape[:1] + want_k.shape[2:3], bool)
+    for t, s, i in L.places(b.q_start.numpy(), b.seq_len.numpy()):
+        touched[b.page_table[s, i // b.page], i % b.page] = True
+    at = np.broadcast_to(touched[:, None, :, None], want_k.shape)
+    # one rounding of the storage type, and two products and a sum in 32 bits of values up to |x| + |y|
+    ulp = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}[dtype]
+    size = 2 * float(torch.cat((b.q.flatten(), b.k.flatten())).abs().max())
+    near = lambda a, w: np.all(np.abs(a - w) <= ulp * np.abs(w) + 4 * 2.0 ** -24 * size)
+    assert near(f64(b.kc)[at], want_k[at]) and np.array_equal(f64(b.vc)[at], want_v[at]) and near(f64(q_out)[lead:n], want_q[lead:n])
+    for got, old in ((b.kc, old_k), (b.vc, old_v)):
+        assert np.array_equal(f64(got)[~at], f64(old)[~at], equal_nan=True), "an entry that no token stands for was written"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lead,q_lens,seq_lens,prefix", [(4, [1, 1], [100, 50], 70), (1, [3], [40], 0), (200, [130, 2], [130, 9], 50),
+                                                         (9, [300], [300], 0)])
+def test_attention_leaves_rows_in_front_of_the_first_sequence_alone(dtype, lead, q_lens, seq_lens, prefix):
+    b = behind(lead, q_lens, seq_lens, prefix, 4, 2, 64, 16, dtype, extra_rows=2)
+    b.q[:lead] = float("nan")
+    b.to_device()
+    out = b.attend()
+    assert G.griffin_check_device_status(b.ws) == G.OK
+    n = int(b.q_start[-1])
+    assert torch.all(out[:lead] == 77.0) and torch.all(out[n:] == 77.0), "rows of no sequence were written"
+    b.q[:lead] = 0.0
+    want, mass = b.reference()
+    assert np.all(np.abs(f64(out) - want)[lead:n] <= b.bound(want, mass)[lead:n])
