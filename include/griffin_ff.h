@@ -448,7 +448,8 @@ griffin_status griffin_kv_append(const griffin_attn_desc *desc, const griffin_at
                                  void *q_out, int64_t ld_q_out, void *workspace, void *stream);
 
 /* Bytes of workspace for griffin_attn_prefix calls of at most n_tokens_max new tokens and n_seq_max
- * sequences; 0 if desc is NULL or invalid.  Clear it with griffin_workspace_init. */
+ * sequences; 0 if desc is NULL or invalid.  Any 16-byte boundary will do.  Clear it with
+ * griffin_workspace_init. */
 size_t griffin_attn_workspace_bytes(const griffin_attn_desc *desc, int32_t n_tokens_max, int32_t n_seq_max);
 
 /* Attention of the new tokens over the shared prefix and their own sequence, causal:

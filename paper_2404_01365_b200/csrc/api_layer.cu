@@ -7,6 +7,14 @@
 using namespace griffin;
 
 static inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// The attention scratch begins at the first 32-byte boundary behind the header (partials are stored 32 bytes at a time); a
+// workspace may begin on any 16-byte boundary.
+static inline uint8_t *scratch_of(void *ws) {
+    return reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(ws) + WS_HEADER_BYTES + 31) & ~uintptr_t(31));
+}
+static inline size_t attn_ws_bytes(const griffin_attn_desc *desc, int n_tokens, int n_seq) {
+    return WS_HEADER_BYTES + 16 + attn_scratch_bytes(desc, n_tokens, n_seq);
+}
 static inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 static inline int elem_bytes(int dtype) { return dtype == GRIFFIN_DT_F32 ? 4 : 2; }
 static inline bool is_dtype(int t) { return t == GRIFFIN_DT_F32 || t == GRIFFIN_DT_BF16; }
@@ -104,7 +112,7 @@ griffin_status griffin_kv_append(const griffin_attn_desc *desc, const griffin_at
 
 size_t griffin_attn_workspace_bytes(const griffin_attn_desc *desc, int32_t n_tokens_max, int32_t n_seq_max) {
     if (check_attn_desc(desc) != GRIFFIN_OK || n_tokens_max < 0 || n_seq_max < 1) return 0;
-    return WS_HEADER_BYTES + attn_scratch_bytes(desc, n_tokens_max, n_seq_max);
+    return attn_ws_bytes(desc, n_tokens_max, n_seq_max);
 }
 
 griffin_status griffin_attn_prefix(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
@@ -121,10 +129,10 @@ griffin_status griffin_attn_prefix(const griffin_attn_desc *desc, const griffin_
     if (st != GRIFFIN_OK) return st;
     if (workspace == nullptr) return GRIFFIN_ERR_WORKSPACE;
     if (!aligned16(workspace)) return GRIFFIN_ERR_ALIGNMENT;
-    if (ws_bytes < WS_HEADER_BYTES + attn_scratch_bytes(desc, batch->n_tokens, batch->n_seq)) return GRIFFIN_ERR_WORKSPACE;
+    if (ws_bytes < attn_ws_bytes(desc, batch->n_tokens, batch->n_seq)) return GRIFFIN_ERR_WORKSPACE;
     if (batch->n_tokens == 0) return GRIFFIN_OK;
-    return launch_attn_prefix(desc, batch, cache, q, ld_q, out, ld_out, static_cast<uint8_t *>(workspace) + WS_HEADER_BYTES,
-                              workspace, static_cast<cudaStream_t>(stream));
+    return launch_attn_prefix(desc, batch, cache, q, ld_q, out, ld_out, scratch_of(workspace), workspace,
+                              static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

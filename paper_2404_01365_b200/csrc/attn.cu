@@ -40,7 +40,7 @@ static AttnScratch attn_scratch(const griffin_attn_desc *desc, const AttnShape &
     AttnScratch s;
     const size_t row = (size_t)(desc->head_dim + 2) * sizeof(float), streams = sh.alt ? 2 : 1;
     const long long by_token = n_tokens * desc->n_q_heads, by_seq = n_seq * desc->n_kv_heads * 128;
-    s.own_rows = ((by_token < by_seq ? by_token : by_seq) + 3) / 4 * 4;  // (16-byte alignment of what follows the rows)
+    s.own_rows = ((by_token < by_seq ? by_token : by_seq) + 3) / 4 * 4;  // (what follows the rows' m and l, 8 bytes each, is on a 32-byte boundary again)
     s.cuts_off = ((size_t)(n_seq + 3) * 4 + 255) / 256 * 256;
     s.own_off = s.cuts_off + ATTN_MAX_GRID * sizeof(CutJob);
     s.pre_off = s.own_off + streams * s.own_rows * row;

@@ -98,7 +98,7 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
         : "memory");
 }
-// 32 bytes, a whole sector, in one store (the partials' rows start on 32-byte boundaries)
+// 32 bytes, a whole sector, in one store (the scratch, its parts and the partials' rows start on 32-byte boundaries)
 __device__ __forceinline__ void store_8f(float *to, const float *v) {
     asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
                  "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])

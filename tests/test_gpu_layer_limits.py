@@ -60,3 +60,23 @@ def test_attention_leaves_rows_in_front_of_the_first_sequence_alone(dtype, lead,
     b.q[:lead] = 0.0
     want, mass = b.reference()
     assert np.all(np.abs(f64(out) - want)[lead:n] <= b.bound(want, mass)[lead:n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_lens,seq_lens,prefix,hq,hkv,hd", [
+    ([1, 1, 1], [100, 50, 7], 300, 16, 1, 128),      # more rows than the few-row kernel's blocks: partials of the prefix and of own keys
+    ([5, 6, 5], [30, 6, 80], 333, 4, 4, 256),        # one accumulator
+    ([3], [3000], 0, 8, 1, 64),                      # one sequence, its keys cut over the CTAs
+    ([300], [300], 0, 2, 2, 72),
+])
+def test_attention_with_a_workspace_on_a_16_byte_boundary(dtype, q_lens, seq_lens, prefix, hq, hkv, hd):
+    b = Batch(q_lens, seq_lens, prefix, hq, hkv, hd, 16, dtype).to_device()
+    plain, n = b.attend(), b.ws.numel()
+    room = torch.full((n + 64,), 0xA5, dtype=torch.uint8, device=DEV)
+    assert room.data_ptr() % 32 == 0
+    for at in (0, 16):
+        b.ws = room[at:at + n]
+        G.griffin_workspace_init(b.ws)
+        assert torch.equal(b.attend(), plain) and G.griffin_check_device_status(b.ws) == G.OK
+        assert torch.all(room[:at] == 0xA5) and torch.all(room[at + n:] == 0xA5), "written outside the workspace"
+        room.fill_(0xA5)
