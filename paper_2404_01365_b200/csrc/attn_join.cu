@@ -54,6 +54,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     pdl_launch_dependents();
     pdl_wait_prior_grids();
     const AttnTotals tot = attn_totals(p, p.bases);
+    if (tot.W < 0) return;   // the call was not run, and the first tiles of its sequences mean nothing
     if (tot.queued && blockIdx.x == 0 && threadIdx.x == 0) *p.queue = 0;
     const AttnShares sh(tot.W, p.grid);
     JobParts a;

@@ -172,7 +172,7 @@ __device__ __forceinline__ long long attn_sum_tiles(const AttnPlan &p, const Att
 
 // What the CTAs know of a call after the scan.
 struct AttnTotals {
-    int W;         // tiles
+    int W;         // tiles; -1: more than the kernels can count
     int jobs;      // of the sequences
     bool queued;   // whether jobs are handed out whole, from a queue
 };
@@ -180,8 +180,9 @@ constexpr int ATTN_QUEUE_JOBS = 3;   // jobs per CTA from which a call is queued
 
 // First tile of every sequence into bases[0 .. n_seq] (shared memory), by all threads of the CTA; bases[n_seq] is
 // the number of tiles of the call, and the two entries behind it say how many jobs there are and how long the longest is.
-// The first CTA also leaves them in the scratch for the joining kernel.  A call of 2^31 tiles or more (10^14
-// bytes of keys) is not run: no tiles, and the status word is raised.
+// The first CTA also leaves them in the scratch for the joining kernel.  A call of 2^31 tiles or more is not run: its
+// number of tiles is -1, at which the kernels return, and the status word is raised.  (Tiles are counted by key head and row
+// block: one prompt of 32 heads over 8, 128 wide, gets there with 2.1 million tokens in bf16, with 0.74 million in fp32.)
 __device__ __forceinline__ void attn_scan(const AttnPlan &p, int *bases) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const long long most = 1ll << 31;
@@ -235,7 +236,7 @@ __device__ __forceinline__ void attn_scan(const AttnPlan &p, int *bases) {
             longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
         }
         if (lane == 0) {
-            bases[p.n_seq] = bad ? 0 : (int)sum;
+            bases[p.n_seq] = bad ? -1 : (int)sum;
             bases[p.n_seq + 1] = jobs * p.hkv;
             bases[p.n_seq + 2] = longest;
             if (bad) attn_bad(p.ws, 43);

@@ -80,3 +80,34 @@ def test_attention_with_a_workspace_on_a_16_byte_boundary(dtype, q_lens, seq_len
         assert torch.equal(b.attend(), plain) and G.griffin_check_device_status(b.ws) == G.OK
         assert torch.all(room[:at] == 0xA5) and torch.all(room[at + n:] == 0xA5), "written outside the workspace"
         room.fill_(0xA5)
+
+
+@pytest.mark.parametrize("dtype,tokens,hkv,group,n_seq", [
+    ("bf16", 1, 256, 1, 1),       # the few-row kernel, one sequence behind a prefix of 2^30 tokens (one page, again and again)
+    ("bf16", 300, 128, 1, 1),     # two row blocks under every head, the second in one row tile
+    ("bf16", 256, 256, 1, 1),     # one block of two row tiles
+    ("bf16", 2, 256, 4, 2),       # a prefix that is read once for the batch
+    ("f32", 1, 128, 1, 1),
+    ("f32", 2, 128, 2, 2),
+])
+def test_attention_of_more_tiles_than_can_be_counted_is_not_run(dtype, tokens, hkv, group, n_seq):
+    page, prefix, hd, dt = 1024, 1 << 30, 64, {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    desc = G.make_attn_desc(hkv * group, hkv, hd, page, dtype)
+    kc, vc = (torch.randn(1, hkv, page, hd, device=DEV, dtype=dt) for _ in range(2))
+    pages = torch.zeros(prefix // page, dtype=torch.int32, device=DEV)
+    ints = lambda *a: torch.tensor(a, dtype=torch.int32, device=DEV)
+    starts, lens = ints(0, tokens) if n_seq == 1 else ints(0, 1, tokens), ints(*[0] * n_seq)
+    q, out = (torch.full((tokens, hkv * group, hd), x, device=DEV, dtype=dt) for x in (0.1, 77.0))
+    ws, cache = G.alloc_attn_workspace(desc, tokens, n_seq, DEV), G.make_kv_cache(kc, vc)
+    table = torch.zeros(n_seq, 1, dtype=torch.int32, device=DEV)
+    G.griffin_attn_prefix(desc, G.make_attn_batch(starts, lens, table, tokens, pages, prefix), cache, q, out, ws)
+    assert G.griffin_check_device_status(ws) == G.ERR_INVALID_ARG
+    assert torch.all(out == 77.0)
+    # the workspace is fit for the next call
+    G.griffin_workspace_init(ws)
+    G.griffin_attn_prefix(desc, G.make_attn_batch(starts, lens, table, tokens, pages, page), cache, q, out, ws)
+    assert G.griffin_check_device_status(ws) == G.OK
+    # a query of equal entries: softmax of 0.1 scale times the keys' sums
+    p = torch.softmax(q[0, 0, 0].double() * hd ** -0.5 * kc[0].double().sum(2), 1)
+    want = (p[:, None] @ vc[0].double())[:, 0].repeat_interleave(group, 0)
+    assert torch.all((out.double() - want[None]).abs() < (2.0 ** -7 if dtype == "bf16" else 2.0 ** -16))
