@@ -341,6 +341,7 @@ griffin_status griffin_check_device_status(const void *workspace, void *stream);
 
 #define GRIFFIN_MAX_NORM_D 16384    /* widest row of griffin_norm_residual                       */
 #define GRIFFIN_MAX_ATTN_SEQ 1024   /* sequences per griffin_kv_append / griffin_attn_prefix call */
+#define GRIFFIN_MAX_ATTN_TOKENS (1 << 30) /* tokens of a prefix; own tokens of a sequence         */
 #define GRIFFIN_MAX_HEAD_GROUP 64   /* query heads per key head                                   */
 
 typedef enum {
@@ -439,9 +440,9 @@ typedef struct {
  * row of q_out is zero.  q, q_out [n_tokens, Hq, D], k, v [n_tokens, Hkv, D] with ld_* elements
  * from token to token (multiples of 16 bytes), so slices of one projection's output will do; q and
  * q_out may both be NULL, and q_out may be q.  rope NULL: no rotation.  A page number outside
- * [0, n_pages), an index beyond the table's row or a position from n_pos on is not followed: the
- * token is not written (its q_out row is zero) and the workspace's status word (workspace may be
- * NULL) is raised.  Two tokens of a call must not share a place. */
+ * [0, n_pages), an index beyond the table's row or from GRIFFIN_MAX_ATTN_TOKENS on, or a position
+ * from n_pos on is not followed: the token is not written (its q_out row is zero) and the workspace's
+ * status word (workspace may be NULL) is raised.  Two tokens of a call must not share a place. */
 griffin_status griffin_kv_append(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
                                  const griffin_kv_cache *cache, const griffin_rope *rope,
                                  const void *q, int64_t ld_q, const void *k, int64_t ld_k, const void *v, int64_t ld_v,
@@ -462,8 +463,8 @@ size_t griffin_attn_workspace_bytes(const griffin_attn_desc *desc, int32_t n_tok
  * count as nothing seen); among the tokens of the call, a value (v) that is not finite may also
  * reach tokens in front of it.  Probabilities are rounded to bf16 for the second product when the
  * storage is bf16.  q, out [n_tokens, Hq, D], ld_* as above; out may be q only if they are the same
- * rows.  Page numbers outside [0, n_pages) read as zeros, lengths beyond the table's row are cut, and
- * both raise the workspace's status word.
+ * rows.  Page numbers outside [0, n_pages) read as zeros, lengths beyond the table's row or
+ * GRIFFIN_MAX_ATTN_TOKENS are cut, and both raise the workspace's status word.
  * The work is cut into tiles: for each key head and block of rows (a row: token and query head of the
  * group), 128 keys and up to 256 rows (bf16), 64 keys and 128 rows (bf16, heads over 128), 64 keys (32 for
  * heads over 128) and 64 rows (fp32), fewer rows where a call has few.  A call of 2^31 tiles or more is

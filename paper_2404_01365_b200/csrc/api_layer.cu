@@ -35,7 +35,7 @@ static griffin_status check_batch(const griffin_attn_batch *b) {
     if (b->q_start == nullptr || b->seq_len == nullptr) return GRIFFIN_ERR_INVALID_ARG;
     if (b->table_stride > 0 && b->page_table == nullptr) return GRIFFIN_ERR_INVALID_ARG;
     if (b->prefix_len > 0 && b->prefix_pages == nullptr) return GRIFFIN_ERR_INVALID_ARG;
-    if (b->n_seq > GRIFFIN_MAX_ATTN_SEQ || b->prefix_len > (1 << 30) || b->n_tokens > (1 << 22)) return GRIFFIN_ERR_UNSUPPORTED;
+    if (b->n_seq > GRIFFIN_MAX_ATTN_SEQ || b->prefix_len > GRIFFIN_MAX_ATTN_TOKENS || b->n_tokens > (1 << 22)) return GRIFFIN_ERR_UNSUPPORTED;
     if (!aligned4(b->q_start) || !aligned4(b->seq_len) || !aligned4(b->page_table) || !aligned4(b->prefix_pages))
         return GRIFFIN_ERR_ALIGNMENT;
     return GRIFFIN_OK;

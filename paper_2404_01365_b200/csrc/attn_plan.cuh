@@ -74,10 +74,11 @@ static __device__ __noinline__ void attn_bad(void *ws, int where) { raise_status
 struct AttnSeq {
     int q0, nq, len;  // first new token, how many, own tokens
 };
-// A sequence's lengths as the arrays q_start (a, b) and seq_len have them, held to what the call can hold.
+// A sequence's lengths as the arrays q_start (a, b) and seq_len have them, held to what the call can hold (and to 2^30 own
+// tokens, as a prefix is: places and tile counts stay in 32 bits).
 __device__ __forceinline__ AttnSeq attn_seq_of(const AttnPlan &p, int a, int b, int len) {
     AttnSeq r;
-    const long long cap = (long long)p.table_stride << p.page_shift;
+    const long long cap = min((long long)p.table_stride << p.page_shift, (long long)GRIFFIN_MAX_ATTN_TOKENS);
     const bool bad = a < 0 || b < a || b > p.n_tokens || len < 0 || len > cap;
     a = min(max(a, 0), p.n_tokens);
     b = min(max(b, a), p.n_tokens);

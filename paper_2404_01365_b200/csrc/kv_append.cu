@@ -100,12 +100,13 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const __grid_
             len = __ldg(p.seq_len + seq);
         }
         if (t >= first) {   // (rows in front of the first sequence's, as those behind the last one's, belong to none)
-            const int k = len - (end - t);   // index among its own tokens
+            const long long own = (long long)len - (end - t);   // index among its own tokens
+            const int k = (int)max(min(own, (long long)GRIFFIN_MAX_ATTN_TOKENS), -1ll);
             at1 = -1;
-            pos1 = p.prefix_len + k;
+            pos1 = p.prefix_len + k;   // (2^31 - 1 at most for an index below the limit)
             if (k >= 0) {
                 const int col = k >> p.page_shift;
-                const int page = col < p.table_stride ? __ldg(p.page_table + (long long)seq * p.table_stride + col) : -1;
+                const int page = k < GRIFFIN_MAX_ATTN_TOKENS && col < p.table_stride ? __ldg(p.page_table + (long long)seq * p.table_stride + col) : -1;
                 if (page >= 0 && page < p.n_pages && (p.rot == 0 || pos1 < p.n_pos))
                     at1 = page * p.stride_page + (k & ((1 << p.page_shift) - 1)) * p.stride_token;
                 else if (blockIdx.y == 0 && threadIdx.x < TPC)

@@ -111,3 +111,28 @@ def test_attention_of_more_tiles_than_can_be_counted_is_not_run(dtype, tokens, h
     p = torch.softmax(q[0, 0, 0].double() * hd ** -0.5 * kc[0].double().sum(2), 1)
     want = (p[:, None] @ vc[0].double())[:, 0].repeat_interleave(group, 0)
     assert torch.all((out.double() - want[None]).abs() < (2.0 ** -7 if dtype == "bf16" else 2.0 ** -16))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_lengths_near_the_end_of_32_bits(dtype):
+    # a table of 2^21 entries of one page, so that its row holds 2^31 tokens: place, position and tiles must not run over
+    page, hkv, hd, n, dt = 1024, 64, 64, 1300, {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    desc = G.make_attn_desc(hkv, hkv, hd, page, dtype)
+    kc, vc = (torch.zeros(1, hkv, page, hd, device=DEV, dtype=dt) for _ in range(2))
+    ints = lambda *a: torch.tensor(a, dtype=torch.int32, device=DEV)
+    table, pre = torch.zeros(1, 1 << 21, dtype=torch.int32, device=DEV), torch.zeros(1 << 20, dtype=torch.int32, device=DEV)
+    ws, cache = G.alloc_attn_workspace(desc, n, 1, DEV), G.make_kv_cache(kc, vc)
+    q, out = (torch.full((n, hkv, hd), x, device=DEV, dtype=dt) for x in (0.1, 77.0))
+    rope = G.make_rope(G.rope_table(64, 64, device=DEV))
+    for length in (2 ** 31 - 1, 2 ** 30 + n, -2 ** 31):
+        for prefix in (0, 1 << 30):
+            batch = G.make_attn_batch(ints(0, n), ints(length), table, n, pre if prefix else None, prefix)
+            q_out = torch.full_like(q, 33.0)
+            G.griffin_kv_append(desc, batch, cache, rope, q, q, q, q_out, ws)
+            assert G.griffin_check_device_status(ws) == (G.ERR_INVALID_ARG if length > 0 else G.OK)
+            assert torch.all(q_out == 0) and not kc.any() and not vc.any()
+            G.griffin_workspace_init(ws)
+        if length > 0:      # cut to 2^30 tokens, and those are more tiles than can be counted
+            G.griffin_attn_prefix(desc, G.make_attn_batch(ints(0, n), ints(length), table, n), cache, q, out, ws)
+            assert G.griffin_check_device_status(ws) == G.ERR_INVALID_ARG and torch.all(out == 77.0)
+            G.griffin_workspace_init(ws)
