@@ -464,7 +464,8 @@ size_t griffin_attn_workspace_bytes(const griffin_attn_desc *desc, int32_t n_tok
  * reach tokens in front of it.  Probabilities are rounded to bf16 for the second product when the
  * storage is bf16.  q, out [n_tokens, Hq, D], ld_* as above; out may be q only if they are the same
  * rows.  Page numbers outside [0, n_pages) read as zeros, lengths beyond the table's row or
- * GRIFFIN_MAX_ATTN_TOKENS are cut, and both raise the workspace's status word.
+ * GRIFFIN_MAX_ATTN_TOKENS are cut, as are rows of q_start that do not ascend within [0, n_tokens]; all
+ * of them raise the workspace's status word.
  * The work is cut into tiles: for each key head and block of rows (a row: token and query head of the
  * group), 128 keys and up to 256 rows (bf16), 64 keys and 128 rows (bf16, heads over 128), 64 keys (32 for
  * heads over 128) and 64 rows (fp32), fewer rows where a call has few.  A call of 2^31 tiles or more is

@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
         }
         q = attn_seq_of(p, q_start, q_end, len);
         n_blocks = ceil_div(q.nq, p.block_tokens);
-        if (b >= n_blocks) return;
+        if (b < 0 || b >= n_blocks) return;   // (b < 0: q_start does not ascend, which attn_seq_of has reported)
     }
 #pragma unroll 1
     for (;;) {

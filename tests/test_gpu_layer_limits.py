@@ -136,3 +136,26 @@ def test_lengths_near_the_end_of_32_bits(dtype):
             G.griffin_attn_prefix(desc, G.make_attn_batch(ints(0, n), ints(length), table, n), cache, q, out, ws)
             assert G.griffin_check_device_status(ws) == G.ERR_INVALID_ARG and torch.all(out == 77.0)
             G.griffin_workspace_init(ws)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("starts", [(0, 300, 0, 10), (-5000, -3000, 0, 4), (0, 1000000, 5, 10), (290, 200, 100, 300), (5, -2 ** 31, 2 ** 31 - 1, 7)])
+@pytest.mark.parametrize("prefix", [0, 100])
+def test_rows_that_do_not_ascend_are_reported_and_stay_inside(dtype, starts, prefix):
+    b = Batch([100, 100, 100], [120, 150, 100], prefix, 2, 2, 64, 16, dtype, fill=0.0).to_device()
+    room = torch.full((b.T + 600, b.hq, b.hd), 77.0, dtype=b.dt, device=DEV)
+    out = room[300:300 + b.T]
+    good = b.attend()
+    b.dev[0].copy_(torch.tensor(starts, dtype=torch.int32))
+    b.attend(out=out)
+    assert G.griffin_check_device_status(b.ws) == G.ERR_INVALID_ARG
+    rope, qd = G.make_rope(G.rope_table(400, 64, device=DEV)), b.q.to(DEV)
+    kc = b.kc.clone()
+    G.griffin_kv_append(b.desc, b.batch, b.cache, rope, qd, b.k.to(DEV), b.v.to(DEV), out, b.ws)
+    torch.cuda.synchronize()
+    assert torch.all(room[:300] == 77.0) and torch.all(room[300 + b.T:] == 77.0), "written outside the output"
+    b.kc.copy_(kc)
+    b.vc.copy_(b.v_host.to(DEV) if b.layout == "hnd" else b.vc)
+    b.dev[0].copy_(b.q_start)
+    G.griffin_workspace_init(b.ws)
+    assert torch.equal(b.attend(), good) and G.griffin_check_device_status(b.ws) == G.OK
