@@ -76,6 +76,7 @@ class NormDesc(C.Structure):
 
 class NormWeights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("pre_w", "pre_b", "post_w", "post_b")]
+    _form = None     # (torch dtype, width) of the tensors it was made of
 
 
 class AttnDesc(C.Structure):
@@ -85,12 +86,14 @@ class AttnDesc(C.Structure):
 class KVCache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32)] + \
                [(n, C.c_int64) for n in ("stride_page", "stride_head", "stride_token")]
+    _form = None     # (griffin_dtype, heads, page size, head width) of the tensors it was made of
 
 
 class AttnBatch(C.Structure):
     _fields_ = [("n_seq", C.c_int32), ("n_tokens", C.c_int32)] + \
                [(n, C.c_void_p) for n in ("q_start", "seq_len", "page_table")] + \
                [("table_stride", C.c_int32), ("prefix_len", C.c_int32), ("prefix_pages", C.c_void_p)]
+    _prefix_pages = None     # how many pages the prefix's list has
 
 
 class Rope(C.Structure):
@@ -344,6 +347,7 @@ def griffin_check_device_status(ws, stream=None):
 
 # ---- around the FF block: norms and the residual stream, the paged cache, attention over it ---------------------
 _TORCH_DTYPE = {DT_F32: torch.float32, DT_BF16: torch.bfloat16}
+_DTYPE_CODE = {t: c for c, t in _TORCH_DTYPE.items()}
 
 
 def _dtype(v):
@@ -371,8 +375,16 @@ def make_norm_desc(d, dtype, res_dtype=None, pre="rms", post="none", eps=1e-6, w
 
 
 def make_norm_weights(pre_w=None, pre_b=None, post_w=None, post_b=None):
+    """Vectors [d] of the descriptor's dtype, consecutive entries (checked against it when the call is made)."""
     w = NormWeights(_ptr(pre_w), _ptr(pre_b), _ptr(post_w), _ptr(post_b))
     w._keep = (pre_w, pre_b, post_w, post_b)
+    for t in w._keep:
+        if t is None:
+            continue
+        if t.dim() != 1 or not t.is_contiguous() or w._form not in (None, (t.dtype, t.shape[0])):
+            raise ValueError("norm weights: expected vectors of one dtype and width with consecutive entries, got "
+                             + ", ".join(f"{x.dtype} {tuple(x.shape)} with strides {x.stride()}" for x in w._keep if x is not None))
+        w._form = (t.dtype, t.shape[0])
     return w
 
 
@@ -391,6 +403,8 @@ def griffin_norm_residual(desc, weights, res, res_out, h, y=None, gate=None, str
     if T == 0:
         return
     dt, rdt = _TORCH_DTYPE[desc.dtype], _TORCH_DTYPE[desc.res_dtype]
+    if weights._form is not None and weights._form != (dt, d):
+        raise ValueError(f"norm weights: expected {dt} [{d}], got {weights._form[0]} [{weights._form[1]}]")
     y_p = g_p = ro_p = h_p = None
     ld_y = ld_g = ld_ro = ld_h = 0
     ld_r = _norm_rows(res, d, rdt, T, "res")
@@ -425,7 +439,18 @@ def make_kv_cache(k, v):
                          f"{v.dtype} {tuple(v.shape)} {v.stride()}")
     c = KVCache(_ptr(k), _ptr(v), k.shape[0], k.stride(0), k.stride(1), k.stride(2))
     c._keep = (k, v)
+    c._form = (_DTYPE_CODE.get(k.dtype, str(k.dtype)), *k.shape[1:])
     return c
+
+
+def _check_cache(form, batch, cache):
+    """That the cache's pages are the descriptor's (form: dtype, heads, page size, head width), and the prefix's list as
+    long as the prefix."""
+    if cache._form != form and cache._form is not None:
+        raise ValueError("cache: expected pages [{1}, {2}, {3}] of griffin_dtype {0}, got [{5}, {6}, {7}] of {4}"
+                         .format(*form, *cache._form))
+    if batch._prefix_pages is not None and batch.prefix_len > batch._prefix_pages * form[2]:
+        raise ValueError(f"prefix_pages: {batch._prefix_pages} pages of {form[2]} tokens for a prefix of {batch.prefix_len}")
 
 
 def make_attn_batch(q_start, seq_len, page_table, n_tokens, prefix_pages=None, prefix_len=0):
@@ -441,6 +466,7 @@ def make_attn_batch(q_start, seq_len, page_table, n_tokens, prefix_pages=None, p
     b = AttnBatch(n_seq, int(n_tokens), _ptr(q_start), _ptr(seq_len), _ptr(page_table),
                   page_table.shape[1], int(prefix_len), _ptr(prefix_pages))
     b._keep = (q_start, seq_len, page_table, prefix_pages)
+    b._prefix_pages = None if prefix_pages is None else prefix_pages.numel()
     return b
 
 
@@ -464,6 +490,7 @@ def griffin_kv_append(desc, batch, cache, rope, q, k, v, q_out, ws=None, stream=
     """New keys and values [n_tokens, n_kv_heads, head_dim] into the cache, keys and queries rotated; q and q_out may be
     None, q_out may be q."""
     n, hq, hk, d, dt = batch.n_tokens, desc.n_q_heads, desc.n_kv_heads, desc.head_dim, desc.dtype
+    _check_cache((dt, hk, desc.page_size, d), batch, cache)
     q_p = o_p = None
     ld_q = ld_o = 0
     if q is not None:
@@ -494,6 +521,7 @@ def griffin_attn_prefix(desc, batch, cache, q, out, ws, stream=None):
     """Attention of the batch's new tokens over the shared prefix and their own sequences; q, out [n_tokens, n_q_heads,
     head_dim]."""
     n, hq, d, dt = batch.n_tokens, desc.n_q_heads, desc.head_dim, desc.dtype
+    _check_cache((dt, desc.n_kv_heads, desc.page_size, d), batch, cache)
     st = load().griffin_attn_prefix(C.byref(desc), C.byref(batch), C.byref(cache), q.data_ptr(), _rows(q, n, hq, d, dt, "q"),
                                     out.data_ptr(), _rows(out, n, hq, d, dt, "out"), ws.data_ptr(), ws.numel(), _stream(stream))
     if st != OK:
