@@ -248,9 +248,10 @@ __device__ __forceinline__ void attn_scan(const AttnPlan &p, int *bases) {
         for (int s = threadIdx.x; s <= p.n_seq + 2; s += blockDim.x) p.bases[s] = bases[s];
 }
 // Whether a call's jobs are handed out whole.  Cut shares are even to a tile, but every cut costs two partials of a
-// block, written and read again (a 4096-token prompt of 32 heads: 20 of 200 us).  With several jobs per CTA and none of
-// them longer than a fair share, taking whole jobs from a queue, the longest of a sequence first, comes within a short
-// job of even.  Only fused calls: the others have partials to join anyway.
+// block, written and read again.  With several jobs per CTA and none of them longer than a fair share, whole jobs are taken
+// from a queue, the longest of a sequence first: with one sequence that comes within a short job of even, with several
+// within the last sequence's longest.  Queue / cut shares, us a pass, 32 heads over 8: a 4096-token prompt 150 / 215, 8 of 2048
+// tokens 275 / 358, 64 of 256 106 / 171, 512 of 64 187 / 239.  Only fused calls: the others have partials to join anyway.
 __device__ __forceinline__ AttnTotals attn_totals(const AttnPlan &p, const int *bases) {
     AttnTotals t;
     t.W = bases[p.n_seq];
@@ -294,22 +295,45 @@ static __device__ __noinline__ AttnJob attn_find(const AttnPlan &p, const int *b
         at += __shfl_sync(0xffffffffu, upto, 31);
     }
 }
+// Where a CTA's last job from the queue was: its sequence, and the jobs of the sequences in front of it.
+struct AttnQueueAt {
+    int seq, before;
+};
 // Job i of a queued call: sequence by sequence, its row blocks from the last (the longest) to the first, each under
-// every key head.
-static __device__ __noinline__ AttnJob attn_queued(const AttnPlan &p, int i) {
-    int s = -1, nb = 0;
-    AttnSeq q{};
+// every key head; by a whole warp.  A CTA's jobs ascend, so it goes on from its last one's sequence, 32 sequences at a time:
+// it passes each of them once, not once a job.
+static __device__ __noinline__ AttnJob attn_queued(const AttnPlan &p, int i, AttnQueueAt &at) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll 1
     for (;;) {
-        do q = attn_seq(p, ++s); while (q.nq == 0 || attn_block_tiles(p, q, (q.nq - 1) / p.block_tokens) == 0);
-        nb = ceil_div(q.nq, p.block_tokens);
-        if (i < nb * p.hkv) break;
-        i -= nb * p.hkv;
+        AttnSeq q{};
+        int nb = 0;   // (a sequence that sees nothing has no jobs)
+        if (at.seq + lane < p.n_seq) {
+            q = attn_seq(p, at.seq + lane);
+            nb = ceil_div(q.nq, p.block_tokens);
+            if (nb > 0 && attn_block_tiles(p, q, nb - 1) == 0) nb = 0;
+        }
+        int upto = nb * p.hkv;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const unsigned here = __ballot_sync(0xffffffffu, i < at.before + upto);
+        if (here != 0) {
+            const int f = __ffs(here) - 1;
+            at.before += __shfl_sync(0xffffffffu, upto - nb * p.hkv, f);
+            at.seq += f;
+            nb = __shfl_sync(0xffffffffu, nb, f);
+            q = AttnSeq{__shfl_sync(0xffffffffu, q.q0, f), __shfl_sync(0xffffffffu, q.nq, f), __shfl_sync(0xffffffffu, q.len, f)};
+            const int of = i - at.before, k = (int)((uint32_t)of / (uint32_t)p.hkv);
+            AttnJob j = attn_own_job(p, q, at.seq, of - k * p.hkv, nb - 1 - k, 0);
+            j.alt = false;   // (its result is not joined with another)
+            return j;
+        }
+        at.before += __shfl_sync(0xffffffffu, upto, 31);
+        at.seq += 32;
     }
-    const int k = (int)((uint32_t)i / (uint32_t)p.hkv);
-    AttnJob j = attn_own_job(p, q, s, i - k * p.hkv, nb - 1 - k, 0);
-    j.alt = false;   // (its result is not joined with another)
-    return j;
 }
 // The job behind j, whose first tile is j.g1 < bases[n_seq].
 static __device__ __noinline__ AttnJob attn_next(const AttnPlan &p, const int *bases, const AttnJob &j) {

@@ -477,22 +477,25 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
             j = attn_find(p, bases, g);
             if (lane == 0) attn_note_cut(p, shares, j, g, min(g_end, j.g1));
         }
-        if (lane == 0) {
-            Ring at{0, 0};
-            for (uint32_t k = 0;; ++k) {
-                if (k >= ATC_SEGS && !wait_bar(&seg_empty[at.slot], at.parity ^ 1u, abort, p.ws, 46)) break;
-                if (totals.queued) {
-                    // the next job of the queue, once the copies of the one before have been asked for
-                    if (!wait_bar(seg_want, k & 1, abort, p.ws, 44)) break;
-                    do {
-                        const int i = (int)atomicAdd(p.queue, 1u);
-                        more = i < totals.jobs;
-                        if (!more) break;
-                        j = attn_queued(p, i);
-                        g = j.g0;
-                    } while (j.g1 == j.g0);   // (blocks that see nothing are the joining kernel's)
-                }
-                const int stop = totals.queued ? j.g1 : min(g_end, j.g1);
+        Ring at{0, 0};
+        AttnQueueAt from{0, 0};
+        for (uint32_t k = 0;; ++k) {
+            if (k >= ATC_SEGS && !warp_wait(&seg_empty[at.slot], at.parity ^ 1u, abort, p.ws, 46)) break;
+            if (totals.queued) {
+                // the next job of the queue, once the copies of the one before have been asked for
+                if (!warp_wait(seg_want, k & 1, abort, p.ws, 44)) break;
+                do {
+                    int i = 0;
+                    if (lane == 0) i = (int)atomicAdd(p.queue, 1u);
+                    i = __shfl_sync(0xffffffffu, i, 0);
+                    more = i < totals.jobs;
+                    if (!more) break;
+                    j = attn_queued(p, i, from);
+                    g = j.g0;
+                } while (j.g1 == j.g0);   // (blocks that see nothing are the joining kernel's)
+            }
+            const int stop = totals.queued ? j.g1 : min(g_end, j.g1);
+            if (lane == 0) {
                 Segment s;
                 s.t0 = g - j.g0;
                 s.n = more ? stop - g : 0;
@@ -508,13 +511,14 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                 s.direct = attn_direct(p, j, s.first && stop == j.g1);
                 segs[at.slot] = s;
                 mbar_arrive(&seg_full[at.slot]);
-                if (!more) break;
-                at.step(1, ATC_SEGS);
-                if (!totals.queued) {
-                    g = stop;
-                    more = g < g_end;
-                    if (more) j = attn_next(p, bases, j);
-                }
+            }
+            __syncwarp();
+            if (!more) break;
+            at.step(1, ATC_SEGS);
+            if (!totals.queued) {
+                g = stop;
+                more = g < g_end;
+                if (more) j = attn_next(p, bases, j);
             }
         }
     } else if (warp >= 4 && (NS == 2 || warp < 8)) {
