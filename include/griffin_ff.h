@@ -459,10 +459,9 @@ size_t griffin_attn_workspace_bytes(const griffin_attn_desc *desc, int32_t n_tok
  * that sees nothing gets zeros.  The prefix is read once for all sequences of the call when their
  * queries are few; a batch of long pieces, whose rows fill the tensor cores' tiles anyway, reads it
  * sequence by sequence.  What lies in the cache behind a sequence's end may be anything, NaN
- * included; a logit of NaN or +inf that a token sees makes its row NaN (logits that are all -inf
- * count as nothing seen); among the tokens of the call, a value (v) that is not finite may also
- * reach tokens in front of it.  Probabilities are rounded to bf16 for the second product when the
- * storage is bf16.  q, out [n_tokens, Hq, D], ld_* as above; out may be q only if they are the same
+ * included, and a value (v) that is not finite reaches the tokens that see it and no others; a logit
+ * of NaN or +inf that a token sees makes its row NaN (logits that are all -inf count as nothing
+ * seen).  Probabilities are rounded to bf16 for the second product when the storage is bf16.  q, out [n_tokens, Hq, D], ld_* as above; out may be q only if they are the same
  * rows.  Page numbers outside [0, n_pages) read as zeros, lengths beyond the table's row or
  * GRIFFIN_MAX_ATTN_TOKENS are cut, as are rows of q_start that do not ascend within [0, n_tokens]; all
  * of them raise the workspace's status word.

@@ -42,6 +42,30 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
     return *reinterpret_cast<float2 *>(&d);
 }
+// Whether any of many bf16 is an infinity or NaN: 0 times each, summed, is 0 or NaN.
+struct NotFinite8 {
+    __nv_bfloat162 sum[4];
+    __device__ __forceinline__ NotFinite8() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = __floats2bfloat162_rn(0.f, 0.f);
+    }
+    __device__ __forceinline__ void add(uint4 x) {
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&w[i]), __floats2bfloat162_rn(0.f, 0.f), sum[i]);
+    }
+    __device__ __forceinline__ bool any() const {
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w |= *reinterpret_cast<const uint32_t *>(&sum[i]);
+        return (w & 0x7fff7fffu) != 0;
+    }
+};
+// Eight bf16, those that are not finite (their exponent is all ones) set to zero.
+__device__ __forceinline__ uint4 finite_or_zero8(uint4 x) {
+    const auto two = [](uint32_t w) { return w & ~(((((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu); };
+    return make_uint4(two(x.x), two(x.y), two(x.z), two(x.w));
+}
 // 16 bytes to shared memory, asynchronously; zeros where nothing is there
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");

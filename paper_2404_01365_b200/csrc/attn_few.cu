@@ -129,6 +129,41 @@ __device__ __forceinline__ int2 few_start(const AttnPlan &p, const AttnData &x, 
     return page[Cfg::STAGES - 1];
 }
 
+// Values that are not finite, of keys that not all rows of the block see: P = 0 would not keep them from the rows that do not
+// (0 times them is NaN).  They are replaced by zero before the product,
+template <int DP> static __device__ __noinline__ void few_clear_not_finite(uint8_t *values) {
+    __syncwarp();
+    for (int i = threadIdx.x & 31; i < 16 * FewCfg<DP>::PIECES; i += 32) {
+        uint4 *const at = reinterpret_cast<uint4 *>(values) + i;
+        *at = finite_or_zero8(*at);
+    }
+    __syncwarp();
+}
+// and added to the warp's results (rows LDO apart) of the rows that do see them: whatever P, the sum is what P times them
+// gives.  t0, n: the segment's tiles.  (The 16 keys are cleared together, so those are looked at from their first on.)
+template <int DP>
+static __device__ __noinline__ void few_add_not_finite(const AttnPlan &p, const AttnData &x, const AttnJob &j, int pre_tiles, int t0, int n,
+                                                       float *results) {
+    using Cfg = FewCfg<DP>;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int k0 = max(max(j.seen0, 0) & ~15, (t0 - pre_tiles) * Cfg::KT), k1 = min(j.own_len, (t0 + n - pre_tiles) * Cfg::KT);
+    __syncwarp();
+    for (int k = k0; k < k1; ++k) {
+        if (k / 16 % Cfg::WARPS != warp || lane >= Cfg::PIECES || lane * 8 >= p.d) continue;
+        const int page = __ldg(p.page_table + (long long)j.seq * p.table_stride + (k >> p.page_shift));
+        if ((unsigned)page >= (unsigned)p.n_pages) continue;
+        const __nv_bfloat16 *const v = static_cast<const __nv_bfloat16 *>(x.v) + page * x.stride_page + j.head * x.stride_head +
+                                       (k & ((1 << p.page_shift) - 1)) * x.stride_token + lane * 8;
+        for (int e = 0; e < 8; ++e) {
+            const float f = __bfloat162float(v[e]);
+            if (fabsf(f) < INFINITY) continue;
+            for (int r = 0; r < j.rows; ++r)
+                if (k < j.seen0 + attn_row_token(p, r)) results[r * Cfg::LDO + lane * 8 + e] += f;
+        }
+    }
+    __syncwarp();
+}
+
 // The queries of a job as the first product takes them: row lane / 4.
 template <int DP>
 __device__ __forceinline__ void few_queries(const AttnPlan &p, const AttnData &x, const AttnJob &j, uint32_t (&q)[DP / 16][2]) {
@@ -180,6 +215,7 @@ __global__ void __launch_bounds__(FewCfg<DP>::THREADS, 1) attn_few_kernel(const 
         for (int i = 0; i < NC; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
 
         int used = 0;
+        bool marked = false;   // whether values were cleared, and have to be added to the rows that see them
 #pragma unroll 1
         for (int i = 0; i < n; ++i) {
             asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
@@ -246,6 +282,14 @@ __global__ void __launch_bounds__(FewCfg<DP>::THREADS, 1) attn_few_kernel(const 
                 l_a += s[2 * h];
                 l_b += s[2 * h + 1];
             }
+            if (!t.pre && j.seen0 < t.len && t.key0 + 16 > j.seen0) {   // keys that some rows see and some do not
+                NotFinite8 bad;
+                for (int e = lane; e < 16 * Cfg::PIECES; e += 32) bad.add(*reinterpret_cast<const uint4 *>(mine + used + Cfg::BUF + e * 16));
+                if (__any_sync(0xffffffffu, bad.any())) {
+                    few_clear_not_finite<DP>(mine + used + Cfg::BUF);
+                    marked = true;
+                }
+            }
             const uint32_t w0 = movmatrix_t(few_pack(s[0], s[1])), w1 = movmatrix_t(few_pack(s[2], s[3]));
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
@@ -285,6 +329,7 @@ __global__ void __launch_bounds__(FewCfg<DP>::THREADS, 1) attn_few_kernel(const 
                 so[Cfg::LDO + c * 16 + 8] = o[c][3];
             }
         }
+        if (marked) few_add_not_finite<DP>(p, x, j, j.seq < 0 || p.fused ? p.prefix_tiles : 0, t0, n, reinterpret_cast<float *>(mine + used));
         if (g < g_end) few_queries<DP>(p, x, next, q);
         __syncthreads();
         const bool direct = attn_direct(p, j, whole);

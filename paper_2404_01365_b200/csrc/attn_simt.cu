@@ -11,6 +11,8 @@
 //
 // Bound by latency: 5 steps behind 1003 shared tokens (16 heads over 4, 64 wide) take 12.7 us, half of them here and the
 // rest in the joining kernel; 1000 causal tokens of 8 heads over 2 take 72 us, 14 TFLOP/s of the 75 of the pipes.
+#include <type_traits>
+
 #include "attn.h"
 #include "attn_join.cuh"
 #include "vec8.cuh"
@@ -144,24 +146,34 @@ __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &
                 for (int c = 0; c < 2; ++c) o[a][b][c].x *= f, o[a][b][c].y *= f;
         }
         __syncwarp();
-#pragma unroll 2
-        for (int k = 0; k < KT; k += 4) {
-            float4 w[A];
+        // A tile with keys that some of the block's rows see and some do not: there P = 0 is no protection, since 0 times a
+        // value that is not finite is NaN, so each row leaves the others' keys out.
+        const int apart = pre || j.seen0 >= keys.own_len ? KT : j.seen0 - k0;   // from this key of the tile on
+        const auto products = [&](const int from, const int to, const auto all_see) {
+#pragma unroll(decltype(all_see)::value ? 2 : 1)
+            for (int k = from; k < to; k += 4) {
+                float4 w[A];
 #pragma unroll
-            for (int a = 0; a < A; ++a) w[a] = *reinterpret_cast<const float4 *>(sp + (ty + Cfg::HALVES * a) * LDP + k);
+                for (int a = 0; a < A; ++a) w[a] = *reinterpret_cast<const float4 *>(sp + (ty + Cfg::HALVES * a) * LDP + k);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+                for (int u = 0; u < 4; ++u)
 #pragma unroll
-                for (int b = 0; b < NE; ++b) {
-                    const float4 v = *reinterpret_cast<const float4 *>(sv + (k + u) * LD + b * 64 + tx * 4);
+                    for (int b = 0; b < NE; ++b) {
+                        const float4 v = *reinterpret_cast<const float4 *>(sv + (k + u) * LD + b * 64 + tx * 4);
 #pragma unroll
-                    for (int a = 0; a < A; ++a) {
-                        const float f = u == 0 ? w[a].x : u == 1 ? w[a].y : u == 2 ? w[a].z : w[a].w;
-                        o[a][b][0] = fma2(make_float2(f, f), make_float2(v.x, v.y), o[a][b][0]);
-                        o[a][b][1] = fma2(make_float2(f, f), make_float2(v.z, v.w), o[a][b][1]);
+                        for (int a = 0; a < A; ++a) {
+                            const float f = u == 0 ? w[a].x : u == 1 ? w[a].y : u == 2 ? w[a].z : w[a].w;
+                            if constexpr (!decltype(all_see)::value)
+                                if (k0 + k + u >= j.seen0 + attn_row_token(p, ty + Cfg::HALVES * a)) continue;
+                            o[a][b][0] = fma2(make_float2(f, f), make_float2(v.x, v.y), o[a][b][0]);
+                            o[a][b][1] = fma2(make_float2(f, f), make_float2(v.z, v.w), o[a][b][1]);
+                        }
                     }
-                }
-        }
+            }
+        };
+        const int cut = apart >= KT ? KT : max(apart, 0) & ~3;
+        products(0, cut, std::true_type{});
+        if (cut < KT) products(cut, KT, std::false_type{});
         __syncwarp();
     }
     // the segment's result

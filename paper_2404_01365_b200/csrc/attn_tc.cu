@@ -6,7 +6,8 @@
 // One persistent CTA per SM, each with its share of the call's key tiles (attn_plan.cuh), 384 threads:
 //   warp 0      TMA producer: query tiles and, page by page, key and value tiles (128-byte swizzle) into a ring
 //   warp 1      MMA issuer: one thread issues tcgen05.mma; it also owns the TMEM allocation
-//   warp 2      clears the rows of a value tile that no key stands for (0 * NaN would reach the sum)
+//   warp 2      clears what must not be multiplied with in a value tile, since 0 * NaN would reach the sum: rows that no
+//               key stands for, and values that are not finite of keys that not every row sees (add_not_finite)
 //   warp 3      scheduler: walks the share, segment by segment (a segment: what the share has of one job), and
 //               hands descriptions of the segments to the others through a ring in shared memory
 //   warps 4-7, 8-11   two softmax groups, a row per thread: S from TMEM, P (bf16) back to TMEM over S,
@@ -54,6 +55,8 @@ struct AtcParams {
     AttnPlan plan;
     void *out;
     long long ld_out;
+    const __nv_bfloat16 *v;
+    long long stride_page, stride_head, stride_token;
     int n_slots, box_rows, q_box_bytes;
 };
 
@@ -198,6 +201,7 @@ struct __align__(16) Segment {
     int alt, direct, first;
 };
 constexpr int ATC_SEGS = 4;
+constexpr int ATC_MARKS = 2 * ATC_SEGS;   // segments that the value warp may be ahead of a softmax warp, and the one at work
 
 // One key tile of a job: where its keys are and how many there are.
 struct KeyTile {
@@ -210,6 +214,45 @@ __device__ __forceinline__ KeyTile key_tile(const AttnPlan &p, const Segment &s,
     k.k0 = (k.prefix ? t : t - s.pre_tiles) << p.kt_shift;
     k.len = k.prefix ? p.prefix_len : s.own_len;
     return k;
+}
+
+// The values that the value warp has set to zero in this segment's tiles because they are not finite and not every row
+// of the block sees their keys: added to the rows that do (whatever P, the sum is what P times them gives).  A thread has a
+// row of `lanes`' accumulator at `to`; own_seen: the row's own tokens; 0: none.
+template <int DP>
+static __device__ __noinline__ void add_not_finite(const AtcParams &prm, const Segment &s, int own_seen, uint32_t to) {
+    const AttnPlan &p = prm.plan;
+    const int first = max(s.t0 - s.pre_tiles, 0) << p.kt_shift, last = max(s.t0 + s.n - s.pre_tiles, 0) << p.kt_shift;
+    const int k0 = max(max(s.seen0, 0), first), k1 = min(min(own_seen, s.own_len), last);
+#pragma unroll 1
+    for (int c = 0; c < DP; c += 32) {
+        float o[32];
+        tmem_ld32(to + c, o);
+#pragma unroll 1
+        for (int k = k0; k < k1; ++k) {
+            const int page = __ldg(p.page_table + (long long)s.seq * p.table_stride + (k >> p.page_shift));
+            if (page < 0 || page >= p.n_pages) continue;
+            const uint4 *const v = reinterpret_cast<const uint4 *>(prm.v + page * prm.stride_page + s.head * prm.stride_head +
+                                                                   (k & ((1 << p.page_shift) - 1)) * prm.stride_token + c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (c + 8 * e >= p.d) continue;
+                const uint4 x = __ldg(v + e);
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float f = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+                    if (!(fabsf(f) < INFINITY)) o[8 * e + i] += f;
+                }
+            }
+        }
+        uint32_t r[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(o[i]);
+        __syncwarp();
+        tmem_st32(to + c, r);
+    }
+    tmem_wait_st();
 }
 
 // A reader's place in the ring of segments.
@@ -258,7 +301,8 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
     Segment *const segs = reinterpret_cast<Segment *>(bars + ATC_BARS);
     uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(segs + ATC_SEGS);
     volatile int *const abort = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    int *const bases = reinterpret_cast<int *>(tmem_slot + 2);
+    volatile int *const marks = reinterpret_cast<volatile int *>(tmem_slot + 2);   // segments with values that are not finite
+    int *const bases = reinterpret_cast<int *>(tmem_slot + 2 + ATC_MARKS);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_launch_dependents();
@@ -442,7 +486,9 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
         // that it missed would leave it waiting for one that needs its own word.)
         Ring kv{0, 0}, done{0, 0};
         bool ok = true;
-        while (ok && (ok = seg.take(w, abort, p.ws, 47)) && w.n > 0) {
+        for (uint32_t at = 0; ok && (ok = seg.take(w, abort, p.ws, 47)) && w.n > 0; ++at) {
+            // (at most ATC_SEGS segments ahead of the slowest softmax warp: nobody reads this mark any more)
+            if (lane == 0) marks[at % ATC_MARKS] = 0;
             for (int t = 0; t < w.n && ok; ++t, done.step(1, n_slots)) {
                 const KeyTile k = key_tile(p, w, w.t0 + t);
                 if (!(ok = warp_wait(&kv_full[kv.slot], kv.parity, abort, p.ws, 56))) break;
@@ -452,6 +498,25 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                 if (!(ok = warp_wait(&kv_full[slot], kv.parity, abort, p.ws, 56))) break;
                 kv.step(1, n_slots);
                 const int valid = k.len - k.k0;
+                // keys of the tile from `apart` on are seen by some rows of the block and not by others
+                const int apart = k.prefix ? KT : max(w.seen0 - k.k0, 0), upto = min(valid, KT);
+                if (apart < upto) {
+                    uint4 *const rows = reinterpret_cast<uint4 *>(s_kv + slot * Cfg::KV_BYTES + apart * 128) + lane;
+                    const int n = (upto - apart) * 8 - lane;   // 16-byte pieces of a column block, this lane's every 32nd
+                    NotFinite8 bad;
+#pragma unroll 1
+                    for (int c = 0; c < CB; ++c)
+#pragma unroll 8
+                        for (int i = 0; i < n; i += 32) bad.add(rows[c * (KT * 8) + i]);
+                    if (__any_sync(0xffffffffu, bad.any())) {
+#pragma unroll 1
+                        for (int c = 0; c < CB; ++c)
+#pragma unroll 1
+                            for (int i = 0; i < n; i += 32) rows[c * (KT * 8) + i] = finite_or_zero8(rows[c * (KT * 8) + i]);
+                        if (lane == 0) marks[at % ATC_MARKS] = 1;
+                        fence_proxy_async_smem();
+                    }
+                }
                 if (valid < KT) {
 #pragma unroll 1
                     for (int i = lane; i < (KT - valid) * 8 * CB; i += 32) {
@@ -530,7 +595,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
         Segment j;
         uint32_t U0 = 0, n_o = 0;  // units before this segment; segments finished by this group
         bool ok = true;
-        while (ok && (ok = seg.take(j, abort, p.ws, 45)) && j.n > 0) {
+        for (uint32_t at_seg = 0; ok && (ok = seg.take(j, abort, p.ws, 45)) && j.n > 0; ++at_seg) {
             const bool dual = NS == 2 && !j.alt;
             const uint32_t n = (uint32_t)j.n << (dual ? 1 : 0);
             uint32_t u = NS == 2 ? (U0 ^ grp) & 1 : 0;             // the group's first unit
@@ -630,6 +695,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                 if (ok && warp_on) {
                     tc_fence_after_sync();
                     const uint32_t to = lanes + Cfg::O_COL + (NS == 2 ? grp : 0) * DP;
+                    if (marks[at_seg % ATC_MARKS] != 0) add_not_finite<DP>(prm, j, valid ? own_seen : 0, to);
                     if (j.direct) {
                         const float inv = m == -INFINITY ? 0.f : 1.0f / l;
                         __nv_bfloat16 *const dst = static_cast<__nv_bfloat16 *>(prm.out) + (j.tok0 + tok) * prm.ld_out +
@@ -694,6 +760,8 @@ template <int DP> static griffin_status launch_dp(const AttnPlan &plan, const At
     prm.plan = plan;
     prm.out = x.out;
     prm.ld_out = x.ld_out;
+    prm.v = static_cast<const __nv_bfloat16 *>(x.v);
+    prm.stride_page = x.stride_page; prm.stride_head = x.stride_head; prm.stride_token = x.stride_token;
     const int page = 1 << plan.page_shift;
     prm.box_rows = page < Cfg::KT ? page : Cfg::KT;
     prm.q_box_bytes = plan.tile_tokens * plan.group * 128;
@@ -718,7 +786,7 @@ template <int DP> static griffin_status launch_dp(const AttnPlan &plan, const At
             return GRIFFIN_ERR_UNSUPPORTED;  // (strides that the copy engine does not take)
     }
     // as many ring slots as fit beside the list of the sequences' first tiles
-    const size_t tail = ATC_BARS * 8 + ATC_SEGS * sizeof(Segment) + 8 + ((size_t)plan.n_seq + 3) * 4, fixed = 1024 + Cfg::NS * Cfg::Q_BYTES + tail;
+    const size_t tail = ATC_BARS * 8 + ATC_SEGS * sizeof(Segment) + 8 + ATC_MARKS * 4 + ((size_t)plan.n_seq + 3) * 4, fixed = 1024 + Cfg::NS * Cfg::Q_BYTES + tail;
     prm.n_slots = (int)((232448 - fixed) / Cfg::KV_BYTES);
     if (prm.n_slots > Cfg::MAX_SLOTS) prm.n_slots = Cfg::MAX_SLOTS;
     const size_t smem = fixed + (size_t)prm.n_slots * Cfg::KV_BYTES;
