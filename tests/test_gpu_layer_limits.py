@@ -159,3 +159,35 @@ def test_rows_that_do_not_ascend_are_reported_and_stay_inside(dtype, starts, pre
     b.dev[0].copy_(b.q_start)
     G.griffin_workspace_init(b.ws)
     assert torch.equal(b.attend(), good) and G.griffin_check_device_status(b.ws) == G.OK
+
+
+@pytest.mark.parametrize("dtype,res", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("pre,post", [("rms", "none"), ("layer", "none"), ("none", "layer"), ("layer", "rms"), ("rms", "layer")])
+@pytest.mark.parametrize("d", [320, 1360])
+def test_norm_rows_that_are_not_finite(dtype, res, pre, post, d):
+    # in the residual stream, the block's output or the gate: what the formula makes of them, and other rows as they were
+    dts = {"f32": torch.float32, "bf16": torch.bfloat16}
+    g = torch.Generator().manual_seed(d)
+    rnd = lambda *s, t=dts[dtype], b=0.0: (torch.randn(*s, generator=g) + b).to(t)
+    T, bad = 12, [float("nan"), float("inf"), -float("inf")]
+    r, y, gate = rnd(T, d, t=dts[res]), rnd(T, d), rnd(T, d)
+    for i, value in enumerate(bad):
+        r[i, 5 + 40 * i], y[4 + i, 7 + 50 * i], gate[8 + i, 9 + 60 * i] = value, value, value
+    w = [rnd(d, b=1.0) for _ in range(2)]
+    b = [rnd(d) for _ in range(2)]
+    up = lambda t: t.to(DEV)
+    desc = G.make_norm_desc(d, dtype, res, pre, post, 1e-5, 0.0, 0.7, 1.3, "linear")
+    weights = G.make_norm_weights(up(w[0]), up(b[0]), up(w[1]), up(b[1]))
+    ro, h = torch.empty(T, d, dtype=dts[res], device=DEV), torch.empty(T, d, dtype=dts[dtype], device=DEV)
+    G.griffin_norm_residual(desc, weights, up(r), ro, h, up(y), up(gate))
+    with np.errstate(all="ignore"):
+        want = L.norm_residual(f64(r), f64(y), f64(gate), pre, post, f64(w[0]), f64(b[0]), f64(w[1]), f64(b[1]), 1e-5, 0.0, 0.7, 1.3, "linear")
+    ulp = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+    for got, ref, kind in ((f64(ro), want[0], res), (f64(h), want[1], dtype)):
+        assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.array_equal(np.isinf(got), np.isinf(ref))
+        assert np.all(got[np.isinf(ref)] == ref[np.isinf(ref)]) and not np.all(np.isfinite(ref[[0, 1, 2, 4, 5, 6, 8, 9, 10]]))
+        # one rounding, and fp32 arithmetic relative to the row's largest entry (as the tests of finite rows have it)
+        fine = np.isfinite(ref)
+        size = np.abs(np.where(fine, ref, 0.0)).max(1, keepdims=True) + 1.0
+        err = np.abs(np.where(fine, got, 0.0) - np.where(fine, ref, 0.0))
+        assert np.all(err <= ulp[kind] * np.abs(np.where(fine, ref, 0.0)) * 1.01 + 64 * 2.0 ** -24 * size)
