@@ -17,14 +17,17 @@ constexpr int ATTN_MAX_GRID = 148;  // CTAs at most (one per SM of a B200)
 // Two blocks of a sequence's keys: 4 sequences of 16 tokens of 8 heads 11.7 / 14.6; 4 tokens, 32 heads over 8, 9000 keys (37 MB)
 // 20.9 / 21.8, 16000 (66 MB) 27.6 / 26.5; 16 tokens of 32 heads, 2600 keys (43 MB) 23.4 / 22.7.  Two blocks of a shared prefix: 2
 // sequences of 2 tokens, 16 heads over 4, 3000 tokens (6 MB) 12.4 / 14.9; 4 sequences, 32 over 8, 2048 (8 MB) 15.2 / 15.1.
+// The lengths are on the device, so the rule for two blocks goes by what the page table could hold: with tables that are as
+// long as the sequences, as they were for these figures, the limit is where the two kernels meet; with a table for a longer
+// context the tcgen05 kernel takes such calls earlier than it need.  (The limit for a prefix stands on these two calls alone.)
 constexpr long long FEW_OWN_TWICE = 36ll << 20, FEW_PREFIX_TWICE = 7ll << 20;   // bytes
 static bool attn_few(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
     const long long rows = (long long)batch->n_tokens * (desc->n_q_heads / desc->n_kv_heads), n = batch->n_seq;
     if (desc->dtype != GRIFFIN_DT_BF16 || desc->n_q_heads > 8 * desc->n_kv_heads || n * desc->n_kv_heads > 2 * ATTN_MAX_GRID) return false;
     const long long token = 4ll * desc->n_kv_heads * desc->head_dim, prefix = batch->prefix_len * token;
-    const long long own = n * batch->table_stride * desc->page_size * token;   // (at most: the lengths are on the device)
+    const double own = (double)n * batch->table_stride * desc->page_size * token;   // (what the table could hold; past 64 bits for the widest)
     if (n > 1 && prefix > 0 && rows > 8 && (rows > 16 || prefix > FEW_PREFIX_TWICE)) return false;
-    return rows <= 8 * n || (rows <= 16 * n && own + prefix <= FEW_OWN_TWICE);
+    return rows <= 8 * n || (rows <= 16 * n && own + (double)prefix <= (double)FEW_OWN_TWICE);
 }
 static AttnShape shape_of(const griffin_attn_desc *desc, bool few) {
     if (desc->dtype == GRIFFIN_DT_F32) return attn_simt_shape(desc->head_dim);
