@@ -1,7 +1,8 @@
 // Attention over the shared prefix and each sequence's own keys, bf16 storage, blocks of up to 8 query rows: single
 // tokens and a few drafted ones.  The mathematics is attn_tc.cu's:
 //   S = scale Q K^T, masked by place;  m' = max(m, max S);  P = 2^(S - m');
-//   l = l 2^(m - m') + sum P;  O = O 2^(m - m') + P V        (S in units of log2; fp32, P rounded to bf16 for P V)
+//   l = l 2^(m - m') + sum P;  O = O 2^(m - m') + P V        (S in units of log2; fp32, P rounded to bf16 for P V, whose
+//   two operands are of one type)
 //
 // With 8 rows the products fit the time of the keys' bytes even on the warp-level matrix instruction, so nothing is
 // gained by the 128-row tcgen05 tiles, and their long way to the first result (barriers, tensor memory, descriptors, a
@@ -15,8 +16,8 @@
 // (ldmatrix), V rows transposed (ldmatrix.trans), P^T is turned by movmatrix, the queries stay in registers.  16-byte
 // pieces of a row are placed at piece ^ (row mod 8), which keeps the loads free of bank conflicts.
 //
-// Measured, the joining kernel included: one sequence of 32 heads behind 20000 tokens (332 MB) 60.4 us, 5.5 TB/s, 0.84 of
-// the measured copy; behind 512 tokens (10 MB) 12.3 us, of which the bytes are 1.6: the launches, the schedule's loads, the
+// Measured, the joining kernel included: one sequence of 32 heads behind 20000 tokens (332 MB) 61.2 us, 5.4 TB/s, 0.83 of
+// the measured copy; behind 512 tokens (10 MB) 12.8 us, of which the bytes are 1.6: the launches, the schedule's loads, the
 // pages', the keys', and the partials' follow one another.
 #include "attn.h"
 #include "attn_join.cuh"

@@ -251,7 +251,7 @@ __device__ __forceinline__ void attn_scan(const AttnPlan &p, int *bases) {
 // block, written and read again.  With several jobs per CTA and none of them longer than a fair share, whole jobs are taken
 // from a queue, the longest of a sequence first: with one sequence that comes within a short job of even, with several
 // within the last sequence's longest.  Queue / cut shares, us a pass, 32 heads over 8: a 4096-token prompt 150 / 215, 8 of 2048
-// tokens 275 / 358, 64 of 256 106 / 171, 512 of 64 187 / 239.  Only fused calls: the others have partials to join anyway.
+// tokens 275 / 358, 64 of 256 110 / 171, 512 of 64 192 / 239.  Only fused calls: the others have partials to join anyway.
 __device__ __forceinline__ AttnTotals attn_totals(const AttnPlan &p, const int *bases) {
     AttnTotals t;
     t.W = bases[p.n_seq];

@@ -9,8 +9,8 @@
 // products, and their pages are looked up a tile ahead.  Keys and values behind what any row of the block sees are
 // read as zeros, whatever the cache holds there.
 //
-// Bound by latency: 5 steps behind 1003 shared tokens (16 heads over 4, 64 wide) take 12.7 us, half of them here and the
-// rest in the joining kernel; 1000 causal tokens of 8 heads over 2 take 72 us, 14 TFLOP/s of the 75 of the pipes.
+// Bound by latency: 5 steps behind 1003 shared tokens (16 heads over 4, 64 wide) take 13.0 us, half of them here and the
+// rest in the joining kernel; 1000 causal tokens of 8 heads over 2 take 73 us, 14 TFLOP/s of the 75 of the pipes.
 #include <type_traits>
 
 #include "attn.h"

@@ -10,7 +10,7 @@
 // same ones), while the data of all the tokens is on the way.
 //
 // Bound by memory where there is much of it: 4096 tokens of 32 query heads and 8 key heads of 128, bf16 (101 MB), take
-// 20.6 us, 4.9 TB/s, where a copy of the same bytes takes 16; 8 tokens of 40 heads take 2.0 us, the launch and the trips.
+// 20.7 us, 4.9 TB/s, where a copy of the same bytes takes 16; 8 tokens of 40 heads take 2.1 us, the launch and the trips.
 #include "common.cuh"
 #include "layer.h"
 #include "vec8.cuh"
