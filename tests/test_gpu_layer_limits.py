@@ -191,3 +191,18 @@ def test_norm_rows_that_are_not_finite(dtype, res, pre, post, d):
         size = np.abs(np.where(fine, ref, 0.0)).max(1, keepdims=True) + 1.0
         err = np.abs(np.where(fine, got, 0.0) - np.where(fine, ref, 0.0))
         assert np.all(err <= ulp[kind] * np.abs(np.where(fine, ref, 0.0)) * 1.01 + 64 * 2.0 ** -24 * size)
+
+
+@pytest.mark.parametrize("hq,hkv,hd", [(2, 1, 128), (2, 2, 256)])
+@pytest.mark.parametrize("n,prefix", [(330, 0), (360, 150), (1024, 40)])
+def test_attention_of_many_sequences_beside_a_smaller_ring(hq, hkv, hd, n, prefix):
+    # the list of the sequences' first tiles takes the room of one of the ring's five tiles
+    lens = [(17 * i) % 140 + 4 for i in range(n)]
+    b = Batch([(i % 3) + 1 for i in range(n)], lens, prefix, hq, hkv, hd, 64, "bf16").to_device()
+    out = b.attend()
+    assert G.griffin_check_device_status(b.ws) == G.OK and torch.isfinite(out).all()
+    rows = {0, 1, 2, 3, b.T // 2, b.T - 2, b.T - 1}
+    want, mass = b.reference(rows)
+    at = sorted(rows)
+    assert np.all(np.abs(f64(out)[at] - want[at]) <= b.bound(want, mass)[at])
+    assert torch.equal(b.attend(), out)
