@@ -144,6 +144,7 @@ def _quantise(x):
     ok = torch.isfinite(g).all(-1)
     m, e = torch.frexp(torch.where(ok, a, 0.0) / torch.full_like(a, 7.0))     # m in [1/2, 1)
     b = ((torch.round(m * 16) - 8).int() + 8 * (e - 1 + 21)).clamp(0, 254)    # (a mantissa rounded up to 16 goes on in the exponent)
+    b = torch.where(m > 0, b, 0)
     s = torch.ldexp(1 + (b % 8) / 8, b // 8 - 21)
     c = torch.round(torch.where(ok[..., None], g, 0.0) / s[..., None]).clamp(-7, 7).int() + 8
     w = c.flatten(-2).unflatten(-1, (-1, 4, 2))                               # [..., word, i, entry 2i or 2i + 1]
