@@ -474,6 +474,47 @@ griffin_status griffin_attn_prefix(const griffin_attn_desc *desc, const griffin_
                                    const griffin_kv_cache *cache, const void *q, int64_t ld_q, void *out, int64_t ld_out,
                                    void *workspace, size_t ws_bytes, void *stream);
 
+/* The same cache in 4 bits: what three and a half bf16 caches of tokens take.  16 consecutive entries of a head are a
+ * group with one scale:
+ *   s    = max |x| / 7 of the group rounded to 4 significant bits, held to [2^-21, 1792];
+ *   b    = 8 (e + 21) + m, the byte for s = 2^e (1 + m / 8); 255: an entry is not finite, and the group reads as NaN;
+ *   code = rint(x / s) held to [-7, 7], plus 8; it stands for (code - 8) s.
+ * No entry up to 12544 is off by more than s / 2; larger ones become 12544 at most.  The values are exact in bf16.
+ * Of the 8 entries in a 32-bit word, entry 2i has bits 4i .. 4i + 3, entry 2i + 1 the same bits of the upper half.  The
+ * part of a page that belongs to one head is at base + page * stride_page + head * stride_head (bytes, multiples of 16,
+ * >= 0) and griffin_kv_q4_block_bytes long: page_size * D / 2 bytes of codes, token by token, then
+ * page_size * 4 ceil(D / 64) bytes of scales, of which each token's last ones are not used where D / 16 is not a
+ * multiple of 4.  D must be a multiple of 16 (GRIFFIN_ERR_UNSUPPORTED). */
+typedef struct {
+    void *k, *v;
+    int32_t n_pages;
+    int64_t stride_page, stride_head;
+} griffin_kv_cache_q4;
+
+/* Bytes of one head's part of a page; 0 if desc is NULL or invalid, or D is not a multiple of 16. */
+size_t griffin_kv_q4_block_bytes(const griffin_attn_desc *desc);
+
+/* griffin_kv_append into such a cache: keys (behind their rotation, unrounded) and values are quantised as they are
+ * written, q goes to q_out in desc->dtype.  Same argument rules.  The rotation's products and sums, the quotients and
+ * their roundings are those of fp32, each by itself. */
+griffin_status griffin_kv_append_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
+                                    const griffin_kv_cache_q4 *cache, const griffin_rope *rope,
+                                    const void *q, int64_t ld_q, const void *k, int64_t ld_k, const void *v, int64_t ld_v,
+                                    void *q_out, int64_t ld_q_out, void *workspace, void *stream);
+
+/* The batch's tokens back out of the cache: row t of k and v [n_tokens, Hkv, D] (desc->dtype, ld_* as above) gets what the
+ * cache holds of token t, whose place is that of griffin_kv_append (so a batch of whole sequences, q_start counting their
+ * lengths, reads them whole; with prefix_pages as the page table of one sequence, the prefix).  Padding, and tokens that
+ * have no place (the status word is raised as there), read as zeros; rows of no sequence are left alone. */
+griffin_status griffin_kv_read_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch, const griffin_kv_cache_q4 *cache,
+                                  void *k, int64_t ld_k, void *v, int64_t ld_v, void *workspace, void *stream);
+
+/* griffin_attn_prefix over such a cache, with the same rules, limits and workspace (griffin_attn_workspace_bytes); what
+ * is said there of values that are not finite holds of groups that read as NaN. */
+griffin_status griffin_attn_prefix_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
+                                      const griffin_kv_cache_q4 *cache, const void *q, int64_t ld_q, void *out, int64_t ld_out,
+                                      void *workspace, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -100,3 +100,68 @@ def attention(q, k_pages, v_pages, q_start, seq_len, page_table, prefix_pages, p
             out[t, h] = p @ v[:, h // (hq // hkv)]
             mass[t, h] = p @ np.abs(v[:, h // (hq // hkv)])
     return out, mass
+
+
+# ---- a cache held in 4 bits --------------------------------------------------------------------------------------
+def q4_scale(group):
+    """Scale of 16 entries: max |x| / 7 to the nearest number of 4 significant bits (ties to even), in [2^-21, 1792]; NaN for a
+    group with an entry that is not finite."""
+    a = max(abs(float(x)) for x in group) if all(math.isfinite(x) for x in group) else math.nan
+    if not math.isfinite(a):
+        return math.nan
+    if a == 0:
+        return 2.0 ** -21
+    m, e = math.frexp(a / 7)                       # m in [1/2, 1); round() takes ties to even
+    return min(max(math.ldexp(round(m * 16), e - 4), 2.0 ** -21), 1792.0)
+
+
+def q4_codes(group, scale):
+    """Integers of -7 .. 7 that stand for the entries: the nearest multiples of the scale (ties to even)."""
+    return [max(-7, min(7, round(float(x) / scale))) for x in group]
+
+
+def q4_held(x):
+    """What an array [..., D] becomes in the cache."""
+    flat = np.asarray(x, np.float64).reshape(-1, 16)
+    out = np.empty_like(flat)
+    for i, g in enumerate(flat):
+        s = q4_scale(g)
+        out[i] = np.nan if math.isnan(s) else np.array(q4_codes(g, s)) * s
+    return out.reshape(np.shape(x))
+
+
+def q4_pack(head_rows):
+    """One head's part of a page: tokens [page, D] to bytes, codes first, then the scales (padded to 4 bytes a token)."""
+    rows = np.asarray(head_rows, np.float64)
+    page, d = rows.shape
+    codes, scales = np.zeros((page, d // 2), np.uint8), np.zeros((page, -(-d // 64) * 4), np.uint8)
+    for t in range(page):
+        nibbles = []
+        for g in range(d // 16):
+            x = rows[t, 16 * g:16 * g + 16]
+            s = q4_scale(x)
+            if math.isnan(s):
+                scales[t, g] = 255
+                nibbles += [8] * 16
+                continue
+            m, e = math.frexp(s)
+            scales[t, g] = 8 * (e - 1 + 21) + int(m * 16) - 8
+            nibbles += [c + 8 for c in q4_codes(x, s)]
+        for w in range(d // 8):                    # entry 2i: bits 4i .. 4i + 3; entry 2i + 1: those of the upper half
+            word = sum(nibbles[8 * w + 2 * i + half] << (4 * i + 16 * half) for i in range(4) for half in range(2))
+            codes[t, 4 * w:4 * w + 4] = list(word.to_bytes(4, "little"))
+    return np.concatenate((codes.ravel(), scales.ravel()))
+
+
+def q4_unpack(block, page, d):
+    """The values [page, D] that one head's part of a page stands for."""
+    block = np.asarray(block, np.uint8)
+    codes, scales = block[:page * d // 2].reshape(page, d // 2), block[page * d // 2:].reshape(page, -1)
+    out = np.empty((page, d))
+    for t in range(page):
+        for j in range(d):
+            word = int.from_bytes(bytes(codes[t, j // 8 * 4:j // 8 * 4 + 4]), "little")
+            b = int(scales[t, j // 16])
+            s = math.nan if b == 255 else 2.0 ** (b // 8 - 21) * (1 + b % 8 / 8)
+            out[t, j] = ((word >> (j % 8 // 2 * 4 + j % 2 * 16) & 15) - 8) * s
+    return out

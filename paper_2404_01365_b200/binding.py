@@ -43,6 +43,7 @@ EXPORTS = (
     "griffin_ff_decode_static", "griffin_ff_decode_indexed", "griffin_ff_prefill_score_chunk",
     "griffin_kernel_launches", "griffin_ff_decode_static_status", "griffin_compact_experts_nm",
     "griffin_norm_residual", "griffin_kv_append", "griffin_attn_workspace_bytes", "griffin_attn_prefix",
+    "griffin_kv_q4_block_bytes", "griffin_kv_append_q4", "griffin_kv_read_q4", "griffin_attn_prefix_q4",
 )
 
 
@@ -87,6 +88,11 @@ class KVCache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32)] + \
                [(n, C.c_int64) for n in ("stride_page", "stride_head", "stride_token")]
     _form = None     # (griffin_dtype, heads, page size, head width) of the tensors it was made of
+
+
+class KVCacheQ4(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32)] + [(n, C.c_int64) for n in ("stride_page", "stride_head")]
+    _form = None     # (heads, bytes of one head's part of a page) of the tensors it was made of
 
 
 class AttnBatch(C.Structure):
@@ -161,6 +167,16 @@ def load(path=None):
     lib.griffin_attn_prefix.restype = C.c_int
     lib.griffin_attn_prefix.argtypes = [C.POINTER(AttnDesc), C.POINTER(AttnBatch), C.POINTER(KVCache), vp, i64, vp, i64, vp, sz,
                                         vp]
+    lib.griffin_kv_q4_block_bytes.restype = sz
+    lib.griffin_kv_q4_block_bytes.argtypes = [C.POINTER(AttnDesc)]
+    lib.griffin_kv_append_q4.restype = C.c_int
+    lib.griffin_kv_append_q4.argtypes = [C.POINTER(AttnDesc), C.POINTER(AttnBatch), C.POINTER(KVCacheQ4), C.POINTER(Rope), vp, i64,
+                                         vp, i64, vp, i64, vp, i64, vp, vp]
+    lib.griffin_kv_read_q4.restype = C.c_int
+    lib.griffin_kv_read_q4.argtypes = [C.POINTER(AttnDesc), C.POINTER(AttnBatch), C.POINTER(KVCacheQ4), vp, i64, vp, i64, vp, vp]
+    lib.griffin_attn_prefix_q4.restype = C.c_int
+    lib.griffin_attn_prefix_q4.argtypes = [C.POINTER(AttnDesc), C.POINTER(AttnBatch), C.POINTER(KVCacheQ4), vp, i64, vp, i64, vp,
+                                           sz, vp]
     lib.griffin_check_device_status.restype = C.c_int
     lib.griffin_check_device_status.argtypes = [vp, vp]
     _lib = lib
@@ -449,8 +465,12 @@ def _check_cache(form, batch, cache):
     if cache._form != form and cache._form is not None:
         raise ValueError("cache: expected pages [{1}, {2}, {3}] of griffin_dtype {0}, got [{5}, {6}, {7}] of {4}"
                          .format(*form, *cache._form))
-    if batch._prefix_pages is not None and batch.prefix_len > batch._prefix_pages * form[2]:
-        raise ValueError(f"prefix_pages: {batch._prefix_pages} pages of {form[2]} tokens for a prefix of {batch.prefix_len}")
+    _check_prefix(batch, form[2])
+
+
+def _check_prefix(batch, page_size):
+    if batch._prefix_pages is not None and batch.prefix_len > batch._prefix_pages * page_size:
+        raise ValueError(f"prefix_pages: {batch._prefix_pages} pages of {page_size} tokens for a prefix of {batch.prefix_len}")
 
 
 def make_attn_batch(q_start, seq_len, page_table, n_tokens, prefix_pages=None, prefix_len=0):
@@ -526,3 +546,79 @@ def griffin_attn_prefix(desc, batch, cache, q, out, ws, stream=None):
                                     out.data_ptr(), _rows(out, n, hq, d, dt, "out"), ws.data_ptr(), ws.numel(), _stream(stream))
     if st != OK:
         raise GriffinError(st, "griffin_attn_prefix")
+
+
+# ---- the same cache in 4 bits ------------------------------------------------------------------------------------
+def griffin_kv_q4_block_bytes(desc):
+    """Bytes of one head's part of a page."""
+    return int(load().griffin_kv_q4_block_bytes(C.byref(desc)))
+
+
+def _q4_block(desc):
+    return desc.page_size * (desc.head_dim // 2 + (desc.head_dim + 63) // 64 * 4)
+
+
+def make_kv_cache_q4(k, v):
+    """A paged cache in 4 bits from two uint8 tensors [n_pages, n_kv_heads, griffin_kv_q4_block_bytes] of the same strides
+    (any, as long as the bytes of a head are consecutive)."""
+    if k.shape != v.shape or k.stride() != v.stride() or k.dim() != 3 or k.stride(2) != 1 or k.dtype != torch.uint8 or v.dtype != torch.uint8:
+        raise ValueError(f"k and v must be alike, uint8 [pages, heads, bytes]: got {k.dtype} {tuple(k.shape)} {k.stride()}, "
+                         f"{v.dtype} {tuple(v.shape)} {v.stride()}")
+    c = KVCacheQ4(_ptr(k), _ptr(v), k.shape[0], k.stride(0), k.stride(1))
+    c._keep = (k, v)
+    c._form = tuple(k.shape[1:])
+    return c
+
+
+def alloc_kv_cache_q4(desc, n_pages, device):
+    """A cache in 4 bits for the descriptor's heads and pages (torch owns the memory)."""
+    n = griffin_kv_q4_block_bytes(desc)
+    if n == 0:
+        raise GriffinError(ERR_INVALID_ARG, "griffin_kv_q4_block_bytes")
+    return make_kv_cache_q4(*(torch.empty((n_pages, desc.n_kv_heads, n), dtype=torch.uint8, device=device) for _ in range(2)))
+
+
+def _check_cache_q4(desc, batch, cache):
+    if cache._form is not None and cache._form != (desc.n_kv_heads, _q4_block(desc)):
+        raise ValueError(f"cache: expected pages [{desc.n_kv_heads}, {_q4_block(desc)}], got {list(cache._form)}")
+    _check_prefix(batch, desc.page_size)
+
+
+def griffin_kv_append_q4(desc, batch, cache, rope, q, k, v, q_out, ws=None, stream=None):
+    """griffin_kv_append into a cache in 4 bits: keys, rotated, and values are quantised as they are written."""
+    n, hq, hk, d, dt = batch.n_tokens, desc.n_q_heads, desc.n_kv_heads, desc.head_dim, desc.dtype
+    _check_cache_q4(desc, batch, cache)
+    q_p = o_p = None
+    ld_q = ld_o = 0
+    if q is not None:
+        ld_q, q_p = _rows(q, n, hq, d, dt, "q"), q.data_ptr()
+    if q_out is not None:
+        ld_o, o_p = _rows(q_out, n, hq, d, dt, "q_out"), q_out.data_ptr()
+    ld_k, ld_v = _rows(k, n, hk, d, dt, "k"), _rows(v, n, hk, d, dt, "v")
+    st = load().griffin_kv_append_q4(C.byref(desc), C.byref(batch), C.byref(cache), None if rope is None else C.byref(rope), q_p, ld_q,
+                                     k.data_ptr(), ld_k, v.data_ptr(), ld_v, o_p, ld_o, None if ws is None else ws.data_ptr(),
+                                     _stream(stream))
+    if st != OK:
+        raise GriffinError(st, "griffin_kv_append_q4")
+
+
+def griffin_kv_read_q4(desc, batch, cache, k, v, ws=None, stream=None):
+    """The batch's tokens out of a cache in 4 bits: k, v [n_tokens, n_kv_heads, head_dim] of the descriptor's dtype."""
+    n, hk, d, dt = batch.n_tokens, desc.n_kv_heads, desc.head_dim, desc.dtype
+    _check_cache_q4(desc, batch, cache)
+    ld_k, ld_v = _rows(k, n, hk, d, dt, "k"), _rows(v, n, hk, d, dt, "v")
+    st = load().griffin_kv_read_q4(C.byref(desc), C.byref(batch), C.byref(cache), k.data_ptr(), ld_k, v.data_ptr(), ld_v,
+                                   None if ws is None else ws.data_ptr(), _stream(stream))
+    if st != OK:
+        raise GriffinError(st, "griffin_kv_read_q4")
+
+
+def griffin_attn_prefix_q4(desc, batch, cache, q, out, ws, stream=None):
+    """griffin_attn_prefix over a cache in 4 bits."""
+    n, hq, d, dt = batch.n_tokens, desc.n_q_heads, desc.head_dim, desc.dtype
+    _check_cache_q4(desc, batch, cache)
+    ld_q, ld_o = _rows(q, n, hq, d, dt, "q"), _rows(out, n, hq, d, dt, "out")
+    st = load().griffin_attn_prefix_q4(C.byref(desc), C.byref(batch), C.byref(cache), q.data_ptr(), ld_q, out.data_ptr(), ld_o,
+                                       ws.data_ptr(), ws.numel(), _stream(stream))
+    if st != OK:
+        raise GriffinError(st, "griffin_attn_prefix_q4")

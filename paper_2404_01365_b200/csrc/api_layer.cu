@@ -3,6 +3,7 @@
 
 #include "common.cuh"
 #include "layer.h"
+#include "q4.cuh"
 
 using namespace griffin;
 
@@ -50,11 +51,52 @@ static griffin_status check_cache(const griffin_attn_desc *d, const griffin_kv_c
     return GRIFFIN_OK;
 }
 
+// A cache held in 4 bits: its groups are of 16 entries.
+static griffin_status check_cache_q4(const griffin_attn_desc *d, const griffin_kv_cache_q4 *c) {
+    if (c == nullptr || c->k == nullptr || c->v == nullptr || c->n_pages < 1) return GRIFFIN_ERR_INVALID_ARG;
+    if (d->head_dim % 16 != 0) return GRIFFIN_ERR_UNSUPPORTED;
+    if (c->stride_page < 0 || c->stride_head < 0) return GRIFFIN_ERR_INVALID_ARG;
+    if (c->stride_page % 16 != 0 || c->stride_head % 16 != 0 || !aligned16(c->k) || !aligned16(c->v)) return GRIFFIN_ERR_ALIGNMENT;
+    return GRIFFIN_OK;
+}
+
 // A matrix of n rows of `width` entries, `ld` apart.
 static griffin_status check_rows(const void *p, int64_t ld, int64_t width, int dtype) {
     if (ld < width) return GRIFFIN_ERR_INVALID_ARG;
     if (!aligned16(p) || ld % (16 / elem_bytes(dtype)) != 0) return GRIFFIN_ERR_ALIGNMENT;
     return GRIFFIN_OK;
+}
+
+// What an append is given beside the descriptor, the batch and the cache.
+static griffin_status check_append(const griffin_attn_desc *desc, const griffin_rope *rope, const void *q, int64_t ld_q, const void *k,
+                                   int64_t ld_k, const void *v, int64_t ld_v, const void *q_out, int64_t ld_q_out, const void *workspace) {
+    if (k == nullptr || v == nullptr || (q == nullptr) != (q_out == nullptr)) return GRIFFIN_ERR_INVALID_ARG;
+    if (rope != nullptr) {
+        if (rope->table == nullptr || rope->n_pos < 1 || rope->rot_dim < 16 || rope->rot_dim > desc->head_dim) return GRIFFIN_ERR_INVALID_ARG;
+        if (rope->style != GRIFFIN_ROPE_HALF && rope->style != GRIFFIN_ROPE_PAIRS) return GRIFFIN_ERR_UNSUPPORTED;
+        if (rope->rot_dim % 16 != 0 || !aligned16(rope->table)) return GRIFFIN_ERR_ALIGNMENT;
+    }
+    const int64_t wq = (int64_t)desc->n_q_heads * desc->head_dim, wk = (int64_t)desc->n_kv_heads * desc->head_dim;
+    griffin_status st = GRIFFIN_OK;
+    if (q != nullptr) st = check_rows(q, ld_q, wq, desc->dtype);
+    if (st == GRIFFIN_OK && q != nullptr) st = check_rows(q_out, ld_q_out, wq, desc->dtype);
+    if (st == GRIFFIN_OK) st = check_rows(k, ld_k, wk, desc->dtype);
+    if (st == GRIFFIN_OK) st = check_rows(v, ld_v, wk, desc->dtype);
+    if (st == GRIFFIN_OK && !aligned16(workspace)) st = GRIFFIN_ERR_ALIGNMENT;
+    return st;
+}
+
+// What attention is given beside them.
+static griffin_status check_attn(const griffin_attn_desc *desc, const griffin_attn_batch *batch, const void *q, int64_t ld_q,
+                                 const void *out, int64_t ld_out, const void *workspace, size_t ws_bytes) {
+    if (q == nullptr || out == nullptr) return GRIFFIN_ERR_INVALID_ARG;
+    const int64_t wq = (int64_t)desc->n_q_heads * desc->head_dim;
+    griffin_status st = check_rows(q, ld_q, wq, desc->dtype);
+    if (st == GRIFFIN_OK) st = check_rows(out, ld_out, wq, desc->dtype);
+    if (st != GRIFFIN_OK) return st;
+    if (workspace == nullptr) return GRIFFIN_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return GRIFFIN_ERR_ALIGNMENT;
+    return ws_bytes < attn_ws_bytes(desc, batch->n_tokens, batch->n_seq) ? GRIFFIN_ERR_WORKSPACE : GRIFFIN_OK;
 }
 
 extern "C" {
@@ -93,18 +135,7 @@ griffin_status griffin_kv_append(const griffin_attn_desc *desc, const griffin_at
     if (st == GRIFFIN_OK) st = check_batch(batch);
     if (st == GRIFFIN_OK) st = check_cache(desc, cache);
     if (st != GRIFFIN_OK) return st;
-    if (k == nullptr || v == nullptr || (q == nullptr) != (q_out == nullptr)) return GRIFFIN_ERR_INVALID_ARG;
-    if (rope != nullptr) {
-        if (rope->table == nullptr || rope->n_pos < 1 || rope->rot_dim < 16 || rope->rot_dim > desc->head_dim) return GRIFFIN_ERR_INVALID_ARG;
-        if (rope->style != GRIFFIN_ROPE_HALF && rope->style != GRIFFIN_ROPE_PAIRS) return GRIFFIN_ERR_UNSUPPORTED;
-        if (rope->rot_dim % 16 != 0 || !aligned16(rope->table)) return GRIFFIN_ERR_ALIGNMENT;
-    }
-    const int64_t wq = (int64_t)desc->n_q_heads * desc->head_dim, wk = (int64_t)desc->n_kv_heads * desc->head_dim;
-    if (q != nullptr) st = check_rows(q, ld_q, wq, desc->dtype);
-    if (st == GRIFFIN_OK && q != nullptr) st = check_rows(q_out, ld_q_out, wq, desc->dtype);
-    if (st == GRIFFIN_OK) st = check_rows(k, ld_k, wk, desc->dtype);
-    if (st == GRIFFIN_OK) st = check_rows(v, ld_v, wk, desc->dtype);
-    if (st == GRIFFIN_OK && !aligned16(workspace)) st = GRIFFIN_ERR_ALIGNMENT;
+    st = check_append(desc, rope, q, ld_q, k, ld_k, v, ld_v, q_out, ld_q_out, workspace);
     if (st != GRIFFIN_OK || batch->n_tokens == 0) return st;
     return launch_kv_append(desc, batch, cache, rope, q, ld_q, k, ld_k, v, ld_v, q_out, ld_q_out, workspace,
                             static_cast<cudaStream_t>(stream));
@@ -122,17 +153,55 @@ griffin_status griffin_attn_prefix(const griffin_attn_desc *desc, const griffin_
     if (st == GRIFFIN_OK) st = check_batch(batch);
     if (st == GRIFFIN_OK) st = check_cache(desc, cache);
     if (st != GRIFFIN_OK) return st;
-    if (q == nullptr || out == nullptr) return GRIFFIN_ERR_INVALID_ARG;
-    const int64_t wq = (int64_t)desc->n_q_heads * desc->head_dim;
-    st = check_rows(q, ld_q, wq, desc->dtype);
-    if (st == GRIFFIN_OK) st = check_rows(out, ld_out, wq, desc->dtype);
-    if (st != GRIFFIN_OK) return st;
-    if (workspace == nullptr) return GRIFFIN_ERR_WORKSPACE;
-    if (!aligned16(workspace)) return GRIFFIN_ERR_ALIGNMENT;
-    if (ws_bytes < attn_ws_bytes(desc, batch->n_tokens, batch->n_seq)) return GRIFFIN_ERR_WORKSPACE;
-    if (batch->n_tokens == 0) return GRIFFIN_OK;
+    st = check_attn(desc, batch, q, ld_q, out, ld_out, workspace, ws_bytes);
+    if (st != GRIFFIN_OK || batch->n_tokens == 0) return st;
     return launch_attn_prefix(desc, batch, cache, q, ld_q, out, ld_out, scratch_of(workspace), workspace,
                               static_cast<cudaStream_t>(stream));
+}
+
+size_t griffin_kv_q4_block_bytes(const griffin_attn_desc *desc) {
+    if (check_attn_desc(desc) != GRIFFIN_OK || desc->head_dim % 16 != 0) return 0;
+    return (size_t)q4_block_bytes(desc->head_dim, desc->page_size);
+}
+
+griffin_status griffin_kv_append_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
+                                    const griffin_kv_cache_q4 *cache, const griffin_rope *rope,
+                                    const void *q, int64_t ld_q, const void *k, int64_t ld_k, const void *v, int64_t ld_v,
+                                    void *q_out, int64_t ld_q_out, void *workspace, void *stream) {
+    griffin_status st = check_attn_desc(desc);
+    if (st == GRIFFIN_OK) st = check_batch(batch);
+    if (st == GRIFFIN_OK) st = check_cache_q4(desc, cache);
+    if (st == GRIFFIN_OK) st = check_append(desc, rope, q, ld_q, k, ld_k, v, ld_v, q_out, ld_q_out, workspace);
+    if (st != GRIFFIN_OK || batch->n_tokens == 0) return st;
+    return launch_kv_append_q4(desc, batch, cache, rope, q, ld_q, k, ld_k, v, ld_v, q_out, ld_q_out, workspace,
+                               static_cast<cudaStream_t>(stream));
+}
+
+griffin_status griffin_kv_read_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch, const griffin_kv_cache_q4 *cache,
+                                  void *k, int64_t ld_k, void *v, int64_t ld_v, void *workspace, void *stream) {
+    griffin_status st = check_attn_desc(desc);
+    if (st == GRIFFIN_OK) st = check_batch(batch);
+    if (st == GRIFFIN_OK) st = check_cache_q4(desc, cache);
+    if (st != GRIFFIN_OK) return st;
+    if (k == nullptr || v == nullptr) return GRIFFIN_ERR_INVALID_ARG;
+    const int64_t wk = (int64_t)desc->n_kv_heads * desc->head_dim;
+    st = check_rows(k, ld_k, wk, desc->dtype);
+    if (st == GRIFFIN_OK) st = check_rows(v, ld_v, wk, desc->dtype);
+    if (st == GRIFFIN_OK && !aligned16(workspace)) st = GRIFFIN_ERR_ALIGNMENT;
+    if (st != GRIFFIN_OK || batch->n_tokens == 0) return st;
+    return launch_kv_read_q4(desc, batch, cache, k, ld_k, v, ld_v, workspace, static_cast<cudaStream_t>(stream));
+}
+
+griffin_status griffin_attn_prefix_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
+                                      const griffin_kv_cache_q4 *cache, const void *q, int64_t ld_q, void *out, int64_t ld_out,
+                                      void *workspace, size_t ws_bytes, void *stream) {
+    griffin_status st = check_attn_desc(desc);
+    if (st == GRIFFIN_OK) st = check_batch(batch);
+    if (st == GRIFFIN_OK) st = check_cache_q4(desc, cache);
+    if (st == GRIFFIN_OK) st = check_attn(desc, batch, q, ld_q, out, ld_out, workspace, ws_bytes);
+    if (st != GRIFFIN_OK || batch->n_tokens == 0) return st;
+    return launch_attn_prefix_q4(desc, batch, cache, q, ld_q, out, ld_out, scratch_of(workspace), workspace,
+                                 static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -57,18 +57,16 @@ size_t attn_scratch_bytes(const griffin_attn_desc *desc, int n_tokens, int n_seq
     return a > b ? a : b;
 }
 
-griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
-                                  const griffin_kv_cache *cache, const void *q, int64_t ld_q, void *out, int64_t ld_out,
-                                  uint8_t *scratch, void *ws, cudaStream_t stream) {
+static griffin_status launch(const griffin_attn_desc *desc, const griffin_attn_batch *batch, const AttnData &x, int n_pages, bool few,
+                             bool q4, uint8_t *scratch, void *ws, cudaStream_t stream) {
     const int sms = device_sm_count();
     if (sms <= 0) return GRIFFIN_ERR_CUDA;
-    const bool few = attn_few(desc, batch);
     const AttnShape sh = shape_of(desc, few);
     AttnPlan p{};
     p.q_start = batch->q_start; p.seq_len = batch->seq_len; p.page_table = batch->page_table;
     p.prefix_pages = batch->prefix_pages;
     p.n_seq = batch->n_seq; p.n_tokens = batch->n_tokens; p.table_stride = batch->table_stride;
-    p.prefix_len = batch->prefix_len; p.n_pages = cache->n_pages;
+    p.prefix_len = batch->prefix_len; p.n_pages = n_pages;
     while ((1 << p.page_shift) < desc->page_size) ++p.page_shift;
     p.hq = desc->n_q_heads; p.hkv = desc->n_kv_heads; p.group = p.hq / p.hkv;
     p.group_inv = (65536u + p.group - 1) / p.group;
@@ -95,11 +93,25 @@ griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_a
     p.cta = reinterpret_cast<float *>(scratch + s.cta_off);
     p.own_rows = s.own_rows;
     p.cta_rows = 2 * sh.tile_rows;
-    const AttnData x{q, cache->k, cache->v, out, ld_q, ld_out, cache->stride_page, cache->stride_head, cache->stride_token};
-    const griffin_status st = desc->dtype == GRIFFIN_DT_F32 ? launch_attn_simt(p, x, stream)
+    const griffin_status st = desc->dtype == GRIFFIN_DT_F32 ? launch_attn_simt(p, x, q4, stream)
                               : few                         ? launch_attn_few(p, x, stream)
-                                                            : launch_attn_tc(p, x, stream);
-    return st != GRIFFIN_OK ? st : launch_attn_join(p, desc->dtype, out, ld_out, stream);
+                                                            : launch_attn_tc(p, x, q4, stream);
+    return st != GRIFFIN_OK ? st : launch_attn_join(p, desc->dtype, x.out, x.ld_out, stream);
+}
+
+griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
+                                  const griffin_kv_cache *cache, const void *q, int64_t ld_q, void *out, int64_t ld_out,
+                                  uint8_t *scratch, void *ws, cudaStream_t stream) {
+    const AttnData x{q, cache->k, cache->v, out, ld_q, ld_out, cache->stride_page, cache->stride_head, cache->stride_token, {}};
+    return launch(desc, batch, x, cache->n_pages, attn_few(desc, batch), false, scratch, ws, stream);
+}
+
+griffin_status launch_attn_prefix_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
+                                     const griffin_kv_cache_q4 *cache, const void *q, int64_t ld_q, void *out, int64_t ld_out,
+                                     uint8_t *scratch, void *ws, cudaStream_t stream) {
+    const AttnData x{q, cache->k, cache->v, out, ld_q, ld_out, cache->stride_page, cache->stride_head, 0,
+                     q4_layout(desc->head_dim, desc->page_size)};
+    return launch(desc, batch, x, cache->n_pages, false, true, scratch, ws, stream);
 }
 
 }  // namespace griffin

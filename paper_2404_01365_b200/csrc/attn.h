@@ -3,13 +3,15 @@
 
 #include "attn_plan.cuh"
 #include "layer.h"
+#include "q4.cuh"
 
 namespace griffin {
 
 struct AttnData {
     const void *q, *k, *v;
     void *out;
-    long long ld_q, ld_out, stride_page, stride_head, stride_token;
+    long long ld_q, ld_out, stride_page, stride_head, stride_token;   // of a cache held in 4 bits: in bytes
+    Q4Layout q4;
 };
 
 // How a kernel cuts its work (see attn_plan.cuh).
@@ -74,8 +76,8 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there
 AttnShape attn_simt_shape(int head_dim);
 AttnShape attn_tc_shape(int head_dim);
 AttnShape attn_few_shape(int head_dim);
-griffin_status launch_attn_tc(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // bf16
+griffin_status launch_attn_tc(const AttnPlan &plan, const AttnData &data, bool q4, cudaStream_t stream);  // bf16; q4: the cache in 4 bits
 griffin_status launch_attn_few(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // bf16, few rows
-griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // fp32
+griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, bool q4, cudaStream_t stream);  // fp32; q4: the cache in 4 bits
 
 }  // namespace griffin

@@ -37,16 +37,20 @@
 
 namespace griffin {
 
-constexpr int ATC_THREADS = 384, ATC_ROWS = 128;
+constexpr int ATC_ROWS = 128;
 constexpr float ATC_SLACK = 8.f;  // how far (log2) the true maximum may run ahead of the one P is scaled by
 
-template <int DP> struct AtcCfg {
+template <int DP, bool Q4> struct AtcCfg {
     static constexpr int KT = DP == 256 ? 64 : 128;       // keys per tile
     static constexpr int NS = DP == 256 ? 1 : 2;          // O accumulators
+    static constexpr int UNPACK_WARP = NS == 2 ? 12 : 8;  // behind the softmax warps: first of the four that unpack (Q4)
+    static constexpr int THREADS = Q4 && NS == 2 ? 512 : 384;
     static constexpr int CB = DP / 64;                    // 64-entry column blocks (128 swizzled bytes per row)
     static constexpr int Q_BYTES = ATC_ROWS * DP * 2, KV_BYTES = KT * DP * 2;
     static constexpr int O_COL = 2 * KT;                  // TMEM columns: S/P 0, S/P 1, O (0, 1)
     static constexpr int MAX_SLOTS = DP == 64 ? 10 : 5;
+    // a tile of the cache in 4 bits, as it lies: units of 32 entries of a key (16 bytes and two scales), PASSES to a thread
+    static constexpr int UNITS = DP / 32, PASSES = KT * UNITS / 128, RAW_STAGES = Q4 ? 3 : 0, RAW_BYTES = PASSES * 128 * 18;
 };
 constexpr int ATC_BARS = 2 * 10 + 10 + 4 + 6 + 2 * 4 + 2;  // kv full/empty, v_ok, q full/empty, s_full, p_ready, o_full, seg full/empty, seg wanted
 
@@ -57,8 +61,9 @@ struct AtcParams {
     AttnPlan plan;
     void *out;
     long long ld_out;
-    const __nv_bfloat16 *v;
+    const void *k, *v;
     long long stride_page, stride_head, stride_token;
+    Q4Layout q4;
     int n_slots, box_rows, q_box_bytes;
 };
 
@@ -111,6 +116,10 @@ __device__ __forceinline__ void store_8f(float *to, const float *v) {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_proxy_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+template <int BYTES> __device__ __forceinline__ void copy_small(uint32_t dst, const void *src, bool there) {   // 4 or 8
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(there ? BYTES : 0) : "memory");
+}
 
 __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
@@ -223,7 +232,7 @@ __device__ __forceinline__ KeyTile key_tile(const AttnPlan &p, const Segment &s,
 // The values that the value warp has set to zero in this segment's tiles because they are not finite and not every row
 // of the block sees their keys: added to the rows that do (whatever P, the sum is what P times them gives).  A thread has a
 // row of `lanes`' accumulator at `to`; own_seen: the row's own tokens; 0: none.
-template <int DP>
+template <int DP, bool Q4>
 static __device__ __noinline__ void add_not_finite(const AtcParams &prm, const Segment &s, int own_seen, uint32_t to) {
     const AttnPlan &p = prm.plan;
     const int first = max(s.t0 - s.pre_tiles, 0) << p.kt_shift, last = max(s.t0 + s.n - s.pre_tiles, 0) << p.kt_shift;
@@ -236,7 +245,19 @@ static __device__ __noinline__ void add_not_finite(const AtcParams &prm, const S
         for (int k = k0; k < k1; ++k) {
             const int page = __ldg(p.page_table + (long long)s.seq * p.table_stride + (k >> p.page_shift));
             if (page < 0 || page >= p.n_pages) continue;
-            const uint4 *const v = reinterpret_cast<const uint4 *>(prm.v + page * prm.stride_page + s.head * prm.stride_head +
+            if constexpr (Q4) {
+                const uint8_t *const scales = static_cast<const uint8_t *>(prm.v) + page * prm.stride_page + s.head * prm.stride_head +
+                                              prm.q4.scale_off + (k & ((1 << p.page_shift) - 1)) * prm.q4.scale_row + c / 16;
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+                    if (c + 16 * g < p.d && __ldg(scales + g) == Q4_NAN) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[16 * g + i] = __uint_as_float(0x7fffffffu);
+                    }
+                continue;
+            }
+            const uint4 *const v = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(prm.v) + page * prm.stride_page +
+                                                                   s.head * prm.stride_head +
                                                                    (k & ((1 << p.page_shift) - 1)) * prm.stride_token + c);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -287,10 +308,118 @@ struct SegReader {
     }
 };
 
-template <int DP>
-__global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_constant__ AtcMaps maps,
+// The four warps that bring a cache held in 4 bits (q4.cuh) into the ring as bf16.  A thread has units of 32 entries of a key:
+// it asks for them by cp.async, RAW_STAGES - 1 tiles ahead, into shared memory of its own, and writes them out as four
+// 16-byte pieces of the tile (128-byte swizzle), in an order that keeps the eight threads of a phase on different banks.
+template <int DP> struct Unpacker {
+    using Cfg = AtcCfg<DP, true>;
+    static constexpr int UNITS = Cfg::UNITS, PASSES = Cfg::PASSES, KT = Cfg::KT, STAGES = Cfg::RAW_STAGES;
+    const AtcParams &prm;
+    uint8_t *tiles;              // the ring
+    uint32_t raw;                // this thread's 16 bytes of the first pass, first stage
+    uint32_t raw_scale;          // its two scales
+    int row, q, turn;            // first key, unit of the key; what the pieces' order is turned by
+    bool whole, upper;           // both groups of the unit are the head's; the pieces' halves change places
+    uint32_t there = 0;          // by stage asked for, the latest in the last bits: passes whose keys exist
+    int in = 0, out = 0, n = 0;  // stages: next to be asked for, next to be unpacked, how many are between
+
+    __device__ __forceinline__ Unpacker(const AtcParams &prm_, uint8_t *tiles_, uint8_t *raw_) : prm(prm_), tiles(tiles_) {
+        const int tid = threadIdx.x & 127;
+        row = tid / UNITS;
+        q = tid % UNITS;
+        raw = smem_u32(raw_) + tid * 16;
+        raw_scale = smem_u32(raw_) + PASSES * 2048 + tid * 2;
+        whole = q * 32 + 16 < prm.plan.d;
+        const int x = DP == 128 ? (q >> 1) * 2 : DP == 256 ? q >> 1 : 0;   // order of the pieces: j ^ x
+        upper = (x & 2) != 0;
+        turn = x ^ (row & 7) ^ ((q & 1) * 4);
+    }
+    // this thread's pages of a tile (-1: no key)
+    __device__ __forceinline__ void pages(const int *list, int k0, int len, int (&page)[PASSES]) const {
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int key = k0 + row + i * (128 / UNITS);
+            page[i] = key < len ? __ldg(list + (key >> prm.plan.page_shift)) : -1;
+        }
+    }
+    __device__ __forceinline__ void ask(int which, int head, int k0, int len, const int (&page)[PASSES]) {
+        const AttnPlan &p = prm.plan;
+        const uint8_t *const base = static_cast<const uint8_t *>(which ? prm.v : prm.k) + head * prm.stride_head;
+        uint32_t mask = 0;
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int key = k0 + row + i * (128 / UNITS), slot = key & ((1 << p.page_shift) - 1);
+            const bool ok = (unsigned)page[i] < (unsigned)p.n_pages, on = ok && q * 32 < p.d;
+            if (key < len && !ok) attn_bad(p.ws, 42);
+            const uint8_t *const block = base + (on ? page[i] * prm.stride_page : 0);
+            const uint8_t *const codes = on ? block + slot * prm.q4.code_row + q * 16 : base;
+            const uint32_t to = raw + in * Cfg::RAW_BYTES + i * 2048;
+            if ((p.d & 31) == 0) {
+                copy16(to, codes, on);
+            } else {   // (rows of codes are on 8-byte boundaries)
+                copy_small<8>(to, codes, on);
+                copy_small<8>(to + 8, on && whole ? codes + 8 : base, on && whole);
+            }
+            if ((q & 1) == 0)
+                copy_small<4>(raw_scale + in * Cfg::RAW_BYTES + i * 256, on ? block + prm.q4.scale_off + slot * prm.q4.scale_row + q * 2 : base, on);
+            mask |= (on ? 1u : 0u) << i;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        there = there << 4 | mask;
+        in = in + 1 == STAGES ? 0 : in + 1;
+        ++n;
+    }
+    // The oldest stage into a tile of the ring; all but `behind` of the groups of copies have to be there.
+    __device__ __forceinline__ void unpack(uint32_t slot) {
+        uint8_t *const tile = tiles + slot * Cfg::KV_BYTES + (q >> 1) * (KT * 128) + row * 128;
+        const uint32_t mask = there >> (4 * (n - 1));
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const uint32_t at = raw + out * Cfg::RAW_BYTES + i * 2048;
+            uint32_t w[4], b;
+            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(upper ? at + 8 : at) : "memory");
+            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[2]), "=r"(w[3]) : "r"(upper ? at : at + 8) : "memory");
+            asm volatile("ld.shared.u16 %0, [%1];" : "=r"(b) : "r"(raw_scale + out * Cfg::RAW_BYTES + i * 256) : "memory");
+            uint32_t b0 = b & 255u, b1 = b >> 8;
+            if (upper) {
+                const uint32_t t = b0;
+                b0 = b1;
+                b1 = t;
+            }
+            if (!whole || !(mask >> i & 1u)) {   // (the second group of a unit may be beyond the head's width)
+                const bool on = mask >> i & 1u;
+                if (!on || upper) w[0] = w[1] = Q4_ZEROS, b0 = 0;
+                if (!on || !upper) w[2] = w[3] = Q4_ZEROS, b1 = 0;
+            }
+            const uint32_t h0 = q4_scale_bits(b0), h1 = q4_scale_bits(b1);
+            const Q4Scale2 s[2] = {q4_scale2(h0, h0), q4_scale2(h1, h1)};
+            if (DP == 256 && (turn ^ row ^ (q & 1) * 4) & 1) {   // (words within the halves)
+                uint32_t t = w[0];
+                w[0] = w[1];
+                w[1] = t;
+                t = w[2];
+                w[2] = w[3];
+                w[3] = t;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint4 v;
+                v.x = q4_pair(w[j], 0, s[j >> 1]);
+                v.y = q4_pair(w[j], 1, s[j >> 1]);
+                v.z = q4_pair(w[j], 2, s[j >> 1]);
+                v.w = q4_pair(w[j], 3, s[j >> 1]);
+                *reinterpret_cast<uint4 *>(tile + i * (128 / UNITS) * 128 + ((j ^ turn) << 4)) = v;
+            }
+        }
+        out = out + 1 == STAGES ? 0 : out + 1;
+        --n;
+    }
+};
+
+template <int DP, bool Q4>
+__global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(const __grid_constant__ AtcMaps maps,
                                                               const __grid_constant__ AtcParams prm) {
-    using Cfg = AtcCfg<DP>;
+    using Cfg = AtcCfg<DP, Q4>;
     constexpr int KT = Cfg::KT, NS = Cfg::NS, CB = Cfg::CB;
     const AttnPlan &p = prm.plan;
     extern __shared__ uint8_t smem_raw[];
@@ -298,7 +427,8 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
     uint8_t *const s_q = base;                                  // NS query tiles
     uint8_t *const s_kv = base + NS * Cfg::Q_BYTES;             // ring of key and value tiles
     const int n_slots = prm.n_slots;
-    uint64_t *const bars = reinterpret_cast<uint64_t *>(s_kv + n_slots * Cfg::KV_BYTES);
+    uint8_t *const s_raw = s_kv + n_slots * Cfg::KV_BYTES;      // what the unpacking warps have asked for
+    uint64_t *const bars = reinterpret_cast<uint64_t *>(s_raw + Cfg::RAW_STAGES * Cfg::RAW_BYTES);
     uint64_t *const kv_full = bars, *const kv_empty = bars + 10, *const v_ok = bars + 20, *const q_full = bars + 30,
                    *const q_empty = bars + 32, *const s_full = bars + 34, *const p_ready = bars + 36, *const o_full = bars + 38,
                    *const seg_full = bars + 40, *const seg_empty = bars + 44, *const seg_want = bars + 48;
@@ -310,10 +440,10 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_launch_dependents();
-    if (tid < 3) prefetch_tensormap(tid == 0 ? &maps.q : tid == 1 ? &maps.k : &maps.v);
+    if (tid < (Q4 ? 1 : 3)) prefetch_tensormap(tid == 0 ? &maps.q : tid == 1 ? &maps.k : &maps.v);
     if (tid == 0) {
         for (int i = 0; i < n_slots; ++i) {
-            mbar_init(&kv_full[i], 1);
+            mbar_init(&kv_full[i], Q4 ? 4 : 1);   // the copies' producer, or the warps that unpack
             mbar_init(&kv_empty[i], 2);   // the products that read it, and the value warp
             mbar_init(&v_ok[i], 1);
         }
@@ -326,7 +456,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
         }
         for (int i = 0; i < ATC_SEGS; ++i) {
             mbar_init(&seg_full[i], 1);
-            mbar_init(&seg_empty[i], 3 + 4 * NS);  // producer, issuer, value warp, softmax warps
+            mbar_init(&seg_empty[i], 3 + 4 * NS + (Q4 ? 4 : 0));  // producer, issuer, value warp, softmax warps, unpacking warps
         }
         mbar_init(seg_want, 1);
         *abort = 0;
@@ -351,7 +481,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
         Ring kv{0, 0};
         bool ok = true;
         const int per_tile = KT / prm.box_rows;  // boxes per 64-entry block
-        if (lane == 0) mbar_arrive(seg_want);
+        if (!Q4 && lane == 0) mbar_arrive(seg_want);
         while (ok && (ok = seg.take(w, abort, p.ws, 49)) && w.n > 0) {
             const int q_tiles = NS == 2 && !w.alt ? 2 : 1;
             for (int r = 0; r < q_tiles && ok; ++r, ++nq) {
@@ -364,7 +494,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                                     w.tok0 + r * p.tile_tokens, &q_full[b]);
                 }
             }
-            for (int t = 0; t < w.n && ok; ++t) {
+            for (int t = 0; !Q4 && t < w.n && ok; ++t) {
                 const KeyTile k = key_tile(p, w, w.t0 + t);
                 const int *const pages = k.prefix ? p.prefix_pages : p.page_table + (long long)w.seq * p.table_stride;
                 for (int which = 0; which < 2; ++which) {
@@ -392,7 +522,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                     ++kv_n;
                 }
             }
-            if (lane == 0) mbar_arrive(seg_want);
+            if (!Q4 && lane == 0) mbar_arrive(seg_want);
         }
         // stay until every copy that was started has landed
         if (lane == 0) {
@@ -521,7 +651,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                         fence_proxy_async_smem();
                     }
                 }
-                if (valid < KT) {
+                if (!Q4 && valid < KT) {   // (what is unpacked has zeros there)
 #pragma unroll 1
                     for (int i = lane; i < (KT - valid) * 8 * CB; i += 32) {
                         const int c = i % CB, r = valid + i / CB / 8, e = i / CB % 8;
@@ -590,7 +720,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                 if (more) j = attn_next(p, bases, j);
             }
         }
-    } else if (warp >= 4 && (NS == 2 || warp < 8)) {
+    } else if (warp >= 4 && warp < Cfg::UNPACK_WARP) {
         // ---------------- softmax ----------------
         const uint32_t grp = (warp - 4) >> 2;
         const int wr = (warp & 3) * 32;                            // the group's rows of this warp: wr .. wr + 31
@@ -699,7 +829,7 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
                 if (ok && warp_on) {
                     tc_fence_after_sync();
                     const uint32_t to = lanes + Cfg::O_COL + (NS == 2 ? grp : 0) * DP;
-                    if (marks[at_seg % ATC_MARKS] != 0) add_not_finite<DP>(prm, j, valid ? own_seen : 0, to);
+                    if (marks[at_seg % ATC_MARKS] != 0) add_not_finite<DP, Q4>(prm, j, valid ? own_seen : 0, to);
                     if (j.direct) {
                         const float inv = m == -INFINITY ? 0.f : 1.0f / l;
                         __nv_bfloat16 *const dst = static_cast<__nv_bfloat16 *>(prm.out) + (j.tok0 + tok) * prm.ld_out +
@@ -748,6 +878,59 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
         }
     }
 
+    if constexpr (Q4) {
+        if (warp >= Cfg::UNPACK_WARP && warp < Cfg::UNPACK_WARP + 4) {
+            // ---------------- the cache in 4 bits: unpacked into the ring ----------------
+            Unpacker<DP> u(prm, s_kv, s_raw);
+            Segment w;
+            Ring kv{0, 0};
+            uint32_t kv_n = 0;
+            bool ok = true;
+            const auto unpack = [&](bool last) {
+                if (kv_n >= (uint32_t)n_slots && !warp_wait(&kv_empty[kv.slot], kv.parity ^ 1u, abort, p.ws, 51)) return false;
+                if (last) asm volatile("cp.async.wait_group 0;" ::: "memory");
+                else asm volatile("cp.async.wait_group %0;" ::"n"(Cfg::RAW_STAGES - 1) : "memory");
+                __syncwarp();   // (scales come by fours)
+                u.unpack(kv.slot);
+                fence_proxy_async_smem();
+                __syncwarp();   // (and the stage may be filled again)
+                if (lane == 0) mbar_arrive(&kv_full[kv.slot]);
+                kv.step(1, n_slots);
+                ++kv_n;
+                return true;
+            };
+            const auto drain = [&] {
+                while (ok && u.n > 0) ok = unpack(true);
+            };
+            const bool asks = warp == Cfg::UNPACK_WARP && lane == 0;   // for the next segment
+            if (asks) mbar_arrive(seg_want);
+            for (;;) {
+                if (!__all_sync(0xffffffffu, mbar_try_wait(&seg_full[seg.slot], seg.parity))) drain();   // (nothing to be asked for meanwhile)
+                if (!ok || !(ok = seg.take(w, abort, p.ws, 49)) || w.n == 0) break;
+                int page[Cfg::PASSES], next[Cfg::PASSES];
+                KeyTile k = key_tile(p, w, w.t0);
+                const auto list = [&](const KeyTile &t) { return t.prefix ? p.prefix_pages : p.page_table + (long long)w.seq * p.table_stride; };
+                u.pages(list(k), k.k0, k.len, page);
+#pragma unroll 1
+                for (int t = 0; t < w.n && ok; ++t) {
+                    const KeyTile after = key_tile(p, w, w.t0 + min(t + 1, w.n - 1));
+                    u.pages(list(after), after.k0, after.len, next);
+                    if (asks && t == max(w.n - 2, 0)) mbar_arrive(seg_want);
+#pragma unroll 1
+                    for (int which = 0; which < 2 && ok; ++which) {
+                        u.ask(which, w.head, k.k0, k.len, page);
+                        if (u.n == Cfg::RAW_STAGES) ok = unpack(false);
+                    }
+                    k = after;
+#pragma unroll
+                    for (int i = 0; i < Cfg::PASSES; ++i) page[i] = next[i];
+                }
+            }
+            drain();
+            asm volatile("cp.async.wait_all;" ::: "memory");
+        }
+    }
+
     // ---------------- teardown: everybody meets, the allocating warp frees TMEM ----------------
     tc_fence_before_sync();
     __syncthreads();
@@ -757,14 +940,16 @@ __global__ void __launch_bounds__(ATC_THREADS, 1) attn_tc_kernel(const __grid_co
     }
 }
 
-template <int DP> static griffin_status launch_dp(const AttnPlan &plan, const AttnData &x, cudaStream_t stream) {
-    using Cfg = AtcCfg<DP>;
+template <int DP, bool Q4> static griffin_status launch_dp(const AttnPlan &plan, const AttnData &x, cudaStream_t stream) {
+    using Cfg = AtcCfg<DP, Q4>;
     AtcMaps maps;
     AtcParams prm{};
     prm.plan = plan;
     prm.out = x.out;
     prm.ld_out = x.ld_out;
-    prm.v = static_cast<const __nv_bfloat16 *>(x.v);
+    prm.k = x.k;
+    prm.v = x.v;
+    prm.q4 = x.q4;
     prm.stride_page = x.stride_page; prm.stride_head = x.stride_head; prm.stride_token = x.stride_token;
     const int page = 1 << plan.page_shift;
     prm.box_rows = page < Cfg::KT ? page : Cfg::KT;
@@ -780,7 +965,7 @@ template <int DP> static griffin_status launch_dp(const AttnPlan &plan, const At
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return GRIFFIN_ERR_CUDA;
     }
-    for (int which = 0; which < 2; ++which) {
+    for (int which = 0; !Q4 && which < 2; ++which) {
         const cuuint64_t dims[4] = {(cuuint64_t)plan.d, (cuuint64_t)page, (cuuint64_t)plan.hkv, (cuuint64_t)plan.n_pages};
         const cuuint64_t strides[3] = {(cuuint64_t)x.stride_token * 2, (cuuint64_t)x.stride_head * 2, (cuuint64_t)x.stride_page * 2};
         const cuuint32_t box[4] = {64, (cuuint32_t)prm.box_rows, 1, 1}, ones[4] = {1, 1, 1, 1};
@@ -790,26 +975,29 @@ template <int DP> static griffin_status launch_dp(const AttnPlan &plan, const At
             return GRIFFIN_ERR_UNSUPPORTED;  // (strides that the copy engine does not take)
     }
     // as many ring slots as fit beside the list of the sequences' first tiles
-    const size_t tail = ATC_BARS * 8 + ATC_SEGS * sizeof(Segment) + 8 + ATC_MARKS * 4 + ((size_t)plan.n_seq + 3) * 4, fixed = 1024 + Cfg::NS * Cfg::Q_BYTES + tail;
+    const size_t tail = ATC_BARS * 8 + ATC_SEGS * sizeof(Segment) + 8 + ATC_MARKS * 4 + ((size_t)plan.n_seq + 3) * 4, fixed = 1024 + Cfg::NS * Cfg::Q_BYTES + Cfg::RAW_STAGES * Cfg::RAW_BYTES + tail;
     prm.n_slots = (int)((232448 - fixed) / Cfg::KV_BYTES);
     if (prm.n_slots > Cfg::MAX_SLOTS) prm.n_slots = Cfg::MAX_SLOTS;
     const size_t smem = fixed + (size_t)prm.n_slots * Cfg::KV_BYTES;
-    const void *fn = reinterpret_cast<const void *>(attn_tc_kernel<DP>);
+    const void *fn = reinterpret_cast<const void *>(attn_tc_kernel<DP, Q4>);
     if (ensure_dynamic_smem(fn, smem) != cudaSuccess) return GRIFFIN_ERR_CUDA;
     void *args[] = {&maps, &prm};
-    return launch_maybe_overlapped(fn, dim3(plan.grid), dim3(ATC_THREADS), smem, stream, true, args) == cudaSuccess
+    return launch_maybe_overlapped(fn, dim3(plan.grid), dim3(Cfg::THREADS), smem, stream, true, args) == cudaSuccess
                ? GRIFFIN_OK
                : GRIFFIN_ERR_CUDA;
 }
 
 AttnShape attn_tc_shape(int head_dim) {
-    return head_dim > 128 ? AttnShape{ATC_ROWS, 1, AtcCfg<256>::KT, 0} : AttnShape{ATC_ROWS, 2, AtcCfg<128>::KT, 1};
+    return head_dim > 128 ? AttnShape{ATC_ROWS, 1, AtcCfg<256, false>::KT, 0} : AttnShape{ATC_ROWS, 2, AtcCfg<128, false>::KT, 1};
 }
 
-griffin_status launch_attn_tc(const AttnPlan &plan, const AttnData &data, cudaStream_t stream) {
-    if (plan.d <= 64) return launch_dp<64>(plan, data, stream);
-    if (plan.d <= 128) return launch_dp<128>(plan, data, stream);
-    return launch_dp<256>(plan, data, stream);
+template <bool Q4> static griffin_status launch_q4(const AttnPlan &plan, const AttnData &data, cudaStream_t stream) {
+    if (plan.d <= 64) return launch_dp<64, Q4>(plan, data, stream);
+    if (plan.d <= 128) return launch_dp<128, Q4>(plan, data, stream);
+    return launch_dp<256, Q4>(plan, data, stream);
+}
+griffin_status launch_attn_tc(const AttnPlan &plan, const AttnData &data, bool q4, cudaStream_t stream) {
+    return q4 ? launch_q4<true>(plan, data, stream) : launch_q4<false>(plan, data, stream);
 }
 
 }  // namespace griffin
