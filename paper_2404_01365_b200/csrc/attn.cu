@@ -29,9 +29,16 @@ static bool attn_few(const griffin_attn_desc *desc, const griffin_attn_batch *ba
     if (n > 1 && prefix > 0 && rows > 8 && (rows > 16 || prefix > FEW_PREFIX_TWICE)) return false;
     return rows <= 8 * n || (rows <= 16 * n && own + (double)prefix <= (double)FEW_OWN_TWICE);
 }
-static AttnShape shape_of(const griffin_attn_desc *desc, bool few) {
+// The same over a cache held in 4 bits (attn_few_q4.cu).
+static bool attn_few_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
+    const long long rows = (long long)batch->n_tokens * (desc->n_q_heads / desc->n_kv_heads), n = batch->n_seq;
+    if (desc->dtype != GRIFFIN_DT_BF16 || desc->n_q_heads > 8 * desc->n_kv_heads) return false;
+    if (n > 1 && batch->prefix_len > 0 && rows > 16) return false;
+    return rows <= 16 * n;
+}
+static AttnShape shape_of(const griffin_attn_desc *desc, bool few, bool q4) {
     if (desc->dtype == GRIFFIN_DT_F32) return attn_simt_shape(desc->head_dim);
-    return few ? attn_few_shape(desc->head_dim) : attn_tc_shape(desc->head_dim);
+    return !few ? attn_tc_shape(desc->head_dim) : q4 ? attn_few_q4_shape(desc->head_dim) : attn_few_shape(desc->head_dim);
 }
 
 struct AttnScratch {
@@ -52,8 +59,9 @@ static AttnScratch attn_scratch(const griffin_attn_desc *desc, const AttnShape &
     return s;
 }
 
+// (the two kernels for few rows have the same scratch)
 size_t attn_scratch_bytes(const griffin_attn_desc *desc, int n_tokens, int n_seq) {
-    const size_t a = attn_scratch(desc, shape_of(desc, false), n_tokens, n_seq).total, b = attn_scratch(desc, shape_of(desc, true), n_tokens, n_seq).total;
+    const size_t a = attn_scratch(desc, shape_of(desc, false, false), n_tokens, n_seq).total, b = attn_scratch(desc, shape_of(desc, true, false), n_tokens, n_seq).total;
     return a > b ? a : b;
 }
 
@@ -61,7 +69,7 @@ static griffin_status launch(const griffin_attn_desc *desc, const griffin_attn_b
                              bool q4, uint8_t *scratch, void *ws, cudaStream_t stream) {
     const int sms = device_sm_count();
     if (sms <= 0) return GRIFFIN_ERR_CUDA;
-    const AttnShape sh = shape_of(desc, few);
+    const AttnShape sh = shape_of(desc, few, q4);
     AttnPlan p{};
     p.q_start = batch->q_start; p.seq_len = batch->seq_len; p.page_table = batch->page_table;
     p.prefix_pages = batch->prefix_pages;
@@ -94,6 +102,7 @@ static griffin_status launch(const griffin_attn_desc *desc, const griffin_attn_b
     p.own_rows = s.own_rows;
     p.cta_rows = 2 * sh.tile_rows;
     const griffin_status st = desc->dtype == GRIFFIN_DT_F32 ? launch_attn_simt(p, x, q4, stream)
+                              : few && q4                   ? launch_attn_few_q4(p, x, stream)
                               : few                         ? launch_attn_few(p, x, stream)
                                                             : launch_attn_tc(p, x, q4, stream);
     return st != GRIFFIN_OK ? st : launch_attn_join(p, desc->dtype, x.out, x.ld_out, stream);
@@ -111,7 +120,7 @@ griffin_status launch_attn_prefix_q4(const griffin_attn_desc *desc, const griffi
                                      uint8_t *scratch, void *ws, cudaStream_t stream) {
     const AttnData x{q, cache->k, cache->v, out, ld_q, ld_out, cache->stride_page, cache->stride_head, 0,
                      q4_layout(desc->head_dim, desc->page_size)};
-    return launch(desc, batch, x, cache->n_pages, false, true, scratch, ws, stream);
+    return launch(desc, batch, x, cache->n_pages, attn_few_q4(desc, batch), true, scratch, ws, stream);
 }
 
 }  // namespace griffin

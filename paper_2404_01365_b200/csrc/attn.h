@@ -76,8 +76,10 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there
 AttnShape attn_simt_shape(int head_dim);
 AttnShape attn_tc_shape(int head_dim);
 AttnShape attn_few_shape(int head_dim);
+AttnShape attn_few_q4_shape(int head_dim);
 griffin_status launch_attn_tc(const AttnPlan &plan, const AttnData &data, bool q4, cudaStream_t stream);  // bf16; q4: the cache in 4 bits
 griffin_status launch_attn_few(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // bf16, few rows
+griffin_status launch_attn_few_q4(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // and the cache in 4 bits
 griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, bool q4, cudaStream_t stream);  // fp32; q4: the cache in 4 bits
 
 }  // namespace griffin

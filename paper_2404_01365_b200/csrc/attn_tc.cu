@@ -404,10 +404,10 @@ template <int DP> struct Unpacker {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 uint4 v;
-                v.x = q4_pair(w[j], 0, s[j >> 1]);
-                v.y = q4_pair(w[j], 1, s[j >> 1]);
-                v.z = q4_pair(w[j], 2, s[j >> 1]);
-                v.w = q4_pair(w[j], 3, s[j >> 1]);
+                v.x = q4_pair(w[j], 0, s[j >> 1], prm.q4.magic);
+                v.y = q4_pair(w[j], 1, s[j >> 1], prm.q4.magic);
+                v.z = q4_pair(w[j], 2, s[j >> 1], prm.q4.magic);
+                v.w = q4_pair(w[j], 3, s[j >> 1], prm.q4.magic);
                 *reinterpret_cast<uint4 *>(tile + i * (128 / UNITS) * 128 + ((j ^ turn) << 4)) = v;
             }
         }

@@ -20,8 +20,12 @@ namespace griffin {
 // Bytes of one head's part of a page.
 struct Q4Layout {
     int code_row, scale_row, scale_off;   // a token's codes, a token's scales, where the scales begin
+    uint32_t magic;                       // Q4_MAGIC, for q4_pair
 };
-__host__ __device__ inline Q4Layout q4_layout(int d, int page_size) { return {d / 2, (d + 63) / 64 * 4, page_size * (d / 2)}; }
+constexpr uint32_t Q4_MAGIC = 0x43004300u;   // 128 as bf16, twice
+__host__ __device__ inline Q4Layout q4_layout(int d, int page_size) {
+    return {d / 2, (d + 63) / 64 * 4, page_size * (d / 2), Q4_MAGIC};
+}
 __host__ __device__ inline long long q4_block_bytes(int d, int page_size) {
     return (long long)page_size * (d / 2 + (d + 63) / 64 * 4);
 }
@@ -57,9 +61,13 @@ __device__ __forceinline__ Q4Scale2 q4_scale2(uint32_t lo, uint32_t hi) {   // t
     return {s, q4_mul2(s, 0xc308c308u)};   // -136
 }
 // Entries 2i and 2i + 1 of a word as bf16, i = 0 .. 3: the code in the last bits of 128's mantissa is 128 + code, and
-// (128 + code) s - 136 s is exact.
-__device__ __forceinline__ uint32_t q4_pair(uint32_t w, int i, Q4Scale2 s) {
-    return q4_fma2(((w >> (4 * i)) & 0x000f000fu) | 0x43004300u, s.s, s.off);
+// (128 + code) s - 136 s is exact.  A shift, a logical instruction, an fma.  (The magic number is an argument of the kernel,
+// Q4Layout::magic: as a constant it would be an immediate like the mask, of which an instruction takes one, and the logical
+// instruction became two; they are half of what a kernel that unpacks issues to the integer pipe.)
+__device__ __forceinline__ uint32_t q4_pair(uint32_t w, int i, Q4Scale2 s, uint32_t magic) {
+    uint32_t x;
+    asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xEA;" : "=r"(x) : "r"(w >> (4 * i)), "r"(magic));   // (a & b) | c
+    return q4_fma2(x, s.s, s.off);
 }
 
 // 16 entries to two words of codes and the scale's byte.
