@@ -29,12 +29,26 @@ static bool attn_few(const griffin_attn_desc *desc, const griffin_attn_batch *ba
     if (n > 1 && prefix > 0 && rows > 8 && (rows > 16 || prefix > FEW_PREFIX_TWICE)) return false;
     return rows <= 8 * n || (rows <= 16 * n && own + (double)prefix <= (double)FEW_OWN_TWICE);
 }
-// The same over a cache held in 4 bits (attn_few_q4.cu).
+// The same over a cache held in 4 bits (attn_few_q4.cu).  That kernel unpacks the keys once for every 8 rows, at about 4 TB/s
+// of a bf16 cache's bytes; the tcgen05 one unpacks them once for up to 256, and a job that ends costs it as much as two of its tiles.
+// Both sides, us a pass, few / tcgen05, 128-wide heads unless said otherwise.  Up to 16 rows of a sequence: 1 sequence, 8 key
+// heads, 2000 keys 14.8 / 16.3, 8000 21.2 / 23.0; 16 sequences of 8000 keys 82.7 / 133; 64 of 2000 89 / 169; 48 with 4 rows and
+// 2560 keys 48 / 126.  32 rows: 1 sequence, 300 keys 12.9 / 16.1, 2000 16.8 / 16.3; 16 of 2000 50.6 / 51.8, of 8000 146 / 138.  64 rows: 300 keys 13.3
+// / 17.8, 2000 20.1 / 17.0.  So from 16 rows on only what is a tile or two for every warp stays here.
+// A shared prefix, whose rows are the whole call's, under 8 key heads: 24 rows of 6 sequences, 2000 keys 16.7 / 18.8, 8000 26.2 / 25.4, of 24
+// sequences 24.9 / 30.7; 48 of 6, 2000 23.6 / 19.8; 64 of 16, 2000 22.1 / 21.0; 128 of 32, 300 19.5 / 21.3, 2000 31.2 / 26.3.
+// Under 2 key heads: 64 rows of 8, 2000 15.9 / 17.7, 8000 24.5 / 20.4.  256 wide, 20 rows of 20 sequences, 16 key heads, 4000 38 / 57.
+// (The sequences' lengths are on the device; what the page table could hold stands for them.)
+constexpr double FQ_FEW_KEYS = 72000, FQ_KEYS_PER_SEQ = 800, FQ_KEYS_PER_CALL = 24000;
 static bool attn_few_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
-    const long long rows = (long long)batch->n_tokens * (desc->n_q_heads / desc->n_kv_heads), n = batch->n_seq;
-    if (desc->dtype != GRIFFIN_DT_BF16 || desc->n_q_heads > 8 * desc->n_kv_heads) return false;
-    if (n > 1 && batch->prefix_len > 0 && rows > 16) return false;
-    return rows <= 16 * n;
+    const int group = desc->n_q_heads / desc->n_kv_heads;
+    if (desc->dtype != GRIFFIN_DT_BF16 || group > 8) return false;
+    const long long rows = (long long)batch->n_tokens * group, n = batch->n_seq;
+    const double blocks = (double)((rows + 7) / 8), prefix = batch->prefix_len, room = (double)batch->table_stride * desc->page_size;
+    const double hkv = desc->n_kv_heads, width = desc->head_dim / 128.0;
+    if (blocks * hkv * (prefix + room) * width <= FQ_FEW_KEYS) return true;
+    if (rows > 16 * n) return false;
+    return n == 1 || (blocks - 1) * prefix * width <= FQ_KEYS_PER_SEQ * n + FQ_KEYS_PER_CALL / hkv;
 }
 static AttnShape shape_of(const griffin_attn_desc *desc, bool few, bool q4) {
     if (desc->dtype == GRIFFIN_DT_F32) return attn_simt_shape(desc->head_dim);
@@ -65,11 +79,8 @@ size_t attn_scratch_bytes(const griffin_attn_desc *desc, int n_tokens, int n_seq
     return a > b ? a : b;
 }
 
-static griffin_status launch(const griffin_attn_desc *desc, const griffin_attn_batch *batch, const AttnData &x, int n_pages, bool few,
-                             bool q4, uint8_t *scratch, void *ws, cudaStream_t stream) {
-    const int sms = device_sm_count();
-    if (sms <= 0) return GRIFFIN_ERR_CUDA;
-    const AttnShape sh = shape_of(desc, few, q4);
+static AttnPlan make_plan(const griffin_attn_desc *desc, const griffin_attn_batch *batch, int n_pages, int sms, const AttnShape &sh,
+                          uint8_t *scratch, void *ws) {
     AttnPlan p{};
     p.q_start = batch->q_start; p.seq_len = batch->seq_len; p.page_table = batch->page_table;
     p.prefix_pages = batch->prefix_pages;
@@ -91,7 +102,7 @@ static griffin_status launch(const griffin_attn_desc *desc, const griffin_attn_b
     p.grid = sms < ATTN_MAX_GRID ? sms : ATTN_MAX_GRID;
     p.scale_log2 = desc->scale * 1.4426950408889634f;
     p.ws = ws;
-    p.may_queue = p.fused && desc->dtype == GRIFFIN_DT_BF16 && !few;
+    p.may_queue = p.fused && desc->dtype == GRIFFIN_DT_BF16 && sh.tiles_per_block * sh.tile_rows >= 128;   // (attn_tc.cu)
     p.queue = &static_cast<WsHeader *>(ws)->queue_attn;
     const AttnScratch s = attn_scratch(desc, sh, p.n_tokens, p.n_seq);
     p.bases = reinterpret_cast<int *>(scratch);
@@ -101,10 +112,17 @@ static griffin_status launch(const griffin_attn_desc *desc, const griffin_attn_b
     p.cta = reinterpret_cast<float *>(scratch + s.cta_off);
     p.own_rows = s.own_rows;
     p.cta_rows = 2 * sh.tile_rows;
-    const griffin_status st = desc->dtype == GRIFFIN_DT_F32 ? launch_attn_simt(p, x, q4, stream)
-                              : few && q4                   ? launch_attn_few_q4(p, x, stream)
-                              : few                         ? launch_attn_few(p, x, stream)
-                                                            : launch_attn_tc(p, x, q4, stream);
+    return p;
+}
+
+static griffin_status launch(const griffin_attn_desc *desc, const griffin_attn_batch *batch, const AttnData &x, int n_pages, bool few, bool q4, uint8_t *scratch, void *ws, cudaStream_t stream) {
+    const int sms = device_sm_count();
+    if (sms <= 0) return GRIFFIN_ERR_CUDA;
+    const AttnPlan p = make_plan(desc, batch, n_pages, sms, shape_of(desc, few, q4), scratch, ws);
+    const griffin_status st = desc->dtype == GRIFFIN_DT_F32          ? launch_attn_simt(p, x, q4, stream)
+                              : !few                                  ? launch_attn_tc(p, x, q4, stream)
+                              : q4                                   ? launch_attn_few_q4(p, x, stream)
+                                                                     : launch_attn_few(p, x, stream);
     return st != GRIFFIN_OK ? st : launch_attn_join(p, desc->dtype, x.out, x.ld_out, stream);
 }
 

@@ -40,6 +40,8 @@ namespace griffin {
 constexpr int ATC_ROWS = 128;
 constexpr float ATC_SLACK = 8.f;  // how far (log2) the true maximum may run ahead of the one P is scaled by
 
+constexpr int ATC_BARS = 2 * 10 + 10 + 4 + 6 + 2 * 4 + 2;  // kv full/empty, v_ok, q full/empty, s_full, p_ready, o_full, seg full/empty, seg wanted
+
 template <int DP, bool Q4> struct AtcCfg {
     static constexpr int KT = DP == 256 ? 64 : 128;       // keys per tile
     static constexpr int NS = DP == 256 ? 1 : 2;          // O accumulators
@@ -49,10 +51,11 @@ template <int DP, bool Q4> struct AtcCfg {
     static constexpr int Q_BYTES = ATC_ROWS * DP * 2, KV_BYTES = KT * DP * 2;
     static constexpr int O_COL = 2 * KT;                  // TMEM columns: S/P 0, S/P 1, O (0, 1)
     static constexpr int MAX_SLOTS = DP == 64 ? 10 : 5;
-    // a tile of the cache in 4 bits, as it lies: units of 32 entries of a key (16 bytes and two scales), PASSES to a thread
-    static constexpr int UNITS = DP / 32, PASSES = KT * UNITS / 128, RAW_STAGES = Q4 ? 3 : 0, RAW_BYTES = PASSES * 128 * 18;
+    // a tile of the cache in 4 bits, as it lies: codes, scales, a note; unpacked in units of 32 entries of a key, PASSES to a thread
+    static constexpr int UNITS = DP / 32, PASSES = KT * UNITS / 128, RAW_STAGES = Q4 ? 3 : 0;
+    static constexpr int RAW_SCALES = KT * DP / 2, RAW_NOTE = RAW_SCALES + KT * DP / 16, RAW_BYTES = RAW_NOTE + 128;
+    static constexpr int BARS = ATC_BARS + 2 * RAW_STAGES;   // and raw full/empty
 };
-constexpr int ATC_BARS = 2 * 10 + 10 + 4 + 6 + 2 * 4 + 2;  // kv full/empty, v_ok, q full/empty, s_full, p_ready, o_full, seg full/empty, seg wanted
 
 struct AtcMaps {
     CUtensorMap q, k, v;
@@ -116,10 +119,6 @@ __device__ __forceinline__ void store_8f(float *to, const float *v) {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_proxy_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-template <int BYTES> __device__ __forceinline__ void copy_small(uint32_t dst, const void *src, bool there) {   // 4 or 8
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(there ? BYTES : 0) : "memory");
-}
 
 __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
@@ -308,113 +307,85 @@ struct SegReader {
     }
 };
 
-// The four warps that bring a cache held in 4 bits (q4.cuh) into the ring as bf16.  A thread has units of 32 entries of a key:
-// it asks for them by cp.async, RAW_STAGES - 1 tiles ahead, into shared memory of its own, and writes them out as four
-// 16-byte pieces of the tile (128-byte swizzle), in an order that keeps the eight threads of a phase on different banks.
-template <int DP> struct Unpacker {
-    using Cfg = AtcCfg<DP, true>;
-    static constexpr int UNITS = Cfg::UNITS, PASSES = Cfg::PASSES, KT = Cfg::KT, STAGES = Cfg::RAW_STAGES;
-    const AtcParams &prm;
-    uint8_t *tiles;              // the ring
-    uint32_t raw;                // this thread's 16 bytes of the first pass, first stage
-    uint32_t raw_scale;          // its two scales
-    int row, q, turn;            // first key, unit of the key; what the pieces' order is turned by
-    bool whole, upper;           // both groups of the unit are the head's; the pieces' halves change places
-    uint32_t there = 0;          // by stage asked for, the latest in the last bits: passes whose keys exist
-    int in = 0, out = 0, n = 0;  // stages: next to be asked for, next to be unpacked, how many are between
-
-    __device__ __forceinline__ Unpacker(const AtcParams &prm_, uint8_t *tiles_, uint8_t *raw_) : prm(prm_), tiles(tiles_) {
-        const int tid = threadIdx.x & 127;
-        row = tid / UNITS;
-        q = tid % UNITS;
-        raw = smem_u32(raw_) + tid * 16;
-        raw_scale = smem_u32(raw_) + PASSES * 2048 + tid * 2;
-        whole = q * 32 + 16 < prm.plan.d;
-        const int x = DP == 128 ? (q >> 1) * 2 : DP == 256 ? q >> 1 : 0;   // order of the pieces: j ^ x
-        upper = (x & 2) != 0;
-        turn = x ^ (row & 7) ^ ((q & 1) * 4);
-    }
-    // this thread's pages of a tile (-1: no key)
-    __device__ __forceinline__ void pages(const int *list, int k0, int len, int (&page)[PASSES]) const {
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-            const int key = k0 + row + i * (128 / UNITS);
-            page[i] = key < len ? __ldg(list + (key >> prm.plan.page_shift)) : -1;
-        }
-    }
-    __device__ __forceinline__ void ask(int which, int head, int k0, int len, const int (&page)[PASSES]) {
-        const AttnPlan &p = prm.plan;
-        const uint8_t *const base = static_cast<const uint8_t *>(which ? prm.v : prm.k) + head * prm.stride_head;
-        uint32_t mask = 0;
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-            const int key = k0 + row + i * (128 / UNITS), slot = key & ((1 << p.page_shift) - 1);
-            const bool ok = (unsigned)page[i] < (unsigned)p.n_pages, on = ok && q * 32 < p.d;
-            if (key < len && !ok) attn_bad(p.ws, 42);
-            const uint8_t *const block = base + (on ? page[i] * prm.stride_page : 0);
-            const uint8_t *const codes = on ? block + slot * prm.q4.code_row + q * 16 : base;
-            const uint32_t to = raw + in * Cfg::RAW_BYTES + i * 2048;
-            if ((p.d & 31) == 0) {
-                copy16(to, codes, on);
-            } else {   // (rows of codes are on 8-byte boundaries)
-                copy_small<8>(to, codes, on);
-                copy_small<8>(to + 8, on && whole ? codes + 8 : base, on && whole);
-            }
-            if ((q & 1) == 0)
-                copy_small<4>(raw_scale + in * Cfg::RAW_BYTES + i * 256, on ? block + prm.q4.scale_off + slot * prm.q4.scale_row + q * 2 : base, on);
-            mask |= (on ? 1u : 0u) << i;
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        there = there << 4 | mask;
-        in = in + 1 == STAGES ? 0 : in + 1;
-        ++n;
-    }
-    // The oldest stage into a tile of the ring; all but `behind` of the groups of copies have to be there.
-    __device__ __forceinline__ void unpack(uint32_t slot) {
-        uint8_t *const tile = tiles + slot * Cfg::KV_BYTES + (q >> 1) * (KT * 128) + row * 128;
-        const uint32_t mask = there >> (4 * (n - 1));
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-            const uint32_t at = raw + out * Cfg::RAW_BYTES + i * 2048;
-            uint32_t w[4], b;
-            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(upper ? at + 8 : at) : "memory");
-            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[2]), "=r"(w[3]) : "r"(upper ? at : at + 8) : "memory");
-            asm volatile("ld.shared.u16 %0, [%1];" : "=r"(b) : "r"(raw_scale + out * Cfg::RAW_BYTES + i * 256) : "memory");
-            uint32_t b0 = b & 255u, b1 = b >> 8;
-            if (upper) {
-                const uint32_t t = b0;
-                b0 = b1;
-                b1 = t;
-            }
-            if (!whole || !(mask >> i & 1u)) {   // (the second group of a unit may be beyond the head's width)
-                const bool on = mask >> i & 1u;
-                if (!on || upper) w[0] = w[1] = Q4_ZEROS, b0 = 0;
-                if (!on || !upper) w[2] = w[3] = Q4_ZEROS, b1 = 0;
-            }
-            const uint32_t h0 = q4_scale_bits(b0), h1 = q4_scale_bits(b1);
-            const Q4Scale2 s[2] = {q4_scale2(h0, h0), q4_scale2(h1, h1)};
-            if (DP == 256 && (turn ^ row ^ (q & 1) * 4) & 1) {   // (words within the halves)
-                uint32_t t = w[0];
-                w[0] = w[1];
-                w[1] = t;
-                t = w[2];
-                w[2] = w[3];
-                w[3] = t;
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint4 v;
-                v.x = q4_pair(w[j], 0, s[j >> 1], prm.q4.magic);
-                v.y = q4_pair(w[j], 1, s[j >> 1], prm.q4.magic);
-                v.z = q4_pair(w[j], 2, s[j >> 1], prm.q4.magic);
-                v.w = q4_pair(w[j], 3, s[j >> 1], prm.q4.magic);
-                *reinterpret_cast<uint4 *>(tile + i * (128 / UNITS) * 128 + ((j ^ turn) << 4)) = v;
-            }
-        }
-        out = out + 1 == STAGES ? 0 : out + 1;
-        --n;
-    }
+// A tile of a cache held in 4 bits (q4.cuh) comes by bulk copies as it lies, page by page, and four warps write it out as bf16
+// into the ring.  With it comes a note of what is not there.  Behind the last key, and beyond the head's width, they write what happens to
+// lie there: it is a number, whatever the bits, and meets P = 0, or a logit that is masked, or a query's zeros, or no output.
+struct __align__(16) RawNote {
+    int valid;      // keys; < 0: there are no more tiles
+    uint32_t boxes; // bit i: the page with the i-th box_rows of them is one
 };
+// Groups that are NaN, for which unpack_tile has written numbers, and keys of pages that are none, which read as zeros.
+template <int DP>
+static __device__ __noinline__ void unpack_rest(const AtcParams &prm, RawNote note, const uint8_t *raw, uint8_t *tile, int block, int row0, int half) {
+    using Cfg = AtcCfg<DP, true>;
+    constexpr int ROWS = 128 / Cfg::UNITS;
+    const int box_shift = 31 - __clz(prm.box_rows), q = block * 2 + half;
+#pragma unroll 1
+    for (int i = 0; i < Cfg::PASSES; ++i) {
+        const int row = row0 + i * ROWS;
+        const bool there = (note.boxes >> (row >> box_shift) & 1u) != 0;
+#pragma unroll 1
+        for (int j = 0; j < 4; ++j) {
+            const int group = q * 2 + (j >> 1);
+            uint32_t v = 0;
+            if (row >= note.valid || group * 16 >= prm.plan.d) continue;
+            if (there) {
+                if (raw[Cfg::RAW_SCALES + row * prm.q4.scale_row + group] != Q4_NAN) continue;
+                v = 0x7fff7fffu;
+            }
+            *reinterpret_cast<uint4 *>(tile + block * (Cfg::KT * 128) + row * 128 + ((j ^ (half * 4) ^ (row & 7)) << 4)) = make_uint4(v, v, v, v);
+        }
+    }
+}
+// A thread has units of 32 entries.  Eight neighbours, which store at once, have the two halves of a 64-entry block of four
+// keys: with the swizzle by the key's number that meets all banks.
+template <int DP> __device__ __forceinline__ void unpack_tile(const AtcParams &prm, const uint8_t *raw, uint8_t *tile) {
+    using Cfg = AtcCfg<DP, true>;
+    constexpr int UNITS = Cfg::UNITS, BLOCKS = UNITS / 2, ROWS = 128 / UNITS;   // keys that 128 threads have at once
+    const int t = threadIdx.x & 127, block = (t >> 3) % BLOCKS, q = block * 2 + (t & 1);
+    const int row0 = (t >> 3) / BLOCKS * 4 + ((t >> 1) & 3);
+    const RawNote note = *reinterpret_cast<const RawNote *>(raw + Cfg::RAW_NOTE);
+    const int d = prm.plan.d, code_row = prm.q4.code_row, scale_row = prm.q4.scale_row;
+    const bool wide = (d & 31) == 0;   // rows on 16 bytes
+    const uint32_t groups = (q * 32 < d ? 0x80u : 0u) | (q * 32 + 16 < d ? 0x8000u : 0u);   // the head's
+    const uint32_t magic = prm.q4.magic;
+    uint32_t codes = smem_u32(raw) + row0 * code_row + q * 16, scales = smem_u32(raw) + Cfg::RAW_SCALES + row0 * scale_row + q * 2;
+    uint32_t to[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) to[j] = smem_u32(tile) + block * (Cfg::KT * 128) + row0 * 128 + ((j ^ ((t & 1) * 4) ^ (row0 & 7)) << 4);   // (ROWS is a multiple of 8)
+    // (one unit is read ahead: four warps have little else to hide its way behind, and more code than this loop costs the other
+    // roles their place in the instruction cache)
+    uint32_t w[4], b;
+    const auto read = [&] {
+        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(b) : "r"(scales));
+        if (wide) {
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(codes));
+        } else {
+            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(codes));
+            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[2]), "=r"(w[3]) : "r"(codes + 8));
+        }
+        codes += ROWS * code_row;
+        scales += ROWS * scale_row;
+    };
+    uint32_t nan = 0;   // whether a scale's byte was 255
+    read();
+#pragma unroll 1
+    for (int i = 0; i < Cfg::PASSES; ++i) {
+        const uint32_t h0 = (b & 0xffu) * 0x00100010u + 0x35003500u, h1 = (b >> 8) * 0x00100010u + 0x35003500u;   // q4_scale_bits, twice each
+        const Q4Scale2 s[2] = {{h0, q4_mul2(h0, 0xc308c308u)}, {h1, q4_mul2(h1, 0xc308c308u)}};   // -136
+        const uint32_t c[4] = {w[0], w[1], w[2], w[3]};
+        nan |= (0xfefeu - b) & b & 0x8080u;
+        if (i + 1 < Cfg::PASSES) read();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to[j]), "r"(q4_pair(c[j], 0, s[j >> 1], magic)),
+                         "r"(q4_pair(c[j], 1, s[j >> 1], magic)), "r"(q4_pair(c[j], 2, s[j >> 1], magic)), "r"(q4_pair(c[j], 3, s[j >> 1], magic)));
+            to[j] += ROWS * 128;
+        }
+    }
+    const bool rare = (nan & groups) != 0 || note.boxes != (1u << ((note.valid + prm.box_rows - 1) / (uint32_t)prm.box_rows)) - 1u;
+    if (__any_sync(0xffffffffu, rare)) unpack_rest<DP>(prm, note, raw, tile, block, row0, t & 1);
+}
 
 template <int DP, bool Q4>
 __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(const __grid_constant__ AtcMaps maps,
@@ -427,12 +398,13 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
     uint8_t *const s_q = base;                                  // NS query tiles
     uint8_t *const s_kv = base + NS * Cfg::Q_BYTES;             // ring of key and value tiles
     const int n_slots = prm.n_slots;
-    uint8_t *const s_raw = s_kv + n_slots * Cfg::KV_BYTES;      // what the unpacking warps have asked for
+    uint8_t *const s_raw = s_kv + n_slots * Cfg::KV_BYTES;      // tiles of a cache in 4 bits, as they lie
     uint64_t *const bars = reinterpret_cast<uint64_t *>(s_raw + Cfg::RAW_STAGES * Cfg::RAW_BYTES);
     uint64_t *const kv_full = bars, *const kv_empty = bars + 10, *const v_ok = bars + 20, *const q_full = bars + 30,
                    *const q_empty = bars + 32, *const s_full = bars + 34, *const p_ready = bars + 36, *const o_full = bars + 38,
-                   *const seg_full = bars + 40, *const seg_empty = bars + 44, *const seg_want = bars + 48;
-    Segment *const segs = reinterpret_cast<Segment *>(bars + ATC_BARS);
+                   *const seg_full = bars + 40, *const seg_empty = bars + 44, *const seg_want = bars + 48, *const raw_full = bars + 50,
+                   *const raw_empty = bars + 53;
+    Segment *const segs = reinterpret_cast<Segment *>(bars + Cfg::BARS);
     uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(segs + ATC_SEGS);
     volatile int *const abort = reinterpret_cast<volatile int *>(tmem_slot + 1);
     volatile int *const marks = reinterpret_cast<volatile int *>(tmem_slot + 2);   // segments with values that are not finite
@@ -456,9 +428,13 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
         }
         for (int i = 0; i < ATC_SEGS; ++i) {
             mbar_init(&seg_full[i], 1);
-            mbar_init(&seg_empty[i], 3 + 4 * NS + (Q4 ? 4 : 0));  // producer, issuer, value warp, softmax warps, unpacking warps
+            mbar_init(&seg_empty[i], 3 + 4 * NS);  // producer, issuer, value warp, softmax warps
         }
         mbar_init(seg_want, 1);
+        for (int i = 0; i < Cfg::RAW_STAGES; ++i) {
+            mbar_init(&raw_full[i], 1);
+            mbar_init(&raw_empty[i], 4);   // the warps that unpack
+        }
         *abort = 0;
         mbar_fence_init();
     }
@@ -478,10 +454,11 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
         // ---------------- TMA producer ----------------
         Segment w;
         uint32_t kv_n = 0, nq = 0;  // ring slots and query buffers handed out so far
-        Ring kv{0, 0};
+        Ring kv{0, 0}, raw{0, 0};
+        uint32_t raw_n = 0;
         bool ok = true;
         const int per_tile = KT / prm.box_rows;  // boxes per 64-entry block
-        if (!Q4 && lane == 0) mbar_arrive(seg_want);
+        if (lane == 0) mbar_arrive(seg_want);
         while (ok && (ok = seg.take(w, abort, p.ws, 49)) && w.n > 0) {
             const int q_tiles = NS == 2 && !w.alt ? 2 : 1;
             for (int r = 0; r < q_tiles && ok; ++r, ++nq) {
@@ -494,8 +471,40 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
                                     w.tok0 + r * p.tile_tokens, &q_full[b]);
                 }
             }
-            for (int t = 0; !Q4 && t < w.n && ok; ++t) {
+            int next_page = -1;   // of this lane's box of the next tile (Q4)
+            const auto look_up = [&](int t) {
+                const KeyTile k = key_tile(p, w, t);
+                const int key = k.k0 + lane * prm.box_rows;
+                return lane < per_tile && key < k.len ? __ldg((k.prefix ? p.prefix_pages : p.page_table + (long long)w.seq * p.table_stride) + (key >> p.page_shift)) : -1;
+            };
+            if constexpr (Q4) next_page = look_up(w.t0);
+            for (int t = 0; t < w.n && ok; ++t) {
                 const KeyTile k = key_tile(p, w, w.t0 + t);
+                if constexpr (Q4) {
+                    const int page = next_page, key = k.k0 + lane * prm.box_rows;
+                    if (t + 1 < w.n) next_page = look_up(w.t0 + t + 1);
+                    const bool has = lane < per_tile && key < k.len, there = has && (unsigned)page < (unsigned)p.n_pages;
+                    if (has && !there) attn_bad(p.ws, 42);
+                    const uint32_t boxes = __ballot_sync(0xffffffffu, there);
+                    for (int which = 0; which < 2; ++which, ++raw_n) {
+                        if (raw_n >= (uint32_t)Cfg::RAW_STAGES && !(ok = warp_wait(&raw_empty[raw.slot], raw.parity ^ 1u, abort, p.ws, 51))) break;
+                        uint8_t *const to = s_raw + raw.slot * Cfg::RAW_BYTES;
+                        if (lane == 0) {
+                            *reinterpret_cast<RawNote *>(to + Cfg::RAW_NOTE) = RawNote{min(k.len - k.k0, KT), boxes};
+                            mbar_arrive_expect_tx(&raw_full[raw.slot], __popc(boxes) * prm.box_rows * (prm.q4.code_row + prm.q4.scale_row));
+                        }
+                        __syncwarp();
+                        if (there) {
+                            const uint8_t *const from = static_cast<const uint8_t *>(which ? prm.v : prm.k) + page * prm.stride_page + w.head * prm.stride_head;
+                            const int slot = key & ((1 << p.page_shift) - 1), r = lane * prm.box_rows;
+                            bulk_g2s(to + r * prm.q4.code_row, from + slot * prm.q4.code_row, prm.box_rows * prm.q4.code_row, &raw_full[raw.slot]);
+                            bulk_g2s(to + Cfg::RAW_SCALES + r * prm.q4.scale_row, from + prm.q4.scale_off + slot * prm.q4.scale_row,
+                                     prm.box_rows * prm.q4.scale_row, &raw_full[raw.slot]);
+                        }
+                        raw.step(1, Cfg::RAW_STAGES);
+                    }
+                    continue;
+                }
                 const int *const pages = k.prefix ? p.prefix_pages : p.page_table + (long long)w.seq * p.table_stride;
                 for (int which = 0; which < 2; ++which) {
                     const uint32_t slot = kv.slot;
@@ -522,11 +531,24 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
                     ++kv_n;
                 }
             }
-            if (!Q4 && lane == 0) mbar_arrive(seg_want);
+            if (lane == 0) mbar_arrive(seg_want);
+        }
+        uint32_t raw_seen = raw_n > (uint32_t)Cfg::RAW_STAGES ? raw_n - Cfg::RAW_STAGES : 0;   // of the tiles, how many are known to have landed
+        if constexpr (Q4) {   // a note that there are no more
+            if (ok && (raw_n < (uint32_t)Cfg::RAW_STAGES || warp_wait(&raw_empty[raw.slot], raw.parity ^ 1u, abort, p.ws, 51))) {
+                if (lane == 0) {
+                    reinterpret_cast<RawNote *>(s_raw + raw.slot * Cfg::RAW_BYTES + Cfg::RAW_NOTE)->valid = -1;
+                    mbar_arrive(&raw_full[raw.slot]);
+                }
+                if (raw_n >= (uint32_t)Cfg::RAW_STAGES) ++raw_seen;   // (the one that was in its place)
+            }
         }
         // stay until every copy that was started has landed
         if (lane == 0) {
             const long long t_0 = clock64();
+            for (uint32_t i = raw_seen; Q4 && i < raw_n; ++i)
+                while (!mbar_try_wait(&raw_full[i % 3], (i / 3) & 1))
+                    if (clock64() - t_0 > WAIT_LIMIT_CYCLES) break;
             for (uint32_t i = kv_n > (uint32_t)n_slots ? kv_n - n_slots : 0; i < kv_n; ++i)
                 while (!mbar_try_wait(&kv_full[i % n_slots], (i / n_slots) & 1))
                     if (clock64() - t_0 > WAIT_LIMIT_CYCLES) break;
@@ -881,53 +903,22 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
     if constexpr (Q4) {
         if (warp >= Cfg::UNPACK_WARP && warp < Cfg::UNPACK_WARP + 4) {
             // ---------------- the cache in 4 bits: unpacked into the ring ----------------
-            Unpacker<DP> u(prm, s_kv, s_raw);
-            Segment w;
-            Ring kv{0, 0};
-            uint32_t kv_n = 0;
-            bool ok = true;
-            const auto unpack = [&](bool last) {
-                if (kv_n >= (uint32_t)n_slots && !warp_wait(&kv_empty[kv.slot], kv.parity ^ 1u, abort, p.ws, 51)) return false;
-                if (last) asm volatile("cp.async.wait_group 0;" ::: "memory");
-                else asm volatile("cp.async.wait_group %0;" ::"n"(Cfg::RAW_STAGES - 1) : "memory");
-                __syncwarp();   // (scales come by fours)
-                u.unpack(kv.slot);
-                fence_proxy_async_smem();
-                __syncwarp();   // (and the stage may be filled again)
-                if (lane == 0) mbar_arrive(&kv_full[kv.slot]);
-                kv.step(1, n_slots);
-                ++kv_n;
-                return true;
-            };
-            const auto drain = [&] {
-                while (ok && u.n > 0) ok = unpack(true);
-            };
-            const bool asks = warp == Cfg::UNPACK_WARP && lane == 0;   // for the next segment
-            if (asks) mbar_arrive(seg_want);
-            for (;;) {
-                if (!__all_sync(0xffffffffu, mbar_try_wait(&seg_full[seg.slot], seg.parity))) drain();   // (nothing to be asked for meanwhile)
-                if (!ok || !(ok = seg.take(w, abort, p.ws, 49)) || w.n == 0) break;
-                int page[Cfg::PASSES], next[Cfg::PASSES];
-                KeyTile k = key_tile(p, w, w.t0);
-                const auto list = [&](const KeyTile &t) { return t.prefix ? p.prefix_pages : p.page_table + (long long)w.seq * p.table_stride; };
-                u.pages(list(k), k.k0, k.len, page);
-#pragma unroll 1
-                for (int t = 0; t < w.n && ok; ++t) {
-                    const KeyTile after = key_tile(p, w, w.t0 + min(t + 1, w.n - 1));
-                    u.pages(list(after), after.k0, after.len, next);
-                    if (asks && t == max(w.n - 2, 0)) mbar_arrive(seg_want);
-#pragma unroll 1
-                    for (int which = 0; which < 2 && ok; ++which) {
-                        u.ask(which, w.head, k.k0, k.len, page);
-                        if (u.n == Cfg::RAW_STAGES) ok = unpack(false);
-                    }
-                    k = after;
-#pragma unroll
-                    for (int i = 0; i < Cfg::PASSES; ++i) page[i] = next[i];
+            Ring kv{0, 0}, raw{0, 0};
+            for (uint32_t kv_n = 0;; ++kv_n) {
+                if (!warp_wait(&raw_full[raw.slot], raw.parity, abort, p.ws, 60)) break;
+                const uint8_t *const from = s_raw + raw.slot * Cfg::RAW_BYTES;
+                if (reinterpret_cast<const RawNote *>(from + Cfg::RAW_NOTE)->valid < 0) break;
+                if (kv_n >= (uint32_t)n_slots && !warp_wait(&kv_empty[kv.slot], kv.parity ^ 1u, abort, p.ws, 51)) break;
+                unpack_tile<DP>(prm, from, s_kv + kv.slot * Cfg::KV_BYTES);
+                fence_proxy_async_smem();   // (orders the stores above, which are volatile like it)
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&kv_full[kv.slot]);
+                    mbar_arrive(&raw_empty[raw.slot]);
                 }
+                kv.step(1, n_slots);
+                raw.step(1, Cfg::RAW_STAGES);
             }
-            drain();
-            asm volatile("cp.async.wait_all;" ::: "memory");
         }
     }
 
@@ -975,7 +966,7 @@ template <int DP, bool Q4> static griffin_status launch_dp(const AttnPlan &plan,
             return GRIFFIN_ERR_UNSUPPORTED;  // (strides that the copy engine does not take)
     }
     // as many ring slots as fit beside the list of the sequences' first tiles
-    const size_t tail = ATC_BARS * 8 + ATC_SEGS * sizeof(Segment) + 8 + ATC_MARKS * 4 + ((size_t)plan.n_seq + 3) * 4, fixed = 1024 + Cfg::NS * Cfg::Q_BYTES + Cfg::RAW_STAGES * Cfg::RAW_BYTES + tail;
+    const size_t tail = Cfg::BARS * 8 + ATC_SEGS * sizeof(Segment) + 8 + ATC_MARKS * 4 + ((size_t)plan.n_seq + 3) * 4, fixed = 1024 + Cfg::NS * Cfg::Q_BYTES + Cfg::RAW_STAGES * Cfg::RAW_BYTES + tail;
     prm.n_slots = (int)((232448 - fixed) / Cfg::KV_BYTES);
     if (prm.n_slots > Cfg::MAX_SLOTS) prm.n_slots = Cfg::MAX_SLOTS;
     const size_t smem = fixed + (size_t)prm.n_slots * Cfg::KV_BYTES;
