@@ -1,12 +1,11 @@
 // Tokens of the cache held in 4 bits (q4.cuh) back to the storage type: out = (code - 8) s, which rounds nothing.
 //
-// A thread has one group of 16 entries of one key or value, of TPC tokens: 9 bytes in, 32 (bf16) or 64 out.  Bound by the
-// bytes that are written.
+// A thread has one group of 16 entries of one key or value, of every SUBS-th of the CTA's TPC tokens: 9 bytes in, 32 (bf16) or 64
+// out.  A CTA takes its tokens' places together, which is three dependent trips to L2.
 #include "common.cuh"
 #include "kv_place.cuh"
 #include "layer.h"
 #include "q4.cuh"
-#include "vec8.cuh"
 
 namespace griffin {
 
@@ -17,55 +16,81 @@ struct ReadParams {
     long long ld_k, ld_v, stride_page, stride_head;
     Q4Layout q4;
     int units, groups, hkv;   // units: groups of a token's keys and values; groups: of a head
+    int per, wide;            // units of a token that a CTA has; whether rows begin on 32-byte boundaries
 };
 
 constexpr int READ_THREADS = 128;
 
+// 16 entries of a row.
+template <typename T> __device__ __forceinline__ void store16(T *to, uint2 w, float s, bool wide) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {   // 32 bytes each
+        uint32_t v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (sizeof(T) == 2) {
+                const uint32_t x = e < 4 ? w.x : w.y;
+                const __nv_bfloat162 h = __floats2bfloat162_rn(q4_value(x, 2 * (e & 3), s), q4_value(x, 2 * (e & 3) + 1, s));
+                v[e] = *reinterpret_cast<const uint32_t *>(&h);
+            } else {
+                v[e] = __float_as_uint(q4_value(i ? w.y : w.x, e, s));
+            }
+        }
+        uint32_t *const at = reinterpret_cast<uint32_t *>(to) + 8 * i;
+        if (wide) {
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+                         "r"(v[5]), "r"(v[6]), "r"(v[7])
+                         : "memory");
+        } else {
+            reinterpret_cast<uint4 *>(at)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+            reinterpret_cast<uint4 *>(at)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+        }
+    }
+}
+
 template <typename T, int TPC> __global__ void __launch_bounds__(READ_THREADS) kv_read_q4_kernel(const __grid_constant__ ReadParams p) {
     __shared__ Place s_at[TPC];
-    const int t0 = blockIdx.x * TPC, unit = blockIdx.y * READ_THREADS + threadIdx.x;
+    const int t0 = blockIdx.x * TPC, sub = threadIdx.x / p.per, subs = READ_THREADS / p.per, unit = blockIdx.y * p.per + threadIdx.x - sub * p.per;
     const int h = unit / p.groups, g = unit - h * p.groups;
     const bool is_v = h >= p.hkv;
     const int head = is_v ? h - p.hkv : h;
     pdl_launch_dependents();
     pdl_wait_prior_grids();
     const Place mine = place_token<TPC, READ_THREADS>(p.place, t0, -1);
-    if (TPC > 1) {
-        if (threadIdx.x < TPC) s_at[threadIdx.x] = mine;
-        __syncthreads();
-    }
-    if (unit >= p.units) return;
-    uint2 w[TPC];
-    uint32_t b[TPC];
-#pragma unroll
-    for (int u = 0; u < TPC; ++u) {
-        const Place at = TPC > 1 ? s_at[u] : mine;
-        w[u] = make_uint2(Q4_ZEROS, Q4_ZEROS);
-        b[u] = 0;
-        if (at.page < 0) continue;   // (padding, or a token that has no place, reads as zeros)
-        const uint8_t *const block = (is_v ? p.v : p.k) + at.page * p.stride_page + head * p.stride_head;
-        w[u] = __ldg(reinterpret_cast<const uint2 *>(block + at.slot * p.q4.code_row + g * 8));
-        b[u] = __ldg(block + p.q4.scale_off + at.slot * p.q4.scale_row + g);
-    }
-    T *const out = static_cast<T *>(is_v ? p.v_out : p.k_out) + (long long)(head * p.groups + g) * 16;
+    if (threadIdx.x < TPC) s_at[threadIdx.x] = mine;
+    __syncthreads();
+    if (unit >= p.units || sub >= subs) return;
+    const uint8_t *const block = (is_v ? p.v : p.k) + head * p.stride_head;
     const long long ld = is_v ? p.ld_v : p.ld_k;
+    T *const out = static_cast<T *>(is_v ? p.v_out : p.k_out) + (long long)(head * p.groups + g) * 16;
+    constexpr int AT_ONCE = TPC < 4 ? TPC : 4;
+#pragma unroll 1
+    for (int t = sub; t < TPC; t += AT_ONCE * subs) {
+        uint2 w[AT_ONCE];
+        uint32_t b[AT_ONCE];
 #pragma unroll
-    for (int u = 0; u < TPC; ++u) {
-        if ((TPC > 1 ? s_at[u] : mine).page == -2) continue;
-        const float s = q4_scale(b[u]);
-        float f[8];
+        for (int u = 0; u < AT_ONCE; ++u) {
+            w[u] = make_uint2(Q4_ZEROS, Q4_ZEROS);
+            b[u] = 0;
+            if (t + u * subs >= TPC) continue;
+            const Place at = s_at[t + u * subs];
+            if (at.page < 0) continue;   // (padding, or a token that has no place, reads as zeros)
+            const uint8_t *const from = block + at.page * p.stride_page;
+            w[u] = __ldg(reinterpret_cast<const uint2 *>(from + at.slot * p.q4.code_row + g * 8));
+            b[u] = __ldg(from + p.q4.scale_off + at.slot * p.q4.scale_row + g);
+        }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = q4_value(i ? w[u].y : w[u].x, j, s);
-            store8<T>(out, (t0 + u) * ld + 8 * i, f);
+        for (int u = 0; u < AT_ONCE; ++u) {
+            if (t + u * subs >= TPC || s_at[t + u * subs].page == -2) continue;
+            store16<T>(out + (t0 + t + u * subs) * ld, w[u], q4_scale(b[u]), p.wide != 0);
         }
     }
 }
 
-constexpr int READ_TOKENS = 4;
-template <typename T> static const void *read_kernel(bool many) {
-    return many ? reinterpret_cast<const void *>(kv_read_q4_kernel<T, READ_TOKENS>) : reinterpret_cast<const void *>(kv_read_q4_kernel<T, 1>);
+template <typename T> static const void *read_kernel(int tpc) {
+    return tpc == 1 ? reinterpret_cast<const void *>(kv_read_q4_kernel<T, 1>)
+           : tpc == 4 ? reinterpret_cast<const void *>(kv_read_q4_kernel<T, 4>)
+                      : reinterpret_cast<const void *>(kv_read_q4_kernel<T, 16>);
 }
 
 griffin_status launch_kv_read_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch, const griffin_kv_cache_q4 *cache,
@@ -79,9 +104,13 @@ griffin_status launch_kv_read_q4(const griffin_attn_desc *desc, const griffin_at
     p.groups = desc->head_dim / 16; p.hkv = desc->n_kv_heads; p.units = 2 * p.hkv * p.groups;
     const int sms = device_sm_count(), n = batch->n_tokens;
     if (sms <= 0) return GRIFFIN_ERR_CUDA;
-    const bool many = n >= 16 * sms;
-    const int tpc = many ? READ_TOKENS : 1, x = (n + tpc - 1) / tpc, y = (p.units + READ_THREADS - 1) / READ_THREADS;
-    const void *fn = desc->dtype == GRIFFIN_DT_F32 ? read_kernel<float>(many) : read_kernel<__nv_bfloat16>(many);
+    p.per = p.units < READ_THREADS ? p.units : READ_THREADS;
+    const int unit = desc->dtype == GRIFFIN_DT_F32 ? 4 : 2;
+    p.wide = ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | (uintptr_t)(ld_k * unit) | (uintptr_t)(ld_v * unit)) & 31) == 0;
+    const int y = (p.units + p.per - 1) / p.per;
+    const long long ctas = (long long)n * y;
+    const int tpc = ctas >= 64ll * sms ? 16 : ctas >= 16ll * sms ? 4 : 1, x = (n + tpc - 1) / tpc;
+    const void *fn = desc->dtype == GRIFFIN_DT_F32 ? read_kernel<float>(tpc) : read_kernel<__nv_bfloat16>(tpc);
     void *args[] = {&p};
     return launch_maybe_overlapped(fn, dim3(x, y), dim3(READ_THREADS), 0, stream, true, args) == cudaSuccess ? GRIFFIN_OK
                                                                                                             : GRIFFIN_ERR_CUDA;

@@ -142,6 +142,43 @@ def check_append_not_finite(b):
         assert np.all(np.abs(want[~held]) == 12544.0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_codes_next_to_their_borders(dtype):
+    # (n + 1/2) s and its neighbours in the storage type, for every scale of an octave: ties and what is next to them
+    n_tok, step = 2048, {"bf16": 2.0 ** -7, "f32": 2.0 ** -22}[dtype]
+    b = BatchQ4([n_tok], [n_tok], 0, 4, 4, 64, 64, dtype)
+    rng = np.random.default_rng(3)
+    s = (8 + rng.integers(0, 8, (n_tok, 4, 4, 1))) * 2.0 ** rng.integers(-20, 6, (n_tok, 4, 4, 1))
+    x = (rng.integers(-7, 7, (n_tok, 4, 4, 16)) + 0.5) * s * (1 + step * rng.integers(-4, 5, (n_tok, 4, 4, 16)) / 4)
+    x[..., :1] = 7 * s
+    b.k = torch.from_numpy(x.reshape(n_tok, 4, 64)).to(b.dt)
+    b.v = (b.v.float() * 3.0).to(b.dt)
+    b.to_device()
+    G.griffin_kv_append_q4(b.desc, b.batch, b.cache, None, None, b.k.to(DEV), b.v.to(DEV), None, b.ws)
+    for x, out in zip((b.k, b.v), b.read()):
+        assert np.array_equal(f64(out), Q.values(*Q.quantise(x.float().numpy())))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hkv,hd,n", [(1, 64, 900), (1, 64, 12000), (3, 80, 9000), (16, 256, 700), (33, 64, 2500)])
+def test_read_of_few_and_many_heads(dtype, hkv, hd, n):
+    # units that a CTA's threads have several tokens of, or that several CTAs share; rows on 16-byte boundaries only
+    b = BatchQ4([1, 1], [3, 5], 0, hkv, hkv, hd, 16, dtype)
+    pages = torch.randint(0, b.k_bytes.shape[0], (2, -(-n // 16)), dtype=torch.int32, generator=torch.Generator().manual_seed(1))
+    lens = [n, n // 3]
+    b.to_device()
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)
+    batch = G.make_attn_batch(i32([0, n, n + n // 3]), i32(lens), pages.to(DEV), n + n // 3)
+    pad = 16 // b.dt.itemsize
+    k = torch.full((n + n // 3, hkv * hd + pad), 5.0, dtype=b.dt, device=DEV)
+    v = torch.full((n + n // 3, hkv * hd), 5.0, dtype=b.dt, device=DEV)
+    G.griffin_kv_read_q4(b.desc, batch, b.cache, k[:, :hkv * hd], v, b.ws)
+    assert G.griffin_check_device_status(b.ws) == G.OK and torch.all(k[:, hkv * hd:] == 5.0)
+    for out, host in ((k[:, :hkv * hd], b.k_host), (v, b.v_host)):
+        want = torch.cat([host.transpose(1, 2)[pages[s].long()].flatten(0, 1)[:lens[s]] for s in range(2)]).flatten(1)
+        assert torch.equal(torch.nan_to_num(out.cpu(), nan=77.0), torch.nan_to_num(want, nan=77.0))
+
+
 def test_what_cannot_be_placed_is_reported():
     def run(b, table=None):
         b.to_device()
