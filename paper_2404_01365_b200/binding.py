@@ -554,10 +554,6 @@ def griffin_kv_q4_block_bytes(desc):
     return int(load().griffin_kv_q4_block_bytes(C.byref(desc)))
 
 
-def _q4_block(desc):
-    return desc.page_size * (desc.head_dim // 2 + (desc.head_dim + 63) // 64 * 4)
-
-
 def make_kv_cache_q4(k, v):
     """A paged cache in 4 bits from two uint8 tensors [n_pages, n_kv_heads, griffin_kv_q4_block_bytes] of the same strides
     (any, as long as the bytes of a head are consecutive)."""
@@ -578,16 +574,20 @@ def alloc_kv_cache_q4(desc, n_pages, device):
     return make_kv_cache_q4(*(torch.empty((n_pages, desc.n_kv_heads, n), dtype=torch.uint8, device=device) for _ in range(2)))
 
 
-def _check_cache_q4(desc, batch, cache):
-    if cache._form is not None and cache._form != (desc.n_kv_heads, _q4_block(desc)):
-        raise ValueError(f"cache: expected pages [{desc.n_kv_heads}, {_q4_block(desc)}], got {list(cache._form)}")
-    _check_prefix(batch, desc.page_size)
+def _check_q4(batch, cache, heads, d, page):
+    """That the cache's pages are the descriptor's, and the prefix's list as long as the prefix."""
+    form, block = cache._form, page * (d // 2 + (d + 63) // 64 * 4)
+    if form is not None and form != (heads, block):
+        raise ValueError(f"cache: expected pages [{heads}, {block}], got {list(form)}")
+    if batch._prefix_pages is not None:
+        _check_prefix(batch, page)
 
 
+# (structures are handed to ctypes as they are, which passes their address)
 def griffin_kv_append_q4(desc, batch, cache, rope, q, k, v, q_out, ws=None, stream=None):
     """griffin_kv_append into a cache in 4 bits: keys, rotated, and values are quantised as they are written."""
     n, hq, hk, d, dt = batch.n_tokens, desc.n_q_heads, desc.n_kv_heads, desc.head_dim, desc.dtype
-    _check_cache_q4(desc, batch, cache)
+    _check_q4(batch, cache, hk, d, desc.page_size)
     q_p = o_p = None
     ld_q = ld_o = 0
     if q is not None:
@@ -595,9 +595,10 @@ def griffin_kv_append_q4(desc, batch, cache, rope, q, k, v, q_out, ws=None, stre
     if q_out is not None:
         ld_o, o_p = _rows(q_out, n, hq, d, dt, "q_out"), q_out.data_ptr()
     ld_k, ld_v = _rows(k, n, hk, d, dt, "k"), _rows(v, n, hk, d, dt, "v")
-    st = load().griffin_kv_append_q4(C.byref(desc), C.byref(batch), C.byref(cache), None if rope is None else C.byref(rope), q_p, ld_q,
-                                     k.data_ptr(), ld_k, v.data_ptr(), ld_v, o_p, ld_o, None if ws is None else ws.data_ptr(),
-                                     _stream(stream))
+    if n == 0:       # (empty tensors have no address)
+        return
+    st = load().griffin_kv_append_q4(desc, batch, cache, rope, q_p, ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, o_p, ld_o,
+                                     None if ws is None else ws.data_ptr(), _stream(stream))
     if st != OK:
         raise GriffinError(st, "griffin_kv_append_q4")
 
@@ -605,9 +606,11 @@ def griffin_kv_append_q4(desc, batch, cache, rope, q, k, v, q_out, ws=None, stre
 def griffin_kv_read_q4(desc, batch, cache, k, v, ws=None, stream=None):
     """The batch's tokens out of a cache in 4 bits: k, v [n_tokens, n_kv_heads, head_dim] of the descriptor's dtype."""
     n, hk, d, dt = batch.n_tokens, desc.n_kv_heads, desc.head_dim, desc.dtype
-    _check_cache_q4(desc, batch, cache)
+    _check_q4(batch, cache, hk, d, desc.page_size)
     ld_k, ld_v = _rows(k, n, hk, d, dt, "k"), _rows(v, n, hk, d, dt, "v")
-    st = load().griffin_kv_read_q4(C.byref(desc), C.byref(batch), C.byref(cache), k.data_ptr(), ld_k, v.data_ptr(), ld_v,
+    if n == 0:
+        return
+    st = load().griffin_kv_read_q4(desc, batch, cache, k.data_ptr(), ld_k, v.data_ptr(), ld_v,
                                    None if ws is None else ws.data_ptr(), _stream(stream))
     if st != OK:
         raise GriffinError(st, "griffin_kv_read_q4")
@@ -616,9 +619,11 @@ def griffin_kv_read_q4(desc, batch, cache, k, v, ws=None, stream=None):
 def griffin_attn_prefix_q4(desc, batch, cache, q, out, ws, stream=None):
     """griffin_attn_prefix over a cache in 4 bits."""
     n, hq, d, dt = batch.n_tokens, desc.n_q_heads, desc.head_dim, desc.dtype
-    _check_cache_q4(desc, batch, cache)
+    _check_q4(batch, cache, desc.n_kv_heads, d, desc.page_size)
     ld_q, ld_o = _rows(q, n, hq, d, dt, "q"), _rows(out, n, hq, d, dt, "out")
-    st = load().griffin_attn_prefix_q4(C.byref(desc), C.byref(batch), C.byref(cache), q.data_ptr(), ld_q, out.data_ptr(), ld_o,
-                                       ws.data_ptr(), ws.numel(), _stream(stream))
+    if n == 0:
+        return
+    st = load().griffin_attn_prefix_q4(desc, batch, cache, q.data_ptr(), ld_q, out.data_ptr(), ld_o, ws.data_ptr(), ws.numel(),
+                                       _stream(stream))
     if st != OK:
         raise GriffinError(st, "griffin_attn_prefix_q4")

@@ -96,7 +96,7 @@ __device__ __forceinline__ void append_group(const Piece<T> &x, const Piece<T> &
 }
 
 template <typename T, int TPC, bool Q4>
-__global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(APPEND_THREADS, Q4 ? 8 : 1) kv_append_kernel(const __grid_constant__ AppendParams p) {
     __shared__ Place s_at[TPC];
     __shared__ __align__(16) float s_table[TPC][TPC > 1 ? 256 : 4];
     const int t0 = blockIdx.x * TPC, pieces = (p.d + 15) >> 4, per_round = APPEND_THREADS / pieces;  // heads side by side

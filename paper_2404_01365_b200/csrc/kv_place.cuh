@@ -24,9 +24,9 @@ struct Place {
     int pos;    // position: prefix_len + index among the sequence's own tokens
 };
 
-// The place of this thread's token, t0 + threadIdx.x of t0 .. t0 + TPC - 1 (with TPC = 1 every thread's is t0); called by
-// the whole CTA of THREADS threads.  n_pos: positions from there on cannot be placed (-1: all can).
-template <int TPC, int THREADS> __device__ __forceinline__ Place place_token(const PlaceParams &p, int t0, int n_pos) {
+// The place of this thread's token, t0 + threadIdx.x of t0 .. t0 + count - 1 (with TPC = 1 every thread's is t0; count <= TPC);
+// called by the whole CTA of THREADS threads.  n_pos: positions from there on cannot be placed (-1: all can).
+template <int TPC, int THREADS> __device__ __forceinline__ Place place_token(const PlaceParams &p, int t0, int n_pos, int count = TPC) {
     // the first token's sequence: how many sequences end at or before it (empty ones included)
     int seq = 0;
     if (p.n_seq > 1) {
@@ -36,7 +36,7 @@ template <int TPC, int THREADS> __device__ __forceinline__ Place place_token(con
         }
     }
     Place r{-2, 0, 0};
-    if (TPC > 1 && threadIdx.x >= TPC) return r;
+    if (TPC > 1 && (int)threadIdx.x >= count) return r;
     const int t = TPC == 1 ? t0 : t0 + threadIdx.x;
     if (TPC > 1 || p.n_seq == 1)  // (otherwise the count above was this token's)
         while (seq < p.n_seq && __ldg(p.q_start + seq + 1) <= t) ++seq;

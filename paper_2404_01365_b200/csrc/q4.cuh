@@ -36,10 +36,6 @@ constexpr uint32_t Q4_ZEROS = 0x88888888u;   // eight codes that stand for 0
 __device__ __forceinline__ float q4_scale(uint32_t b) {
     return b == Q4_NAN ? __uint_as_float(0x7fc00000u) : __uint_as_float((b << 20) + (106u << 23));
 }
-// Entry j of a word, times the scale.
-__device__ __forceinline__ float q4_value(uint32_t w, int j, float s) {
-    return (float)((int)((w >> ((j & 1) * 16 + (j >> 1) * 4)) & 15u) - 8) * s;
-}
 
 // The scale of a group as bf16 in both halves of a register, and -136 times it, for q4_pair.
 struct Q4Scale2 {
@@ -71,24 +67,34 @@ __device__ __forceinline__ uint32_t q4_pair(uint32_t w, int i, Q4Scale2 s, uint3
 }
 
 // 16 entries to two words of codes and the scale's byte.
-__device__ __forceinline__ uint32_t q4_quantise(const float (&f)[16], uint2 &codes) {
-    float a = 0.f;   // NaN if any entry is
+__device__ __forceinline__ uint32_t q4_quantise(const float (&in)[16], uint2 &codes) {
+    float f[16], a = 0.f;   // a: NaN if any entry is
 #pragma unroll
-    for (int j = 0; j < 16; ++j) asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(a), "f"(fabsf(f[j])));
+    for (int j = 0; j < 16; ++j) f[j] = in[j];
+#pragma unroll
+    for (int j = 0; j < 16; j += 2) asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(a), "f"(fabsf(f[j])), "f"(fabsf(f[j + 1])));
     const bool finite = a < INFINITY;
     const uint32_t q = __float_as_uint(__fdiv_rn(a, 7.f));
     const int t = (int)((q + 0x7ffffu + ((q >> 20) & 1u)) >> 20) - (106 << 3);
     const uint32_t b = (uint32_t)min(max(t, 0), 254);
     const float s = q4_scale(b), r = __frcp_rn(s);
-    uint32_t w[2] = {0u, 0u};
+    if (t > 254) {   // (only then can a quotient be 7.5 or more)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        // x / s, rounded to nearest (Markstein's theorem: a quotient from the rounded reciprocal, corrected once by its exact
-        // remainder; with the 4-bit divisors here it holds for every x, by trial of all mantissas).  Nothing overflows:
-        // 1 / s is 2^21 at most, and x then below 2^-18.
-        const float y = f[j] * r, x = fmaf(fmaf(-y, s, f[j]), r, y);
-        // to the nearest integer, ties to even, in the last bits of 1.5 * 2^23, and 8 more
-        w[j >> 3] += (__float_as_uint(fminf(fmaxf(x, -7.f), 7.f) + 12582920.f) & 15u) << ((j & 1) * 16 + ((j & 7) >> 1) * 4);
+        for (int j = 0; j < 16; ++j) f[j] = fminf(fmaxf(f[j], -7.f * s), 7.f * s);
+    }
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float half[2] = {0.f, 0.f};   // the codes of a half word, less 8 each, as one number
+#pragma unroll
+        for (int j = 7; j >= 0; --j) {
+            // x / s, rounded to nearest (Markstein's theorem: a quotient from the rounded reciprocal, corrected once by its exact
+            // remainder; with the 4-bit divisors here it holds for every x, by trial of all mantissas), then to the nearest
+            // integer, ties to even.  Nothing overflows: 1 / s is 2^21 at most, and x then below 2^-18.
+            const float x = f[8 * i + j], y = x * r, c = __fadd_rn(__fadd_rn(fmaf(fmaf(-y, s, x), r, y), 12582912.f), -12582912.f);
+            half[j & 1] = fmaf(half[j & 1], 16.f, c);
+        }
+        w[i] = __byte_perm(__float_as_uint(half[0] + (8388608.f + 34952.f)), __float_as_uint(half[1] + (8388608.f + 34952.f)), 0x5410);   // 0x8888
     }
     codes = finite ? make_uint2(w[0], w[1]) : make_uint2(Q4_ZEROS, Q4_ZEROS);
     return finite ? b : Q4_NAN;

@@ -3,8 +3,8 @@
 What each layer does, in the order of its calls (projections are plain torch matrix products):
 
   h = norm(r)                                 griffin_norm_residual
-  q, k, v = h W_qkv; into the cache, rotated  griffin_kv_append
-  o = softmax(q K^T) V                        griffin_attn_prefix
+  q, k, v = h W_qkv; into the cache, rotated  griffin_kv_append (griffin_kv_append_q4: the cache in 4 bits)
+  o = softmax(q K^T) V                        griffin_attn_prefix (griffin_attn_prefix_q4)
   r += o W_o;  h = norm(r)                    griffin_norm_residual
   y = FF(h)                                   griffin_ff_prefill_score (prompt: full block and the statistic), then
                                               griffin_select_topk and griffin_compact_experts;
@@ -14,7 +14,7 @@ What each layer does, in the order of its calls (projections are plain torch mat
 The prompt's keys and values are kept once.  Its continuations have it as their shared prefix, and the expert set that
 the prompt selected as theirs, so a step reads both once for all of them.
 
-  python -m paper_2404_01365_b200.decoder --continuations 8 --steps 32      (random weights)
+  python -m paper_2404_01365_b200.decoder --continuations 8 --steps 32 --cache q4     (random weights)
 """
 from __future__ import annotations
 
@@ -40,6 +40,7 @@ class DecoderConfig:
     page_size: int = 64
     eps: float = 1e-6
     theta: float = 10000.0
+    cache: str = "storage"      # keys and values in dtype, or "q4": in 4 bits
 
     @property
     def torch_dtype(self):
@@ -82,9 +83,16 @@ class Decoder:
         self.attn_ws = G.alloc_attn_workspace(self.attn, max(max_prompt, n_seq), n_seq, device)
         self.rope = G.make_rope(G.rope_table(max_prompt + max_new, cfg.head_dim, cfg.theta, device))
         pre, own = -(-max_prompt // page), -(-max_new // page)
+        if cfg.cache not in ("storage", "q4"):
+            raise ValueError(f"cache: expected storage or q4, got {cfg.cache}")
         shape = (pre + n_seq * own, cfg.n_kv_heads, page, cfg.head_dim)
-        self.caches = [G.make_kv_cache(torch.empty(shape, device=device, dtype=dt), torch.empty(shape, device=device, dtype=dt))
-                       for _ in range(cfg.n_layers)]
+        if cfg.cache == "q4":
+            self.append, self.attend = G.griffin_kv_append_q4, G.griffin_attn_prefix_q4
+            self.caches = [G.alloc_kv_cache_q4(self.attn, shape[0], device) for _ in range(cfg.n_layers)]
+        else:
+            self.append, self.attend = G.griffin_kv_append, G.griffin_attn_prefix
+            self.caches = [G.make_kv_cache(torch.empty(shape, device=device, dtype=dt), torch.empty(shape, device=device, dtype=dt))
+                           for _ in range(cfg.n_layers)]
         ints = lambda *a: torch.arange(*a, dtype=torch.int32, device=device)
         self.prefix_pages, self.own_pages = ints(pre), ints(pre, pre + n_seq * own).view(n_seq, own)
         self.q_start = ints(n_seq + 1)
@@ -101,8 +109,8 @@ class Decoder:
         for i, l in enumerate(self.w["layers"]):
             qkv = h @ l["w_qkv"].t()
             q, k, v = qkv.split((nq, nk, nk), 1)
-            G.griffin_kv_append(self.attn, batch, self.caches[i], self.rope, q, k, v, q, self.attn_ws)
-            G.griffin_attn_prefix(self.attn, batch, self.caches[i], q, o, self.attn_ws)
+            self.append(self.attn, batch, self.caches[i], self.rope, q, k, v, q, self.attn_ws)
+            self.attend(self.attn, batch, self.caches[i], q, o, self.attn_ws)
             G.griffin_norm_residual(self.norm, self.norm_w[2 * i + 1], x, x, h, o @ l["w_o"].t())
             y = torch.empty_like(x)
             feed_forward(i, h, y)
@@ -143,6 +151,22 @@ class Decoder:
             G.griffin_ff_decode(self.ff, self.set_arrays[i], None, h, y, self.ff_ws)
         return self._layers(self.w["embed"][tokens], self.batch, pruned) @ self.w["head"].t()
 
+    def held(self, layer):
+        """Keys and values of a layer as a cache in 4 bits holds them: (k, v) of the prompt's tokens [P, heads, D], and of each
+        continuation's [n_seq, steps so far, heads, D]."""
+        if self.cfg.cache != "q4":
+            raise ValueError("the cache is not in 4 bits: its tensors hold the keys and values")
+        c, out = self.cfg, []
+        i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device=self.device)
+        prompt = ([0, self.prompt_len], i32(self.prompt_len), self.prefix_pages[None])
+        own = ([s * self.done for s in range(self.n_seq + 1)], self.seq_len, self.own_pages)
+        for starts, lens, pages in (prompt, own):
+            kv = [torch.empty(starts[-1], c.n_kv_heads, c.head_dim, device=self.device, dtype=c.torch_dtype) for _ in range(2)]
+            G.griffin_kv_read_q4(self.attn, G.make_attn_batch(i32(*starts), lens, pages, starts[-1]), self.caches[layer], *kv, self.attn_ws)
+            out.append(kv)
+        own = [x.view(self.n_seq, self.done, c.n_kv_heads, c.head_dim) for x in out[1]]
+        return tuple(out[0]), tuple(own)
+
     def status(self):
         """OK, or what a call of the path reported from the device (synchronises)."""
         st = G.griffin_check_device_status(self.ff_ws)
@@ -156,8 +180,9 @@ def main(argv=None):
     ap.add_argument("--continuations", type=int, default=8)
     ap.add_argument("--steps", type=int, default=32)
     ap.add_argument("--keep", type=float, default=0.5)
+    ap.add_argument("--cache", choices=("storage", "q4"), default="storage")
     a = ap.parse_args(argv)
-    cfg = DecoderConfig(vocab=32000, d=4096, n_layers=a.layers, n_q_heads=32, n_kv_heads=8, head_dim=128, d_ff=14336)
+    cfg = DecoderConfig(vocab=32000, d=4096, n_layers=a.layers, n_q_heads=32, n_kv_heads=8, head_dim=128, d_ff=14336, cache=a.cache)
     dec = Decoder(cfg, random_weights(cfg, device="cuda"), a.prompt, a.continuations, a.steps, a.keep)
     tokens = torch.randint(0, cfg.vocab, (a.prompt,), generator=torch.Generator().manual_seed(1)).cuda()
     nxt = torch.empty(a.continuations, dtype=torch.long, device="cuda")

@@ -51,7 +51,7 @@ def test_pages(page, d):
     assert np.array_equal(Q.pack(c, b), block) and np.array_equal(Q.values(c, b), L.q4_held(x), equal_nan=True)
     desc = G.make_attn_desc(2, 2, d, page, "bf16")
     build.build()
-    assert G.griffin_kv_q4_block_bytes(desc) == G._q4_block(desc) == block.size
+    assert G.griffin_kv_q4_block_bytes(desc) == block.size
 
 
 def q4(args, **kw):
@@ -162,3 +162,13 @@ def test_the_binding_checks_tensors(monkeypatch):
             run(which, q=torch.zeros(2, 4, 64, dtype=BF))
     with pytest.raises(ValueError):
         G.make_kv_cache_q4(u8(8, 2, n), u8(9, 2, n))
+
+
+def test_calls_without_tokens_do_nothing(lib):
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)
+    desc = G.make_attn_desc(4, 2, 64, 16, "bf16")
+    batch, cache = G.make_attn_batch(i32(3), i32(2), i32(2, 4), 0), G.alloc_kv_cache_q4(desc, 8, "cpu")
+    q, k, ws = torch.zeros(0, 4, 64, dtype=torch.bfloat16), torch.zeros(0, 2, 64, dtype=torch.bfloat16), torch.zeros(64, dtype=torch.uint8)
+    G.griffin_kv_append_q4(desc, batch, cache, None, q, k, k, q, ws)
+    G.griffin_kv_read_q4(desc, batch, cache, k, k, ws)
+    G.griffin_attn_prefix_q4(desc, batch, cache, q, q, ws)
