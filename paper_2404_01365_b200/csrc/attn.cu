@@ -29,6 +29,42 @@ static bool attn_few(const griffin_attn_desc *desc, const griffin_attn_batch *ba
     if (n > 1 && prefix > 0 && rows > 8 && (rows > 16 || prefix > FEW_PREFIX_TWICE)) return false;
     return rows <= 8 * n || (rows <= 16 * n && own + (double)prefix <= (double)FEW_OWN_TWICE);
 }
+// Over a cache held in 4 bits the kernel for blocks of up to 8 rows (attn_few_q4.cu) may give its jobs (a block under a key head, with the
+// prefix's keys and the sequence's own) to clusters of CTAs whole: then nothing is left to the joining kernel, which is 4 us, but the
+// call waits for its longest job.  us a pass by cluster, - more than are resident at once; cut: the call's tiles dealt out evenly, and joined:
+//   jobs  keys   cut     1     2     4     8       jobs  keys   cut     1     2     4
+//      1   200  10.7   8.4   9.3   9.3   9.9         40   500  13.1  10.9  10.6     -
+//      1  1000  12.7  12.9  11.9  10.2   9.7         40  4000  22.6  27.8  20.1     -
+//      1  4000  19.2  26.1  19.0  14.5  12.4         40 16000  38.3  85.9  51.0     -
+//      8   500  12.3  10.5  10.3   9.6   9.9         72  1000  16.6  13.6  12.9     -
+//      8 16000  21.0  83.0  48.0  29.3  20.3         72  4000  26.4  28.3  21.3     -
+//     16  4000  16.0  27.0  19.4  14.9  24.0         80  4000  27.8  28.2     -     -
+//     32  1000  13.5  13.4  12.6  10.6     -        128  1000  21.4  14.4     -     -
+//     32 16000  33.4  84.8  49.7  32.2     -        128  4000  34.0  30.2     -     -
+// (The table fits base + slope * keys for each cluster and 12.3 + 0.0058 * keys * jobs / 148 for cut calls to 2 us; 8 CTAs fit a GPC twice.)
+// The sequences' lengths are on the device; what the page table could hold stands for them, here and below.
+struct WholeFit {
+    int cluster, most_jobs;
+    double base, slope, slack;   // slack: how far base may be from the fit of cut calls, which lies low for the fewest jobs
+};
+constexpr WholeFit WHOLE_FITS[] = {{1, 148, 7.8, 0.0050, 0.0}, {2, 72, 8.7, 0.0026, 1.4}, {4, 32, 9.0, 0.00138, 0.0}, {8, 8, 9.4, 0.00068, 5.0}};
+struct WholeJobs {
+    int jobs, cluster;   // cluster 0: not whole
+    double us;
+};
+static WholeJobs attn_whole(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
+    const int block_tokens = 8 / (desc->n_q_heads / desc->n_kv_heads);
+    const long long n = batch->n_seq, blocks = batch->n_tokens <= n ? n : n + batch->n_tokens / block_tokens, jobs = blocks * desc->n_kv_heads;
+    // (keys 128 wide, of the longest job)
+    const double keys = ((double)batch->prefix_len + (double)batch->table_stride * desc->page_size) * (desc->head_dim / 128.0);
+    WholeJobs best{0, 0, 0.0};
+    for (const WholeFit &f : WHOLE_FITS) {
+        const double us = f.base + f.slope * keys;
+        if (jobs > f.most_jobs || (best.cluster > 0 && us >= best.us)) continue;
+        best = WholeJobs{(int)jobs, us <= 12.3 + f.slack + 0.0058 * keys * (double)jobs / ATTN_MAX_GRID ? f.cluster : 0, us};
+    }
+    return best;
+}
 // The same over a cache held in 4 bits (attn_few_q4.cu).  That kernel unpacks the keys once for every 8 rows, at about 4 TB/s
 // of a bf16 cache's bytes; the tcgen05 one unpacks them once for up to 256, and a job that ends costs it as much as two of its tiles.
 // Both sides, us a pass, few / tcgen05, 128-wide heads unless said otherwise.  Up to 16 rows of a sequence: 1 sequence, 8 key
@@ -38,14 +74,16 @@ static bool attn_few(const griffin_attn_desc *desc, const griffin_attn_batch *ba
 // A shared prefix, whose rows are the whole call's, under 8 key heads: 24 rows of 6 sequences, 2000 keys 16.7 / 18.8, 8000 26.2 / 25.4, of 24
 // sequences 24.9 / 30.7; 48 of 6, 2000 23.6 / 19.8; 64 of 16, 2000 22.1 / 21.0; 128 of 32, 300 19.5 / 21.3, 2000 31.2 / 26.3.
 // Under 2 key heads: 64 rows of 8, 2000 15.9 / 17.7, 8000 24.5 / 20.4.  256 wide, 20 rows of 20 sequences, 16 key heads, 4000 38 / 57.
-// (The sequences' lengths are on the device; what the page table could hold stands for them.)
-constexpr double FQ_FEW_KEYS = 72000, FQ_KEYS_PER_SEQ = 800, FQ_KEYS_PER_CALL = 24000;
+// Calls whose jobs are whole, which take 17 us at most, are shorter than any of the tcgen05 kernel's.
+constexpr double FQ_WHOLE_US = 17, FQ_FEW_KEYS = 72000, FQ_KEYS_PER_SEQ = 800, FQ_KEYS_PER_CALL = 24000;
 static bool attn_few_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
     const int group = desc->n_q_heads / desc->n_kv_heads;
     if (desc->dtype != GRIFFIN_DT_BF16 || group > 8) return false;
     const long long rows = (long long)batch->n_tokens * group, n = batch->n_seq;
     const double blocks = (double)((rows + 7) / 8), prefix = batch->prefix_len, room = (double)batch->table_stride * desc->page_size;
     const double hkv = desc->n_kv_heads, width = desc->head_dim / 128.0;
+    const WholeJobs whole = attn_whole(desc, batch);
+    if (whole.cluster > 0 && whole.us <= FQ_WHOLE_US) return true;
     if (blocks * hkv * (prefix + room) * width <= FQ_FEW_KEYS) return true;
     if (rows > 16 * n) return false;
     return n == 1 || (blocks - 1) * prefix * width <= FQ_KEYS_PER_SEQ * n + FQ_KEYS_PER_CALL / hkv;
@@ -115,14 +153,19 @@ static AttnPlan make_plan(const griffin_attn_desc *desc, const griffin_attn_batc
     return p;
 }
 
-static griffin_status launch(const griffin_attn_desc *desc, const griffin_attn_batch *batch, const AttnData &x, int n_pages, bool few, bool q4, uint8_t *scratch, void *ws, cudaStream_t stream) {
+static griffin_status launch(const griffin_attn_desc *desc, const griffin_attn_batch *batch, const AttnData &x, int n_pages, bool few,
+                             bool q4, uint8_t *scratch, void *ws, cudaStream_t stream) {
     const int sms = device_sm_count();
     if (sms <= 0) return GRIFFIN_ERR_CUDA;
     const AttnPlan p = make_plan(desc, batch, n_pages, sms, shape_of(desc, few, q4), scratch, ws);
-    const griffin_status st = desc->dtype == GRIFFIN_DT_F32          ? launch_attn_simt(p, x, q4, stream)
-                              : !few                                  ? launch_attn_tc(p, x, q4, stream)
-                              : q4                                   ? launch_attn_few_q4(p, x, stream)
-                                                                     : launch_attn_few(p, x, stream);
+    if (few && q4) {
+        const WholeJobs whole = attn_whole(desc, batch);
+        if (whole.cluster > 0) return launch_attn_few_q4(p, x, whole.jobs, whole.cluster, stream);
+    }
+    const griffin_status st = desc->dtype == GRIFFIN_DT_F32 ? launch_attn_simt(p, x, q4, stream)
+                              : !few                        ? launch_attn_tc(p, x, q4, stream)
+                              : q4                          ? launch_attn_few_q4(p, x, 0, 0, stream)
+                                                            : launch_attn_few(p, x, stream);
     return st != GRIFFIN_OK ? st : launch_attn_join(p, desc->dtype, x.out, x.ld_out, stream);
 }
 

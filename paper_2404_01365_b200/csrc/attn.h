@@ -79,7 +79,9 @@ AttnShape attn_few_shape(int head_dim);
 AttnShape attn_few_q4_shape(int head_dim);
 griffin_status launch_attn_tc(const AttnPlan &plan, const AttnData &data, bool q4, cudaStream_t stream);  // bf16; q4: the cache in 4 bits
 griffin_status launch_attn_few(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // bf16, few rows
-griffin_status launch_attn_few_q4(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // and the cache in 4 bits
+// and the cache in 4 bits; cluster > 0: so many CTAs take each of at most `jobs` jobs whole, the prefix's keys with them, and no partials
+// are left
+griffin_status launch_attn_few_q4(const AttnPlan &plan, const AttnData &data, int jobs, int cluster, cudaStream_t stream);
 griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, bool q4, cudaStream_t stream);  // fp32; q4: the cache in 4 bits
 
 }  // namespace griffin

@@ -315,10 +315,11 @@ __device__ __forceinline__ void fq_queries(const AttnPlan &p, const AttnData &x,
     }
 }
 
-// One warp's share, tiles at .. at_end - 1 of the call's (the CTA's are cta_at .. cta_end - 1).
+// One warp's share, tiles at .. at_end - 1 of the call's (the CTA's are cta_at .. cta_end - 1), the first of them of job j.
+// to_piece: whatever it has of a job is put together with others'.
 template <int DP, bool EXACT>
-__device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, const int *bases, const AttnShares &shares, int cta_at, int cta_end,
-                                        int at, int at_end, uint8_t *mine, FqSegment *segs, uint8_t *piece, FqPiece *pieces) {
+__device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, const int *bases, const AttnJob &j, int cta_at, int cta_end,
+                                        int at, int at_end, bool to_piece, uint8_t *mine, FqSegment *segs, uint8_t *piece, FqPiece *pieces) {
     using Cfg = FqCfg<DP>;
     constexpr int NC = DP / 16;
     constexpr int KW = DP / 32, KG = DP / 64;        // words of codes and scales of a lane's quarter of a key
@@ -334,11 +335,7 @@ __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, co
         if ((t4 * KG + i) * 16 < p.d) k_groups |= 0xffu << (8 * i);
     const uint32_t v_groups = (DP == 64 ? g >> 1 : g * VG) * 16 < p.d ? 0x80808080u : 0u;
 
-    {
-        const AttnJob j = attn_find(p, bases, at);
-        if (threadIdx.x == 0) attn_note_cut(p, shares, j, at, min(cta_end, j.g1));
-        fq_fill(p, segs[0], j, at, min(at_end, j.g1));
-    }
+    fq_fill(p, segs[0], j, at, min(at_end, j.g1));
     FqCopies<DP, EXACT> copies(p, x, segs, bases, at_end);
     int slot = 0;   // buffer of the tile at work
 #pragma unroll
@@ -534,7 +531,7 @@ __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, co
         // The result: a lane has an eighth of the entries of two rows.  What the CTA has of the job, all of it here: to the output or
         // the partials; else to the pieces.
         const int job_at = max(seg.j.g0, cta_at), job_end = min(seg.j.g1, cta_end);
-        const bool first = job_at == seg.j.g0, whole = first && job_end == seg.j.g1, alone = seg.at == job_at && seg.stop == job_end;
+        const bool first = job_at == seg.j.g0, whole = first && job_end == seg.j.g1, alone = seg.at == job_at && seg.stop == job_end && !to_piece;
         const bool last_one = seg.stop >= at_end;
         if (!alone) {
             if (last_one && at_seg > 0) {   // (nothing is on its way into the ring any more, and nothing read from it)
@@ -635,28 +632,168 @@ static __device__ __noinline__ void fq_join_pieces(const AttnPlan &p, const Attn
     }
 }
 
+// A call whose jobs go to the CTAs, or clusters of them, whole, so that nothing is left to join.  First job of every sequence into bases[0 .. n_seq], by all threads.
+static __device__ __noinline__ void fq_scan_jobs(const AttnPlan &p, int *bases) {
+    const int lane = threadIdx.x & 31;
+    for (int s = threadIdx.x; s < p.n_seq; s += blockDim.x) bases[s] = ceil_div(attn_seq(p, s).nq, p.block_tokens) * p.hkv;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        int sum = 0;
+        for (int s0 = 0; s0 < p.n_seq; s0 += 32) {
+            const int mine = s0 + lane < p.n_seq ? bases[s0 + lane] : 0;
+            int upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            if (s0 + lane < p.n_seq) bases[s0 + lane] = sum + upto - mine;
+            sum += __shfl_sync(0xffffffffu, upto, 31);
+        }
+        if (lane == 0) bases[p.n_seq] = sum;
+    }
+    __syncthreads();
+}
+// Job i of such a call; its tiles begin at 0.
+static __device__ __noinline__ AttnJob fq_whole_job(const AttnPlan &p, const int *bases, int i) {
+    int lo = 0, hi = p.n_seq;  // bases[lo] <= i < bases[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (bases[mid] <= i) lo = mid; else hi = mid;
+    }
+    const int of = i - bases[lo], block = (int)((uint32_t)of / (uint32_t)p.hkv);
+    return attn_own_job(p, attn_seq(p, lo), lo, of - block * p.hkv, block, 0);
+}
+
+
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// m and l of a row and four entries of its results, from a piece of any CTA of the cluster.
+struct FqPart {
+    float2 ml;
+    float4 o;
+};
+__device__ __forceinline__ FqPart fq_remote(uint32_t ml, uint32_t o, int rank) {
+    FqPart v;
+    asm volatile("{\n\t.reg .u32 a, b;\n\tmapa.shared::cluster.u32 a, %6, %8;\n\tmapa.shared::cluster.u32 b, %7, %8;\n\t"
+                 "ld.shared::cluster.v2.f32 {%0, %1}, [a];\n\tld.shared::cluster.v4.f32 {%2, %3, %4, %5}, [b];\n\t}"
+                 : "=f"(v.ml.x), "=f"(v.ml.y), "=f"(v.o.x), "=f"(v.o.y), "=f"(v.o.z), "=f"(v.o.w)
+                 : "r"(ml), "r"(o), "r"(rank)
+                 : "memory");
+    return v;
+}
+// A running sum of parts, scaled by the largest m so far.
+struct FqSum {
+    float M = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    __device__ __forceinline__ void add(const FqPart &v) {
+        const float m = fmaxf(M, v.ml.x), f = m == -INFINITY ? 0.f : fast_exp2(M - m), w = v.ml.x == -INFINITY ? 0.f : fast_exp2(v.ml.x - m);
+        M = m;
+        l = fmaf(l, f, w * v.ml.y);
+        o.x *= f, o.y *= f, o.z *= f, o.w *= f;
+        if (w != 0.f) {   // (a part in which the row sees nothing has no results)
+            o.x = fmaf(w, v.o.x, o.x);
+            o.y = fmaf(w, v.o.y, o.y);
+            o.z = fmaf(w, v.o.z, o.z);
+            o.w = fmaf(w, v.o.w, o.w);
+        }
+    }
+};
+__device__ __forceinline__ void fq_output(const AttnPlan &p, const AttnData &x, const PartJob &j, int r, int e, const FqSum &s) {
+    const int tok = attn_row_token(p, r);
+    const float inv = s.M == -INFINITY ? 0.f : 1.0f / s.l;
+    *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(x.out) + (j.tok0 + tok) * x.ld_out + (j.head * p.group + r - tok * p.group) * p.d + e) =
+        make_uint2(fq_pack(s.o.x * inv, s.o.y * inv), fq_pack(s.o.z * inv, s.o.w * inv));
+}
+// A whole job's pieces put together: those of the CTA's first n warps, then the sums of the cluster's CTAs, which are left in the ring.
+template <int DP>
+static __device__ __noinline__ void fq_join_whole(const AttnPlan &p, const AttnData &x, uint8_t *smem_raw, const AttnJob &j, int n, int cluster, int rank) {
+    using Cfg = FqCfg<DP>;
+    const int items = j.rows * (DP / 4);
+    // (a part of the pieces to each of four neighbouring threads, where there are enough)
+    const int per = 4 * items <= Cfg::THREADS ? 4 : 1;
+    for (int i = threadIdx.x; i < items * per; i += Cfg::THREADS) {
+        const int item = i / per, r = item / (DP / 4), e = item % (DP / 4) * 4;
+        FqSum s;
+#pragma unroll 4
+        for (int w = i % per; w < n; w += per) {
+            const float *const from = reinterpret_cast<const float *>(smem_raw + Cfg::PIECES_AT + w * Cfg::PIECE);
+            s.add(FqPart{*reinterpret_cast<const float2 *>(from + 2 * r), *reinterpret_cast<const float4 *>(from + 2 * FQ_ROWS + r * Cfg::LDO + e)});
+        }
+        for (int o = 1; o < per; o *= 2) {   // (one turn, of whole warps)
+            FqPart v;
+            v.ml = make_float2(__shfl_xor_sync(0xffffffffu, s.M, o), __shfl_xor_sync(0xffffffffu, s.l, o));
+            v.o = make_float4(__shfl_xor_sync(0xffffffffu, s.o.x, o), __shfl_xor_sync(0xffffffffu, s.o.y, o), __shfl_xor_sync(0xffffffffu, s.o.z, o),
+                              __shfl_xor_sync(0xffffffffu, s.o.w, o));
+            s.add(v);
+        }
+        if (i % per != 0) continue;
+        if (cluster == 1) {
+            if (e < p.d) fq_output(p, x, j, r, e, s);
+        } else {
+            float *const to = reinterpret_cast<float *>(smem_raw);
+            if (e == 0) *reinterpret_cast<float2 *>(to + 2 * r) = make_float2(s.M, s.l);
+            *reinterpret_cast<float4 *>(to + 2 * FQ_ROWS + r * Cfg::LDO + e) = s.o;
+        }
+    }
+    if (cluster == 1) return;
+    cluster_meet();
+    const uint32_t base = smem_u32(smem_raw);
+    for (int i = threadIdx.x * cluster + rank; i < items; i += Cfg::THREADS * cluster) {
+        const int r = i / (DP / 4), e = i % (DP / 4) * 4;
+        if (e >= p.d) continue;
+        FqSum s;
+#pragma unroll 4
+        for (int c = 0; c < cluster; ++c) s.add(fq_remote(base + 8 * r, base + 4 * (2 * FQ_ROWS + r * Cfg::LDO + e), c));
+        fq_output(p, x, j, r, e, s);
+    }
+    cluster_meet();   // (nobody leaves, or writes again, while its sum is read)
+}
+
+// cluster: 0: the call's tiles are dealt out evenly to the CTAs; else so many CTAs, side by side, take a job whole.
 template <int DP, bool EXACT>
 __global__ void __launch_bounds__(FqCfg<DP>::THREADS, 1) attn_few_q4_kernel(const __grid_constant__ AttnPlan p,
-                                                                          const __grid_constant__ AttnData x) {
+                                                                          const __grid_constant__ AttnData x, const int cluster) {
     using Cfg = FqCfg<DP>;
     extern __shared__ __align__(128) uint8_t smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint8_t *const mine = smem_raw + warp * (Cfg::STAGES * Cfg::STAGE);
+    uint8_t *const mine = smem_raw + warp * (Cfg::STAGES * Cfg::STAGE), *const piece = smem_raw + Cfg::PIECES_AT + warp * Cfg::PIECE;
     FqSegment *const segs = reinterpret_cast<FqSegment *>(smem_raw + Cfg::SEGS_AT) + warp * FQ_SEGS;
     FqPiece *const all_pieces = reinterpret_cast<FqPiece *>(smem_raw + Cfg::SEGS_AT + Cfg::WARPS * FQ_SEGS * sizeof(FqSegment));
     int *const bases = reinterpret_cast<int *>(all_pieces + 2 * Cfg::WARPS);
     pdl_launch_dependents();
     pdl_wait_prior_grids();
+    if (cluster != 0) {
+        fq_scan_jobs(p, bases);
+        const int rank = blockIdx.x % cluster;
+#pragma unroll 1
+        for (int i = blockIdx.x / cluster; i < bases[p.n_seq]; i += gridDim.x / cluster) {
+            const AttnJob j = fq_whole_job(p, bases, i);
+            // the CTA's tiles, and this warp's of them
+            const AttnShares of_cta(j.g1, cluster);
+            const int cta_at = rank < of_cta.G ? of_cta.first(rank) : 0, cta_end = rank < of_cta.G ? of_cta.first(rank + 1) : 0;
+            const AttnShares of_warp(cta_end - cta_at, Cfg::WARPS);
+            if (warp < of_warp.G)
+                fq_work<DP, EXACT>(p, x, bases, j, cta_at, cta_end, cta_at + of_warp.first(warp), cta_at + of_warp.first(warp + 1), true, mine, segs,
+                                   piece, all_pieces + 2 * warp);
+            __syncthreads();
+            fq_join_whole<DP>(p, x, smem_raw, j, of_warp.G, cluster, rank);
+            __syncthreads();   // the pieces may be written again
+        }
+        return;
+    }
     attn_scan(p, bases);
     const AttnShares shares(bases[p.n_seq], p.grid);
     if ((int)blockIdx.x >= shares.G) return;
-    // the CTA's tiles, and this warp's of them
     const int cta_at = shares.first(blockIdx.x), cta_end = shares.first(blockIdx.x + 1);
-    const AttnShares mine_of(cta_end - cta_at, Cfg::WARPS);
+    const AttnShares of_warp(cta_end - cta_at, Cfg::WARPS);
     if (lane < 2) all_pieces[2 * warp + lane].rows = 0;
-    if (warp < mine_of.G) {
-        fq_work<DP, EXACT>(p, x, bases, shares, cta_at, cta_end, cta_at + mine_of.first(warp), cta_at + mine_of.first(warp + 1), mine, segs,
-                           smem_raw + Cfg::PIECES_AT + warp * Cfg::PIECE, all_pieces + 2 * warp);
+    if (warp < of_warp.G) {
+        const int at = cta_at + of_warp.first(warp);
+        const AttnJob j = attn_find(p, bases, at);
+        if (threadIdx.x == 0) attn_note_cut(p, shares, j, at, min(cta_end, j.g1));
+        fq_work<DP, EXACT>(p, x, bases, j, cta_at, cta_end, at, cta_at + of_warp.first(warp + 1), false, mine, segs, piece, all_pieces + 2 * warp);
     }
     __syncthreads();
     fq_join_pieces<DP>(p, x, smem_raw, all_pieces);
@@ -666,21 +803,27 @@ AttnShape attn_few_q4_shape(int) {
     return {FQ_ROWS, 1, FQ_KEYS, 0};
 }
 
-template <int DP> static griffin_status launch_dp(AttnPlan p, AttnData x, cudaStream_t stream) {
+template <int DP> static griffin_status launch_dp(AttnPlan p, AttnData x, int jobs, int cluster, cudaStream_t stream) {
     const void *fn = p.d == DP ? reinterpret_cast<const void *>(attn_few_q4_kernel<DP, true>)
                                : reinterpret_cast<const void *>(attn_few_q4_kernel<DP, false>);
     const size_t smem = FqCfg<DP>::smem(p.n_seq);
     if (ensure_dynamic_smem(fn, smem) != cudaSuccess) return GRIFFIN_ERR_CUDA;
-    void *args[] = {&p, &x};
-    return launch_maybe_overlapped(fn, dim3(p.grid), dim3(FqCfg<DP>::THREADS), smem, stream, true, args) == cudaSuccess
-               ? GRIFFIN_OK
-               : GRIFFIN_ERR_CUDA;
+    void *args[] = {&p, &x, &cluster};
+    const dim3 block(FqCfg<DP>::THREADS);
+    const cudaError_t e = cluster > 1 ? launch_clusters(fn, dim3(jobs * cluster), block, cluster, smem, stream, args)
+                                      : launch_maybe_overlapped(fn, dim3(cluster == 1 ? jobs : p.grid), block, smem, stream, true, args);
+    return e == cudaSuccess ? GRIFFIN_OK : GRIFFIN_ERR_CUDA;
 }
 
-griffin_status launch_attn_few_q4(const AttnPlan &plan, const AttnData &data, cudaStream_t stream) {
-    if (plan.d <= 64) return launch_dp<64>(plan, data, stream);
-    if (plan.d <= 128) return launch_dp<128>(plan, data, stream);
-    return launch_dp<256>(plan, data, stream);
+griffin_status launch_attn_few_q4(const AttnPlan &plan, const AttnData &data, int jobs, int cluster, cudaStream_t stream) {
+    AttnPlan p = plan;
+    if (cluster > 0) {   // (a job has the prefix's keys and the sequence's own)
+        p.fused = 1;
+        p.prefix_blocks = 0;
+    }
+    if (p.d <= 64) return launch_dp<64>(p, data, jobs, cluster, stream);
+    if (p.d <= 128) return launch_dp<128>(p, data, jobs, cluster, stream);
+    return launch_dp<256>(p, data, jobs, cluster, stream);
 }
 
 }  // namespace griffin

@@ -317,6 +317,24 @@ cudaError_t launch_maybe_overlapped(const void *func, dim3 grid, dim3 block, siz
     return cudaLaunchKernelExC(&cfg, func, args);
 }
 
+cudaError_t launch_clusters(const void *func, dim3 grid, dim3 block, int cluster, size_t smem, cudaStream_t stream, void **args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    count_launches(1);
+    return cudaLaunchKernelExC(&cfg, func, args);
+}
+
 #ifndef GRIFFIN_DEC_STAGE_KB
 #define GRIFFIN_DEC_STAGE_KB 96
 #endif

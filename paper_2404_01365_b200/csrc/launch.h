@@ -21,6 +21,8 @@ void count_launches(int n);
 // anything that kernel writes.
 cudaError_t launch_maybe_overlapped(const void *func, dim3 grid, dim3 block, size_t smem, cudaStream_t stream, bool overlap,
                                     void **args);
+// The same overlapped, in clusters of `cluster` CTAs along x.
+cudaError_t launch_clusters(const void *func, dim3 grid, dim3 block, int cluster, size_t smem, cudaStream_t stream, void **args);
 
 // Raises the opt-in dynamic shared memory limit of `fn` on the current device when needed.
 cudaError_t ensure_dynamic_smem(const void *fn, size_t bytes);
