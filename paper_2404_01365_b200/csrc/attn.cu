@@ -48,13 +48,20 @@ struct WholeFit {
     double base, slope, slack;   // slack: how far base may be from the fit of cut calls, which lies low for the fewest jobs
 };
 constexpr WholeFit WHOLE_FITS[] = {{1, 148, 7.8, 0.0050, 0.0}, {2, 72, 8.7, 0.0026, 1.4}, {4, 32, 9.0, 0.00138, 0.0}, {8, 8, 9.4, 0.00068, 5.0}};
+// Query heads of a block of that kernel: all of a key head, or an even part of them.
+static int few_group(const griffin_attn_desc *desc) {
+    const int group = desc->n_q_heads / desc->n_kv_heads;
+    int n = group < 8 ? group : 8;
+    while (group % n != 0) --n;
+    return n;
+}
 struct WholeJobs {
     int jobs, cluster;   // cluster 0: not whole
     double us;
 };
 static WholeJobs attn_whole(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
-    const int block_tokens = 8 / (desc->n_q_heads / desc->n_kv_heads);
-    const long long n = batch->n_seq, blocks = batch->n_tokens <= n ? n : n + batch->n_tokens / block_tokens, jobs = blocks * desc->n_kv_heads;
+    const int group = few_group(desc), block_tokens = 8 / group;
+    const long long n = batch->n_seq, blocks = batch->n_tokens <= n ? n : n + batch->n_tokens / block_tokens, jobs = blocks * (desc->n_q_heads / group);
     // (keys 128 wide, of the longest job)
     const double keys = ((double)batch->prefix_len + (double)batch->table_stride * desc->page_size) * (desc->head_dim / 128.0);
     WholeJobs best{0, 0, 0.0};
@@ -78,7 +85,8 @@ static WholeJobs attn_whole(const griffin_attn_desc *desc, const griffin_attn_ba
 constexpr double FQ_WHOLE_US = 17, FQ_FEW_KEYS = 72000, FQ_KEYS_PER_SEQ = 800, FQ_KEYS_PER_CALL = 24000;
 static bool attn_few_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
     const int group = desc->n_q_heads / desc->n_kv_heads;
-    if (desc->dtype != GRIFFIN_DT_BF16 || group > 8) return false;
+    if (desc->dtype != GRIFFIN_DT_BF16) return true;   // (the only one for fp32)
+    if (group > 8) return false;
     const long long rows = (long long)batch->n_tokens * group, n = batch->n_seq;
     const double blocks = (double)((rows + 7) / 8), prefix = batch->prefix_len, room = (double)batch->table_stride * desc->page_size;
     const double hkv = desc->n_kv_heads, width = desc->head_dim / 128.0;
@@ -89,8 +97,9 @@ static bool attn_few_q4(const griffin_attn_desc *desc, const griffin_attn_batch 
     return n == 1 || (blocks - 1) * prefix * width <= FQ_KEYS_PER_SEQ * n + FQ_KEYS_PER_CALL / hkv;
 }
 static AttnShape shape_of(const griffin_attn_desc *desc, bool few, bool q4) {
+    if (few && q4) return attn_few_q4_shape();
     if (desc->dtype == GRIFFIN_DT_F32) return attn_simt_shape(desc->head_dim);
-    return !few ? attn_tc_shape(desc->head_dim) : q4 ? attn_few_q4_shape(desc->head_dim) : attn_few_shape(desc->head_dim);
+    return few ? attn_few_shape(desc->head_dim) : attn_tc_shape(desc->head_dim);
 }
 
 struct AttnScratch {
@@ -111,13 +120,14 @@ static AttnScratch attn_scratch(const griffin_attn_desc *desc, const AttnShape &
     return s;
 }
 
-// (the two kernels for few rows have the same scratch)
+// (the kernel for few rows over a cache in 4 bits has the scratch of the other one, less than that of fp32)
 size_t attn_scratch_bytes(const griffin_attn_desc *desc, int n_tokens, int n_seq) {
     const size_t a = attn_scratch(desc, shape_of(desc, false, false), n_tokens, n_seq).total, b = attn_scratch(desc, shape_of(desc, true, false), n_tokens, n_seq).total;
     return a > b ? a : b;
 }
 
-static AttnPlan make_plan(const griffin_attn_desc *desc, const griffin_attn_batch *batch, int n_pages, int sms, const AttnShape &sh,
+// group: query heads of a block, a part of those of a key head.
+static AttnPlan make_plan(const griffin_attn_desc *desc, const griffin_attn_batch *batch, int n_pages, int sms, const AttnShape &sh, int group,
                           uint8_t *scratch, void *ws) {
     AttnPlan p{};
     p.q_start = batch->q_start; p.seq_len = batch->seq_len; p.page_table = batch->page_table;
@@ -125,11 +135,12 @@ static AttnPlan make_plan(const griffin_attn_desc *desc, const griffin_attn_batc
     p.n_seq = batch->n_seq; p.n_tokens = batch->n_tokens; p.table_stride = batch->table_stride;
     p.prefix_len = batch->prefix_len; p.n_pages = n_pages;
     while ((1 << p.page_shift) < desc->page_size) ++p.page_shift;
-    p.hq = desc->n_q_heads; p.hkv = desc->n_kv_heads; p.group = p.hq / p.hkv;
+    p.hq = desc->n_q_heads; p.hkv = p.hq / group; p.group = group;
     p.group_inv = (65536u + p.group - 1) / p.group;
     p.d = desc->head_dim;
-    p.fused = attn_fused(p.n_seq, p.n_tokens, p.group, p.prefix_len);
-    p.by_token = attn_by_token(p.n_seq, p.n_tokens, p.group);
+    // (by all of a key head's rows, as the scratch is; the kernel whose groups are parts keeps partials by row by token only)
+    p.fused = attn_fused(p.n_seq, p.n_tokens, desc->n_q_heads / desc->n_kv_heads, p.prefix_len);
+    p.by_token = attn_by_token(p.n_seq, p.n_tokens, desc->n_q_heads / desc->n_kv_heads);
     p.alt = sh.alt;
     p.tile_tokens = sh.tile_rows / p.group;
     p.tiles_per_block = sh.tiles_per_block;
@@ -157,22 +168,25 @@ static griffin_status launch(const griffin_attn_desc *desc, const griffin_attn_b
                              bool q4, uint8_t *scratch, void *ws, cudaStream_t stream) {
     const int sms = device_sm_count();
     if (sms <= 0) return GRIFFIN_ERR_CUDA;
-    const AttnPlan p = make_plan(desc, batch, n_pages, sms, shape_of(desc, few, q4), scratch, ws);
+    const int group = few && q4 ? few_group(desc) : desc->n_q_heads / desc->n_kv_heads;
+    const AttnPlan p = make_plan(desc, batch, n_pages, sms, shape_of(desc, few, q4), group, scratch, ws);
+    griffin_status st;
     if (few && q4) {
         const WholeJobs whole = attn_whole(desc, batch);
-        if (whole.cluster > 0) return launch_attn_few_q4(p, x, whole.jobs, whole.cluster, stream);
+        st = launch_attn_few_q4(p, x, desc->dtype, whole.jobs, whole.cluster, stream);
+        if (whole.cluster > 0) return st;
+    } else {
+        st = desc->dtype == GRIFFIN_DT_F32 ? launch_attn_simt(p, x, stream)
+             : few                         ? launch_attn_few(p, x, stream)
+                                           : launch_attn_tc(p, x, q4, stream);
     }
-    const griffin_status st = desc->dtype == GRIFFIN_DT_F32 ? launch_attn_simt(p, x, q4, stream)
-                              : !few                        ? launch_attn_tc(p, x, q4, stream)
-                              : q4                          ? launch_attn_few_q4(p, x, 0, 0, stream)
-                                                            : launch_attn_few(p, x, stream);
     return st != GRIFFIN_OK ? st : launch_attn_join(p, desc->dtype, x.out, x.ld_out, stream);
 }
 
 griffin_status launch_attn_prefix(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
                                   const griffin_kv_cache *cache, const void *q, int64_t ld_q, void *out, int64_t ld_out,
                                   uint8_t *scratch, void *ws, cudaStream_t stream) {
-    const AttnData x{q, cache->k, cache->v, out, ld_q, ld_out, cache->stride_page, cache->stride_head, cache->stride_token, {}};
+    const AttnData x{q, cache->k, cache->v, out, ld_q, ld_out, cache->stride_page, cache->stride_head, cache->stride_token, {}, 1};
     return launch(desc, batch, x, cache->n_pages, attn_few(desc, batch), false, scratch, ws, stream);
 }
 
@@ -180,7 +194,7 @@ griffin_status launch_attn_prefix_q4(const griffin_attn_desc *desc, const griffi
                                      const griffin_kv_cache_q4 *cache, const void *q, int64_t ld_q, void *out, int64_t ld_out,
                                      uint8_t *scratch, void *ws, cudaStream_t stream) {
     const AttnData x{q, cache->k, cache->v, out, ld_q, ld_out, cache->stride_page, cache->stride_head, 0,
-                     q4_layout(desc->head_dim, desc->page_size)};
+                     q4_layout(desc->head_dim, desc->page_size), desc->n_q_heads / desc->n_kv_heads / few_group(desc)};
     return launch(desc, batch, x, cache->n_pages, attn_few_q4(desc, batch), true, scratch, ws, stream);
 }
 

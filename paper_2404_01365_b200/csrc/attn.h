@@ -12,6 +12,7 @@ struct AttnData {
     void *out;
     long long ld_q, ld_out, stride_page, stride_head, stride_token;   // of a cache held in 4 bits: in bytes
     Q4Layout q4;
+    int heads_per_key;   // of the plan's key heads, how many share a key (attn_few_q4.cu)
 };
 
 // How a kernel cuts its work (see attn_plan.cuh).
@@ -76,12 +77,12 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there
 AttnShape attn_simt_shape(int head_dim);
 AttnShape attn_tc_shape(int head_dim);
 AttnShape attn_few_shape(int head_dim);
-AttnShape attn_few_q4_shape(int head_dim);
+AttnShape attn_few_q4_shape();
 griffin_status launch_attn_tc(const AttnPlan &plan, const AttnData &data, bool q4, cudaStream_t stream);  // bf16; q4: the cache in 4 bits
 griffin_status launch_attn_few(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // bf16, few rows
 // and the cache in 4 bits; cluster > 0: so many CTAs take each of at most `jobs` jobs whole, the prefix's keys with them, and no partials
 // are left
-griffin_status launch_attn_few_q4(const AttnPlan &plan, const AttnData &data, int jobs, int cluster, cudaStream_t stream);
-griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, bool q4, cudaStream_t stream);  // fp32; q4: the cache in 4 bits
+griffin_status launch_attn_few_q4(const AttnPlan &plan, const AttnData &data, int dtype, int jobs, int cluster, cudaStream_t stream);
+griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, cudaStream_t stream);  // fp32
 
 }  // namespace griffin

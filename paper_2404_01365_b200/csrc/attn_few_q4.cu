@@ -1,4 +1,4 @@
-// Attention over a cache held in 4 bits (q4.cuh), bf16 queries, blocks of up to 8 query rows.  The mathematics is attn_few.cu's:
+// Attention over a cache held in 4 bits (q4.cuh), bf16 or fp32 queries, blocks of up to 8 query rows.  The mathematics is attn_few.cu's:
 // S^T = K Q^T and O^T = V^T P^T on m16n8k16, a warp with its own m, l and O.
 //
 // The keys are unpacked between shared memory and the matrix instruction: codes become bf16 values, exactly, with a
@@ -19,6 +19,8 @@
 // the walk and the look for a new maximum (which is not exchanged while the sums, in fp32, stay below 2^8) cost as much
 // as the products for 16 keys, so a warp takes 32 at a time: the instructions that it issues are what bounds this kernel,
 // those of the integer pipe, every other clock, first.
+// fp32 calls run on the same instruction: keys and values are exact in bf16, a query's entry and P are sums of three bf16 numbers, so
+// three products of each kind replace one; the unpacking is shared.
 #include "attn.h"
 #include "attn_join.cuh"
 #include "decode_mma.cuh"
@@ -28,9 +30,11 @@ namespace griffin {
 constexpr int FQ_ROWS = 8, FQ_KEYS = 32;  // query rows of a block; keys of a tile
 constexpr float FQ_SLACK = 8.f;  // how far (log2) the true maximum may run ahead of the one P is scaled by
 
-// DP: the head's width rounded up to 64, 128 or 256.
-template <int DP> struct FqCfg {
-    static constexpr int WARPS = DP == 256 ? 8 : 16, THREADS = 32 * WARPS, STAGES = 2;
+// DP: the head's width rounded up to 64, 128 or 256.  T: of queries and output.
+template <int DP, typename T> struct FqCfg {
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int PARTS = F32 ? 3 : 1;   // bf16 numbers that a query's entry, or P, is the sum of
+    static constexpr int WARPS = DP == 256 || (F32 && DP == 128) ? 8 : 16, THREADS = 32 * WARPS, STAGES = 2;
     // rows of codes and scales in shared memory
     static constexpr int KROW = DP == 256 ? 144 : DP / 2, VROW = DP / 2, SROW = DP / 16;
     static constexpr int V_AT = FQ_KEYS * KROW, KS_AT = V_AT + FQ_KEYS * VROW, VS_AT = KS_AT + FQ_KEYS * SROW, STAGE = VS_AT + FQ_KEYS * SROW;
@@ -102,7 +106,7 @@ struct FqPiece {
     int rows, begin, end;   // rows 0: none; begin: whether it is the first; end: whether it is the last
     int first, whole;       // of what the CTA has of the job: it has the job's first tile; all of them
 };
-template <int DP> size_t FqCfg<DP>::smem(int n_seq) {
+template <int DP, typename T> size_t FqCfg<DP, T>::smem(int n_seq) {
     return SEGS_AT + WARPS * (FQ_SEGS * sizeof(FqSegment) + 2 * sizeof(FqPiece)) + ((size_t)n_seq + 3) * 4;
 }
 
@@ -155,8 +159,8 @@ struct FqWalk {
 };
 
 // Eight keys of a page that is not there read as zeros; by the eight lanes that bring them.
-template <int DP> static __device__ __noinline__ void fq_no_page(void *ws, uint32_t buf, int first) {
-    using Cfg = FqCfg<DP>;
+template <int DP, typename T> static __device__ __noinline__ void fq_no_page(void *ws, uint32_t buf, int first) {
+    using Cfg = FqCfg<DP, T>;
     raise_status(ws, DEV_STATUS_BAD_INDEX, 42);
     const auto put = [](uint32_t at, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); };
     for (int i = threadIdx.x & 7; i < 8 * (DP / 8); i += 8) {
@@ -173,8 +177,8 @@ template <int DP> static __device__ __noinline__ void fq_no_page(void *ws, uint3
 // What brings a warp's keys, STAGES - 1 tiles ahead of the products, from segment to segment.  Eight lanes have eight of the 32
 // keys, which are of one page.  The pages are looked up a tile earlier still.
 // EXACT: the head is DP wide, so that the rows' distances are constants.
-template <int DP, bool EXACT> struct FqCopies {
-    using Cfg = FqCfg<DP>;
+template <int DP, bool EXACT, typename T> struct FqCopies {
+    using Cfg = FqCfg<DP, T>;
     static constexpr int PPR = DP / 32, RP = 8 / PPR;     // 16-byte pieces of a key's codes; keys that 8 lanes bring at once
     static constexpr int WPR = DP / 64, RS = 8 / WPR;     // 4-byte pieces of a key's scales; keys at once
     const AttnPlan &p;
@@ -215,7 +219,7 @@ template <int DP, bool EXACT> struct FqCopies {
         own_pages = p.page_table + (long long)s.j.seq * p.table_stride;
         own0 = s.own0;
         own1 = s.own1;
-        head = s.j.head * x.stride_head;
+        head = (s.j.head / x.heads_per_key) * x.stride_head;
         at.begin(s);
         look_up();
     }
@@ -260,7 +264,7 @@ template <int DP, bool EXACT> struct FqCopies {
                 }
             }
         } else if (key < at.end) {
-            fq_no_page<DP>(p.ws, buf, first());
+            fq_no_page<DP, T>(p.ws, buf, first());
         }
     }
     // Asks for the tile that is next, if there is one, and goes on to the one behind it.
@@ -282,8 +286,8 @@ template <int DP, bool EXACT> struct FqCopies {
 
 // The scales of values that must not be multiplied with, since 0 * NaN would reach the sum, become finite: of keys from `from`
 // on (none of the block's rows sees them, or not all do).  Whether any of the latter was NaN.
-template <int DP> static __device__ __noinline__ bool fq_clear_scales(uint8_t *scales, int from, int end, bool all) {
-    using Cfg = FqCfg<DP>;
+template <int DP, typename T> static __device__ __noinline__ bool fq_clear_scales(uint8_t *scales, int from, int end, bool all) {
+    using Cfg = FqCfg<DP, T>;
     bool found = false;
     __syncwarp();
     for (int i = threadIdx.x & 31; i < FQ_KEYS * Cfg::SROW; i += 32) {
@@ -299,29 +303,50 @@ template <int DP> static __device__ __noinline__ bool fq_clear_scales(uint8_t *s
     __syncwarp();
     return __any_sync(0xffffffffu, found);
 }
+// An fp32 number as a sum of bf16 ones, each the rest of those before to the nearest: 24 bits in three.
+template <int PARTS> __device__ __forceinline__ void fq_split(float a, float b, uint32_t (&to)[PARTS]) {
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        to[i] = fq_pack(a, b);
+        a -= __uint_as_float(to[i] << 16);
+        b -= __uint_as_float(to[i] & 0xffff0000u);
+    }
+}
 // The queries of a job as the first product takes them: row lane / 4, entries of quarter lane % 4.
-template <int DP>
-__device__ __forceinline__ void fq_queries(const AttnPlan &p, const AttnData &x, const AttnJob &j, uint32_t (&q)[DP / 16][2]) {
+template <int DP, typename T>
+__device__ __forceinline__ void fq_queries(const AttnPlan &p, const AttnData &x, const AttnJob &j, uint32_t (&q)[DP / 16][2][FqCfg<DP, T>::PARTS]) {
     const int lane = threadIdx.x & 31, r = lane >> 2, tok = attn_row_token(p, r);
-    const __nv_bfloat16 *const at = static_cast<const __nv_bfloat16 *>(x.q) + (j.tok0 + tok) * x.ld_q +
-                                    (j.head * p.group + r - tok * p.group) * p.d;
+    const T *const at = static_cast<const T *>(x.q) + (j.tok0 + tok) * x.ld_q + (j.head * p.group + r - tok * p.group) * p.d;
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) {
         const int e = (lane & 3) * (DP / 4) + 4 * c;
-        uint2 v = make_uint2(0u, 0u);
-        if (r < j.rows && e < p.d) v = *reinterpret_cast<const uint2 *>(at + e);
-        q[c][0] = v.x;
-        q[c][1] = v.y;
+        const bool on = r < j.rows && e < p.d;
+        if constexpr (sizeof(T) == 2) {
+            uint2 v = make_uint2(0u, 0u);
+            if (on) v = *reinterpret_cast<const uint2 *>(at + e);
+            q[c][0][0] = v.x;
+            q[c][1][0] = v.y;
+        } else {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (on) v = *reinterpret_cast<const float4 *>(at + e);
+            fq_split(v.x, v.y, q[c][0]);
+            fq_split(v.z, v.w, q[c][1]);
+        }
     }
+}
+// Four entries of a row to the output.
+template <typename T> __device__ __forceinline__ void fq_store4(T *to, float a, float b, float c, float d) {
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(to) = make_uint2(fq_pack(a, b), fq_pack(c, d));
+    else *reinterpret_cast<float4 *>(to) = make_float4(a, b, c, d);
 }
 
 // One warp's share, tiles at .. at_end - 1 of the call's (the CTA's are cta_at .. cta_end - 1), the first of them of job j.
 // to_piece: whatever it has of a job is put together with others'.
-template <int DP, bool EXACT>
+template <int DP, bool EXACT, typename T>
 __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, const int *bases, const AttnJob &j, int cta_at, int cta_end,
                                         int at, int at_end, bool to_piece, uint8_t *mine, FqSegment *segs, uint8_t *piece, FqPiece *pieces) {
-    using Cfg = FqCfg<DP>;
-    constexpr int NC = DP / 16;
+    using Cfg = FqCfg<DP, T>;
+    constexpr int NC = DP / 16, PARTS = Cfg::PARTS;
     constexpr int KW = DP / 32, KG = DP / 64;        // words of codes and scales of a lane's quarter of a key
     constexpr int VW = DP / 64, VG = DP == 256 ? 2 : 1;   // and of its eighth of a value
     const int lane = threadIdx.x & 31;
@@ -336,7 +361,7 @@ __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, co
     const uint32_t v_groups = (DP == 64 ? g >> 1 : g * VG) * 16 < p.d ? 0x80808080u : 0u;
 
     fq_fill(p, segs[0], j, at, min(at_end, j.g1));
-    FqCopies<DP, EXACT> copies(p, x, segs, bases, at_end);
+    FqCopies<DP, EXACT, T> copies(p, x, segs, bases, at_end);
     int slot = 0;   // buffer of the tile at work
 #pragma unroll
     for (int i = 0; i < Cfg::STAGES - 1; ++i) copies.go(ring + i * Cfg::STAGE);
@@ -350,8 +375,8 @@ __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, co
     }
     const uint32_t vs_from = Cfg::VS_AT + t4 * Cfg::SROW + (DP == 64 ? g >> 1 : g * VG);
     const uint32_t magic = x.q4.magic;
-    uint32_t q[NC][2];
-    fq_queries<DP>(p, x, segs[0].j, q);
+    uint32_t q[NC][2][PARTS];
+    fq_queries<DP, T>(p, x, segs[0].j, q);
 #pragma unroll 1
     for (int at_seg = 0;; ++at_seg) {
         const FqSegment &seg = segs[at_seg % FQ_SEGS];
@@ -375,7 +400,7 @@ __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, co
             const bool edge = t.key0 + FQ_KEYS > (t.pre ? t.end : min(t.end, seen0));
             if (edge) {
                 const bool apart = !t.pre && seen0 < t.end;
-                marked |= fq_clear_scales<DP>(mine + (buf - ring) + Cfg::VS_AT, apart ? max(seen0 - t.key0, 0) : t.end - t.key0, t.end - t.key0, !apart);
+                marked |= fq_clear_scales<DP, T>(mine + (buf - ring) + Cfg::VS_AT, apart ? max(seen0 - t.key0, 0) : t.end - t.key0, t.end - t.key0, !apart);
             }
             float s[2][4];      // 16 keys each
             uint32_t bad = 0;   // bytes of 255 among the keys' scales
@@ -400,9 +425,12 @@ __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, co
                         b = fq_scale2(__byte_perm(ks[1], 0u, sel));
                     }
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        mma_bf16(s[u], q4_pair(kw[0][w], 2 * e, a, magic), q4_pair(kw[1][w], 2 * e, b, magic), q4_pair(kw[0][w], 2 * e + 1, a, magic),
-                                 q4_pair(kw[1][w], 2 * e + 1, b, magic), q[2 * w + e][0], q[2 * w + e][1]);
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t k0 = q4_pair(kw[0][w], 2 * e, a, magic), k1 = q4_pair(kw[1][w], 2 * e, b, magic),
+                                       k2 = q4_pair(kw[0][w], 2 * e + 1, a, magic), k3 = q4_pair(kw[1][w], 2 * e + 1, b, magic);
+#pragma unroll
+                        for (int i = PARTS - 1; i >= 0; --i) mma_bf16(s[u], k0, k1, k2, k3, q[2 * w + e][0][i], q[2 * w + e][1][i]);
+                    }
                 }
             }
             if (__any_sync(0xffffffffu, bad != 0)) {   // a group of a key is NaN, and so is the logit
@@ -469,8 +497,12 @@ __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, co
                     fq_lds(vw[h], buf + v_from[h & 1] + (16 * u + (h >> 1) * 8) * Cfg::VROW);
                     vs[h] = fq_lds_bytes<VG>(buf + vs_from + (16 * u + 4 * h) * Cfg::SROW);
                 }
-                // (bf16, as the values are: 2^-8 of each P at most)
-                const uint32_t w0 = fq_movmatrix(fq_pack(s[u][0], s[u][1])), w1 = fq_movmatrix(fq_pack(s[u][2], s[u][3]));
+                // (P in bf16, as the values are: 2^-8 of each at most; fp32 calls in three parts)
+                uint32_t w0[PARTS], w1[PARTS];
+                fq_split(s[u][0], s[u][1], w0);
+                fq_split(s[u][2], s[u][3], w1);
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) w0[i] = fq_movmatrix(w0[i]), w1[i] = fq_movmatrix(w1[i]);
                 Q4Scale2 lo, hi;
                 const uint32_t s01 = vs[0] | vs[1] << 16, s23 = vs[2] | vs[3] << 16;
                 const uint32_t v_bad = VG == 2 ? fq_nan_bytes(s01) | fq_nan_bytes(s23) : fq_nan_bytes(s01 | s23 << 8);
@@ -483,9 +515,12 @@ __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, co
                     const uint32_t even0 = __byte_perm(vw[0][w], vw[1][w], 0x5410), odd0 = __byte_perm(vw[0][w], vw[1][w], 0x7632);
                     const uint32_t even1 = __byte_perm(vw[2][w], vw[3][w], 0x5410), odd1 = __byte_perm(vw[2][w], vw[3][w], 0x7632);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)   // entries 2e and 2e + 1 of the word
-                        mma_bf16(o[4 * w + e], q4_pair(even0, e, lo, magic), q4_pair(odd0, e, lo, magic), q4_pair(even1, e, hi, magic),
-                                 q4_pair(odd1, e, hi, magic), w0, w1);
+                    for (int e = 0; e < 4; ++e) {   // entries 2e and 2e + 1 of the word
+                        const uint32_t v0 = q4_pair(even0, e, lo, magic), v1 = q4_pair(odd0, e, lo, magic), v2 = q4_pair(even1, e, hi, magic),
+                                       v3 = q4_pair(odd1, e, hi, magic);
+#pragma unroll
+                        for (int i = PARTS - 1; i >= 0; --i) mma_bf16(o[4 * w + e], v0, v1, v2, v3, w0[i], w1[i]);
+                    }
                 }
                 if (__any_sync(0xffffffffu, (v_bad & v_groups) != 0)) {   // a group of values is NaN, for all rows (all of them see it)
 #pragma unroll
@@ -507,7 +542,7 @@ __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, co
             for (int k = max(seen0, seg.own0); k < seg.own1; ++k) {
                 const int page = __ldg(p.page_table + (long long)seg.j.seq * p.table_stride + (k >> p.page_shift));
                 if ((unsigned)page >= (unsigned)p.n_pages) continue;
-                const uint8_t *const scales = static_cast<const uint8_t *>(x.v) + page * x.stride_page + seg.j.head * x.stride_head +
+                const uint8_t *const scales = static_cast<const uint8_t *>(x.v) + page * x.stride_page + (seg.j.head / x.heads_per_key) * x.stride_head +
                                               x.q4.scale_off + (k & ((1 << p.page_shift) - 1)) * x.q4.scale_row;
                 const float nan = __uint_as_float(0x7fffffffu);
                 const bool sees_a = k < seen0 + attn_row_token(p, ra), sees_b = k < seen0 + attn_row_token(p, ra + 1);
@@ -551,14 +586,17 @@ __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, co
             if (alone && direct) {
                 const int tok = attn_row_token(p, r);
                 const float inv = m == -INFINITY ? 0.f : 1.0f / l;
-                __nv_bfloat16 *const to = static_cast<__nv_bfloat16 *>(x.out) + (seg.j.tok0 + tok) * x.ld_out +
-                                          (seg.j.head * p.group + r - tok * p.group) * p.d + e0;
+                T *const to = static_cast<T *>(x.out) + (seg.j.tok0 + tok) * x.ld_out + (seg.j.head * p.group + r - tok * p.group) * p.d + e0;
 #pragma unroll
-                for (int c = 0; c < NC; c += 4)
-                    if (EXACT || e0 + 2 * c < p.d)
-                        *reinterpret_cast<uint4 *>(to + 2 * c) =
-                            make_uint4(fq_pack(o[c][h] * inv, o[c][2 + h] * inv), fq_pack(o[c + 1][h] * inv, o[c + 1][2 + h] * inv),
-                                       fq_pack(o[c + 2][h] * inv, o[c + 2][2 + h] * inv), fq_pack(o[c + 3][h] * inv, o[c + 3][2 + h] * inv));
+                for (int c = 0; c < NC; c += Cfg::F32 ? 2 : 4)   // (16 bytes)
+                    if (EXACT || e0 + 2 * c < p.d) {
+                        if constexpr (sizeof(T) == 2)
+                            *reinterpret_cast<uint4 *>(to + 2 * c) =
+                                make_uint4(fq_pack(o[c][h] * inv, o[c][2 + h] * inv), fq_pack(o[c + 1][h] * inv, o[c + 1][2 + h] * inv),
+                                           fq_pack(o[c + 2][h] * inv, o[c + 2][2 + h] * inv), fq_pack(o[c + 3][h] * inv, o[c + 3][2 + h] * inv));
+                        else
+                            *reinterpret_cast<float4 *>(to + 2 * c) = make_float4(o[c][h] * inv, o[c][2 + h] * inv, o[c + 1][h] * inv, o[c + 1][2 + h] * inv);
+                    }
             } else {
                 PartPlace to{reinterpret_cast<float *>(piece) + 2 * r, reinterpret_cast<float *>(piece) + 2 * FQ_ROWS + r * Cfg::LDO};
                 if (alone) to = attn_place(p, seg.j, first, 0, r);
@@ -570,15 +608,15 @@ __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, co
             }
         }
         if (segs[(at_seg + 1) % FQ_SEGS].tiles == 0) return;
-        fq_queries<DP>(p, x, segs[(at_seg + 1) % FQ_SEGS].j, q);
+        fq_queries<DP, T>(p, x, segs[(at_seg + 1) % FQ_SEGS].j, q);
     }
 }
 
 // The pieces of jobs that went to several warps of the CTA, put together in their order: the output, or its partial.  As many
 // warps to a job as there are for each.
-template <int DP>
+template <int DP, typename T>
 static __device__ __noinline__ void fq_join_pieces(const AttnPlan &p, const AttnData &x, const uint8_t *smem_raw, const FqPiece *pieces) {
-    using Cfg = FqCfg<DP>;
+    using Cfg = FqCfg<DP, T>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // (lane i: piece i, in the order of the keys; a warp's first, then its last)
     const FqPiece mine = lane < 2 * Cfg::WARPS ? pieces[lane] : FqPiece{};
@@ -620,9 +658,8 @@ static __device__ __noinline__ void fq_join_pieces(const AttnPlan &p, const Attn
             if (p.fused && a.whole != 0) {
                 const int tok = attn_row_token(p, r);
                 const float inv = M == -INFINITY ? 0.f : 1.0f / sum;
-                *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(x.out) + (a.job.tok0 + tok) * x.ld_out +
-                                           (a.job.head * p.group + r - tok * p.group) * p.d + e) =
-                    make_uint2(fq_pack(acc.x * inv, acc.y * inv), fq_pack(acc.z * inv, acc.w * inv));
+                fq_store4(static_cast<T *>(x.out) + (a.job.tok0 + tok) * x.ld_out + (a.job.head * p.group + r - tok * p.group) * p.d + e, acc.x * inv,
+                          acc.y * inv, acc.z * inv, acc.w * inv);
             } else {
                 const PartPlace to = attn_place(p, a.job, a.first != 0, 0, r);
                 if (e == 0) *reinterpret_cast<float2 *>(to.ml) = make_float2(M, sum);
@@ -700,16 +737,16 @@ struct FqSum {
         }
     }
 };
-__device__ __forceinline__ void fq_output(const AttnPlan &p, const AttnData &x, const PartJob &j, int r, int e, const FqSum &s) {
+template <typename T> __device__ __forceinline__ void fq_output(const AttnPlan &p, const AttnData &x, const PartJob &j, int r, int e, const FqSum &s) {
     const int tok = attn_row_token(p, r);
     const float inv = s.M == -INFINITY ? 0.f : 1.0f / s.l;
-    *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(x.out) + (j.tok0 + tok) * x.ld_out + (j.head * p.group + r - tok * p.group) * p.d + e) =
-        make_uint2(fq_pack(s.o.x * inv, s.o.y * inv), fq_pack(s.o.z * inv, s.o.w * inv));
+    fq_store4(static_cast<T *>(x.out) + (j.tok0 + tok) * x.ld_out + (j.head * p.group + r - tok * p.group) * p.d + e, s.o.x * inv, s.o.y * inv,
+              s.o.z * inv, s.o.w * inv);
 }
 // A whole job's pieces put together: those of the CTA's first n warps, then the sums of the cluster's CTAs, which are left in the ring.
-template <int DP>
+template <int DP, typename T>
 static __device__ __noinline__ void fq_join_whole(const AttnPlan &p, const AttnData &x, uint8_t *smem_raw, const AttnJob &j, int n, int cluster, int rank) {
-    using Cfg = FqCfg<DP>;
+    using Cfg = FqCfg<DP, T>;
     const int items = j.rows * (DP / 4);
     // (a part of the pieces to each of four neighbouring threads, where there are enough)
     const int per = 4 * items <= Cfg::THREADS ? 4 : 1;
@@ -730,7 +767,7 @@ static __device__ __noinline__ void fq_join_whole(const AttnPlan &p, const AttnD
         }
         if (i % per != 0) continue;
         if (cluster == 1) {
-            if (e < p.d) fq_output(p, x, j, r, e, s);
+            if (e < p.d) fq_output<T>(p, x, j, r, e, s);
         } else {
             float *const to = reinterpret_cast<float *>(smem_raw);
             if (e == 0) *reinterpret_cast<float2 *>(to + 2 * r) = make_float2(s.M, s.l);
@@ -746,16 +783,16 @@ static __device__ __noinline__ void fq_join_whole(const AttnPlan &p, const AttnD
         FqSum s;
 #pragma unroll 4
         for (int c = 0; c < cluster; ++c) s.add(fq_remote(base + 8 * r, base + 4 * (2 * FQ_ROWS + r * Cfg::LDO + e), c));
-        fq_output(p, x, j, r, e, s);
+        fq_output<T>(p, x, j, r, e, s);
     }
     cluster_meet();   // (nobody leaves, or writes again, while its sum is read)
 }
 
 // cluster: 0: the call's tiles are dealt out evenly to the CTAs; else so many CTAs, side by side, take a job whole.
-template <int DP, bool EXACT>
-__global__ void __launch_bounds__(FqCfg<DP>::THREADS, 1) attn_few_q4_kernel(const __grid_constant__ AttnPlan p,
+template <int DP, bool EXACT, typename T>
+__global__ void __launch_bounds__(FqCfg<DP, T>::THREADS, 1) attn_few_q4_kernel(const __grid_constant__ AttnPlan p,
                                                                           const __grid_constant__ AttnData x, const int cluster) {
-    using Cfg = FqCfg<DP>;
+    using Cfg = FqCfg<DP, T>;
     extern __shared__ __align__(128) uint8_t smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t *const mine = smem_raw + warp * (Cfg::STAGES * Cfg::STAGE), *const piece = smem_raw + Cfg::PIECES_AT + warp * Cfg::PIECE;
@@ -775,10 +812,10 @@ __global__ void __launch_bounds__(FqCfg<DP>::THREADS, 1) attn_few_q4_kernel(cons
             const int cta_at = rank < of_cta.G ? of_cta.first(rank) : 0, cta_end = rank < of_cta.G ? of_cta.first(rank + 1) : 0;
             const AttnShares of_warp(cta_end - cta_at, Cfg::WARPS);
             if (warp < of_warp.G)
-                fq_work<DP, EXACT>(p, x, bases, j, cta_at, cta_end, cta_at + of_warp.first(warp), cta_at + of_warp.first(warp + 1), true, mine, segs,
+                fq_work<DP, EXACT, T>(p, x, bases, j, cta_at, cta_end, cta_at + of_warp.first(warp), cta_at + of_warp.first(warp + 1), true, mine, segs,
                                    piece, all_pieces + 2 * warp);
             __syncthreads();
-            fq_join_whole<DP>(p, x, smem_raw, j, of_warp.G, cluster, rank);
+            fq_join_whole<DP, T>(p, x, smem_raw, j, of_warp.G, cluster, rank);
             __syncthreads();   // the pieces may be written again
         }
         return;
@@ -793,37 +830,40 @@ __global__ void __launch_bounds__(FqCfg<DP>::THREADS, 1) attn_few_q4_kernel(cons
         const int at = cta_at + of_warp.first(warp);
         const AttnJob j = attn_find(p, bases, at);
         if (threadIdx.x == 0) attn_note_cut(p, shares, j, at, min(cta_end, j.g1));
-        fq_work<DP, EXACT>(p, x, bases, j, cta_at, cta_end, at, cta_at + of_warp.first(warp + 1), false, mine, segs, piece, all_pieces + 2 * warp);
+        fq_work<DP, EXACT, T>(p, x, bases, j, cta_at, cta_end, at, cta_at + of_warp.first(warp + 1), false, mine, segs, piece, all_pieces + 2 * warp);
     }
     __syncthreads();
-    fq_join_pieces<DP>(p, x, smem_raw, all_pieces);
+    fq_join_pieces<DP, T>(p, x, smem_raw, all_pieces);
 }
 
-AttnShape attn_few_q4_shape(int) {
+AttnShape attn_few_q4_shape() {
     return {FQ_ROWS, 1, FQ_KEYS, 0};
 }
 
-template <int DP> static griffin_status launch_dp(AttnPlan p, AttnData x, int jobs, int cluster, cudaStream_t stream) {
-    const void *fn = p.d == DP ? reinterpret_cast<const void *>(attn_few_q4_kernel<DP, true>)
-                               : reinterpret_cast<const void *>(attn_few_q4_kernel<DP, false>);
-    const size_t smem = FqCfg<DP>::smem(p.n_seq);
+template <int DP, typename T> static griffin_status launch_dp(AttnPlan p, AttnData x, int jobs, int cluster, cudaStream_t stream) {
+    const void *fn = p.d == DP ? reinterpret_cast<const void *>(attn_few_q4_kernel<DP, true, T>)
+                               : reinterpret_cast<const void *>(attn_few_q4_kernel<DP, false, T>);
+    const size_t smem = FqCfg<DP, T>::smem(p.n_seq);
     if (ensure_dynamic_smem(fn, smem) != cudaSuccess) return GRIFFIN_ERR_CUDA;
     void *args[] = {&p, &x, &cluster};
-    const dim3 block(FqCfg<DP>::THREADS);
+    const dim3 block(FqCfg<DP, T>::THREADS);
     const cudaError_t e = cluster > 1 ? launch_clusters(fn, dim3(jobs * cluster), block, cluster, smem, stream, args)
                                       : launch_maybe_overlapped(fn, dim3(cluster == 1 ? jobs : p.grid), block, smem, stream, true, args);
     return e == cudaSuccess ? GRIFFIN_OK : GRIFFIN_ERR_CUDA;
 }
 
-griffin_status launch_attn_few_q4(const AttnPlan &plan, const AttnData &data, int jobs, int cluster, cudaStream_t stream) {
+template <typename T> static griffin_status launch_type(const AttnPlan &p, const AttnData &data, int jobs, int cluster, cudaStream_t stream) {
+    if (p.d <= 64) return launch_dp<64, T>(p, data, jobs, cluster, stream);
+    if (p.d <= 128) return launch_dp<128, T>(p, data, jobs, cluster, stream);
+    return launch_dp<256, T>(p, data, jobs, cluster, stream);
+}
+griffin_status launch_attn_few_q4(const AttnPlan &plan, const AttnData &data, int dtype, int jobs, int cluster, cudaStream_t stream) {
     AttnPlan p = plan;
     if (cluster > 0) {   // (a job has the prefix's keys and the sequence's own)
         p.fused = 1;
         p.prefix_blocks = 0;
     }
-    if (p.d <= 64) return launch_dp<64>(p, data, jobs, cluster, stream);
-    if (p.d <= 128) return launch_dp<128>(p, data, jobs, cluster, stream);
-    return launch_dp<256>(p, data, jobs, cluster, stream);
+    return dtype == GRIFFIN_DT_F32 ? launch_type<float>(p, data, jobs, cluster, stream) : launch_type<__nv_bfloat16>(p, data, jobs, cluster, stream);
 }
 
 }  // namespace griffin

@@ -7,7 +7,7 @@
 // the softmax stays in registers (four shuffles a row), and P goes through shared memory within its own warp; the CTA
 // meets once a tile, for the keys and values.  Those come by cp.async, the next tile's behind the present one's
 // products, and their pages are looked up a tile ahead.  Keys and values behind what any row of the block sees are
-// read as zeros, whatever the cache holds there.  A cache in 4 bits (q4.cuh) comes through registers instead, as fp32 values.
+// read as zeros, whatever the cache holds there.
 //
 // Bound by latency: 5 steps behind 1003 shared tokens (16 heads over 4, 64 wide) take 13.0 us, half of them here and the
 // rest in the joining kernel; 1000 causal tokens of 8 heads over 2 take 73 us, 14 TFLOP/s of the 75 of the pipes.
@@ -67,55 +67,8 @@ __device__ __forceinline__ void tile_copy(const AttnPlan &p, const AttnData &x, 
     }
 }
 
-// The same from a cache held in 4 bits: codes and scale of the thread's pieces, 4 entries each, into registers, and from
-// there as fp32 to shared memory once the tile's turn comes.
-struct SimtQ4 {
-    uint16_t codes;
-    uint8_t scale;
-};
-template <int DP>
-__device__ __forceinline__ void tile_fetch(const AttnPlan &p, const AttnData &x, const SimtKeys &s, int t,
-                                           const int (&page)[SimtCfg<DP>::PASSES], SimtQ4 (&raw)[2][SimtCfg<DP>::PASSES]) {
-    const bool pre = t < s.pre_tiles;
-    const int k0 = (pre ? t : t - s.pre_tiles) * SimtCfg<DP>::KT, len = pre ? p.prefix_len : s.own_len;
-#pragma unroll
-    for (int i = 0; i < SimtCfg<DP>::PASSES; ++i) {
-        const int c = threadIdx.x + i * SimtCfg<DP>::THREADS, r = c / (DP / 4), e = c % (DP / 4) * 4, key = k0 + r;
-        raw[0][i] = raw[1][i] = SimtQ4{(uint16_t)Q4_ZEROS, 0};
-        if (e >= p.d) continue;
-        const bool there = key < len && page[i] >= 0 && page[i] < p.n_pages;
-        if (key < len && !there) raise_status(p.ws, DEV_STATUS_BAD_INDEX, 42);
-        if (!there) continue;
-        const long long block = page[i] * x.stride_page + s.head * x.stride_head;
-        const int slot = key & ((1 << p.page_shift) - 1);
-#pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const uint8_t *const at = static_cast<const uint8_t *>(which ? x.v : x.k) + block;
-            // entries e .. e + 3 of the word: nibbles n, n + 1 and n + 4, n + 5, n = 0 or 2
-            const uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(at + slot * x.q4.code_row + (e >> 3) * 4)) >> ((e & 4) * 2);
-            raw[which][i].codes = (uint16_t)((w & 0xffu) | (w >> 8 & 0xff00u));
-            raw[which][i].scale = __ldg(at + x.q4.scale_off + slot * x.q4.scale_row + (e >> 4));
-        }
-    }
-}
-template <int DP>
-__device__ __forceinline__ void tile_put(const AttnPlan &p, const SimtQ4 (&raw)[2][SimtCfg<DP>::PASSES], float *sk, float *sv) {
-#pragma unroll
-    for (int i = 0; i < SimtCfg<DP>::PASSES; ++i) {
-        const int c = threadIdx.x + i * SimtCfg<DP>::THREADS, r = c / (DP / 4), e = c % (DP / 4) * 4;
-        if (e >= p.d) continue;
-#pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const uint32_t w = raw[which][i].codes;
-            const float s = q4_scale(raw[which][i].scale);
-            const auto value = [&](int at) { return (float)((int)(w >> at & 15u) - 8) * s; };
-            *reinterpret_cast<float4 *>((which ? sv : sk) + r * SimtCfg<DP>::LD + e) = make_float4(value(0), value(8), value(4), value(12));
-        }
-    }
-}
-
 // The rows of one segment, A to a half warp.  page: of the segment's first tile.
-template <int DP, bool Q4, int A>
+template <int DP, int A>
 __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &x, const AttnJob &j, const SimtKeys &keys, bool first,
                                              bool whole, float *sq, float *skv, float *sp, int (&page)[SimtCfg<DP>::PASSES]) {
     using Cfg = SimtCfg<DP>;
@@ -126,13 +79,7 @@ __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &
     float m[A], l[A];
 #pragma unroll
     for (int a = 0; a < A; ++a) m[a] = -INFINITY, l[a] = 0.f;
-    SimtQ4 raw[2][Cfg::PASSES];
-    if constexpr (Q4) {
-        tile_fetch<DP>(p, x, keys, keys.t0, page, raw);
-        tile_put<DP>(p, raw, skv, skv + Cfg::TILE);
-    } else {
-        tile_copy<DP>(p, x, keys, keys.t0, page, skv, skv + Cfg::TILE);
-    }
+    tile_copy<DP>(p, x, keys, keys.t0, page, skv, skv + Cfg::TILE);
     if (keys.n > 1) tile_pages<DP>(p, keys, keys.t0 + 1, page);
 #pragma unroll 1
     for (int i = 0; i < keys.n; ++i) {
@@ -142,20 +89,10 @@ __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &
         __syncthreads();   // this tile has come; the one before is done with
         if (i + 1 < keys.n) {
             float *const next = skv + (i + 1 & 1) * 2 * Cfg::TILE;
-            if constexpr (Q4) tile_fetch<DP>(p, x, keys, t + 1, page, raw);
-            else tile_copy<DP>(p, x, keys, t + 1, page, next, next + Cfg::TILE);
+            tile_copy<DP>(p, x, keys, t + 1, page, next, next + Cfg::TILE);
             if (i + 2 < keys.n) tile_pages<DP>(p, keys, t + 2, page);
         }
-        const auto arrive = [&] {   // the next tile, of which nothing is read before the barrier
-            if constexpr (Q4) {
-                float *const next = skv + (i + 1 & 1) * 2 * Cfg::TILE;
-                if (i + 1 < keys.n) tile_put<DP>(p, raw, next, next + Cfg::TILE);
-            }
-        };
-        if (!on) {
-            arrive();
-            continue;
-        }
+        if (!on) continue;
         float2 s2[A][NK] = {};   // sums over the even and the odd entries
 #pragma unroll 4
         for (int e = 0; e < p.d; e += 4) {
@@ -237,7 +174,6 @@ __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &
         const int cut = apart >= KT ? KT : max(apart, 0) & ~3;
         products(0, cut, std::true_type{});
         if (cut < KT) products(cut, KT, std::false_type{});
-        arrive();
         __syncwarp();
     }
     // the segment's result
@@ -265,7 +201,7 @@ __device__ __forceinline__ void simt_segment(const AttnPlan &p, const AttnData &
     }
 }
 
-template <int DP, bool Q4>
+template <int DP>
 __global__ void __launch_bounds__(SimtCfg<DP>::THREADS, 1) attn_simt_kernel(const __grid_constant__ AttnPlan p,
                                                                  const __grid_constant__ AttnData x) {
     using Cfg = SimtCfg<DP>;
@@ -297,11 +233,11 @@ __global__ void __launch_bounds__(SimtCfg<DP>::THREADS, 1) attn_simt_kernel(cons
                        static_cast<const float *>(x.q) + (j.tok0 + tok) * x.ld_q + (j.head * p.group + r - tok * p.group) * p.d + e, true);
         }
         constexpr int H = Cfg::HALVES;
-        if (j.rows <= H) simt_segment<DP, Q4, 1>(p, x, j, keys, first, whole, sq, skv, sp, page);
-        else if (2 * H == SIMT_ROWS || j.rows <= 2 * H) simt_segment<DP, Q4, 2>(p, x, j, keys, first, whole, sq, skv, sp, page);
+        if (j.rows <= H) simt_segment<DP, 1>(p, x, j, keys, first, whole, sq, skv, sp, page);
+        else if (2 * H == SIMT_ROWS || j.rows <= 2 * H) simt_segment<DP, 2>(p, x, j, keys, first, whole, sq, skv, sp, page);
         else if constexpr (2 * H < SIMT_ROWS) {
-            if (j.rows <= 3 * H) simt_segment<DP, Q4, 3>(p, x, j, keys, first, whole, sq, skv, sp, page);
-            else simt_segment<DP, Q4, 4>(p, x, j, keys, first, whole, sq, skv, sp, page);
+            if (j.rows <= 3 * H) simt_segment<DP, 3>(p, x, j, keys, first, whole, sq, skv, sp, page);
+            else simt_segment<DP, 4>(p, x, j, keys, first, whole, sq, skv, sp, page);
         }
         g = stop;
         if (g >= g_end) return;
@@ -312,8 +248,8 @@ __global__ void __launch_bounds__(SimtCfg<DP>::THREADS, 1) attn_simt_kernel(cons
 
 AttnShape attn_simt_shape(int head_dim) { return {SIMT_ROWS, 1, head_dim <= 128 ? SimtCfg<64>::KT : SimtCfg<256>::KT, 0}; }
 
-template <int DP, bool Q4> static griffin_status launch_dp(AttnPlan p, AttnData x, cudaStream_t stream) {
-    const void *fn = reinterpret_cast<const void *>(attn_simt_kernel<DP, Q4>);
+template <int DP> static griffin_status launch_dp(AttnPlan p, AttnData x, cudaStream_t stream) {
+    const void *fn = reinterpret_cast<const void *>(attn_simt_kernel<DP>);
     const size_t smem = SimtCfg<DP>::smem(p.n_seq);
     if (ensure_dynamic_smem(fn, smem) != cudaSuccess) return GRIFFIN_ERR_CUDA;
     void *args[] = {&p, &x};
@@ -322,13 +258,10 @@ template <int DP, bool Q4> static griffin_status launch_dp(AttnPlan p, AttnData 
                : GRIFFIN_ERR_CUDA;
 }
 
-template <bool Q4> static griffin_status launch_q4(const AttnPlan &plan, const AttnData &data, cudaStream_t stream) {
-    if (plan.d <= 64) return launch_dp<64, Q4>(plan, data, stream);
-    if (plan.d <= 128) return launch_dp<128, Q4>(plan, data, stream);
-    return launch_dp<256, Q4>(plan, data, stream);
-}
-griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, bool q4, cudaStream_t stream) {
-    return q4 ? launch_q4<true>(plan, data, stream) : launch_q4<false>(plan, data, stream);
+griffin_status launch_attn_simt(const AttnPlan &plan, const AttnData &data, cudaStream_t stream) {
+    if (plan.d <= 64) return launch_dp<64>(plan, data, stream);
+    if (plan.d <= 128) return launch_dp<128>(plan, data, stream);
+    return launch_dp<256>(plan, data, stream);
 }
 
 }  // namespace griffin
