@@ -41,7 +41,7 @@ static bool attn_few(const griffin_attn_desc *desc, const griffin_attn_batch *ba
 //     16  4000  16.0  27.0  19.4  14.9  24.0         80  4000  27.8  28.2     -     -
 //     32  1000  13.5  13.4  12.6  10.6     -        128  1000  21.4  14.4     -     -
 //     32 16000  33.4  84.8  49.7  32.2     -        128  4000  34.0  30.2     -     -
-// (The table fits base + slope * keys for each cluster and 12.3 + 0.0058 * keys * jobs / 148 for cut calls to 2 us; 8 CTAs fit a GPC twice.)
+// (The table fits base + slope * keys for each cluster and 12.3 + 0.0058 * keys * jobs / 148 for cut calls to 2 us.)
 // The sequences' lengths are on the device; what the page table could hold stands for them, here and below.
 struct WholeFit {
     int cluster, most_jobs;
@@ -62,13 +62,15 @@ struct WholeJobs {
 static WholeJobs attn_whole(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
     const int group = few_group(desc), block_tokens = 8 / group;
     const long long n = batch->n_seq, blocks = batch->n_tokens <= n ? n : n + batch->n_tokens / block_tokens, jobs = blocks * (desc->n_q_heads / group);
-    // (keys 128 wide, of the longest job)
-    const double keys = ((double)batch->prefix_len + (double)batch->table_stride * desc->page_size) * (desc->head_dim / 128.0);
+    // Keys 128 wide: of the longest job, and of all blocks of a cut call, which reads a shared prefix once for 8 rows of the batch.
+    const double width = desc->head_dim / 128.0, prefix = batch->prefix_len * width, own = (double)batch->table_stride * desc->page_size * width;
+    const double keys = prefix + own, shared = n > 1 ? (double)(((long long)batch->n_tokens * group + 7) / 8 * (desc->n_q_heads / group)) : (double)jobs;
+    const double cut = 12.3 + 0.0058 / ATTN_MAX_GRID * (jobs * own + shared * prefix);
     WholeJobs best{0, 0, 0.0};
     for (const WholeFit &f : WHOLE_FITS) {
         const double us = f.base + f.slope * keys;
         if (jobs > f.most_jobs || (best.cluster > 0 && us >= best.us)) continue;
-        best = WholeJobs{(int)jobs, us <= 12.3 + f.slack + 0.0058 * keys * (double)jobs / ATTN_MAX_GRID ? f.cluster : 0, us};
+        best = WholeJobs{(int)jobs, us <= cut + f.slack ? f.cluster : 0, us};
     }
     return best;
 }
@@ -169,10 +171,14 @@ static griffin_status launch(const griffin_attn_desc *desc, const griffin_attn_b
     const int sms = device_sm_count();
     if (sms <= 0) return GRIFFIN_ERR_CUDA;
     const int group = few && q4 ? few_group(desc) : desc->n_q_heads / desc->n_kv_heads;
-    const AttnPlan p = make_plan(desc, batch, n_pages, sms, shape_of(desc, few, q4), group, scratch, ws);
+    AttnPlan p = make_plan(desc, batch, n_pages, sms, shape_of(desc, few, q4), group, scratch, ws);
     griffin_status st;
     if (few && q4) {
         const WholeJobs whole = attn_whole(desc, batch);
+        // A short prefix is walked by every sequence: most jobs then lie in one warp's share and need no joining.  us a pass, each / once for
+        // the batch: 24 sequences, 8 key heads, 64 keys in front of 200 14.9 / 17.2, 128 16.0 / 16.6, 256 19.9 / 17.9; 35, 40 key heads, 256 wide,
+        // 64 53 / 80, 128 57 / 68, 256 66 / 66.
+        if (p.prefix_len <= 128) p.fused = 1, p.prefix_blocks = 0;
         st = launch_attn_few_q4(p, x, desc->dtype, whole.jobs, whole.cluster, stream);
         if (whole.cluster > 0) return st;
     } else {
