@@ -45,14 +45,15 @@ constexpr int ATC_BARS = 2 * 10 + 10 + 4 + 6 + 2 * 4 + 2;  // kv full/empty, v_o
 template <int DP, bool Q4> struct AtcCfg {
     static constexpr int KT = DP == 256 ? 64 : 128;       // keys per tile
     static constexpr int NS = DP == 256 ? 1 : 2;          // O accumulators
-    static constexpr int UNPACK_WARP = NS == 2 ? 12 : 8;  // behind the softmax warps: first of the four that unpack (Q4)
-    static constexpr int THREADS = Q4 && NS == 2 ? 512 : 384;
+    static constexpr int UNPACK_WARP = NS == 2 ? 12 : 8;  // behind the softmax warps: first of those that unpack (Q4)
+    static constexpr int UNPACKERS = 8, THREADS = Q4 ? (UNPACK_WARP + UNPACKERS) * 32 : 384;
+    static constexpr int CH = Q4 ? 32 : 64;    // columns of S that a softmax thread takes at once (of 640 threads each has 96 registers)
     static constexpr int CB = DP / 64;                    // 64-entry column blocks (128 swizzled bytes per row)
     static constexpr int Q_BYTES = ATC_ROWS * DP * 2, KV_BYTES = KT * DP * 2;
     static constexpr int O_COL = 2 * KT;                  // TMEM columns: S/P 0, S/P 1, O (0, 1)
     static constexpr int MAX_SLOTS = DP == 64 ? 10 : 5;
     // a tile of the cache in 4 bits, as it lies: codes, scales, a note; unpacked in units of 32 entries of a key, PASSES to a thread
-    static constexpr int UNITS = DP / 32, PASSES = KT * UNITS / 128, RAW_STAGES = Q4 ? 3 : 0;
+    static constexpr int UNITS = DP / 32, PASSES = KT * UNITS / (32 * UNPACKERS), RAW_STAGES = Q4 ? 3 : 0;
     static constexpr int RAW_SCALES = KT * DP / 2, RAW_NOTE = RAW_SCALES + KT * DP / 16, RAW_BYTES = RAW_NOTE + 128;
     static constexpr int BARS = ATC_BARS + 2 * RAW_STAGES;   // and raw full/empty
 };
@@ -111,6 +112,18 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
         : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]), "r"(r[1]),
+        "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+        "r"(r[15]), "r"(taddr)
+        : "memory");
+}
+// S of the columns that a softmax thread takes at once, and P of them.
+__device__ __forceinline__ void load_s(uint32_t taddr, float (&s)[64]) { tmem_ld64(taddr, s); }
+__device__ __forceinline__ void load_s(uint32_t taddr, float (&s)[32]) { tmem_ld32(taddr, s); }
+__device__ __forceinline__ void store_p(uint32_t taddr, const uint32_t (&p)[32]) { tmem_st32(taddr, p); }
+__device__ __forceinline__ void store_p(uint32_t taddr, const uint32_t (&p)[16]) { tmem_st16(taddr, p); }
 // 32 bytes, a whole sector, in one store (the scratch, its parts and the partials' rows start on 32-byte boundaries)
 __device__ __forceinline__ void store_8f(float *to, const float *v) {
     asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
@@ -144,16 +157,16 @@ __device__ __forceinline__ float2 poly_exp2(float2 x) {
     y.y = __int_as_float(__float_as_int(y.y) + (__float_as_int(n.y) << 23));
     return y;
 }
-// P of 64 keys: 2^(c S - m), summed in fp32 and packed to bf16: the product's two operands are of one type, and the values are
+// P of N keys: 2^(c S - m), summed in fp32 and packed to bf16: the product's two operands are of one type, and the values are
 // bf16 as they are stored.  That rounding (2^-8 of each P at most) brings the error against 64 bits from 0.0017 of the output,
 // which is the output's own rounding, to 0.0021 to 0.0023.  POLY of every 8 pairs go through poly_exp2: the
 // special-function unit gives 16 results a clock and SM, and 32768 of them per tile would take as long as the
 // four products of the tile do.
 constexpr int ATC_POLY = 3;
-template <int POLY>
-__device__ __forceinline__ void exp_pairs(const float (&s)[64], float2 scale2, float2 off2, float2 (&sum)[4], uint32_t (&pk)[32]) {
+template <int POLY, int N>
+__device__ __forceinline__ void exp_pairs(const float (&s)[N], float2 scale2, float2 off2, float2 (&sum)[4], uint32_t (&pk)[N / 2]) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
+    for (int i = 0; i < N / 2; ++i) {
         float2 e = fma2(make_float2(s[2 * i], s[2 * i + 1]), scale2, off2);
         if ((i * 3 & 7) < POLY) {
             e = poly_exp2(e);
@@ -168,9 +181,9 @@ __device__ __forceinline__ void exp_pairs(const float (&s)[64], float2 scale2, f
 }
 
 // Keys from `lim` on are not seen.
-__device__ __forceinline__ void mask_keys(float (&s)[64], int lim) {
+template <int N> __device__ __forceinline__ void mask_keys(float (&s)[N], int lim) {
 #pragma unroll
-    for (int i = 0; i < 64; ++i) s[i] = i < lim ? s[i] : -INFINITY;
+    for (int i = 0; i < N; ++i) s[i] = i < lim ? s[i] : -INFINITY;
 }
 
 // The bounded wait with its slow path in one place: the loops below stay small enough for the instruction cache
@@ -307,7 +320,7 @@ struct SegReader {
     }
 };
 
-// A tile of a cache held in 4 bits (q4.cuh) comes by bulk copies as it lies, page by page, and four warps write it out as bf16
+// A tile of a cache held in 4 bits (q4.cuh) comes by bulk copies as it lies, page by page, and eight warps write it out as bf16
 // into the ring.  With it comes a note of what is not there.  Behind the last key, and beyond the head's width, they write what happens to
 // lie there: it is a number, whatever the bits, and meets P = 0, or a logit that is masked, or a query's zeros, or no output.
 struct __align__(16) RawNote {
@@ -318,7 +331,7 @@ struct __align__(16) RawNote {
 template <int DP>
 static __device__ __noinline__ void unpack_rest(const AtcParams &prm, RawNote note, const uint8_t *raw, uint8_t *tile, int block, int row0, int half) {
     using Cfg = AtcCfg<DP, true>;
-    constexpr int ROWS = 128 / Cfg::UNITS;
+    constexpr int ROWS = 32 * Cfg::UNPACKERS / Cfg::UNITS;
     const int box_shift = 31 - __clz(prm.box_rows), q = block * 2 + half;
 #pragma unroll 1
     for (int i = 0; i < Cfg::PASSES; ++i) {
@@ -341,8 +354,8 @@ static __device__ __noinline__ void unpack_rest(const AtcParams &prm, RawNote no
 // keys: with the swizzle by the key's number that meets all banks.
 template <int DP> __device__ __forceinline__ void unpack_tile(const AtcParams &prm, const uint8_t *raw, uint8_t *tile) {
     using Cfg = AtcCfg<DP, true>;
-    constexpr int UNITS = Cfg::UNITS, BLOCKS = UNITS / 2, ROWS = 128 / UNITS;   // keys that 128 threads have at once
-    const int t = threadIdx.x & 127, block = (t >> 3) % BLOCKS, q = block * 2 + (t & 1);
+    constexpr int UNITS = Cfg::UNITS, BLOCKS = UNITS / 2, ROWS = 32 * Cfg::UNPACKERS / UNITS;   // keys that the warps have at once
+    const int t = threadIdx.x - 32 * Cfg::UNPACK_WARP, block = (t >> 3) % BLOCKS, q = block * 2 + (t & 1);
     const int row0 = (t >> 3) / BLOCKS * 4 + ((t >> 1) & 3);
     const RawNote note = *reinterpret_cast<const RawNote *>(raw + Cfg::RAW_NOTE);
     const int d = prm.plan.d, code_row = prm.q4.code_row, scale_row = prm.q4.scale_row;
@@ -353,7 +366,7 @@ template <int DP> __device__ __forceinline__ void unpack_tile(const AtcParams &p
     uint32_t to[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) to[j] = smem_u32(tile) + block * (Cfg::KT * 128) + row0 * 128 + ((j ^ ((t & 1) * 4) ^ (row0 & 7)) << 4);   // (ROWS is a multiple of 8)
-    // (one unit is read ahead: four warps have little else to hide its way behind, and more code than this loop costs the other
+    // (one unit is read ahead: the warps have little else to hide its way behind, and more code than this loop costs the other
     // roles their place in the instruction cache)
     uint32_t w[4], b;
     const auto read = [&] {
@@ -415,7 +428,7 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
     if (tid < (Q4 ? 1 : 3)) prefetch_tensormap(tid == 0 ? &maps.q : tid == 1 ? &maps.k : &maps.v);
     if (tid == 0) {
         for (int i = 0; i < n_slots; ++i) {
-            mbar_init(&kv_full[i], Q4 ? 4 : 1);   // the copies' producer, or the warps that unpack
+            mbar_init(&kv_full[i], Q4 ? Cfg::UNPACKERS : 1);   // the copies' producer, or the warps that unpack
             mbar_init(&kv_empty[i], 2);   // the products that read it, and the value warp
             mbar_init(&v_ok[i], 1);
         }
@@ -433,7 +446,7 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
         mbar_init(seg_want, 1);
         for (int i = 0; i < Cfg::RAW_STAGES; ++i) {
             mbar_init(&raw_full[i], 1);
-            mbar_init(&raw_empty[i], 4);   // the warps that unpack
+            mbar_init(&raw_empty[i], Cfg::UNPACKERS);   // the warps that unpack
         }
         *abort = 0;
         mbar_fence_init();
@@ -778,12 +791,12 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
                     const bool masked = __any_sync(0xffffffffu, lim < KT);
                     float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
-                    for (int c = 0; c < KT; c += 64) {
-                        float s[64];
-                        tmem_ld64(ts + c, s);
+                    for (int c = 0; c < KT; c += Cfg::CH) {
+                        float s[Cfg::CH];
+                        load_s(ts + c, s);
                         if (masked) mask_keys(s, lim - c);
 #pragma unroll
-                        for (int i = 0; i < 64; i += 8)
+                        for (int i = 0; i < Cfg::CH; i += 8)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) mx4[e] = max3(mx4[e], s[i + e], s[i + 4 + e]);
                     }
@@ -822,17 +835,17 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
                     const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), off2 = make_float2(-off, -off);
                     float2 sum[4] = {};
 #pragma unroll 1
-                    for (int c = 0; c < KT; c += 64) {
-                        float s[64];
-                        tmem_ld64(ts + c, s);
-                        uint32_t pk[32];
+                    for (int c = 0; c < KT; c += Cfg::CH) {
+                        float s[Cfg::CH];
+                        load_s(ts + c, s);
+                        uint32_t pk[Cfg::CH / 2];
                         if (masked) {
                             mask_keys(s, lim - c);   // 2^-inf = 0
                             exp_pairs<0>(s, scale2, off2, sum, pk);
                         } else {
                             exp_pairs<ATC_POLY>(s, scale2, off2, sum, pk);
                         }
-                        tmem_st32(ts + c / 2, pk);
+                        store_p(ts + c / 2, pk);
                     }
                     const float2 s4 = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
                     l += s4.x + s4.y;
@@ -901,7 +914,7 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
     }
 
     if constexpr (Q4) {
-        if (warp >= Cfg::UNPACK_WARP && warp < Cfg::UNPACK_WARP + 4) {
+        if (warp >= Cfg::UNPACK_WARP) {
             // ---------------- the cache in 4 bits: unpacked into the ring ----------------
             Ring kv{0, 0}, raw{0, 0};
             for (uint32_t kv_n = 0;; ++kv_n) {
