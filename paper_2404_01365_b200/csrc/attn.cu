@@ -74,29 +74,30 @@ static WholeJobs attn_whole(const griffin_attn_desc *desc, const griffin_attn_ba
     }
     return best;
 }
-// The same over a cache held in 4 bits (attn_few_q4.cu).  That kernel unpacks the keys once for every 8 rows, at about 4 TB/s
-// of a bf16 cache's bytes; the tcgen05 one unpacks them once for up to 256, and a job that ends costs it as much as two of its tiles.
-// Both sides, us a pass, few / tcgen05, 128-wide heads unless said otherwise.  Up to 16 rows of a sequence: 1 sequence, 8 key
-// heads, 2000 keys 14.8 / 16.3, 8000 21.2 / 23.0; 16 sequences of 8000 keys 82.7 / 133; 64 of 2000 89 / 169; 48 with 4 rows and
-// 2560 keys 48 / 126.  32 rows: 1 sequence, 300 keys 12.9 / 16.1, 2000 16.8 / 16.3; 16 of 2000 50.6 / 51.8, of 8000 146 / 138.  64 rows: 300 keys 13.3
-// / 17.8, 2000 20.1 / 17.0.  So from 16 rows on only what is a tile or two for every warp stays here.
-// A shared prefix, whose rows are the whole call's, under 8 key heads: 24 rows of 6 sequences, 2000 keys 16.7 / 18.8, 8000 26.2 / 25.4, of 24
-// sequences 24.9 / 30.7; 48 of 6, 2000 23.6 / 19.8; 64 of 16, 2000 22.1 / 21.0; 128 of 32, 300 19.5 / 21.3, 2000 31.2 / 26.3.
-// Under 2 key heads: 64 rows of 8, 2000 15.9 / 17.7, 8000 24.5 / 20.4.  256 wide, 20 rows of 20 sequences, 16 key heads, 4000 38 / 57.
-// Calls whose jobs are whole, which take 17 us at most, are shorter than any of the tcgen05 kernel's.
-constexpr double FQ_WHOLE_US = 17, FQ_FEW_KEYS = 72000, FQ_KEYS_PER_SEQ = 800, FQ_KEYS_PER_CALL = 24000;
+// Whether that kernel takes a call over a cache in 4 bits rather than the tcgen05 one.  It unpacks the keys once for every 8 rows, the
+// other once for every 128 (a row tile; two of them share a key tile, but not the softmax).  In keys of a 128-wide head, over
+// all jobs, few rows take 3e-5 us each on 148 SMs and row tiles 9e-5 (of 64-wide heads not less: their softmax is the same); the
+// tcgen05 kernel's way to the first and from the last result takes 1.2 us more.  270 calls drawn at random (1 to 128 sequences of 1 to 32 tokens, up to 32000 shared and
+// 12000 own keys, 64 to 256 wide, 1 to 32 key heads), each timed with both kernels, take 1.0 % more by this rule than with the
+// better one each time, at worst 1.31 times as long.  us a pass, few / tcgen05, query heads over key heads:
+//   1 sequence of 1 token, 64 over 8, 5000 keys 14.3 / 19.7;  4 of 4 tokens 38.0 / 32.9;  16 tokens, 32 over 16 28.0 / 24.5
+//   24 sequences of 1 token, 64 over 8, 12000 keys 93 / 235;  of 32 tokens, 5000 keys 945 / 190
+//   32 over 8 behind 1000 shared, 600 keys, 8 sequences 14.3 / 20.5;  8 over 8 behind 2000, 64 keys, 48 sequences 24.7 / 27.2
+//   16 over 2 behind 2000 shared, 5000 keys, 48 sequences 41.9 / 83.3;  8 over 4 behind 8000, 64 keys 36.7 / 26.2
+//   256 wide: 64 over 8 behind 2000, 5000 keys, 64 sequences 246 / 558;  16 over 8, 2 tokens behind 2000, 200 keys 69.0 / 55.8
+constexpr double FQ_TILE_KEYS = 3, FQ_START_KEYS = 40000;   // what a key of a row tile, and the start of the tcgen05 kernel, are in keys of 8 rows
+constexpr int FQ_SHORT_PREFIX = 128;
 static bool attn_few_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
     const int group = desc->n_q_heads / desc->n_kv_heads;
     if (desc->dtype != GRIFFIN_DT_BF16) return true;   // (the only one for fp32)
     if (group > 8) return false;
-    const long long rows = (long long)batch->n_tokens * group, n = batch->n_seq;
-    const double blocks = (double)((rows + 7) / 8), prefix = batch->prefix_len, room = (double)batch->table_stride * desc->page_size;
-    const double hkv = desc->n_kv_heads, width = desc->head_dim / 128.0;
-    const WholeJobs whole = attn_whole(desc, batch);
-    if (whole.cluster > 0 && whole.us <= FQ_WHOLE_US) return true;
-    if (blocks * hkv * (prefix + room) * width <= FQ_FEW_KEYS) return true;
-    if (rows > 16 * n) return false;
-    return n == 1 || (blocks - 1) * prefix * width <= FQ_KEYS_PER_SEQ * n + FQ_KEYS_PER_CALL / hkv;
+    const double n = batch->n_seq, rows = (double)batch->n_tokens * group, prefix = batch->prefix_len;
+    const double own = (double)batch->table_stride * desc->page_size, width = desc->n_kv_heads * (desc->head_dim / 128.0);
+    const double own8 = n * ceil(rows / (8 * n)), own128 = n * ceil(rows / (128 * n));   // blocks, were the sequences equally long
+    const double few = width * ((n == 1 || prefix <= FQ_SHORT_PREFIX ? own8 : ceil(rows / 8)) * prefix + own8 * own);
+    const double kt = attn_tc_shape(desc->head_dim).kt;
+    const double tiles = fmax(width, desc->n_kv_heads) * kt * (ceil(rows / 128) * ceil(prefix / kt) + own128 * ceil(own / kt));
+    return few <= FQ_TILE_KEYS * tiles + FQ_START_KEYS;
 }
 static AttnShape shape_of(const griffin_attn_desc *desc, bool few, bool q4) {
     if (few && q4) return attn_few_q4_shape();
@@ -178,7 +179,7 @@ static griffin_status launch(const griffin_attn_desc *desc, const griffin_attn_b
         // A short prefix is walked by every sequence: most jobs then lie in one warp's share and need no joining.  us a pass, each / once for
         // the batch: 24 sequences, 8 key heads, 64 keys in front of 200 14.9 / 17.2, 128 16.0 / 16.6, 256 19.9 / 17.9; 35, 40 key heads, 256 wide,
         // 64 53 / 80, 128 57 / 68, 256 66 / 66.
-        if (p.prefix_len <= 128) p.fused = 1, p.prefix_blocks = 0;
+        if (p.prefix_len <= FQ_SHORT_PREFIX) p.fused = 1, p.prefix_blocks = 0;
         st = launch_attn_few_q4(p, x, desc->dtype, whole.jobs, whole.cluster, stream);
         if (whole.cluster > 0) return st;
     } else {
