@@ -85,16 +85,20 @@ static WholeJobs attn_whole(const griffin_attn_desc *desc, const griffin_attn_ba
 //   32 over 8 behind 1000 shared, 600 keys, 8 sequences 14.3 / 20.5;  8 over 8 behind 2000, 64 keys, 48 sequences 24.7 / 27.2
 //   16 over 2 behind 2000 shared, 5000 keys, 48 sequences 41.9 / 83.3;  8 over 4 behind 8000, 64 keys 36.7 / 26.2
 //   256 wide: 64 over 8 behind 2000, 5000 keys, 64 sequences 246 / 558;  16 over 8, 2 tokens behind 2000, 200 keys 69.0 / 55.8
+// More than 8 query heads a key head go in even parts, each of which unpacks the keys (they are read from L2 but once):
+//   32 over 2, 1 sequence, 200 keys 8.6 / 14.5, 12000 18.2 / 19.1;  48 over 4 behind 1000, 2000 keys, 8 sequences 18.1 / 22.3
+//   128 over 8, 2000 keys, 64 sequences 89.7 / 172;  64 over 4, 2 tokens, 300 in front of 12000 keys, 16 sequences 130 / 142;  9 over 1
+//   behind 8000, 64 keys, 64 sequences 55.8 / 30.5
 constexpr double FQ_TILE_KEYS = 3, FQ_START_KEYS = 40000;   // what a key of a row tile, and the start of the tcgen05 kernel, are in keys of 8 rows
 constexpr int FQ_SHORT_PREFIX = 128;
 static bool attn_few_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
     const int group = desc->n_q_heads / desc->n_kv_heads;
     if (desc->dtype != GRIFFIN_DT_BF16) return true;   // (the only one for fp32)
-    if (group > 8) return false;
-    const double n = batch->n_seq, rows = (double)batch->n_tokens * group, prefix = batch->prefix_len;
+    const int part = few_group(desc);
+    const double n = batch->n_seq, tokens = batch->n_tokens, rows = tokens * group, prefix = batch->prefix_len, parts = group / part, most = 8 / part;
     const double own = (double)batch->table_stride * desc->page_size, width = desc->n_kv_heads * (desc->head_dim / 128.0);
-    const double own8 = n * ceil(rows / (8 * n)), own128 = n * ceil(rows / (128 * n));   // blocks, were the sequences equally long
-    const double few = width * ((n == 1 || prefix <= FQ_SHORT_PREFIX ? own8 : ceil(rows / 8)) * prefix + own8 * own);
+    const double own8 = n * parts * ceil(tokens / (most * n)), own128 = n * ceil(rows / (128 * n));   // blocks, were the sequences equally long
+    const double few = width * ((n == 1 || prefix <= FQ_SHORT_PREFIX ? own8 : parts * ceil(tokens / most)) * prefix + own8 * own);
     const double kt = attn_tc_shape(desc->head_dim).kt;
     const double tiles = fmax(width, desc->n_kv_heads) * kt * (ceil(rows / 128) * ceil(prefix / kt) + own128 * ceil(own / kt));
     return few <= FQ_TILE_KEYS * tiles + FQ_START_KEYS;

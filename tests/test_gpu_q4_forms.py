@@ -1,6 +1,6 @@
 """Attention over the cache held in 4 bits, in the forms that its kernels divide calls into: more query heads under a key head than
-the kernel for few rows takes (bf16: the tcgen05 kernel, fp32: parts of the heads), calls whose jobs clusters of one to eight
-CTAs take whole, and calls that are cut."""
+a block of few rows has, tables that are narrow or wide (by what they could hold a bf16 call of many rows goes to the one kernel
+or the other), calls whose jobs clusters of one to eight CTAs take whole, and calls that are cut."""
 import numpy as np
 import pytest
 import torch
@@ -15,48 +15,59 @@ from test_gpu_layer import check_attention
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 NAN = float("nan")
+TABLES = [1, 60000]     # keys that the tables could hold beyond the longest sequence: the second makes pieces of rows tcgen05 calls
 WIDE = [(9, 1, 64), (12, 1, 80), (20, 2, 112), (16, 1, 128), (10, 1, 208), (48, 3, 256)]   # heads, key heads, width
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hq,hkv,hd", WIDE)
 @pytest.mark.parametrize("page", [8, 32, 256])
-def test_large_groups_of_steps_and_pieces(dtype, hq, hkv, hd, page):
-    check_attention(BatchQ4([1, 1, 1, 1], [1, 40, 129, 77], 300, hq, hkv, hd, page, dtype))
-    check_attention(BatchQ4([1], [260], 0, hq, hkv, hd, page, dtype))
-    check_attention(BatchQ4([2, 0, 17, 1], [2, 5, 130, 0], 129, hq, hkv, hd, page, dtype, extra_rows=2))
+@pytest.mark.parametrize("room", TABLES)
+def test_large_groups_of_steps_and_pieces(dtype, hq, hkv, hd, page, room):
+    extra = -(-room // page)
+    check_attention(BatchQ4([1, 1, 1, 1], [1, 40, 129, 77], 300, hq, hkv, hd, page, dtype, table_extra=extra))
+    check_attention(BatchQ4([1], [260], 0, hq, hkv, hd, page, dtype, table_extra=extra))
+    check_attention(BatchQ4([2, 0, 17, 1], [2, 5, 130, 0], 129, hq, hkv, hd, page, dtype, extra_rows=2, table_extra=extra))
+    check_attention(BatchQ4([7, 1, 30], [7, 500, 300], 200, hq, hkv, hd, page, dtype, extra_rows=1, table_extra=extra))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hq,hkv,hd", WIDE + [(11, 1, 128), (13, 1, 64), (64, 1, 256)])
 @pytest.mark.parametrize("n", [1, 5, 33, 150])
-def test_large_groups_of_prompts(dtype, hq, hkv, hd, n):
-    check_attention(BatchQ4([n], [n], 0, hq, hkv, hd, 16, dtype), rows={0, n // 2, n - 1})
-    check_attention(BatchQ4([n, n], [n + 3, n], 65, hq, hkv, hd, 64, dtype), rows={0, n - 1, n, 2 * n - 1})
+@pytest.mark.parametrize("room", TABLES)
+def test_large_groups_of_prompts(dtype, hq, hkv, hd, n, room):
+    check_attention(BatchQ4([n], [n], 0, hq, hkv, hd, 16, dtype, table_extra=-(-room // 16)), rows={0, n // 2, n - 1})
+    check_attention(BatchQ4([n, n], [n + 3, n], 65, hq, hkv, hd, 64, dtype, table_extra=-(-room // 64)), rows={0, n - 1, n, 2 * n - 1})
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("prefix", [1, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 257])
-def test_large_groups_behind_prefixes(dtype, prefix):
+@pytest.mark.parametrize("room", TABLES)
+def test_large_groups_behind_prefixes(dtype, prefix, room):
+    extra = -(-room // 32)
     for hd in (64, 128, 256):
-        check_attention(BatchQ4([1, 2], [1, 33], prefix, 18, 2, hd, 32, dtype))
-        check_attention(BatchQ4([1], [5], prefix, 18, 2, hd, 32, dtype))
+        check_attention(BatchQ4([1, 2], [1, 33], prefix, 18, 2, hd, 32, dtype, table_extra=extra))
+        check_attention(BatchQ4([6, 7], [6, 40], prefix, 18, 2, hd, 32, dtype, table_extra=extra))
+        check_attention(BatchQ4([8], [9], prefix, 18, 2, hd, 32, dtype, table_extra=extra))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hq,hkv,hd", WIDE)
 @pytest.mark.parametrize("fill", [NAN, 12000.0])
-def test_large_groups_do_not_see_what_lies_behind_the_ends(dtype, hq, hkv, hd, fill):
-    check_attention(BatchQ4([1, 2, 1], [5, 70, 129], 37, hq, hkv, hd, 64, dtype, fill=fill))
-    check_attention(BatchQ4([20], [23], 0, hq, hkv, hd, 8, dtype, fill=fill))
+@pytest.mark.parametrize("room", TABLES)
+def test_large_groups_do_not_see_what_lies_behind_the_ends(dtype, hq, hkv, hd, fill, room):
+    check_attention(BatchQ4([1, 2, 1], [5, 70, 129], 37, hq, hkv, hd, 64, dtype, fill=fill, table_extra=-(-room // 64)))
+    check_attention(BatchQ4([9, 12, 1], [9, 70, 129], 37, hq, hkv, hd, 64, dtype, fill=fill, table_extra=-(-room // 64)))
+    check_attention(BatchQ4([20], [23], 0, hq, hkv, hd, 8, dtype, fill=fill, table_extra=-(-room // 8)))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hq,hkv,hd", WIDE)
 @pytest.mark.parametrize("n,own,prefix", [(2, 2, 0), (3, 50, 0), (8, 301, 40), (40, 40, 0), (150, 170, 20)])
-def test_large_groups_and_values_that_are_not_finite(dtype, hq, hkv, hd, n, own, prefix):
+@pytest.mark.parametrize("room", TABLES)
+def test_large_groups_and_values_that_are_not_finite(dtype, hq, hkv, hd, n, own, prefix, room):
     for back in {1, n // 2, n - 1}:
-        b = BatchQ4([n], [own], prefix, hq, hkv, hd, 16, dtype, fill=0.0, seed=back)
+        b = BatchQ4([n], [own], prefix, hq, hkv, hd, 16, dtype, fill=0.0, seed=back, table_extra=-(-room // 16))
         put(b, 0, own - back, hd - 3, NAN)
         put(b, 0, own - 1, 1, NAN, hkv - 1)
         b.requantise()
@@ -65,8 +76,9 @@ def test_large_groups_and_values_that_are_not_finite(dtype, hq, hkv, hd, n, own,
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hd", [64, 112, 256])
-def test_large_groups_report_bad_pages(dtype, hd):
-    b = BatchQ4([1, 3], [300, 9], 40, 12, 1, hd, 8, dtype, fill=0.0)
+@pytest.mark.parametrize("room", TABLES)
+def test_large_groups_report_bad_pages(dtype, hd, room):
+    b = BatchQ4([9, 12], [300, 90], 40, 12, 1, hd, 8, dtype, fill=0.0, table_extra=-(-room // 8))
     b.page_table[0, 17], b.page_table[0, 30], b.prefix_pages[1] = 10 ** 6, -1, -5
     b.to_device()
     out = b.attend()
@@ -79,8 +91,9 @@ def test_large_groups_report_bad_pages(dtype, hd):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hq,hkv,hd", [(16, 1, 128), (10, 1, 256), (4, 2, 64)])
-def test_in_place_captured_and_on_two_streams_at_once(dtype, hq, hkv, hd):
-    bs = [BatchQ4(q, s, 90, hq, hkv, hd, 16, dtype, seed=i).to_device() for i, (q, s) in enumerate((([1, 9], [200, 60]), ([30], [400])))]
+@pytest.mark.parametrize("room", TABLES)
+def test_in_place_captured_and_on_two_streams_at_once(dtype, hq, hkv, hd, room):
+    bs = [BatchQ4(q, s, 90, hq, hkv, hd, 16, dtype, seed=i, table_extra=-(-room // 16)).to_device() for i, (q, s) in enumerate((([1, 9], [200, 60]), ([30], [400])))]
     plain = [b.attend() for b in bs]
     streams = [torch.cuda.Stream() for _ in bs]
     graphs, outs = [], []
@@ -131,9 +144,20 @@ def test_lengths_around_tiles_and_shares():
     for own in (31, 32, 33, 63, 65, 95, 97, 127, 129, 255, 257):
         for hq, hkv, hd in ((2, 1, 128), (16, 1, 128), (16, 1, 256)):
             check_attention(BatchQ4([1, 1], [own, own - 1], 0, hq, hkv, hd, 16, "bf16"))
+            check_attention(BatchQ4([10, 6], [own, own - 1], 0, hq, hkv, hd, 16, "bf16", table_extra=4000))
     for n in (7, 8, 9, 16, 17):
         check_attention(BatchQ4([n], [n + 40], 0, 16, 1, 128, 16, "bf16"), rows={0, n - 1})
+        check_attention(BatchQ4([n], [n + 40], 0, 16, 1, 128, 16, "bf16", table_extra=4000), rows={0, n - 1})
         check_attention(BatchQ4([n, 3], [n + 40, 3], 200, 1, 1, 128, 16, "bf16"))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [64, 128, 256])
+def test_as_many_sequences_as_there_may_be(dtype, hd):
+    n = 1024
+    check_attention(BatchQ4([1] * n, [(13 * i) % 37 for i in range(n)], 130, 2, 1, hd, 8, dtype), rows={0, 1, 500, n - 2, n - 1})
+    check_attention(BatchQ4([1 + i % 2 * 40 for i in range(n)], [50 + i % 7 for i in range(n)], 0, 4, 1, hd, 8, dtype, table_extra=20),
+                    rows={0, 1, 30, 41, 42, 21 * n - 1})
 
 
 def test_two_calls_share_a_captured_workspace():
