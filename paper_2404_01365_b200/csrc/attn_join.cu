@@ -11,7 +11,6 @@
 namespace griffin {
 
 constexpr int JOIN_THREADS = 256, JOIN_WARPS = JOIN_THREADS / 32;
-constexpr int JOIN_ROWS = 16;  // rows of a cut block that one CTA joins
 
 // The partials of one job: n of them on CTAs c0, c0 + 1, ..., `streams` of each.
 struct JobParts {
@@ -43,11 +42,11 @@ template <typename T> __device__ __forceinline__ void store_row4(T *to, const fl
 
 // CTAs 0 .. by_row * split - 1, `split` of them to a job: jobs whose partials are kept by row: in a fused call the last row block of each sequence and
 // key head (no other has just one row tile) and the blocks that see nothing, else every row block.  The others
-// (fused calls): the blocks that were cut, JOIN_ROWS rows each.
+// (fused calls): the blocks that were cut, cut_rows rows each.
 // NV: 128-entry pieces of a row (a lane has 4 entries of each).
 template <typename T, int NV>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ AttnPlan p, T *__restrict__ out,
-                                                                 long long ld_out, int by_row, int split) {
+                                                                 long long ld_out, int by_row, int split, int cut_rows) {
     __shared__ float sh_ml[JOIN_WARPS][2], sh_o[JOIN_WARPS][NV * 128];
     __shared__ int sh_seq[5];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -63,11 +62,11 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     bool cut = false;
     const int id = (int)((uint32_t)blockIdx.x / (uint32_t)split), part = blockIdx.x - id * split;
     if (id >= by_row) {
-        const int at = blockIdx.x - by_row * split, chunks = p.cta_rows / JOIN_ROWS, c = at / chunks;
+        const int at = blockIdx.x - by_row * split, chunks = p.cta_rows / cut_rows, c = at / chunks;
         if (c >= sh.G || tot.queued) return;
         const CutJob j = p.cuts[c];
-        r0 = at % chunks * JOIN_ROWS;
-        r1 = min(j.rows, r0 + JOIN_ROWS);
+        r0 = at % chunks * cut_rows;
+        r1 = min(j.rows, r0 + cut_rows);
         if (r0 >= r1) return;
         a = JobParts{PartJob{0, j.head, j.tok0, false}, j.c0, 1, c - j.c0 + 1};
         cut = true;
@@ -245,7 +244,12 @@ griffin_status launch_attn_join(const AttnPlan &plan, int dtype, void *out, long
     AttnPlan p = plan;
     int by_row = p.hkv * (p.fused ? p.n_seq : p.n_seq + p.n_tokens / p.block_tokens);
     // (with no more tokens than a row tile takes, no block has several; a kernel without streams cuts those too)
-    const int cut = p.fused && (!p.alt || p.n_tokens > p.tile_tokens) ? p.grid * (p.cta_rows / JOIN_ROWS) : 0;
+    // A block that is cut is joined by CTAs of 16 rows, two to a warp, or, while the blocks are so few that each is cut into several
+    // parts, of 8: 8 tokens of 8 heads over 1, 256 wide, behind 5000 95 -> 55 us (four blocks in all), 2000 tokens of 64 over 8 49 -> 38; a
+    // prompt of 512 tokens of 32 over 8 (72) 35.8 -> 37.2, of 4096 147 -> 150: most of the CTAs find no cut.
+    const int blocks = p.hkv * (p.n_seq + p.n_tokens / p.block_tokens);
+    int cut_rows = 4 * blocks <= p.grid ? 8 : 16;
+    const int cut = p.fused && (!p.alt || p.n_tokens > p.tile_tokens) ? p.grid * (p.cta_rows / cut_rows) : 0;
     const void *fn = dtype == GRIFFIN_DT_F32 ? (p.d <= 128 ? reinterpret_cast<const void *>(attn_join_kernel<float, 1>)
                                                            : reinterpret_cast<const void *>(attn_join_kernel<float, 2>))
                                              : (p.d <= 128 ? reinterpret_cast<const void *>(attn_join_kernel<__nv_bfloat16, 1>)
@@ -258,7 +262,7 @@ griffin_status launch_attn_join(const AttnPlan &plan, int dtype, void *out, long
     const int most = (p.n_tokens < p.block_tokens ? p.n_tokens : p.block_tokens) * p.group, room = 2 * p.grid / by_row;
     int split = room < 1 || !rows_here ? 1 : room < most ? room : most;
     const int threads = by_row * split + cut > 2 * p.grid ? JOIN_THREADS / 2 : JOIN_THREADS;
-    void *args[] = {&p, &out, &ld_out, &by_row, &split};
+    void *args[] = {&p, &out, &ld_out, &by_row, &split, &cut_rows};
     return launch_maybe_overlapped(fn, dim3(by_row * split + cut), dim3(threads), 0, stream, true, args) == cudaSuccess ? GRIFFIN_OK
                                                                                                                      : GRIFFIN_ERR_CUDA;
 }
