@@ -76,32 +76,39 @@ static WholeJobs attn_whole(const griffin_attn_desc *desc, const griffin_attn_ba
 }
 // Whether that kernel takes a call over a cache in 4 bits rather than the tcgen05 one.  It unpacks the keys once for every 8 rows, the
 // other once for every 128 (a row tile; two of them share a key tile, but not the softmax).  In keys of a 128-wide head, over
-// all jobs, few rows take 3e-5 us each on 148 SMs and row tiles 9e-5 (of 64-wide heads not less: their softmax is the same); the
-// tcgen05 kernel's way to the first and from the last result takes 1.2 us more.  270 calls drawn at random (1 to 128 sequences of 1 to 32 tokens, up to 32000 shared and
-// 12000 own keys, 64 to 256 wide, 1 to 32 key heads), each timed with both kernels, take 1.0 % more by this rule than with the
-// better one each time, at worst 1.31 times as long.  us a pass, few / tcgen05, query heads over key heads:
+// all jobs, few rows take 3e-5 us each on 148 SMs and row tiles 7.5e-5 (of 64-wide heads not less: their softmax is the same); the
+// tcgen05 kernel's way to the first and from the last result takes 1.8 us more, and blocks that are cut, which the joining kernel has
+// too few CTAs for, 0.5 us a part (of 128 entries).  500 calls drawn at random (1 to 128 sequences of 1 to 128 tokens, up to 32000 shared and
+// 30000 own keys, 64 to 256 wide, 1 to 32 key heads with 1 to 64 query heads each), each timed with both kernels, take 0.9 % more by
+// this rule than with the better one each time, at worst 1.39 times as long.  us a pass, few / tcgen05, query heads over key heads:
 //   1 sequence of 1 token, 64 over 8, 5000 keys 14.3 / 19.7;  4 of 4 tokens 38.0 / 32.9;  16 tokens, 32 over 16 28.0 / 24.5
 //   24 sequences of 1 token, 64 over 8, 12000 keys 93 / 235;  of 32 tokens, 5000 keys 945 / 190
 //   32 over 8 behind 1000 shared, 600 keys, 8 sequences 14.3 / 20.5;  8 over 8 behind 2000, 64 keys, 48 sequences 24.7 / 27.2
 //   16 over 2 behind 2000 shared, 5000 keys, 48 sequences 41.9 / 83.3;  8 over 4 behind 8000, 64 keys 36.7 / 26.2
 //   256 wide: 64 over 8 behind 2000, 5000 keys, 64 sequences 246 / 558;  16 over 8, 2 tokens behind 2000, 200 keys 69.0 / 55.8
+//   cut blocks: 16 tokens, 16 over 1, 12000 keys 31.6 / 54.8, 30000 keys of 64 over 4 143 / 59;  4 tokens, 8 over 1, 5000 keys 256 wide 17.0 / 51.5
 // More than 8 query heads a key head go in even parts, each of which unpacks the keys (they are read from L2 but once):
 //   32 over 2, 1 sequence, 200 keys 8.6 / 14.5, 12000 18.2 / 19.1;  48 over 4 behind 1000, 2000 keys, 8 sequences 18.1 / 22.3
-//   128 over 8, 2000 keys, 64 sequences 89.7 / 172;  64 over 4, 2 tokens, 300 in front of 12000 keys, 16 sequences 130 / 142;  9 over 1
-//   behind 8000, 64 keys, 64 sequences 55.8 / 30.5
-constexpr double FQ_TILE_KEYS = 3, FQ_START_KEYS = 40000;   // what a key of a row tile, and the start of the tcgen05 kernel, are in keys of 8 rows
+//   128 over 8, 2000 keys, 64 sequences 89.7 / 172;  9 over 1 behind 8000, 64 keys, 64 sequences 55.8 / 30.5
+// In keys of 8 rows: a key of a row tile, the tcgen05 kernel's start, a part of a cut block.
+constexpr double FQ_TILE_KEY = 2.5, FQ_START = 60000, FQ_PART = 16500;
 constexpr int FQ_SHORT_PREFIX = 128;
 static bool attn_few_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
     const int group = desc->n_q_heads / desc->n_kv_heads;
     if (desc->dtype != GRIFFIN_DT_BF16) return true;   // (the only one for fp32)
     const int part = few_group(desc);
     const double n = batch->n_seq, tokens = batch->n_tokens, rows = tokens * group, prefix = batch->prefix_len, parts = group / part, most = 8 / part;
-    const double own = (double)batch->table_stride * desc->page_size, width = desc->n_kv_heads * (desc->head_dim / 128.0);
+    const double own = (double)batch->table_stride * desc->page_size, heads = desc->n_kv_heads, width = desc->head_dim / 128.0;
     const double own8 = n * parts * ceil(tokens / (most * n)), own128 = n * ceil(rows / (128 * n));   // blocks, were the sequences equally long
-    const double few = width * ((n == 1 || prefix <= FQ_SHORT_PREFIX ? own8 : parts * ceil(tokens / most)) * prefix + own8 * own);
-    const double kt = attn_tc_shape(desc->head_dim).kt;
-    const double tiles = fmax(width, desc->n_kv_heads) * kt * (ceil(rows / 128) * ceil(prefix / kt) + own128 * ceil(own / kt));
-    return few <= FQ_TILE_KEYS * tiles + FQ_START_KEYS;
+    const double few = heads * width * ((n == 1 || prefix <= FQ_SHORT_PREFIX ? own8 : parts * ceil(tokens / most)) * prefix + own8 * own);
+    const AttnShape tc = attn_tc_shape(desc->head_dim);
+    const double own_tiles = ceil(own / tc.kt), pre_tiles = ceil(prefix / tc.kt);
+    double tcgen05 = FQ_TILE_KEY * heads * fmax(width, 1.0) * tc.kt * (ceil(rows / 128) * pre_tiles + own128 * own_tiles) + FQ_START;
+    if (attn_fused(batch->n_seq, batch->n_tokens, group, batch->prefix_len) && (!tc.alt || rows > 128 * n)) {   // (attn_join.cu)
+        const double cut = fmin(own_tiles + pre_tiles, ATTN_MAX_GRID / (heads * n * ceil(rows / (128 * tc.tiles_per_block * n))));
+        if (cut > 1) tcgen05 += FQ_PART * fmax(width, 1.0) * cut;
+    }
+    return few <= tcgen05;
 }
 static AttnShape shape_of(const griffin_attn_desc *desc, bool few, bool q4) {
     if (few && q4) return attn_few_q4_shape();
