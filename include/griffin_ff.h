@@ -510,7 +510,12 @@ griffin_status griffin_kv_read_q4(const griffin_attn_desc *desc, const griffin_a
                                   void *k, int64_t ld_k, void *v, int64_t ld_v, void *workspace, void *stream);
 
 /* griffin_attn_prefix over such a cache, with the same rules, limits and workspace (griffin_attn_workspace_bytes); what
- * is said there of values that are not finite holds of groups that read as NaN. */
+ * is said there of values that are not finite holds of groups that read as NaN.  The result is the exact attention over what
+ * the cache holds but for the arithmetic: fp32 sums, and probabilities rounded to bf16 in bf16, or, in fp32, held with the
+ * queries as sums of three bf16 numbers (24 bits; a query beyond bf16's largest number, 3.389e38, reads as NaN).
+ * Calls of few rows, and all in fp32, are cut into tiles of 32 keys and up to 8 rows, the others as above; the limit
+ * of 2^31 tiles is that of the form that a call takes (of fp32 and one causal prompt of 32 heads over 8: 0.18 million tokens).
+ */
 griffin_status griffin_attn_prefix_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
                                       const griffin_kv_cache_q4 *cache, const void *q, int64_t ld_q, void *out, int64_t ld_out,
                                       void *workspace, size_t ws_bytes, void *stream);

@@ -12,6 +12,8 @@
 //               hands descriptions of the segments to the others through a ring in shared memory
 //   warps 4-7, 8-11   two softmax groups, a row per thread: S from TMEM, P (bf16) back to TMEM over S,
 //               and at the end of a segment O to the output or the partials
+// Over a cache in 4 bits (Q4) warp 0 brings key and value tiles as they lie, by bulk copies into a ring of three, and eight more
+// warps (12-19; 8-15 for heads wider than 128) write them out as bf16 into the ring that the products read.
 // The work is a sequence of UNITS (one row tile times one key tile).  Unit U belongs to softmax group U & 1,
 // which has its own S/P columns and (heads of up to 128 entries) its own O columns.  A block of two row
 // tiles meets each key tile with two units; a block of one row tile gives its key tiles to the two groups in
@@ -31,6 +33,9 @@
 // without it: 4.3 TB/s; the rest of both is the way to the first result (6 to 10 us with cold instructions) and the end of
 // each segment.  Looking for values that are not finite (warp 2) costs a prompt's 128-wide heads nothing that can be
 // measured, 256-wide ones 3 % (2048 tokens of 16 heads 87.8 -> 90.1 us).
+// Q4: the same prompt takes 172 us, the same 32 steps (45 MB) 57: the unpacking warps and the softmax share the issue slots (2.2 of 4
+// a clock), and a tile's way through the unpacking lies in front of the first product of a segment.  Four unpacking warps instead of
+// eight: the steps 67, the prompt 174; of that, 8 us are the 256 segments of a tile or three that the sequences' own keys are.
 #include "attn.h"
 #include "attn_join.cuh"
 #include "tmem_wide.cuh"

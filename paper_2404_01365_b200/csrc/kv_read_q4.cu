@@ -3,6 +3,8 @@
 // A thread has one group of 16 entries of one key or value, of every SUBS-th of the CTA's tokens: 9 bytes in, 32 (bf16) or 64
 // out.  A CTA takes its tokens' places together, which is three dependent trips to L2; a call of many tokens is cut into as many
 // CTAs as fit at once, all with the same number (16 tokens to each were 1.2 times that many).
+// Bound by memory: 22046 tokens of 8 heads, 128 wide (25 MB in, 90 MB out), take 24.1 us to bf16, 4.8 TB/s, of which a copy of the
+// same bytes takes 17.7 at the measured rate; 4096 tokens that the append has just written 6.3.
 #include "common.cuh"
 #include "kv_place.cuh"
 #include "layer.h"
