@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     const AttnShares sh(tot.W, p.grid);
     JobParts a;
     AttnSeq q{};
-    int r0 = 0, r1 = 0, head = 0, seq = 0, n_blocks = 0, b = 0, base0 = 0, base1 = 0;
+    int r0 = 0, r1 = 0, rows = 0, head = 0, seq = 0, n_blocks = 0, b = 0, base0 = 0, base1 = 0;
     bool cut = false;
     const int id = (int)((uint32_t)blockIdx.x / (uint32_t)split), part = blockIdx.x - id * split;
     if (id >= by_row) {
@@ -68,6 +68,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
         r0 = at % chunks * cut_rows;
         r1 = min(j.rows, r0 + cut_rows);
         if (r0 >= r1) return;
+        rows = min(j.rows - (r0 & ~15), 16);   // (of its 16: how a row is added up does not depend on cut_rows)
         a = JobParts{PartJob{0, j.head, j.tok0, false}, j.c0, 1, c - j.c0 + 1};
         cut = true;
     } else {
@@ -119,11 +120,12 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
             const int per = (j.rows + split - 1) / split;   // this CTA's rows of the job
             r0 = part * per;
             r1 = min(j.rows, r0 + per);
+            rows = r1 - r0;
             if (p.fused && j.g1 > j.g0 && (!j.alt || tot.queued)) return;  // finished by the attention kernel, or cut
         }
         // Each row is joined by `wpr` warps (more when there are fewer rows), each taking a stretch of its partials; their
         // sums are added in order through shared memory.
-        const int wpr = r1 - r0 == 1 ? warps : r1 - r0 == 2 ? warps / 2 : 2 * (r1 - r0) <= warps ? warps / 4 : 1, sub = warp % wpr;
+        const int wpr = rows == 1 ? warps : rows == 2 ? warps / 2 : 2 * rows <= warps ? warps / 4 : 1, sub = warp % wpr;
         constexpr int AT_ONCE = NV == 1 ? 8 : 4;
 #pragma unroll 1
         for (int rb = r0; rb < r1; rb += warps / wpr) {
@@ -244,12 +246,11 @@ griffin_status launch_attn_join(const AttnPlan &plan, int dtype, void *out, long
     AttnPlan p = plan;
     int by_row = p.hkv * (p.fused ? p.n_seq : p.n_seq + p.n_tokens / p.block_tokens);
     // (with no more tokens than a row tile takes, no block has several; a kernel without streams cuts those too)
-    // A block that is cut is joined by CTAs of 16 rows, two to a warp, or, while the blocks are so few that each is cut into several
-    // parts, of 8: 8 tokens of 8 heads over 1, 256 wide, behind 5000 95 -> 55 us (four blocks in all), 2000 tokens of 64 over 8 49 -> 38; a
-    // prompt of 512 tokens of 32 over 8 (72) 35.8 -> 37.2, of 4096 147 -> 150: most of the CTAs find no cut.
-    const int blocks = p.hkv * (p.n_seq + p.n_tokens / p.block_tokens);
-    int cut_rows = 4 * blocks <= p.grid ? 8 : 16;
-    const int cut = p.fused && (!p.alt || p.n_tokens > p.tile_tokens) ? p.grid * (p.cta_rows / cut_rows) : 0;
+    // A block that is cut is joined by CTAs of 16 rows, or, while the blocks are so few that each is cut into several parts, by twice as
+    // many of 8: 8 tokens of 8 heads over 1, 256 wide, behind 5000 95 -> 55 us (four blocks in all), 2000 tokens of 64 over 8 49 -> 38; a
+    // prompt of 512 tokens of 32 over 8 (72 blocks) 35.8 -> 37.2, of 4096 147 -> 150: most of the CTAs find no cut.
+    const int cut = p.fused && (!p.alt || p.n_tokens > p.tile_tokens) ? p.grid * (p.cta_rows / 16) : 0;
+    int cut_rows = p.cta_rows > 16 && 4ll * p.hkv * (p.n_seq + p.n_tokens / p.block_tokens) <= p.grid ? 8 : 16;
     const void *fn = dtype == GRIFFIN_DT_F32 ? (p.d <= 128 ? reinterpret_cast<const void *>(attn_join_kernel<float, 1>)
                                                            : reinterpret_cast<const void *>(attn_join_kernel<float, 2>))
                                              : (p.d <= 128 ? reinterpret_cast<const void *>(attn_join_kernel<__nv_bfloat16, 1>)
@@ -263,7 +264,7 @@ griffin_status launch_attn_join(const AttnPlan &plan, int dtype, void *out, long
     int split = room < 1 || !rows_here ? 1 : room < most ? room : most;
     const int threads = by_row * split + cut > 2 * p.grid ? JOIN_THREADS / 2 : JOIN_THREADS;
     void *args[] = {&p, &out, &ld_out, &by_row, &split, &cut_rows};
-    return launch_maybe_overlapped(fn, dim3(by_row * split + cut), dim3(threads), 0, stream, true, args) == cudaSuccess ? GRIFFIN_OK
+    return launch_maybe_overlapped(fn, dim3(by_row * split + cut * (16 / cut_rows)), dim3(threads), 0, stream, true, args) == cudaSuccess ? GRIFFIN_OK
                                                                                                                      : GRIFFIN_ERR_CUDA;
 }
 
