@@ -557,7 +557,7 @@ __device__ __forceinline__ void fq_work(const AttnPlan &p, const AttnData &x, co
 #pragma unroll
                 for (int i = 0; i < VG; ++i) {
                     const int group = DP == 64 ? g >> 1 : g * VG + i;
-                    if (group * 16 >= p.d || __ldg(scales + group) != Q4_NAN) continue;
+                    if (group * 16 >= p.d || scales[group] != Q4_NAN) continue;
 #pragma unroll
                     for (int c = i * (NC / VG); c < (i + 1) * (NC / VG); ++c) {
                         if (sees_a) o[c][0] = o[c][2] = nan;

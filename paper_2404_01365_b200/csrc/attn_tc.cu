@@ -267,7 +267,7 @@ static __device__ __noinline__ void add_not_finite(const AtcParams &prm, const S
                                               prm.q4.scale_off + (k & ((1 << p.page_shift) - 1)) * prm.q4.scale_row + c / 16;
 #pragma unroll
                 for (int g = 0; g < 2; ++g)
-                    if (c + 16 * g < p.d && __ldg(scales + g) == Q4_NAN) {
+                    if (c + 16 * g < p.d && scales[g] == Q4_NAN) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) o[16 * g + i] = __uint_as_float(0x7fffffffu);
                     }

@@ -83,8 +83,9 @@ __global__ void __launch_bounds__(READ_THREADS, READ_CTAS) kv_read_q4_kernel(con
             const Place at = s_at[t + u * subs];
             if (at.page < 0) continue;   // (padding, or a token that has no place, reads as zeros)
             const uint8_t *const from = block + at.page * p.stride_page;
-            w[u] = __ldg(reinterpret_cast<const uint2 *>(from + at.slot * p.q4.code_row + g * 8));
-            b[u] = __ldg(from + p.q4.scale_off + at.slot * p.q4.scale_row + g);
+            // (coherent loads: the call in front may have written them while this grid was waiting)
+            w[u] = *reinterpret_cast<const uint2 *>(from + at.slot * p.q4.code_row + g * 8);
+            b[u] = from[p.q4.scale_off + at.slot * p.q4.scale_row + g];
         }
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u) {

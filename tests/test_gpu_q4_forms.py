@@ -160,6 +160,37 @@ def test_as_many_sequences_as_there_may_be(dtype, hd):
                     rows={0, 1, 30, 41, 42, 21 * n - 1})
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,hd", [(4, 1, 64), (2, 2, 128), (12, 1, 128), (10, 1, 256)])
+@pytest.mark.parametrize("room", TABLES)
+def test_queries_that_are_not_finite_spoil_their_own_row_only(dtype, hq, hkv, hd, room):
+    for q_lens, seq_lens, prefix in (([1, 1], [40, 300], 200), ([9, 30], [9, 100], 60)):
+        b = BatchQ4(q_lens, seq_lens, prefix, hq, hkv, hd, 16, dtype, table_extra=-(-room // 16))
+        want, mass = b.reference()
+        bound = b.bound(want, mass)
+        b.q[0, 1, 3], b.q[b.T - 1, hq - 1, hd - 1] = NAN, float("inf")
+        b.to_device()
+        got = f64(b.attend())
+        bad = np.zeros(got.shape[:2], bool)
+        bad[0, 1] = bad[b.T - 1, hq - 1] = True
+        assert np.all(np.isnan(got[bad])) and np.all(np.abs(got[~bad] - want[~bad]) <= bound[~bad])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("room", TABLES)
+@pytest.mark.parametrize("starts", [[0, 5, 3, 40], [-3, 2, 20, 40], [0, 900, 30, 40], [7, 9, 30, 38]])
+def test_rows_that_do_not_ascend(dtype, room, starts):
+    # what they lead to is cut or left alone, and reported (the last ones are no mistake: rows in front and behind are no one's)
+    for hq, hkv, hd in ((8, 2, 64), (9, 1, 128), (2, 1, 256)):
+        b = BatchQ4([10, 20, 10], [60, 20, 300], 50, hq, hkv, hd, 16, dtype, table_extra=-(-room // 16)).to_device()
+        b.dev[0].copy_(torch.tensor(starts, dtype=torch.int32))
+        out = b.attend()
+        st = G.griffin_check_device_status(b.ws)
+        assert torch.isfinite(out).all() and st == (G.OK if starts[0] == 7 else G.ERR_INVALID_ARG)
+        if starts[0] == 7:
+            assert torch.all(out[:7] == 77.0) and torch.all(out[38:] == 77.0) and not torch.any(out[7:38] == 77.0)
+
+
 def test_two_calls_share_a_captured_workspace():
     # append, attend, read of one layer behind the other in one graph, the workspace and the cache shared
     b = BatchQ4([1, 1, 1], [30, 140, 1], 70, 12, 1, 128, 16, "bf16").to_device()
