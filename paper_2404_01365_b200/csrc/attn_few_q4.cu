@@ -42,7 +42,9 @@ constexpr float FQ_SLACK = 8.f;  // how far (log2) the true maximum may run ahea
 template <int DP, typename T> struct FqCfg {
     static constexpr bool F32 = sizeof(T) == 4;
     static constexpr int PARTS = F32 ? 3 : 1;   // bf16 numbers that a query's entry, or P, is the sum of
-    static constexpr int WARPS = DP == 256 || (F32 && DP == 128) ? 8 : 16, THREADS = 32 * WARPS, STAGES = 2;
+    // (as many warps as have the registers that the kernel wants: 16 of 128-wide bf16 spill 104 bytes, 48 sequences of up to 4096 keys
+    // 67.6 us, 12 64.2, 8 69.4, and 1 sequence behind 512 tokens 9.9, 8.1, 7.9; 256 wide 8 warps 119, 6 146; 3 stages no faster)
+    static constexpr int WARPS = DP == 256 || (F32 && DP == 128) ? 8 : 12, THREADS = 32 * WARPS, STAGES = 2;
     // rows of codes and scales in shared memory
     static constexpr int KROW = DP == 256 ? 144 : DP / 2, VROW = DP / 2, SROW = DP / 16;
     static constexpr int V_AT = FQ_KEYS * KROW, KS_AT = V_AT + FQ_KEYS * VROW, VS_AT = KS_AT + FQ_KEYS * SROW, STAGE = VS_AT + FQ_KEYS * SROW;
