@@ -41,16 +41,17 @@ static bool attn_few(const griffin_attn_desc *desc, const griffin_attn_batch *ba
 //     16  4000  16.0  27.0  19.4  14.9  24.0         80  4000  27.8  28.2     -     -
 //     32  1000  13.5  13.4  12.6  10.6     -        128  1000  21.4  14.4     -     -
 //     32 16000  33.4  84.8  49.7  32.2     -        128  4000  34.0  30.2     -     -
+// (With 16 warps to a CTA; with the 12 that it has now all are 1 to 2 us less.)
 // Fitted over 150 calls drawn at random, each timed in every form: base + slope * keys (128 wide) for each cluster, to 1.1 us, and for cut
-// calls 15 + 0.0048 * keys * jobs / 148, and 3 more where a prefix is walked apart, to 3.  What is chosen by these takes 0.2 % more than the best
-// form on average, 1.4 times as long at worst.
+// calls 13 + 0.0048 * keys * jobs / 148, and 3 more where a prefix is walked apart, to 3.  What is chosen by these takes 0.4 % more than the best
+// form on average, 1.16 times as long at worst.
 // The sequences' lengths are on the device; what the page table could hold stands for them, here and below.
 struct WholeFit {
     int cluster, most_jobs;
     double base, slope, slack;   // slack: how far a cut call with the fewest jobs, of which each has many parts to join, is above its fit
 };
-constexpr WholeFit WHOLE_FITS[] = {{1, 148, 8.3, 0.0046, 0.0}, {2, 72, 9.2, 0.0024, 0.0}, {4, 32, 9.1, 0.00132, 0.0}, {8, 8, 9.4, 0.00080, 5.0}};
-constexpr double CUT_BASE = 15, CUT_SLOPE = 0.0048 / ATTN_MAX_GRID, CUT_APART = 3;
+constexpr WholeFit WHOLE_FITS[] = {{1, 148, 7.0, 0.0045, 0.0}, {2, 72, 7.7, 0.00236, 0.0}, {4, 32, 7.6, 0.00128, 0.0}, {8, 8, 7.9, 0.0007, 5.0}};
+constexpr double CUT_BASE = 13, CUT_SLOPE = 0.0048 / ATTN_MAX_GRID, CUT_APART = 3;
 constexpr int FQ_SHORT_PREFIX = 128;   // (a prefix up to which every sequence walks it itself, below)
 // Query heads of a block of that kernel: all of a key head, or an even part of them.
 static int few_group(const griffin_attn_desc *desc) {
@@ -81,11 +82,12 @@ static WholeJobs attn_whole(const griffin_attn_desc *desc, const griffin_attn_ba
 }
 // Whether that kernel takes a call over a cache in 4 bits rather than the tcgen05 one.  It unpacks the keys once for every 8 rows, the
 // other once for every 128 (a row tile; two of them share a key tile, but not the softmax).  In keys of a 128-wide head, over
-// all jobs, few rows take 3e-5 us each on 148 SMs and row tiles 7.5e-5 (of 64-wide heads not less: their softmax is the same); the
-// tcgen05 kernel's way to the first and from the last result takes 1.8 us more, and blocks that are cut, which the joining kernel has
-// too few CTAs for, 0.5 us a part (of 128 entries).  500 calls drawn at random (1 to 128 sequences of 1 to 128 tokens, up to 32000 shared and
-// 30000 own keys, 64 to 256 wide, 1 to 32 key heads with 1 to 64 query heads each), each timed with both kernels, take 0.6 % more by
-// this rule than with the better one each time, at worst 1.4 times as long.  us a pass, few / tcgen05, query heads over key heads:
+// all jobs, few rows take 2.5e-5 us each on 148 SMs and row tiles 6.5e-5 (of 64-wide heads not less: their softmax is the same); the
+// tcgen05 kernel's way to the first and from the last result takes 2 us more, and blocks that are cut, which the joining kernel has
+// too few CTAs for, 0.4 us a part (of 128 entries).  500 calls drawn at random (1 to 128 sequences of 1 to 128 tokens, up to 32000 shared and
+// 30000 own keys, 64 to 256 wide, 1 to 32 key heads with 1 to 64 query heads each), each timed with both kernels, take 1.0 % more by
+// this rule than with the better one each time, at worst 1.5 times as long.  us a pass, few / tcgen05, query heads over key heads (the
+// 128-wide figures of the former with 16 warps to a CTA; 12 take 5 to 15 % less):
 //   1 sequence of 1 token, 64 over 8, 5000 keys 14.3 / 19.7;  4 of 4 tokens 38.0 / 32.9;  16 tokens, 32 over 16 28.0 / 24.5
 //   24 sequences of 1 token, 64 over 8, 12000 keys 93 / 235;  of 32 tokens, 5000 keys 945 / 190
 //   32 over 8 behind 1000 shared, 600 keys, 8 sequences 14.3 / 20.5;  8 over 8 behind 2000, 64 keys, 48 sequences 24.7 / 27.2
@@ -96,7 +98,7 @@ static WholeJobs attn_whole(const griffin_attn_desc *desc, const griffin_attn_ba
 //   32 over 2, 1 sequence, 200 keys 8.6 / 14.5, 12000 18.2 / 19.1;  48 over 4 behind 1000, 2000 keys, 8 sequences 18.1 / 22.3
 //   128 over 8, 2000 keys, 64 sequences 89.7 / 172;  9 over 1 behind 8000, 64 keys, 64 sequences 55.8 / 30.5
 // In keys of 8 rows: a key of a row tile, the tcgen05 kernel's start, a part of a cut block.
-constexpr double FQ_TILE_KEY = 2.5, FQ_START = 60000, FQ_PART = 16500;
+constexpr double FQ_TILE_KEY = 2.5, FQ_START = 80000, FQ_PART = 16500;
 static bool attn_few_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch) {
     const int group = desc->n_q_heads / desc->n_kv_heads;
     if (desc->dtype != GRIFFIN_DT_BF16) return true;   // (the only one for fp32)

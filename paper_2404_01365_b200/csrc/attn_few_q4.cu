@@ -24,9 +24,9 @@
 // With few jobs (attn_whole, attn.cu) a cluster of 1, 2, 4 or 8 CTAs takes a job whole instead: the CTAs' sums meet in distributed
 // shared memory, each adds up and stores its share of the entries, and there is no second launch.
 //
-// Measured: 48 sequences of up to 4096 keys, 32 heads over 8, 128 wide (154 MB of codes and scales), 53.5 us, 2.9 TB/s, with
-// the joining kernel (from the cache in bf16, 547 MB, 95); 1 sequence of 32 heads behind 512 tokens 9.9, of which 2 are the launch;
-// 8 sequences of 40 heads behind 2048 21.7.
+// Measured: 48 sequences of up to 4096 keys, 32 heads over 8, 128 wide (154 MB of codes and scales), 51.2 us, 3.0 TB/s, with
+// the joining kernel (from the cache in bf16, 547 MB, 95); 1 sequence of 32 heads behind 512 tokens 8.0, of which 2 are the launch;
+// 8 sequences of 40 heads behind 2048 21.0.
 // fp32 calls run on the same instruction: keys and values are exact in bf16, a query's entry and P are sums of three bf16 numbers, so
 // three products of each kind replace one; the unpacking is shared.
 #include "attn.h"
