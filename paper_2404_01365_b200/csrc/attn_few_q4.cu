@@ -713,8 +713,9 @@ static __device__ __noinline__ AttnJob fq_whole_job(const AttnPlan &p, const int
 }
 
 
+// (not the .aligned forms: the loops in front of a meeting let the lanes of a warp go different ways)
 __device__ __forceinline__ void cluster_meet() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
 // m and l of a row and four entries of its results, from a piece of any CTA of the cluster.
 struct FqPart {
