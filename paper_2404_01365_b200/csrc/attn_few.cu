@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(FewCfg<DP>::THREADS, 1) attn_few_kernel(const 
                 const float m = sh_m[w * FEW_ROWS + r], f = m == -INFINITY ? 0.f : fast_exp2(m - M);
                 const float4 v = *reinterpret_cast<const float4 *>(smem_raw + w * Cfg::WARP_BYTES + used + (r * Cfg::LDO + e) * 4);
                 sum = fmaf(f, sh_l[w * FEW_ROWS + r], sum);
-                if (f != 0.f) {
+                if (m != -INFINITY) {   // (a weight of 0 counts: it keeps NaN)
                     acc.x = fmaf(f, v.x, acc.x);
                     acc.y = fmaf(f, v.y, acc.y);
                     acc.z = fmaf(f, v.z, acc.z);

@@ -657,7 +657,7 @@ static __device__ __noinline__ void fq_join_pieces(const AttnPlan &p, const Attn
                 M = m;
                 sum = fmaf(sum, f, w * ml.y);
                 acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
-                if (w != 0.f) {
+                if (ml.x != -INFINITY) {   // (a weight of 0 counts: it keeps NaN)
                     acc.x = fmaf(w, v.x, acc.x);
                     acc.y = fmaf(w, v.y, acc.y);
                     acc.z = fmaf(w, v.z, acc.z);
@@ -740,7 +740,7 @@ struct FqSum {
         M = m;
         l = fmaf(l, f, w * v.ml.y);
         o.x *= f, o.y *= f, o.z *= f, o.w *= f;
-        if (w != 0.f) {   // (a part in which the row sees nothing has no results)
+        if (v.ml.x != -INFINITY) {   // (a part in which the row sees nothing has no results; a weight of 0 counts, which keeps NaN)
             o.x = fmaf(w, v.o.x, o.x);
             o.y = fmaf(w, v.o.y, o.y);
             o.z = fmaf(w, v.o.z, o.z);

@@ -157,9 +157,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
 #pragma unroll
                     for (int o = 16; o > 0; o >>= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, o));
                     const float m_new = fmaxf(M, mb), f = m_new == -INFINITY ? 0.f : exp2f(M - m_new);
-                    // (a part in which the row sees nothing leaves no output)
+                    // (a part in which the row sees nothing leaves no output; any other counts, at a weight of 0 too, which keeps NaN)
                     const float wgt = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m_new);
-                    if (wgt == 0.f) at.o = nullptr;
+                    if (ml.x == -INFINITY) at.o = nullptr;
                     M = m_new;
                     sum = sum * f + warp_sum(wgt * ml.y);
 #pragma unroll
