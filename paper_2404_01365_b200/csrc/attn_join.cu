@@ -11,6 +11,7 @@
 namespace griffin {
 
 constexpr int JOIN_THREADS = 256, JOIN_WARPS = JOIN_THREADS / 32;
+constexpr int JOIN_MAX_CTAS = 160;   // CTAs of an attention kernel at most (one per SM of a B200), rounded up to a multiple of 32
 
 // The partials of one job: n of them on CTAs c0, c0 + 1, ..., `streams` of each.
 struct JobParts {
@@ -42,16 +43,24 @@ template <typename T> __device__ __forceinline__ void store_row4(T *to, const fl
 
 // CTAs 0 .. by_row * split - 1, `split` of them to a job: jobs whose partials are kept by row: in a fused call the last row block of each sequence and
 // key head (no other has just one row tile) and the blocks that see nothing, else every row block.  The others
-// (fused calls): the blocks that were cut, cut_rows rows each.
+// (fused calls): the blocks that were cut, `chunks` of them to a block, 16 rows each; or 8 (FEW), then to the first, the second, ... of the
+// blocks that were cut rather than to each attention CTA's, whether it has one or not.
 // NV: 128-entry pieces of a row (a lane has 4 entries of each).
 template <typename T, int NV>
 __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_constant__ AttnPlan p, T *__restrict__ out,
-                                                                 long long ld_out, int by_row, int split, int cut_rows) {
+                                                                 long long ld_out, int by_row, int split, int chunks, int few) {
     __shared__ float sh_ml[JOIN_WARPS][2], sh_o[JOIN_WARPS][NV * 128];
     __shared__ int sh_seq[5];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     pdl_launch_dependents();
     pdl_wait_prior_grids();
+    const int id = (int)((uint32_t)blockIdx.x / (uint32_t)split), part = blockIdx.x - id * split;
+    int cut_of[JOIN_MAX_CTAS / 32] = {};   // rows of the attention CTAs' cuts (asked for with the totals, in one trip)
+    if (few && id >= by_row) {
+#pragma unroll
+        for (int i = 0; i < JOIN_MAX_CTAS / 32; ++i)
+            if (32 * i + lane < p.grid) cut_of[i] = p.cuts[32 * i + lane].rows;
+    }
     const AttnTotals tot = attn_totals(p, p.bases);
     if (tot.W < 0) return;   // the call was not run, and the first tiles of its sequences mean nothing
     if (tot.queued && blockIdx.x == 0 && threadIdx.x == 0) *p.queue = 0;
@@ -60,10 +69,23 @@ __global__ void __launch_bounds__(JOIN_THREADS) attn_join_kernel(const __grid_co
     AttnSeq q{};
     int r0 = 0, r1 = 0, rows = 0, head = 0, seq = 0, n_blocks = 0, b = 0, base0 = 0, base1 = 0;
     bool cut = false;
-    const int id = (int)((uint32_t)blockIdx.x / (uint32_t)split), part = blockIdx.x - id * split;
     if (id >= by_row) {
-        const int at = blockIdx.x - by_row * split, chunks = p.cta_rows / cut_rows, c = at / chunks;
+        const int at = blockIdx.x - by_row * split, cut_rows = few ? 8 : 16;
+        int c = at / chunks;
         if (c >= sh.G || tot.queued) return;
+        if (few) {   // the CTA with the c-th cut
+            int n = c;
+            c = -1;
+#pragma unroll
+            for (int i = 0; i < JOIN_MAX_CTAS / 32; ++i) {
+                const bool has = 32 * i + lane < sh.G && cut_of[i] > 0;
+                const unsigned m = __ballot_sync(0xffffffffu, has);
+                const unsigned it = __ballot_sync(0xffffffffu, has && __popc(m & ((1u << lane) - 1u)) == n);
+                if (it != 0) c = 32 * i + __ffs(it) - 1;   // (behind it n is below 0)
+                n -= __popc(m);
+            }
+            if (c < 0) return;
+        }
         const CutJob j = p.cuts[c];
         r0 = at % chunks * cut_rows;
         r1 = min(j.rows, r0 + cut_rows);
@@ -246,11 +268,16 @@ griffin_status launch_attn_join(const AttnPlan &plan, int dtype, void *out, long
     AttnPlan p = plan;
     int by_row = p.hkv * (p.fused ? p.n_seq : p.n_seq + p.n_tokens / p.block_tokens);
     // (with no more tokens than a row tile takes, no block has several; a kernel without streams cuts those too)
-    // A block that is cut is joined by CTAs of 16 rows, or, while the blocks are so few that each is cut into several parts, by twice as
-    // many of 8: 8 tokens of 8 heads over 1, 256 wide, behind 5000 95 -> 55 us (four blocks in all), 2000 tokens of 64 over 8 49 -> 38; a
-    // prompt of 512 tokens of 32 over 8 (72 blocks) 35.8 -> 37.2, of 4096 147 -> 150: most of the CTAs find no cut.
     const int cut = p.fused && (!p.alt || p.n_tokens > p.tile_tokens) ? p.grid * (p.cta_rows / 16) : 0;
-    int cut_rows = p.cta_rows > 16 && 4ll * p.hkv * (p.n_seq + p.n_tokens / p.block_tokens) <= p.grid ? 8 : 16;
+    const int most = (p.n_tokens < p.block_tokens ? p.n_tokens : p.block_tokens) * p.group;   // rows of a block
+    // A block that is cut is joined by CTAs of 16 rows, or, while the blocks are so few that each is cut into several parts, of 8, and
+    // then there are as many as the blocks have rows for.  us a pass, 16 rows / 8, for every attention CTA / 8, for every block: 8 tokens of 8
+    // heads over 1, 256 wide, behind 5000 95.1 / 55.5 / 50.2; 16 tokens of 8 over 2, 256 wide, by themselves 13.6 / 16.6 / 11.8; 40 of 8 over 2
+    // at 100 keys 14.0 / 16.9 / 12.4; fp32, 4 tokens of 4 over 1, 256 wide, behind 5070 146 / 87 / 81, 1 token of 2 over 1 at 5 keys
+    // 9.2 / 9.8 / 9.2.  With many blocks most of the CTAs find no cut: 512 tokens of 32 over 8 (72 blocks) 35.8 / 37.2 (8, for every CTA).
+    const long long blocks = (long long)p.hkv * (p.n_seq + p.n_tokens / p.block_tokens);
+    int few = p.cta_rows > 16 && 4 * blocks <= p.grid, chunks = few ? (most + 7) / 8 : p.cta_rows / 16;
+    const int cut_ctas = cut == 0 ? 0 : few ? (int)blocks * chunks : cut;
     const void *fn = dtype == GRIFFIN_DT_F32 ? (p.d <= 128 ? reinterpret_cast<const void *>(attn_join_kernel<float, 1>)
                                                            : reinterpret_cast<const void *>(attn_join_kernel<float, 2>))
                                              : (p.d <= 128 ? reinterpret_cast<const void *>(attn_join_kernel<__nv_bfloat16, 1>)
@@ -260,11 +287,11 @@ griffin_status launch_attn_join(const AttnPlan &plan, int dtype, void *out, long
     // Jobs of several rows go to several CTAs while there are fewer CTAs than fit at once (8 tokens of one sequence, 32 heads
     // over 8, behind 9000: 52.7 -> 22.1 us), unless the jobs by row are the rare ones (a prompt's last block).
     const bool rows_here = !p.fused || (p.alt && p.n_tokens <= p.n_seq * p.tile_tokens);
-    const int most = (p.n_tokens < p.block_tokens ? p.n_tokens : p.block_tokens) * p.group, room = 2 * p.grid / by_row;
+    const int room = 2 * p.grid / by_row;
     int split = room < 1 || !rows_here ? 1 : room < most ? room : most;
     const int threads = by_row * split + cut > 2 * p.grid ? JOIN_THREADS / 2 : JOIN_THREADS;
-    void *args[] = {&p, &out, &ld_out, &by_row, &split, &cut_rows};
-    return launch_maybe_overlapped(fn, dim3(by_row * split + cut * (16 / cut_rows)), dim3(threads), 0, stream, true, args) == cudaSuccess ? GRIFFIN_OK
+    void *args[] = {&p, &out, &ld_out, &by_row, &split, &chunks, &few};
+    return launch_maybe_overlapped(fn, dim3(by_row * split + cut_ctas), dim3(threads), 0, stream, true, args) == cudaSuccess ? GRIFFIN_OK
                                                                                                                      : GRIFFIN_ERR_CUDA;
 }
 
