@@ -153,18 +153,19 @@ class Decoder:
 
     def held(self, layer):
         """Keys and values of a layer as a cache in 4 bits holds them: (k, v) of the prompt's tokens [P, heads, D], and of each
-        continuation's [n_seq, steps so far, heads, D]."""
+        continuation's [n_seq, steps so far, heads, D] (the device counts the steps, replayed ones too, so this waits for them)."""
         if self.cfg.cache != "q4":
             raise ValueError("the cache is not in 4 bits: its tensors hold the keys and values")
         c, out = self.cfg, []
         i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device=self.device)
         prompt = ([0, self.prompt_len], i32(self.prompt_len), self.prefix_pages[None])
-        own = ([s * self.done for s in range(self.n_seq + 1)], self.seq_len, self.own_pages)
+        steps = int(self.seq_len[0])
+        own = ([s * steps for s in range(self.n_seq + 1)], self.seq_len, self.own_pages)
         for starts, lens, pages in (prompt, own):
             kv = [torch.empty(starts[-1], c.n_kv_heads, c.head_dim, device=self.device, dtype=c.torch_dtype) for _ in range(2)]
             G.griffin_kv_read_q4(self.attn, G.make_attn_batch(i32(*starts), lens, pages, starts[-1]), self.caches[layer], *kv, self.attn_ws)
             out.append(kv)
-        own = [x.view(self.n_seq, self.done, c.n_kv_heads, c.head_dim) for x in out[1]]
+        own = [x.view(self.n_seq, steps, c.n_kv_heads, c.head_dim) for x in out[1]]
         return tuple(out[0]), tuple(own)
 
     def status(self):
