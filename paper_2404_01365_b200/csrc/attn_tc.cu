@@ -279,7 +279,7 @@ static __device__ __noinline__ void add_not_finite(const AtcParams &prm, const S
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if (c + 8 * e >= p.d) continue;
-                const uint4 x = __ldg(v + e);
+                const uint4 x = v[e];   // (a coherent load: the call in front may have written it while this grid was waiting)
                 const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
