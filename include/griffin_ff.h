@@ -515,7 +515,8 @@ griffin_status griffin_kv_read_q4(const griffin_attn_desc *desc, const griffin_a
  * queries as sums of three bf16 numbers (24 bits; a query beyond bf16's largest number, 3.389e38, reads as NaN).
  * Calls of few rows, and all in fp32, are cut into tiles of 32 keys and up to 8 rows, the others as above; the limit
  * of 2^31 tiles is that of the form that a call takes (of fp32 and one causal prompt of 32 heads over 8: 0.18 million tokens).
- */
+ * The form follows from what the page table could hold, since the lengths are on the device: a table (table_stride) that is no
+ * wider than the sequences need serves them best, and changes results by no more than roundings. */
 griffin_status griffin_attn_prefix_q4(const griffin_attn_desc *desc, const griffin_attn_batch *batch,
                                       const griffin_kv_cache_q4 *cache, const void *q, int64_t ld_q, void *out, int64_t ld_out,
                                       void *workspace, size_t ws_bytes, void *stream);

@@ -44,8 +44,12 @@ static bool attn_few(const griffin_attn_desc *desc, const griffin_attn_batch *ba
 // (With 16 warps to a CTA; with the 12 that it has now all are 1 to 2 us less.)
 // Fitted over 150 calls drawn at random, each timed in every form: base + slope * keys (128 wide) for each cluster, to 1.1 us, and for cut
 // calls 13 + 0.0048 * keys * jobs / 148, and 3 more where a prefix is walked apart, to 3.  What is chosen by these takes 0.4 % more than the best
-// form on average, 1.16 times as long at worst.
-// The sequences' lengths are on the device; what the page table could hold stands for them, here and below.
+// form on average, 1.16 times as long at worst, where the tables are about as wide as the sequences are long.
+// The sequences' lengths are on the device; what the page table could hold stands for them, here and below.  Short sequences in tables for
+// a long context are taken by the forms for long ones.  us a pass, tables as wide as need be / for 4096 keys / for 32768: 1 sequence of 32
+// heads behind 512, 128 own 8.0 / 8.0 / 12.6; 5 of 8 heads, 500 keys 8.1 / 8.1 / 12.4; 16 of 32 over 8, 200 keys 7.4 / 7.4 / 13.1; fp32, 5
+// of 16 over 4 behind 1003 8.6 / 8.6 / 13.7; 6 drafted tokens, 32 over 8, behind 1000 9.5 / 9.5 / 15.2; 6 x 5 drafted, 256 wide 21.4 / 21.3 / 26.2; 4
+// pieces of 16, 300 keys 15.8 / 18.1 / 18.0; 48 sequences of 4096 50.1 / 50.3 / 50.3.
 struct WholeFit {
     int cluster, most_jobs;
     double base, slope, slack;   // slack: how far a cut call with the fewest jobs, of which each has many parts to join, is above its fit
@@ -53,7 +57,8 @@ struct WholeFit {
 constexpr WholeFit WHOLE_FITS[] = {{1, 148, 7.0, 0.0045, 0.0}, {2, 72, 7.7, 0.00236, 0.0}, {4, 32, 7.6, 0.00128, 0.0}, {8, 8, 7.9, 0.0007, 5.0}};
 constexpr double CUT_BASE = 13, CUT_SLOPE = 0.0048 / ATTN_MAX_GRID, CUT_APART = 3;
 constexpr int FQ_SHORT_PREFIX = 128;   // (a prefix up to which every sequence walks it itself, below)
-// Query heads of a block of that kernel: all of a key head, or an even part of them.
+// Query heads of a block of that kernel: all of a key head, or an even part of them.  (Groups of a prime number above 8 go one by one, and
+// each unpacks the keys: 64 steps of 13 heads over 1, 2048 keys 26.2 us, of 12 17.2; over the cache in bf16 both 23.3.)
 static int few_group(const griffin_attn_desc *desc) {
     const int group = desc->n_q_heads / desc->n_kv_heads;
     int n = group < 8 ? group : 8;
@@ -86,7 +91,7 @@ static WholeJobs attn_whole(const griffin_attn_desc *desc, const griffin_attn_ba
 // tcgen05 kernel's way to the first and from the last result takes 2 us more, and blocks that are cut, which the joining kernel has
 // too few CTAs for, 0.4 us a part (of 128 entries).  500 calls drawn at random (1 to 128 sequences of 1 to 128 tokens, up to 32000 shared and
 // 30000 own keys, 64 to 256 wide, 1 to 32 key heads with 1 to 64 query heads each), each timed with both kernels, take 1.0 % more by
-// this rule than with the better one each time, at worst 1.5 times as long.  us a pass, few / tcgen05, query heads over key heads (the
+// this rule than with the better one each time, at worst 1.5 times as long (with tables that fit, as above).  us a pass, few / tcgen05, query heads over key heads (the
 // 128-wide figures of the former with 16 warps to a CTA; 12 take 5 to 15 % less):
 //   1 sequence of 1 token, 64 over 8, 5000 keys 14.3 / 19.7;  4 of 4 tokens 38.0 / 32.9;  16 tokens, 32 over 16 28.0 / 24.5
 //   24 sequences of 1 token, 64 over 8, 12000 keys 93 / 235;  of 32 tokens, 5000 keys 945 / 190

@@ -17,18 +17,20 @@
 // long on its end as on 512 keys: 256 sequences of 512 keys under 8 heads 140 us, 48 of 2560 61.  Warps that each left their
 // partials to the joining kernel gave it 148 a row: 4 tokens behind 9000 keys, 8 heads, 104 us.)  The loads' addresses, the pages,
 // the walk and the look for a new maximum (which is not exchanged while the sums, in fp32, stay below 2^8) cost as much
-// as the products for 16 keys, so a warp takes 32 at a time: the instructions that it issues are what bounds this kernel,
-// those of the integer pipe, every other clock, first (2.35 issued of 4 a clock, the integer pipe busy for 58 % of it, 20 %
-// the matrix pipe).
+// as the products for 16 keys, so a warp takes 32 at a time.  What bounds it are the instructions: of 4 issue slots a clock 2.30
+// are used, the integer pipe for 56 % of the time, the matrix pipe for 21 %, and with three warps to a scheduler their fixed latencies
+// (1.1 warps at an issue) and the integer pipe (0.75) are what the rest waits for, not memory (0.2 each for device and shared memory): 16 sequences of 4096 keys under
+// 32 heads of their own.  (With 16 warps, which spilled, it was 2.35, 58 % and 20 %.)
 //
 // With few jobs (attn_whole, attn.cu) a cluster of 1, 2, 4 or 8 CTAs takes a job whole instead: the CTAs' sums meet in distributed
 // shared memory, each adds up and stores its share of the entries, and there is no second launch.
 //
-// Measured: 48 sequences of up to 4096 keys, 32 heads over 8, 128 wide (154 MB of codes and scales), 51.2 us, 3.0 TB/s, with
-// the joining kernel (from the cache in bf16, 547 MB, 95); 1 sequence of 32 heads behind 512 tokens 8.0, of which 2 are the launch;
-// 8 sequences of 40 heads behind 2048 21.0.
+// Measured: 48 sequences of 1024 to 4096 keys, 32 heads over 8, 128 wide (154 MB of codes and scales), 51.2 us, 3.0 TB/s, with
+// the joining kernel (from the cache in bf16, 547 MB, 95), all of 4096 (227 MB) 64.9 (139); 1 sequence of 32 heads behind 512
+// tokens 8.0, of which 2 are the launch; 8 sequences of 40 heads behind 2048 21.0.
 // fp32 calls run on the same instruction: keys and values are exact in bf16, a query's entry and P are sums of three bf16 numbers, so
-// three products of each kind replace one; the unpacking is shared.
+// three products of each kind replace one; the unpacking is shared.  Prompts too: 1000 causal tokens of 8 heads of 64 41 us (over the
+// cache in fp32 72), 2048 of 32 over 8, 128 wide, 590 (1409), 64 behind 4096 69 (194).
 #include "attn.h"
 #include "attn_join.cuh"
 #include "decode_mma.cuh"
@@ -42,8 +44,9 @@ constexpr float FQ_SLACK = 8.f;  // how far (log2) the true maximum may run ahea
 template <int DP, typename T> struct FqCfg {
     static constexpr bool F32 = sizeof(T) == 4;
     static constexpr int PARTS = F32 ? 3 : 1;   // bf16 numbers that a query's entry, or P, is the sum of
-    // (as many warps as have the registers that the kernel wants: 16 of 128-wide bf16 spill 104 bytes, 48 sequences of up to 4096 keys
-    // 67.6 us, 12 64.2, 8 69.4, and 1 sequence behind 512 tokens 9.9, 8.1, 7.9; 256 wide 8 warps 119, 6 146; 3 stages no faster)
+    // (as many warps as have the registers that the kernel wants in bf16: 16 of 128-wide bf16 spill 104 bytes, 48 sequences of 4096 keys
+    // each 67.6 us, 12 64.2, 8 69.4, and 1 sequence behind 512 tokens 9.9, 8.1, 7.9; 256 wide 8 warps 119, 6 146; 3 stages no faster.  256-wide
+    // fp32 spills 64 to 80 bytes at 255 registers, bf16 of 80 to 112 entries 4)
     static constexpr int WARPS = DP == 256 || (F32 && DP == 128) ? 8 : 12, THREADS = 32 * WARPS, STAGES = 2;
     // rows of codes and scales in shared memory
     static constexpr int KROW = DP == 256 ? 144 : DP / 2, VROW = DP / 2, SROW = DP / 16;

@@ -653,7 +653,7 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
             }
         }
     } else if (warp == 2) {
-        // ---------------- value tiles: rows that no key stands for become zeros ----------------
+        // ---------------- value tiles: rows that no key stands for become zeros (Q4: they are numbers already) ----------------
         Segment w;
         // (It waits for the key tiles too: a wait for a slot's n-th filling may only begin when the one before has been
         // seen, or the parity of an older one passes for it.  And no slot is filled again before it has looked: a filling
@@ -691,7 +691,9 @@ __global__ void __launch_bounds__(AtcCfg<DP, Q4>::THREADS, 1) attn_tc_kernel(con
                         fence_proxy_async_smem();
                     }
                 }
-                if (!Q4 && valid < KT) {   // (what is unpacked has zeros there)
+                // (Q4: what was unpacked behind the last key is any number, but finite, as the unpacking never writes NaN there, a scale's
+                // byte of 255 included; P is 0 there)
+                if (!Q4 && valid < KT) {
 #pragma unroll 1
                     for (int i = lane; i < (KT - valid) * 8 * CB; i += 32) {
                         const int c = i % CB, r = valid + i / CB / 8, e = i / CB % 8;

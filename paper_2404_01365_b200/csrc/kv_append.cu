@@ -15,7 +15,8 @@
 // Bound by memory where there is much of it: 4096 tokens of 32 query heads and 8 key heads of 128, bf16 (101 MB), take
 // 20.7 us, 4.9 TB/s, where a copy of the same bytes takes 16; 8 tokens of 40 heads take 2.1 us, the launch and the trips.  Into 4 bits
 // the same take 23.0 us (88 MB, 3.8 TB/s; a copy 13.5) and 2.5: it issues 2.5 instructions of 4 a clock, the integer
-// pipe busy for half of it; with divisions for the quotients it was 27.5.
+// pipe busy for half of it; with divisions for the quotients it was 27.5.  4096 tokens in fp32 take 38 us (into fp32 35).  For eight
+// CTAs to an SM the kernels into 4 bits have 64 registers, of which the two that take tokens in pairs spill 28 (bf16) and 132 bytes (fp32).
 #include "common.cuh"
 #include "kv_place.cuh"
 #include "layer.h"
