@@ -36,8 +36,8 @@ def far(b, positions, values):
     ([1], [5000], 0, 2500),
     ([1, 1], [40, 90], 300, 300),             # a prefix that is worked on by itself
     ([2, 1, 1], [300, 90, 1], 500, 650),
-    ([1] * 30, [900 + i for i in range(30)], 0, 400),
-    ([1] * 80, [600 + i for i in range(80)], 0, 300),      # more jobs than are taken whole
+    ([1] * 30, [300 + i for i in range(30)], 0, 130),
+    ([1] * 80, [150 + i % 9 for i in range(80)], 0, 70),      # more jobs than are taken whole
     ([5], [900], 64, 500),
     ([40], [1500], 0, 800),
     ([300], [1200], 0, 850),                  # blocks of several row tiles, cut
