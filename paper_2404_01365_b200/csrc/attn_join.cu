@@ -274,7 +274,8 @@ griffin_status launch_attn_join(const AttnPlan &plan, int dtype, void *out, long
     // then there are as many as the blocks have rows for.  us a pass, 16 rows / 8, for every attention CTA / 8, for every block: 8 tokens of 8
     // heads over 1, 256 wide, behind 5000 95.1 / 55.5 / 50.2; 16 tokens of 8 over 2, 256 wide, by themselves 13.6 / 16.6 / 11.8; 40 of 8 over 2
     // at 100 keys 14.0 / 16.9 / 12.4; fp32, 4 tokens of 4 over 1, 256 wide, behind 5070 146 / 87 / 81, 1 token of 2 over 1 at 5 keys
-    // 9.2 / 9.8 / 9.2.  With many blocks most of the CTAs find no cut: 512 tokens of 32 over 8 (72 blocks) 35.8 / 37.2 (8, for every CTA).
+    // 9.2 / 9.8 / 9.2.  (Rows of q_start that do not ascend may make more blocks than are counted here; what is cut of those beyond stays as
+    // it was, and the status word is raised.)  With many blocks most of the CTAs find no cut: 512 tokens of 32 over 8 (72 blocks) 35.8 / 37.2 (8, for every CTA).
     const long long blocks = (long long)p.hkv * (p.n_seq + p.n_tokens / p.block_tokens);
     int few = p.cta_rows > 16 && 4 * blocks <= p.grid, chunks = few ? (most + 7) / 8 : p.cta_rows / 16;
     const int cut_ctas = cut == 0 ? 0 : few ? (int)blocks * chunks : cut;
